@@ -211,6 +211,22 @@ aiq_status aiq_run_join_select(aiq_ctx* ctx, aiq_table build, int32_t build_key,
                                int32_t n_build_preds, aiq_table probe, int32_t probe_key, aiq_model model,
                                const aiq_select* probe_side, aiq_result_h* out);
 
+/* Sampling of a token from its row's logits and a uniform number u in [0, 1).
+ * With the logits in descending order (equal ones by their index), the first
+ * top_k of them, e_i = exp((z_i - z_0) / temperature) and their sums C_m: kept are
+ * the first n, the smaller of the least m with C_m >= top_p * C_k and the number
+ * of e_i >= min_p (the top token's is 1); the token is the first whose C_i exceeds
+ * u * C_n.  Exponentials and sums are 64 bits wide.  temperature > 0; top_k 1 ..
+ * AIQ_SAMPLE_MAX_K and at most the vocabulary; top_p in (0, 1], 1: all; min_p in
+ * [0, 1], 0: all.  (Greedy: top_k = 1.) */
+enum { AIQ_SAMPLE_MAX_K = 1024 };
+typedef struct {
+  double temperature;
+  double top_p;
+  double min_p;
+  int32_t top_k;
+} aiq_sampling;
+
 /* AI_TRANSFORM (Table 1: causal-LM forward with generative decoding, output
  * masked with a pad id; Table 2 Q3 and Q5).  Greedy decoding: every step
  * appends the first index of the largest full-vocabulary logit (final RMSNorm,

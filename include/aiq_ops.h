@@ -77,6 +77,82 @@ aiq_status aiq_op_decode_attention(aiq_ctx* ctx, const void* qkv, int32_t R, int
                                    const void* prefix_kv, int32_t P, const void* own_kv, const int32_t* seq_start,
                                    void* gen_kv, int32_t gen_cap, int32_t slot, void* out);
 
+/* The 8-bit key/value cache: half the bytes of the fp16 one, which bound the
+ * decode steps of AI_TRANSFORM.  (The paper has no counterpart; it is the cache
+ * of its generative decoding, Table 1, held in fewer bits.)
+ *
+ * A block is AIQ_KV_BLOCK = 32 consecutive tokens of one sequence (the last one
+ * may hold fewer).  Per block, KV head and keys / values the scale is
+ * s = max |x| / 127 (fp32), and x is held as the whole number q = 127 x / max |x|,
+ * rounded to the nearest, halves away from zero, -127 .. 127; it stands for q * s.
+ * Sequence i of a packed batch begins at block seq_start[i] / 32 + i: T tokens in n
+ * sequences take T / 32 + n blocks (whole division), some of which stay unused.
+ *
+ *   cache   [blocks][Hkv][64 * hd] bytes, 16-byte aligned: a block's keys, then its
+ *           values, each byte q + 128, in the order in which the attention reads them:
+ *             keys, hd 64 and 128:  [j 4][c hd/64][g 8][t 4][b 16]
+ *                 = key 8 j + g, element 64 c + 16 t + b
+ *             keys, hd 32:          [jp 2][g 8][t 4][jj 2][b 8]
+ *                 = key 16 jp + 8 jj + g, element 8 t + b
+ *             values:               [k 2][c hd/32][gh 4][gl 2][t 4][i 4][jj 2][e 2]
+ *                 = key 16 k + 8 jj + 2 t + e, element 32 c + 8 gh + 2 i + gl
+ *           Bytes of keys that a block does not hold count for nothing.
+ *   scales  fp32 [blocks][Hkv][2] (keys, values), 8-byte aligned. */
+enum { AIQ_KV_BLOCK = 32 };
+
+/* Quantises packed keys and values as they are written.  kv fp16, row t at
+ * kv + t * ldkv: Hkv * hd keys, then Hkv * hd values (a QKV product's rows with kv
+ * at their first key and their own pitch do).  ldkv a multiple of 8, kv 16-byte
+ * aligned.  seq_start int32 [n_seqs + 1] (device), non-decreasing, at most T < 2^31;
+ * rows of kv that no sequence holds are not read, and blocks of the cache that no
+ * token falls into are left as they were.  A NaN or an infinity gives
+ * AIQ_ERR_DEVICE_CHECK, and so does a sequence outside the T rows.  hd in
+ * {32, 64, 128}.  The call synchronises its stream. */
+aiq_status aiq_op_kv_quantize(aiq_ctx* ctx, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                              int32_t n_seqs, int32_t Hkv, int32_t hd, void* cache, float* scales);
+
+/* Reads such a cache back into fp16 rows, q * s rounded once (arguments as
+ * above); rows that no sequence holds are left as they were.  A cache of whole
+ * blocks (the generated tokens' below) is one sequence of 32 * blocks tokens. */
+aiq_status aiq_op_kv_dequantize(aiq_ctx* ctx, const void* cache, const float* scales, int64_t T,
+                                const int32_t* seq_start, int32_t n_seqs, int32_t Hkv, int32_t hd, void* kv,
+                                int64_t ldkv);
+
+/* aiq_op_decode_attention over 8-bit caches.  Row r's token of qkv fp16
+ * [R, (Hq + 2 Hkv) * hd] attends
+ *   the prefix: P tokens, one sequence (NULL when P == 0);
+ *   its own prompt: sequence r of a packed cache of R sequences, seq_start int32
+ *     [R + 1] (device), seq_start[R] <= T (NULL caches when T == 0);
+ *   its generated tokens 0 .. slot - 1 and itself.  Whole blocks of them lie in
+ *     gen_cache / gen_scales, gen_cap / 32 (whole division) blocks per row with no gaps
+ *     (NULL when gen_cap < 32); the open block's, fp16, in gen_tail
+ *     [R][32][2 Hkv hd] (keys, then values), token j at place j % 32.
+ * The call writes this step's key and value to place slot % 32 of gen_tail, and
+ * where that is the last place the block's tiles and scales to gen_cache and
+ * gen_scales: steps 0, 1, 2, ... build the cache, and a block is quantised once,
+ * from what the tail holds.  out fp16 [R, Hq * hd].  hd in {32, 64, 128},
+ * Hq / Hkv <= 8.  qkv, caches, gen_tail and out 16-byte aligned, scales 8-byte.
+ * A sequence outside the T tokens, or an output that is not finite in fp16,
+ * gives AIQ_ERR_DEVICE_CHECK.  The call synchronises its stream. */
+aiq_status aiq_op_decode_attention_q8(aiq_ctx* ctx, const void* qkv, int32_t R, int32_t Hq, int32_t Hkv, int32_t hd,
+                                      const void* prefix_cache, const float* prefix_scales, int32_t P,
+                                      const void* own_cache, const float* own_scales, int64_t T,
+                                      const int32_t* seq_start, void* gen_cache, float* gen_scales, void* gen_tail,
+                                      int32_t gen_cap, int32_t slot, void* out);
+
+typedef enum { AIQ_LOGITS_F32 = 0, AIQ_LOGITS_F16 = 1, AIQ_LOGITS_BF16 = 2 } aiq_logit_type;
+
+/* The next token of R rows of V logits (row pitch ldl elements) for the given
+ * uniform numbers (fp32 [R], device, in [0, 1)); aiq_sampling (aiq.h) defines it.
+ * tokens int32 [R]; probs fp32 [R] (optional): the token's probability among the
+ * kept ones.  -inf marks a token that is ruled out.  Equal inputs give equal
+ * tokens.  A row with a NaN or +inf, a row of -inf alone and a uniform outside
+ * [0, 1) give AIQ_ERR_DEVICE_CHECK; such a row's token and probability are 0, the other
+ * rows' are written.  All pointers are device memory, aligned to their elements;
+ * the call synchronises its stream. */
+aiq_status aiq_op_sample(aiq_ctx* ctx, const void* logits, int32_t type, int64_t ldl, int32_t R, int32_t V,
+                         const float* uniforms, const aiq_sampling* sampling, int32_t* tokens, float* probs);
+
 /* One relational term for aiq_filter_compact_static: `column op constant` on a
  * caller-owned device column of n_rows values (16-byte aligned).  INT32 and
  * INT64 columns compare with `ivalue`, FLOAT32 columns with `fvalue`. */

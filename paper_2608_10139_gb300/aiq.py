@@ -23,6 +23,9 @@ LT, LE, GT, GE, EQ, NE = 0, 1, 2, 3, 4, 5
 AGG_COUNT, AGG_ROW_IDS, AGG_GROUP_LABEL, AGG_GROUP_BUILD_KEY, AGG_SUM = 0, 1, 2, 3, 4
 FLAG_LOGITS, FLAG_RELATIONAL_ONLY = 1, 2
 GEN_MATCH_TOKENS = 1
+LOGITS_F32, LOGITS_F16, LOGITS_BF16 = 0, 1, 2
+KV_BLOCK = 32          # tokens of an 8-bit cache that share a scale
+SAMPLE_MAX_K = 1024    # the largest top_k
 EPI_F16, EPI_ROPE_F16, EPI_RESID_F32, EPI_SWIGLU_F16, EPI_RESID_ADD_F32 = 0, 1, 2, 3, 5
 
 
@@ -76,6 +79,10 @@ class _Generate(C.Structure):
                 ("like_tokens", C.POINTER(C.c_int32)), ("like_len", C.c_int32), ("flags", C.c_int32)]
 
 
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32)]
+
+
 class _Term(C.Structure):
     _fields_ = [("column", C.c_void_p), ("type", C.c_int32), ("op", C.c_int32), ("ivalue", C.c_int64),
                 ("fvalue", C.c_double)]
@@ -118,6 +125,15 @@ _SIGS = {
                          C.c_void_p, C.c_int32, C.c_void_p],
     "aiq_op_decode_attention": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                 C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p],
+    "aiq_op_kv_quantize": [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                           C.c_void_p, C.c_void_p],
+    "aiq_op_kv_dequantize": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                             C.c_void_p, C.c_int64],
+    "aiq_op_decode_attention_q8": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                   C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p],
+    "aiq_op_sample": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
+                      C.POINTER(_Sampling), C.c_void_p, C.c_void_p],
     "aiq_filter_compact_static": [C.POINTER(_Term), C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p],
     "aiq_op_wait_expiry_selftest": [C.c_void_p, C.c_uint64],
 }
@@ -159,6 +175,12 @@ def filter_compact_static(terms, n_rows: int, ids_out: int, count_out: int, stre
     ts = [_Term(p, t, op, int(v) if t != FLOAT32 else 0, float(v)) for p, t, op, v in terms]
     arr = (_Term * max(len(ts), 1))(*ts)
     _check(lib.aiq_filter_compact_static(arr, len(ts), n_rows, ids_out or None, count_out or None, stream or None))
+
+
+def kv_cache_blocks(T: int, n_seqs: int) -> int:
+    """Blocks of an 8-bit cache for T tokens in n_seqs sequences: it holds
+    blocks * Hkv * 64 * hd bytes, and 2 fp32 scales per block and KV head."""
+    return T // KV_BLOCK + n_seqs
 
 
 def _i32(a) -> np.ndarray:
@@ -453,3 +475,31 @@ class Context:
                             gen_kv: int, gen_cap: int, slot: int, out: int, prefix_kv: int = 0, P: int = 0):
         _check(self.lib.aiq_op_decode_attention(self.h, qkv, R, Hq, Hkv, hd, prefix_kv or None, P, own_kv, seq_start,
                                                 gen_kv, gen_cap, slot, out))
+
+    def op_kv_quantize(self, kv: int, ldkv: int, T: int, seq_start: int, n_seqs: int, Hkv: int, hd: int, cache: int,
+                       scales: int):
+        """fp16 keys / values into the 8-bit cache (kv_cache_blocks(T, n_seqs) blocks; see aiq_ops.h)."""
+        _check(self.lib.aiq_op_kv_quantize(self.h, kv or None, ldkv, T, seq_start or None, n_seqs, Hkv, hd,
+                                           cache or None, scales or None))
+
+    def op_kv_dequantize(self, cache: int, scales: int, T: int, seq_start: int, n_seqs: int, Hkv: int, hd: int, kv: int,
+                         ldkv: int):
+        """The 8-bit cache back to fp16 rows."""
+        _check(self.lib.aiq_op_kv_dequantize(self.h, cache or None, scales or None, T, seq_start or None, n_seqs, Hkv,
+                                             hd, kv or None, ldkv))
+
+    def op_decode_attention_q8(self, qkv: int, R: int, Hq: int, Hkv: int, hd: int, own_cache: int, own_scales: int,
+                               T: int, seq_start: int, gen_cache: int, gen_scales: int, gen_tail: int, gen_cap: int,
+                               slot: int, out: int, prefix: int = 0, prefix_scales: int = 0, P: int = 0):
+        """op_decode_attention over 8-bit caches; appends the step's key and value."""
+        _check(self.lib.aiq_op_decode_attention_q8(self.h, qkv or None, R, Hq, Hkv, hd, prefix or None,
+                                                   prefix_scales or None, P, own_cache or None, own_scales or None, T,
+                                                   seq_start or None, gen_cache or None, gen_scales or None,
+                                                   gen_tail or None, gen_cap, slot, out or None))
+
+    def op_sample(self, logits: int, type: int, ldl: int, R: int, V: int, uniforms: int, tokens: int,
+                  temperature: float = 1.0, top_k: int = 50, top_p: float = 1.0, min_p: float = 0.0, probs: int = 0):
+        """A token per row of logits (LOGITS_*) from the uniforms in [0, 1) and, optionally, its probability."""
+        s = _Sampling(temperature, top_p, min_p, top_k)
+        _check(self.lib.aiq_op_sample(self.h, logits or None, type, ldl, R, V, uniforms or None, C.byref(s),
+                                      tokens or None, probs or None))

@@ -8,6 +8,7 @@
 // count, the chunk table) and the final results; no intermediate array
 // crosses PCIe (Section 3.3, H2D boundary consolidation).
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <map>
@@ -1623,6 +1624,33 @@ aiq_status model_alloc(aiq_ctx* c, ModelD& m, size_t count, T** out) {
   return AIQ_OK;
 }
 
+bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// What the two copies between fp16 rows and the 8-bit cache ask of their arguments.
+aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                            int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache, const float* scales) {
+  if (!c || !kv || !seq_start || !cache || !scales || T < 0 || T > INT32_MAX || n_seqs < 0 || Hkv <= 0)
+    return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (!(hd == 32 || hd == 64 || hd == 128)) return fail(AIQ_ERR_UNSUPPORTED, "hd must be 32, 64 or 128");
+  if (ldkv < 2 * int64_t(Hkv) * hd || ldkv % 8)
+    return fail(AIQ_ERR_INVALID_ARG, "ldkv must be at least 2 Hkv hd and a multiple of 8");
+  if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(seq_start, 4))
+    return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
+  if ((T / AIQ_KV_BLOCK + n_seqs) * Hkv > (int64_t(1) << 33))
+    return fail(AIQ_ERR_UNSUPPORTED, "more than 2^33 (block, KV head) pairs");
+  return AIQ_OK;
+}
+
+aiq_status check_sampling(const aiq_sampling& s, int V) {
+  if (!(s.temperature > 0) || std::isinf(s.temperature))
+    return fail(AIQ_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (s.top_k < 1 || s.top_k > V) return fail(AIQ_ERR_INVALID_ARG, "top_k must be 1..vocab");
+  if (s.top_k > AIQ_SAMPLE_MAX_K) return fail(AIQ_ERR_UNSUPPORTED, "top_k above 1024");
+  if (!(s.top_p > 0 && s.top_p <= 1)) return fail(AIQ_ERR_INVALID_ARG, "top_p must be in (0, 1]");
+  if (!(s.min_p >= 0 && s.min_p <= 1)) return fail(AIQ_ERR_INVALID_ARG, "min_p must be in [0, 1]");
+  return AIQ_OK;
+}
+
 int pick_bn(int n) { return n % 256 == 0 ? 256 : 128; }
 
 }  // namespace
@@ -2138,6 +2166,76 @@ aiq_status aiq_op_decode_attention(aiq_ctx* c, const void* qkv, int32_t R, int32
                                         static_cast<const __half*>(own_kv), seq_start, static_cast<__half*>(gen_kv),
                                         gen_cap, slot, static_cast<__half*>(out), c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_kv_quantize(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                              int32_t n_seqs, int32_t Hkv, int32_t hd, void* cache, float* scales) {
+  AIQ_TRY(check_cache_rows(c, kv, ldkv, T, seq_start, n_seqs, Hkv, hd, cache, scales));
+  if (T == 0 || n_seqs == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const int e = launch_kv_quantize(static_cast<const __half*>(kv), ldkv, T, seq_start, n_seqs, Hkv, hd,
+                                   static_cast<uint8_t*>(cache), scales, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("cache quantisation launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_kv_dequantize(aiq_ctx* c, const void* cache, const float* scales, int64_t T, const int32_t* seq_start,
+                                int32_t n_seqs, int32_t Hkv, int32_t hd, void* kv, int64_t ldkv) {
+  AIQ_TRY(check_cache_rows(c, kv, ldkv, T, seq_start, n_seqs, Hkv, hd, cache, scales));
+  if (T == 0 || n_seqs == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const int e = launch_kv_dequantize(static_cast<const uint8_t*>(cache), scales, T, seq_start, n_seqs, Hkv, hd,
+                                     static_cast<__half*>(kv), ldkv, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("cache read-back launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_decode_attention_q8(aiq_ctx* c, const void* qkv, int32_t R, int32_t Hq, int32_t Hkv, int32_t hd,
+                                      const void* prefix_cache, const float* prefix_scales, int32_t P,
+                                      const void* own_cache, const float* own_scales, int64_t T,
+                                      const int32_t* seq_start, void* gen_cache, float* gen_scales, void* gen_tail,
+                                      int32_t gen_cap, int32_t slot, void* out) {
+  if (!c || !qkv || !seq_start || !gen_tail || !out || R < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || P < 0 ||
+      (P > 0 && (!prefix_cache || !prefix_scales)) || T < 0 || (T > 0 && (!own_cache || !own_scales)) || gen_cap < 1 ||
+      (gen_cap >= AIQ_KV_BLOCK && (!gen_cache || !gen_scales)) || slot < 0 || slot >= gen_cap)
+    return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (!(hd == 32 || hd == 64 || hd == 128) || Hq / Hkv > 8)
+    return fail(AIQ_ERR_UNSUPPORTED, "hd must be 32, 64 or 128 and Hq / Hkv <= 8");
+  if (!aligned(qkv, 16) || !aligned(prefix_cache, 16) || !aligned(own_cache, 16) || !aligned(gen_cache, 16) ||
+      !aligned(gen_tail, 16) || !aligned(out, 16) || !aligned(prefix_scales, 8) || !aligned(own_scales, 8) ||
+      !aligned(gen_scales, 8) || !aligned(seq_start, 4))
+    return fail(AIQ_ERR_INVALID_ARG, "qkv, caches, gen_tail and out must be 16-byte aligned, scales 8-byte aligned");
+  if (int64_t(R) * Hkv > INT32_MAX) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^31 - 1 (row, KV head) pairs");
+  if (R == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const DecodeQ8 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, Hq, Hkv, hd,
+                   static_cast<const uint8_t*>(prefix_cache), prefix_scales, P, static_cast<const uint8_t*>(own_cache),
+                   own_scales, T, seq_start, static_cast<uint8_t*>(gen_cache), gen_scales, gen_cap,
+                   static_cast<__half*>(gen_tail), slot, static_cast<__half*>(out)};
+  const int e = launch_decode_attention_q8(d, c->d_err, c->num_sms, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_sample(aiq_ctx* c, const void* logits, int32_t type, int64_t ldl, int32_t R, int32_t V,
+                         const float* uniforms, const aiq_sampling* s, int32_t* tokens, float* probs) {
+  if (!c || !logits || !uniforms || !s || !tokens || R < 0 || V < 1 || ldl < V)
+    return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (type < AIQ_LOGITS_F32 || type > AIQ_LOGITS_BF16) return fail(AIQ_ERR_INVALID_ARG, "unknown logit type");
+  AIQ_TRY(check_sampling(*s, V));
+  if (!aligned(logits, type == AIQ_LOGITS_F32 ? 4 : 2) || !aligned(uniforms, 4) || !aligned(tokens, 4) ||
+      !aligned(probs, 4))
+    return fail(AIQ_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+  if (R == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const int e = launch_sample(logits, type, ldl, R, V, uniforms, s->temperature, s->top_k, s->top_p, s->min_p, tokens,
+                              probs, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("sampling launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);
 }

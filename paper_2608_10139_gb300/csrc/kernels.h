@@ -269,6 +269,47 @@ void launch_like_match(const int32_t* gen_tok, const int32_t* gen_len, int64_t S
                        int plen, int32_t* match, cudaStream_t s);
 void launch_gather_rows_i32(const int32_t* src, int width, const int32_t* pos, int64_t n, int32_t* out,
                             cudaStream_t s);
+// ------------------------------------------------------- 8-bit K/V cache ---
+// Packed fp16 rows (keys at kv + row * ld, values Hkv * hd further) into tiles of
+// 32 tokens of one KV head and two scales each, and back (tile8.cuh).  Sequence i
+// holds rows [seq_start[i], seq_start[i + 1]); rows from T on belong to none.
+// Returns 0 or a cudaError_t value.
+int launch_kv_quantize(const __half* kv, int64_t ld, int64_t T, const int32_t* seq_start, int n_seqs, int Hkv, int hd,
+                       uint8_t* cache, float* scales, int* err, cudaStream_t s);
+int launch_kv_dequantize(const uint8_t* cache, const float* scales, int64_t T, const int32_t* seq_start, int n_seqs,
+                         int Hkv, int hd, __half* kv, int64_t ld, int* err, cudaStream_t s);
+// launch_decode_attention over that cache: prefix and own prompt in tiles, generated
+// tokens in gen_cap / 32 tiles per row, those of the open block in tail
+// [R][32][2 Hkv hd]; this step's key and value are appended to it, and the step
+// that fills a block writes its tiles.
+struct DecodeQ8 {
+  const __half* qkv;
+  int64_t ldq;
+  int R, Hq, Hkv, hd;
+  const uint8_t* prefix;
+  const float* prefix_scales;
+  int P;
+  const uint8_t* own;
+  const float* own_scales;
+  int64_t T;
+  const int32_t* seq_start;
+  uint8_t* gen;
+  float* gen_scales;
+  int gen_cap;
+  __half* tail;
+  int slot;
+  __half* out;
+};
+int launch_decode_attention_q8(const DecodeQ8& d, int* err, int num_sms, cudaStream_t s);
+
+// -------------------------------------------------------------- sampling ---
+enum LogitType : int { LOGITS_F32 = 0, LOGITS_F16 = 1, LOGITS_BF16 = 2 };
+constexpr int kSampleKeepMax = 1024;  // the largest top_k
+// tokens[r] of R rows of V logits (row pitch ld elements) for the uniforms u[r]; probs
+// may be null.  Returns 0 or a cudaError_t value.
+int launch_sample(const void* logits, int type, int64_t ld, int R, int V, const float* u, double temperature, int top_k,
+                  double top_p, double min_p, int32_t* tokens, float* probs, int* err, cudaStream_t s);
+
 // ---------------------------------------------------------------- pairs ---
 // Device scratch of the Q4 self-join over S candidates (sizes in elements):
 // keys, keys_tmp [S] u64; vals, vals_tmp, heads, counts [S] i32; head_excl,
