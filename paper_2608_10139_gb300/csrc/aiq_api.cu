@@ -2216,7 +2216,10 @@ aiq_status aiq_op_decode_attention_q8(aiq_ctx* c, const void* qkv, int32_t R, in
                    static_cast<const uint8_t*>(prefix_cache), prefix_scales, P, static_cast<const uint8_t*>(own_cache),
                    own_scales, T, seq_start, static_cast<uint8_t*>(gen_cache), gen_scales, gen_cap,
                    static_cast<__half*>(gen_tail), slot, static_cast<__half*>(out)};
-  const int e = launch_decode_attention_q8(d, c->d_err, c->num_sms, c->stream);
+  float* partial = nullptr;
+  if (const size_t floats = decode_q8_floats(d, c->num_sms))
+    AIQ_TRY(with_room(c, [&] { return ws(c, "op.q8_partial", floats, &partial); }));
+  const int e = launch_decode_attention_q8(d, partial, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);

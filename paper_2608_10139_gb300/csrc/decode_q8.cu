@@ -2,6 +2,8 @@
 // row r's new token against the shared prefix, its own prompt, the generated
 // tokens in whole blocks (all 8 bits) and the open block of fewer than 32
 // generated tokens, which stays fp16 until the step that fills it quantises it.
+#include <algorithm>
+
 #include "kernels.h"
 #include "tile8.cuh"
 
@@ -29,31 +31,55 @@ struct DecQ8Args {
   int* err;
 };
 
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
-  // rows 8 .. 15 of A are zero
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(0u), "r"(a2), "r"(0u), "r"(b0), "r"(b1));
+// d (+)= A B.
+template <bool FIRST>
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         const uint32_t (&b)[2]) {
+  if constexpr (FIRST)  // the addend is a constant, which takes no register to be cleared
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]), "f"(0.f));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 
-// A warp's running softmax of one (row, KV head): lane 4 g + t holds query head
-// g's elements 32 c + 8 t .. + 7 of the output.
+__device__ __forceinline__ void cp_async16(uint32_t saddr, const void* gmem) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(saddr), "l"(gmem) : "memory");
+}
+
+// 2^x to 2^-22 of it; 0 for -infinity.
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A warp's running softmax of one (row, KV head).  Keys and values are the A
+// operands (16 keys, or 16 elements of the output, as rows), the G <= 8 query
+// heads the eight columns: no row of a product is padding, and a lane's numbers
+// all belong to heads 2 t and 2 t + 1 (lane = 4 g + t).
 template <int HD>
 struct Attn8 {
   static constexpr int KS = HD / 16;
   static constexpr int C32 = HD / 32;
+  static constexpr int C64 = HD == 32 ? 1 : HD / 64;
+  static constexpr int PER = HD == 32 ? 8 : 16;  // a lane's consecutive elements of a key
   uint32_t q[KS][2];
-  float o[HD / 4];
-  float m, l;
+  // [c][i / 2][2 (i % 2) + head]: element 32 c + 8 (g / 2) + 2 i + g % 2 of heads 2 t, 2 t + 1
+  float o[C32][2][4];
+  float m[2], l[2];
 
+  // k-step k takes elements 64 c + 16 t + 4 kk .. + 3 (HD 32: 8 t + 4 k .. + 3) of every lane's key
   __device__ __forceinline__ void begin(const __half* qrow, int G) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    constexpr int PER = HD == 32 ? 8 : 16;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      // k-step k takes elements 64 c + 16 t + 4 kk .. + 3 (HD 32: 8 t + 4 k .. + 3) of every lane's key
       const int at = HD == 32 ? PER * t + 4 * k : 64 * (k / 4) + PER * t + 4 * (k % 4);
       uint2 v = make_uint2(0u, 0u);
       if (g < G) v = *reinterpret_cast<const uint2*>(qrow + g * HD + at);
@@ -61,265 +87,715 @@ struct Attn8 {
       q[k][1] = v.y;
     }
 #pragma unroll
-    for (int i = 0; i < HD / 4; ++i) o[i] = 0.f;
-    m = -INFINITY;
-    l = 0.f;
+    for (int c = 0; c < C32; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) o[c][i][0] = o[c][i][1] = o[c][i][2] = o[c][i][3] = 0.f;
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
   }
 
-  // Scores (log2 units, keys >= n masked) to probabilities relative to the
-  // block's own maximum, so that the largest is exactly 1 in fp16; the block's
-  // product joins the running output in fp32, times its value scale.
-  __device__ __forceinline__ void softmax(float (&sc)[4][4], float scale, int n, uint32_t (&p)[2][2], float& c0,
-                                          float& c1) {
-    const int t = threadIdx.x & 3;
-    float mx = -INFINITY;
+  // Scores of keys 16 k + 8 h + g ([k][2 h + head], keys >= n masked) times scale,
+  // in log2 units, to probabilities relative to m, the largest score so far.  m
+  // follows only when it is left behind by more than 8, and then the output is
+  // scaled down: a probability is at most 256, and the running output need not be
+  // touched for most tiles.  hi is a probability rounded to fp16, lo what the
+  // rounding left: the two keep the output's error at that of its own rounding.
+  __device__ __forceinline__ void softmax(float (&sc)[2][4], float scale, int n, uint32_t (&hi)[2][2],
+                                          uint32_t (&lo)[2][2]) {
+    const int g = (threadIdx.x & 31) >> 2;
+    if (n < kTileKeys) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        sc[j][e] = 8 * j + 2 * t + e < n ? sc[j][e] * scale : -INFINITY;
-        mx = fmaxf(mx, sc[j][e]);
-      }
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    const float mn = fmaxf(m, mx), mb = mx == -INFINITY ? 0.f : mx;
-    c0 = m == -INFINITY ? 0.f : exp2f(m - mn);
-    c1 = mx == -INFINITY ? 0.f : exp2f(mx - mn);
-    m = mn;
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        sc[j][e] = exp2f(sc[j][e] - mb);
-        sum += sc[j][e];
-      }
-    l = l * c0 + sum * c1;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      p[k][0] = as_u32(__floats2half2_rn(sc[2 * k][0], sc[2 * k][1]));
-      p[k][1] = as_u32(__floats2half2_rn(sc[2 * k + 1][0], sc[2 * k + 1][1]));
+        for (int e = 0; e < 4; ++e)
+          if (16 * k + 8 * (e / 2) + g >= n) sc[k][e] = -INFINITY;
     }
+    float mb[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+      mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
+      mb[1] = fmaxf(mb[1], __shfl_xor_sync(0xffffffffu, mb[1], d));
+    }
+    mb[0] *= scale;  // finite: a block has a key, and products of finite numbers do not overflow
+    mb[1] *= scale;
+    if (__any_sync(0xffffffffu, mb[0] > m[0] + 8.f || mb[1] > m[1] + 8.f)) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float mn = fmaxf(m[e], mb[e]), f = exp2_approx(m[e] - mn);
+        m[e] = mn;
+        l[e] *= f;
+#pragma unroll
+        for (int c = 0; c < C32; ++c)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) o[c][i][e] *= f, o[c][i][2 + e] *= f;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = exp2_approx(fmaf(sc[k][2 * h], scale, -m[0]));
+        const float p1 = exp2_approx(fmaf(sc[k][2 * h + 1], scale, -m[1]));
+        l[0] += p0;  // a lane's sums cover its own keys only; sum_keys adds them at the end
+        l[1] += p1;
+        const __half2 p = __floats2half2_rn(p0, p1);
+        const float2 back = __half22float2(p);
+        // key 8 h + g's two heads become head g's two keys
+        hi[k][h] = movmatrix_t(as_u32(p));
+        lo[k][h] = movmatrix_t(as_u32(__floats2half2_rn(p0 - back.x, p1 - back.y)));
+      }
   }
 
-  // One tile of 8 bits: n keys (1 .. 32), scales s.
+  __device__ __forceinline__ void join(int c, const float (&acc)[2][4], float s) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[c][i][e] = fmaf(acc[i][e], s, o[c][i][e]);
+  }
+
+  // One tile of 8 bits: n keys (1 .. 32), scales s.  The key scale multiplies the
+  // scores, the value scale the block's share of the output: the products take
+  // the whole numbers, which fp16 holds exactly.
   __device__ __forceinline__ void tile(const uint8_t* tile, float2 s, int n, float scale_log2) {
     const int lane = threadIdx.x & 31;
     const uint4* kin = reinterpret_cast<const uint4*>(tile);
     const uint4* vin = reinterpret_cast<const uint4*>(tile + kTileKeys * HD);
-    float sc[4][4];
+    float sc[2][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
-    constexpr int LOADS = HD / 16;  // of the keys
+    for (int k = 0; k < 2; ++k)  // keys 16 k + g and + 8
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const uint4 v = kin[i * 32 + lane];
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      for (int c = 0; c < C64; ++c) {
+        uint32_t x[KS / C64][2][2];
+        if constexpr (HD == 32) {
+          const uint4 v = kin[k * 32 + lane];
+          tile8_to_half(v.x, x[0][0][0], x[0][0][1]);
+          tile8_to_half(v.y, x[1][0][0], x[1][0][1]);
+          tile8_to_half(v.z, x[0][1][0], x[0][1][1]);
+          tile8_to_half(v.w, x[1][1][0], x[1][1][1]);
+        } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t b0, b1;
-        tile8_to_half(w[e], b0, b1);
-        const int j = HD == 32 ? 2 * i + e / 2 : i / (HD / 64 + (HD == 32));
-        const int k = HD == 32 ? e % 2 : 4 * (i % (HD / 64 + (HD == 32))) + e;
-        mma16816(sc[j], q[k][0], q[k][1], b0, b1);
+          for (int h = 0; h < 2; ++h) {
+            const uint4 v = kin[((2 * k + h) * C64 + c) * 32 + lane];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tile8_to_half(w[i], x[i][h][0], x[i][h][1]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < KS / C64; ++i) {
+          const uint32_t(&b)[2] = q[c * (KS / C64) + i];
+          if (c == 0 && i == 0)
+            mma16816<true>(sc[k], x[i][0][0], x[i][1][0], x[i][0][1], x[i][1][1], b);
+          else
+            mma16816<false>(sc[k], x[i][0][0], x[i][1][0], x[i][0][1], x[i][1][1], b);
+        }
       }
-    }
-    uint32_t p[2][2];
-    float c0, c1;
-    softmax(sc, scale_log2 * s.x, n, p, c0, c1);
-    c1 *= s.y;
+    uint32_t hi[2][2], lo[2][2];
+    softmax(sc, scale_log2 * s.x, n, hi, lo);
 #pragma unroll
     for (int c = 0; c < C32; ++c) {
-      float acc[4][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      float acc[2][4];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint4 v = vin[(k * C32 + c) * 32 + lane];
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t x[4][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t b0, b1;
-          tile8_to_half(w[i], b0, b1);
-          mma16816(acc[i], p[k][0], p[k][1], b0, b1);
+        for (int i = 0; i < 4; ++i) tile8_to_half(w[i], x[i][0], x[i][1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (k == 0)
+            mma16816<true>(acc[i], x[2 * i][0], x[2 * i + 1][0], x[2 * i][1], x[2 * i + 1][1], hi[k]);
+          else
+            mma16816<false>(acc[i], x[2 * i][0], x[2 * i + 1][0], x[2 * i][1], x[2 * i + 1][1], hi[k]);
+          mma16816<false>(acc[i], x[2 * i][0], x[2 * i + 1][0], x[2 * i][1], x[2 * i + 1][1], lo[k]);
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) o[8 * c + 2 * i + e] = o[8 * c + 2 * i + e] * c0 + acc[i][e] * c1;
+      join(c, acc, s.y);
     }
   }
 
-  // The open block: n fp16 keys and values (k(key) / v(key) point at HD elements).
-  template <typename KRow, typename VRow>
-  __device__ __forceinline__ void open(KRow k_of, VRow v_of, int n, float scale_log2) {
+  // The open block: n fp16 keys and values, [32][HD] each in shared memory.
+  __device__ __forceinline__ void open(const __half* sk, const __half* sv, int n, float scale_log2) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    constexpr int PER = HD == 32 ? 8 : 16, C64 = HD == 32 ? 1 : HD / 64;
-    float sc[4][4];
+    float sc[2][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
-      const bool live = 8 * j + g < n;
-      const __half* row = live ? k_of(8 * j + g) : nullptr;
+    for (int k = 0; k < 2; ++k) {
+      sc[k][0] = sc[k][1] = sc[k][2] = sc[k][3] = 0.f;
+      if (16 * k >= n) continue;
+      const __half* row = sk + (16 * k + g) * HD;  // rows >= n hold anything: their scores are masked
 #pragma unroll
       for (int c = 0; c < C64; ++c)
 #pragma unroll
         for (int w = 0; w < PER / 8; ++w) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (live) v = *reinterpret_cast<const uint4*>(row + 64 * c + PER * t + 8 * w);
-          const int k = HD == 32 ? 0 : 4 * c + 2 * w;
-          mma16816(sc[j], q[k][0], q[k][1], v.x, v.y);
-          mma16816(sc[j], q[k + 1][0], q[k + 1][1], v.z, v.w);
+          const int at = 64 * c + PER * t + 8 * w, i = HD == 32 ? 0 : 4 * c + 2 * w;
+          const uint4 v0 = *reinterpret_cast<const uint4*>(row + at);
+          const uint4 v1 = *reinterpret_cast<const uint4*>(row + 8 * HD + at);
+          mma16816<false>(sc[k], v0.x, v1.x, v0.y, v1.y, q[i]);
+          mma16816<false>(sc[k], v0.z, v1.z, v0.w, v1.w, q[i + 1]);
         }
     }
-    uint32_t p[2][2];
-    float c0, c1;
-    softmax(sc, scale_log2, n, p, c0, c1);
+    uint32_t hi[2][2], lo[2][2];
+    softmax(sc, scale_log2, n, hi, lo);
 #pragma unroll
     for (int c = 0; c < C32; ++c) {
-      float acc[4][4];
+      float acc[2][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      for (int i = 0; i < 2; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        uint4 v[2];
+        if (16 * k >= n) continue;
+        uint32_t x[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int key = 16 * k + 8 * h + g;
-          v[h] = make_uint4(0u, 0u, 0u, 0u);  // a masked key's value may be anything, and 0 times it too
-          if (key < n) v[h] = *reinterpret_cast<const uint4*>(v_of(key) + 32 * c + 8 * t);
+          uint4 v = *reinterpret_cast<const uint4*>(sv + key * HD + 32 * c + 8 * t);
+          if (key >= n) v = make_uint4(0u, 0u, 0u, 0u);  // 0 times anything may be NaN
+          x[h][0] = movmatrix_t(v.x), x[h][1] = movmatrix_t(v.y), x[h][2] = movmatrix_t(v.z), x[h][3] = movmatrix_t(v.w);
         }
-        mma16816(acc[0], p[k][0], p[k][1], movmatrix_t(v[0].x), movmatrix_t(v[1].x));
-        mma16816(acc[1], p[k][0], p[k][1], movmatrix_t(v[0].y), movmatrix_t(v[1].y));
-        mma16816(acc[2], p[k][0], p[k][1], movmatrix_t(v[0].z), movmatrix_t(v[1].z));
-        mma16816(acc[3], p[k][0], p[k][1], movmatrix_t(v[0].w), movmatrix_t(v[1].w));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma16816<false>(acc[i], x[0][2 * i], x[0][2 * i + 1], x[1][2 * i], x[1][2 * i + 1], hi[k]);
+          mma16816<false>(acc[i], x[0][2 * i], x[0][2 * i + 1], x[1][2 * i], x[1][2 * i + 1], lo[k]);
+        }
       }
+      join(c, acc, 1.f);
+    }
+  }
+
+  __device__ __forceinline__ void sum_keys() {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int d = 4; d < 32; d <<= 1) {
+      l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+      l[1] += __shfl_xor_sync(0xffffffffu, l[1], d);
+    }
+  }
+
+  // Head 2 t + g % 2's elements 32 c + 8 (g / 2) .. + 7, of the lane's own and its neighbour's numbers.
+  __device__ __forceinline__ void eight(int c, float (&v)[8]) const {
+    const bool odd = threadIdx.x >> 2 & 1;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) o[8 * c + 2 * i + e] = o[8 * c + 2 * i + e] * c0 + acc[i][e] * c1;
+    for (int i = 0; i < 4; ++i) {
+      const float h0 = o[c][i / 2][2 * (i % 2)], h1 = o[c][i / 2][2 * (i % 2) + 1];
+      const float other = __shfl_xor_sync(0xffffffffu, odd ? h0 : h1, 4);
+      v[2 * i] = odd ? other : h0;
+      v[2 * i + 1] = odd ? h1 : other;
     }
   }
 };
 
-constexpr int kQ8Warps = 8;
-
-// A block per (row, KV head); its warps take the tiles in turns and merge their
-// (maximum, sum, output) at the end.
-template <int HD>
-__global__ void __launch_bounds__(kQ8Warps * 32) k_decode_q8(DecQ8Args a) {
-  grid_launch_next();
-  grid_wait();
-  constexpr int TB = tile8_bytes(HD);
-  __shared__ float sm[kQ8Warps][8], sl[kQ8Warps][8];
-  __shared__ __align__(16) float so[kQ8Warps][8][HD];
-  const int r = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int kd = a.Hkv * HD;
-  const __half* qrow = a.qkv + r * a.ldq;
-  int64_t st = a.seq_start[r];
-  int64_t len = a.seq_start[r + 1] - st;
-  if (st < 0 || len < 0 || st + len > a.T) {
-    if (threadIdx.x == 0) set_dev_error(a.err, DEVERR_BOUNDS);
-    st = len = 0;
+// A (row, KV head): its prompt's place and its number of tiles (prefix, own
+// prompt, generated).  The open block's keys and its values come after them.
+struct Task8 {
+  int r, h;
+  int64_t st;  // first prompt token
+  int len;
+  int tiles;
+};
+__device__ __forceinline__ int tiles_of(int keys) { return (keys + kTileKeys - 1) / kTileKeys; }
+__device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int64_t i, int64_t n_tasks) {
+  Task8 t{0, 0, 0, 0, 0};
+  if (i >= n_tasks) return t;
+  t.r = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(a.Hkv));
+  t.h = static_cast<int>(i) - t.r * a.Hkv;
+  t.st = a.seq_start[t.r];
+  const int64_t end = a.seq_start[t.r + 1];
+  if (t.st < 0 || end < t.st || end > a.T) {
+    set_dev_error(a.err, DEVERR_BOUNDS);
+    t.st = 0;
+  } else {
+    t.len = static_cast<int>(end - t.st);
   }
-  const int np = (a.P + kTileKeys - 1) / kTileKeys;
-  const int64_t no = (len + kTileKeys - 1) / kTileKeys, ng = a.slot / kTileKeys;
-  const int64_t own0 = tile8_first_block(st, r), gen0 = r * a.gen_blocks;
+  t.tiles = tiles_of(a.P) + tiles_of(t.len) + a.slot / kTileKeys;
+  return t;
+}
 
-  Attn8<HD> at;
-  at.begin(qrow + h * a.G * HD, a.G);
-  for (int64_t e = warp; e < np + no + ng; e += kQ8Warps) {
-    const uint8_t* c;
-    const float2* s;
-    int64_t unit;
-    int n = kTileKeys;
-    if (e < np) {
-      unit = e * a.Hkv + h;
-      c = a.pc, s = a.ps;
-      n = min(n, a.P - static_cast<int>(e) * kTileKeys);
-    } else if (e < np + no) {
-      unit = (own0 + (e - np)) * a.Hkv + h;
-      c = a.oc, s = a.os;
-      const int64_t left = len - (e - np) * kTileKeys;
-      n = left < n ? static_cast<int>(left) : n;
-    } else {
-      unit = (gen0 + (e - np - no)) * a.Hkv + h;
-      c = a.gc, s = a.gs;
-    }
-    at.tile(c + unit * TB, s[unit], n, a.scale_log2);
+// A warp's ring of tile-sized slots in shared memory, filled by bulk copies an
+// entry each: a tile, the open block's keys or its values (32 fp16 rows are as
+// many bytes as a tile).  Lane s keeps slot s's scales and number of keys, so that
+// they are on their way as early as the tile.
+__device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t phase, volatile int* abort_flag, int* err) {
+  return mbar_wait_bounded(bar, phase, abort_flag, err);
+}
+template <int HD, int STAGES>
+struct Ring8 {
+  static constexpr int TB = tile8_bytes(HD);
+  uint8_t* slots;
+  uint64_t* full;
+  volatile int* abort_flag;
+  int* err;
+  int put, get;            // slots
+  uint32_t phases;         // bit s: the phase of slot s's barrier that is waited for next
+  uint32_t busy;           // bit s: a tile is on its way to slot s or there
+  float2 scale;            // lane s: slot s's
+  int keys;
+
+  __device__ __forceinline__ void begin(uint8_t* slots_, uint64_t* full_, volatile int* abort_, int* err_) {
+    slots = slots_, full = full_, abort_flag = abort_, err = err_;
+    put = get = keys = 0;
+    busy = 0;
+    phases = 0;
+    scale = make_float2(0.f, 0.f);
   }
-  const int open = a.slot % kTileKeys;
-  if (warp == static_cast<int>((np + no + ng) % kQ8Warps)) {
-    __half* tail = a.tail + static_cast<int64_t>(r) * kTileKeys * 2 * kd + h * HD;
-    const __half* now = qrow + (a.Hq + h) * HD;  // this step's key; its value kd further
-    const auto k_of = [&](int key) { return key == open ? now : tail + static_cast<int64_t>(key) * 2 * kd; };
-    const auto v_of = [&](int key) { return (key == open ? now : tail + static_cast<int64_t>(key) * 2 * kd) + kd; };
-    at.open(k_of, v_of, open + 1, a.scale_log2);
-    // this step's key and value into the open block
-    for (int i = lane; i < HD / 4; i += 32) {
-      const int v = i / (HD / 8), part = i % (HD / 8);
-      reinterpret_cast<uint4*>(tail + static_cast<int64_t>(open) * 2 * kd + v * kd)[part] =
-          reinterpret_cast<const uint4*>(now + v * kd)[part];
-    }
-    if (open == kTileKeys - 1) {  // the block is complete
-      const int64_t unit = (gen0 + ng) * a.Hkv + h;
-      const float ak = tile8_quantize_keys<HD>(k_of, kTileKeys, a.gc + unit * TB);
-      const float av = tile8_quantize_values<HD>(v_of, kTileKeys, a.gc + unit * TB);
-      if (lane == 0) {
-        a.gs[unit] = make_float2(__fdiv_rn(ak, 127.f), __fdiv_rn(av, 127.f));
-        if (!(ak <= 65504.f && av <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);
+  // All lanes call; the slot must have been used up by every lane before.
+  __device__ __forceinline__ void issue_tile(const uint8_t* at, const float2* s, int n) {
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) {
+      // a block's first keys are a prefix of both halves (8 or 16 keys at a time)
+      constexpr int KSTEP = HD == 32 ? 16 : 8;
+      uint8_t* dst = slots + put * TB;
+      if (n == kTileKeys) {
+        mbar_arrive_expect_tx(&full[put], TB);
+        bulk_copy_g2s(dst, at, TB, &full[put]);
+      } else {
+        const uint32_t kb = (n + KSTEP - 1) / KSTEP * KSTEP * HD, vb = (n + 15) / 16 * 16 * HD;
+        mbar_arrive_expect_tx(&full[put], kb + vb);
+        bulk_copy_g2s(dst, at, kb, &full[put]);
+        bulk_copy_g2s(dst + kTileKeys * HD, at + kTileKeys * HD, vb, &full[put]);
       }
     }
-  }
-  at.l += __shfl_xor_sync(0xffffffffu, at.l, 1);
-  at.l += __shfl_xor_sync(0xffffffffu, at.l, 2);
-  if (t == 0) {
-    sm[warp][g] = at.m;
-    sl[warp][g] = at.l;
-  }
-#pragma unroll
-  for (int c = 0; c < HD / 32; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) so[warp][g][32 * c + 8 * t + i] = at.o[8 * c + i];
-  __syncthreads();
-  __half* orow = a.out + (static_cast<int64_t>(r) * a.Hq + h * a.G) * HD;
-  for (int i = threadIdx.x; i < a.G * HD; i += kQ8Warps * 32) {
-    const int head = i / HD, d = i % HD;
-    float M = -INFINITY, L = 0.f, O = 0.f;
-#pragma unroll
-    for (int w = 0; w < kQ8Warps; ++w) M = fmaxf(M, sm[w][head]);
-#pragma unroll
-    for (int w = 0; w < kQ8Warps; ++w) {
-      const float f = sm[w][head] == -INFINITY ? 0.f : exp2f(sm[w][head] - M);
-      L += sl[w][head] * f;
-      O += so[w][head][d] * f;
+    if (lane == put) {
+      scale = *s;
+      keys = n;
     }
-    const float v = O / L;
-    if (!(fabsf(v) <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);
-    orow[i] = __float2half_rn(v);
+    busy |= 1u << put;
+    issued();
+  }
+  // n fp16 rows of HD elements: rows 0 .. n - 2 at `rows` (pitch ld), row n - 1 at
+  // `last`.  Sixteen bytes per lane and copy: a bulk copy per row costs a lane's
+  // turn each (some 400 instructions a task).
+  __device__ __forceinline__ void issue_rows(const __half* rows, int64_t ld, const __half* last, int n) {
+    constexpr int CH = HD / 8, STEP = 32 / CH;  // lanes per row, rows at a time
+    const int lane = threadIdx.x & 31, part = lane % CH * 8;
+    const __half* from = rows + lane / CH * ld + part;
+    uint32_t to = smem_u32(slots + put * TB) + lane * 16;
+    for (int row = lane / CH; row < n; row += STEP, from += STEP * ld, to += 32 * 16)
+      cp_async16(to, row == n - 1 ? last + part : from);
+    issued();
+  }
+  __device__ __forceinline__ void issued() {
+    put = put + 1 == STAGES ? 0 : put + 1;
+  }
+  // The next entry, a tile, has arrived.  False: a wait ran out somewhere; the
+  // warp's copies are then awaited.
+  __device__ __forceinline__ bool wait() {
+    const uint32_t phase = phases >> get & 1;
+    bool ok = mbar_try_wait(&full[get], phase);
+    if (!ok) ok = wait_longer(&full[get], phase, abort_flag, err);
+    if (__all_sync(0xffffffffu, ok)) {
+      phases ^= 1u << get;
+      return true;
+    }
+    wait_rows();
+    volatile int never = 0;
+    for (int i = 0; i < STAGES; ++i)  // a barrier without copies in flight stands at the phase before
+      if (busy >> i & 1) mbar_wait_bounded(&full[i], phases >> i & 1, &never, nullptr, 200000000ull);
+    return false;
+  }
+  __device__ __forceinline__ void wait_rows() {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+  }
+  __device__ __forceinline__ void used() {
+    busy &= ~(1u << get);
+    get = get + 1 == STAGES ? 0 : get + 1;
+  }
+  __device__ __forceinline__ const uint8_t* slot() const { return slots + get * TB; }
+};
+
+// The open block's products, this step's key and value into it, and, where that
+// fills it, its tiles.  sk, sv: its rows in shared memory (the step's own among them).
+template <int HD>
+__device__ __forceinline__ void open_block(const DecQ8Args& a, const Task8& w, Attn8<HD>& at, const __half* sk,
+                                           const __half* sv) {
+  const int lane = threadIdx.x & 31, kd = a.Hkv * HD, open = a.slot % kTileKeys;
+  at.open(sk, sv, open + 1, a.scale_log2);
+  __half* tail = a.tail + (static_cast<int64_t>(w.r) * kTileKeys + open) * 2 * kd + w.h * HD;
+  for (int c = lane; c < HD / 4; c += 32) {
+    const int v = c / (HD / 8), part = c % (HD / 8);
+    reinterpret_cast<uint4*>(tail + v * kd)[part] = reinterpret_cast<const uint4*>((v ? sv : sk) + open * HD)[part];
+  }
+  if (open == kTileKeys - 1) {  // the block is complete
+    const int64_t unit = (w.r * a.gen_blocks + a.slot / kTileKeys) * a.Hkv + w.h;
+    uint8_t* dst = a.gc + unit * tile8_bytes(HD);
+    const float ak = tile8_quantize_keys<HD, true>([&](int key) { return sk + key * HD; }, kTileKeys, dst);
+    const float av = tile8_quantize_values<HD, true>([&](int key) { return sv + key * HD; }, kTileKeys, dst);
+    if (lane == 0) {
+      a.gs[unit] = make_float2(__fdiv_rn(ak, 127.f), __fdiv_rn(av, 127.f));
+      if (!(ak <= 65504.f && av <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);
+    }
+  }
+}
+
+// Eight consecutive elements of an output row, times inv, as fp16; false: not all are finite there.
+__device__ __forceinline__ bool store_eight(__half* dst, const float (&v)[8], float inv) {
+  bool fine = true;
+  uint32_t x[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float x0 = v[2 * k] * inv, x1 = v[2 * k + 1] * inv;
+    fine = fine && fabsf(x0) <= 65504.f && fabsf(x1) <= 65504.f;
+    x[k] = as_u32(__floats2half2_rn(x0, x1));
+  }
+  *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
+  return fine;
+}
+
+template <int HD>
+struct Stream8 {
+  static constexpr int NW = 4;                     // warps per CTA
+  static constexpr int STAGES = HD == 128 ? 3 : 3;
+  static constexpr int CTAS = HD == 128 ? 2 : 4;   // per SM
+  static constexpr int RING = NW * STAGES * tile8_bytes(HD);
+  static constexpr int SMEM = RING + NW * STAGES * 8;
+  static_assert(CTAS * (SMEM + 1024 + 64) <= 233472, "shared memory per SM");
+};
+
+// Many rows: a persistent warp per (row, KV head) task, the entries of all its
+// tasks as one stream through its ring.
+template <int HD>
+__global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_decode_q8_stream(DecQ8Args a, int64_t n_tasks) {
+  using C = Stream8<HD>;
+  constexpr int TB = tile8_bytes(HD);
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING) + warp * C::STAGES;
+  if (lane == 0)
+    for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 1);
+  if (threadIdx.x == 0) abort_word = 0;
+  fence_mbar_init();
+  __syncthreads();
+  grid_launch_next();
+  grid_wait();
+
+  Ring8<HD, C::STAGES> ring;
+  ring.begin(smem + warp * C::STAGES * TB, bars, &abort_word, a.err);
+  const int kd = a.Hkv * HD, open = a.slot % kTileKeys;
+  const int64_t stride = static_cast<int64_t>(a.Hkv) * TB;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * C::NW;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * C::NW + warp;
+
+  // the copies run ahead of the products by the ring's length, over the tasks' borders
+  int64_t pi = first;
+  Task8 pt = task_of(a, pi, n_tasks);
+  const uint8_t* tile = nullptr;
+  const float2* scale = nullptr;
+  int pe = 0, left = 0;  // the task's next entry; keys left in the run of tiles that `tile` is in
+  const auto run_of = [&](const uint8_t* c, const float2* s, int64_t block, int keys) {
+    block = block * a.Hkv + pt.h;
+    tile = c + block * TB;
+    scale = s + block;
+    left = keys;
+  };
+  const auto next_run = [&] {  // entry pe is the first of its run
+    const int np = tiles_of(a.P), no = tiles_of(pt.len);
+    if (pe < np)
+      run_of(a.pc, a.ps, 0, a.P);
+    else if (pe < np + no)
+      run_of(a.oc, a.os, tile8_first_block(pt.st, pt.r), pt.len);
+    else
+      run_of(a.gc, a.gs, pt.r * a.gen_blocks, a.slot - open);
+  };
+  const auto produce = [&] {
+    if (pi >= n_tasks) return;
+    if (pe < pt.tiles) {
+      if (left <= 0) next_run();
+      ring.issue_tile(tile, scale, min(left, kTileKeys));
+      tile += stride;
+      scale += a.Hkv;
+      left -= kTileKeys;
+      ++pe;
+      return;
+    }
+    const int v = pe - pt.tiles;  // keys, values
+    ring.issue_rows(a.tail + static_cast<int64_t>(pt.r) * kTileKeys * 2 * kd + pt.h * HD + v * kd,
+                    2 * static_cast<int64_t>(kd), a.qkv + pt.r * a.ldq + (a.Hq + pt.h) * HD + v * kd, open + 1);
+    ++pe;
+    if (v) {
+      pi += step;
+      pt = task_of(a, pi, n_tasks);
+      pe = left = 0;
+    }
+  };
+#pragma unroll 1
+  for (int i = 0; i < C::STAGES; ++i) produce();
+
+  Attn8<HD> at;
+  for (int64_t i = first; i < n_tasks; i += step) {
+    const Task8 w = task_of(a, i, n_tasks);
+    at.begin(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
+    for (int e = 0; e < w.tiles; ++e) {
+      if (!ring.wait()) return;
+      const float2 s = make_float2(__shfl_sync(0xffffffffu, ring.scale.x, ring.get),
+                                   __shfl_sync(0xffffffffu, ring.scale.y, ring.get));
+      const int n = __shfl_sync(0xffffffffu, ring.keys, ring.get);
+      at.tile(ring.slot(), s, n, a.scale_log2);
+      ring.used();
+      __syncwarp();  // every lane is done with the slot before it is refilled
+      produce();
+    }
+    ring.wait_rows();
+    const __half* sk = reinterpret_cast<const __half*>(ring.slot());
+    ring.used();
+    const __half* sv = reinterpret_cast<const __half*>(ring.slot());
+    ring.used();
+    open_block<HD>(a, w, at, sk, sv);
+    __syncwarp();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) produce();
+    at.sum_keys();
+    const int head = 2 * t + (g & 1);
+    const float inv = 1.f / (g & 1 ? at.l[1] : at.l[0]);
+    __half* orow = a.out + (static_cast<int64_t>(w.r) * a.Hq + w.h * a.G + head) * HD + 8 * (g >> 1);
+    bool fine = true;
+#pragma unroll
+    for (int c = 0; c < HD / 32; ++c) {
+      float v[8];
+      at.eight(c, v);
+      if (head < a.G) fine = store_eight(orow + 32 * c, v, inv) && fine;
+    }
+    if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+  }
+}
+
+// ------------------------------------------- few rows: a CTA or more per task
+// The tiles of a (row, KV head) are cut into `splits` ranges, a CTA each, whose
+// warps take a range's tiles in turns; they merge their (maximum, sum, output) in
+// shared memory, and the ranges' are merged by k_merge_q8.
+template <int HD>
+struct Split8 {
+  static constexpr int NW = 4;
+  static constexpr int STAGES = Stream8<HD>::STAGES;
+  static constexpr int CTAS = Stream8<HD>::CTAS;
+  static constexpr int RING = NW * STAGES * tile8_bytes(HD);
+  static constexpr int SMEM = RING + NW * STAGES * 8;
+  static_assert(NW * 8 * (HD + 2) * 4 <= RING, "the merge reuses the ring");
+};
+constexpr int kMaxSplits = 64;
+
+// Tile e of a task: its bytes, scales and number of keys.
+template <int HD>
+__device__ __forceinline__ void tile_at(const DecQ8Args& a, const Task8& w, int e, const uint8_t*& tile,
+                                        const float2*& scale, int& n) {
+  const int np = tiles_of(a.P), no = tiles_of(w.len);
+  int64_t block;
+  n = kTileKeys;
+  if (e < np) {
+    tile = a.pc, scale = a.ps, block = e;
+    n = min(n, a.P - e * kTileKeys);
+  } else if (e < np + no) {
+    tile = a.oc, scale = a.os, block = tile8_first_block(w.st, w.r) + (e - np);
+    n = min(n, w.len - (e - np) * kTileKeys);
+  } else {
+    tile = a.gc, scale = a.gs, block = w.r * a.gen_blocks + (e - np - no);
+  }
+  block = block * a.Hkv + w.h;
+  tile += block * tile8_bytes(HD);
+  scale += block;
+}
+
+// Of `count` partial states of a head, at m, l (stride 1) and o (stride `ld`): the
+// largest maximum, and the joint sum and element.
+__device__ __forceinline__ float merge_states(const float* m, const float* l, const float* o, int count, int s_ml,
+                                              int s_o) {
+  float M = -INFINITY, L = 0.f, O = 0.f;
+  for (int i = 0; i < count; ++i) M = fmaxf(M, m[i * s_ml]);
+  for (int i = 0; i < count; ++i) {
+    const float f = exp2_approx(m[i * s_ml] - M);  // 0 for a state without keys
+    L += l[i * s_ml] * f;
+    O += o[i * s_o] * f;
+  }
+  return O / L;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
+    k_decode_q8_split(DecQ8Args a, int64_t n_tasks, int splits, float* partial) {
+  using C = Split8<HD>;
+  constexpr int TB = tile8_bytes(HD);
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING) + warp * C::STAGES;
+  if (lane == 0)
+    for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 1);
+  if (threadIdx.x == 0) abort_word = 0;
+  fence_mbar_init();
+  __syncthreads();
+  grid_launch_next();
+  grid_wait();
+
+  Ring8<HD, C::STAGES> ring;
+  ring.begin(smem + warp * C::STAGES * TB, bars, &abort_word, a.err);
+  const int split = blockIdx.x % splits;
+  const int64_t i = blockIdx.x / splits;
+  const Task8 w = task_of(a, i, n_tasks);
+  const int e1 = static_cast<int>(static_cast<int64_t>(w.tiles) * (split + 1) / splits);
+  int e = static_cast<int>(static_cast<int64_t>(w.tiles) * split / splits) + warp, pe = e;
+  const auto produce = [&] {
+    if (pe >= e1) return;
+    const uint8_t* tile;
+    const float2* scale;
+    int n;
+    tile_at<HD>(a, w, pe, tile, scale, n);
+    ring.issue_tile(tile, scale, n);
+    pe += C::NW;
+  };
+#pragma unroll 1
+  for (int k = 0; k < C::STAGES; ++k) produce();
+  Attn8<HD> at;
+  at.begin(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
+  bool ok = true;
+  for (; e < e1 && ok; e += C::NW) {
+    ok = ring.wait();
+    if (!ok) break;
+    const float2 s = make_float2(__shfl_sync(0xffffffffu, ring.scale.x, ring.get),
+                                 __shfl_sync(0xffffffffu, ring.scale.y, ring.get));
+    const int n = __shfl_sync(0xffffffffu, ring.keys, ring.get);
+    at.tile(ring.slot(), s, n, a.scale_log2);
+    ring.used();
+    __syncwarp();
+    produce();
+  }
+  // the open block goes to the warp whose turn it would be, behind its tiles
+  if (ok && split == splits - 1 && warp == (e1 - static_cast<int>(static_cast<int64_t>(w.tiles) * split / splits)) % C::NW) {
+    const int kd = a.Hkv * HD, open = a.slot % kTileKeys;
+    const __half* sk = reinterpret_cast<const __half*>(ring.slots + ring.put * TB);
+    const __half* sv = reinterpret_cast<const __half*>(ring.slots + (ring.put + 1) % C::STAGES * TB);
+#pragma unroll 1
+    for (int v = 0; v < 2; ++v)
+      ring.issue_rows(a.tail + static_cast<int64_t>(w.r) * kTileKeys * 2 * kd + w.h * HD + v * kd,
+                      2 * static_cast<int64_t>(kd), a.qkv + w.r * a.ldq + (a.Hq + w.h) * HD + v * kd, open + 1);
+    ring.wait_rows();
+    open_block<HD>(a, w, at, sk, sv);
+  }
+  at.sum_keys();
+  // merge the warps (a wait that ran out leaves wrong numbers and an error)
+  __syncthreads();
+  float* sm = reinterpret_cast<float*>(smem);  // [NW][8] maxima, [NW][8] sums, [NW][8][HD]
+  float* sl = sm + C::NW * 8;
+  float* so = sl + C::NW * 8;
+  if (g == 0) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sm[warp * 8 + 2 * t + h] = at.m[h];
+      sl[warp * 8 + 2 * t + h] = at.l[h];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < HD / 32; ++c) {
+    float v[8];
+    at.eight(c, v);
+    float4* dst = reinterpret_cast<float4*>(so + (warp * 8 + 2 * t + (g & 1)) * HD + 32 * c + 8 * (g >> 1));
+    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+    dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __syncthreads();
+  if (splits == 1) {
+    __half* orow = a.out + (static_cast<int64_t>(w.r) * a.Hq + w.h * a.G) * HD;
+    for (int k = threadIdx.x; k < a.G * HD; k += C::NW * 32) {
+      const int head = k / HD;
+      const float v = merge_states(sm + head, sl + head, so + k, C::NW, 8, 8 * HD);
+      if (!(fabsf(v) <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);
+      orow[k] = __float2half_rn(v);
+    }
+    return;
+  }
+  // [task][split]: G maxima, G sums, G x HD outputs
+  float* dst = partial + blockIdx.x * static_cast<int64_t>(a.G) * (HD + 2);
+  for (int k = threadIdx.x; k < a.G * HD; k += C::NW * 32) {
+    const int head = k / HD;
+    float M = -INFINITY, L = 0.f, O = 0.f;
+    for (int j = 0; j < C::NW; ++j) M = fmaxf(M, sm[j * 8 + head]);
+    for (int j = 0; j < C::NW; ++j) {
+      const float f = M == -INFINITY ? 0.f : exp2_approx(sm[j * 8 + head] - M);  // a range without tiles
+      L += sl[j * 8 + head] * f;
+      O += so[j * 8 * HD + k] * f;
+    }
+    dst[2 * a.G + k] = O;
+    if (k % HD == 0) {
+      dst[head] = M;
+      dst[a.G + head] = L;
+    }
+  }
+}
+
+__global__ void k_merge_q8(const float* partial, int splits, int G, int HD, int Hq, int Hkv, __half* out, int* err) {
+  grid_launch_next();
+  grid_wait();
+  const int64_t task = blockIdx.x;
+  const int64_t r = task / Hkv, h = task % Hkv;
+  const int size = G * (HD + 2);
+  const float* p = partial + task * splits * size;
+  for (int k = threadIdx.x; k < G * HD; k += blockDim.x) {
+    const int head = k / HD;
+    const float v = merge_states(p + head, p + G + head, p + 2 * G + k, splits, size, size);
+    if (!(fabsf(v) <= 65504.f)) set_dev_error(err, DEVERR_FP16_RANGE);
+    out[(r * Hq + h * G) * HD + k] = __float2half_rn(v);
+  }
+}
+
+// Ranges that a task's tiles are cut into; 0: a warp per task.
+template <int HD>
+int splits_of(int64_t tasks, double tiles, int num_sms) {
+  using C = Stream8<HD>;
+  const int64_t ctas = static_cast<int64_t>(num_sms) * C::CTAS;
+  if (tasks >= 4 * ctas * C::NW) return 0;
+  const int64_t most = static_cast<int64_t>(tiles / (2 * Split8<HD>::NW));  // two tiles a warp at least
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({ctas / tasks, most, kMaxSplits})));
+}
+int splits_of(const DecodeQ8& d, int num_sms) {
+  const int64_t tasks = static_cast<int64_t>(d.R) * d.Hkv;
+  const double tiles = d.P / 32 + static_cast<double>(d.T) / d.R / 32 + d.slot / 32;  // of a task, on average
+  switch (d.hd) {
+    case 32: return splits_of<32>(tasks, tiles, num_sms);
+    case 64: return splits_of<64>(tasks, tiles, num_sms);
+    default: return splits_of<128>(tasks, tiles, num_sms);
   }
 }
 
 template <int HD>
-int launch_q8(const DecQ8Args& a, int R, cudaStream_t s) {
-  return launch_chained(k_decode_q8<HD>, dim3(static_cast<unsigned>(R) * a.Hkv), kQ8Warps * 32, 0, s, 1, a);
+int launch_q8(const DecQ8Args& a, int R, int splits, float* partial, int num_sms, cudaStream_t s) {
+  const int64_t tasks = static_cast<int64_t>(R) * a.Hkv;
+  if (splits == 0) {
+    using C = Stream8<HD>;
+    const cudaError_t e = cudaFuncSetAttribute(k_decode_q8_stream<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess) return e;
+    return launch_chained(k_decode_q8_stream<HD>, dim3(static_cast<unsigned>(num_sms * C::CTAS)), C::NW * 32, C::SMEM, s, 1,
+                          a, tasks);
+  }
+  using C = Split8<HD>;
+  cudaError_t e = cudaFuncSetAttribute(k_decode_q8_split<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  e = launch_chained(k_decode_q8_split<HD>, dim3(static_cast<unsigned>(tasks * splits)), C::NW * 32, C::SMEM, s, 1, a, tasks,
+                     splits, partial);
+  if (e != cudaSuccess || splits == 1) return e;
+  return launch_chained(k_merge_q8, dim3(static_cast<unsigned>(tasks)), 256, 0, s, 1, partial, splits, a.G, HD, a.Hq, a.Hkv,
+                        a.out, a.err);
 }
 
 }  // namespace
 
-int launch_decode_attention_q8(const DecodeQ8& d, int* err, int num_sms, cudaStream_t s) {
+size_t decode_q8_floats(const DecodeQ8& d, int num_sms) {
   if (d.R <= 0) return 0;
-  (void)num_sms;
+  const int splits = splits_of(d, num_sms);
+  return splits < 2 ? 0 : static_cast<size_t>(d.R) * d.Hkv * splits * (d.Hq / d.Hkv) * (d.hd + 2);
+}
+
+int launch_decode_attention_q8(const DecodeQ8& d, float* partial, int* err, int num_sms, cudaStream_t s) {
+  if (d.R <= 0) return 0;
+  const int splits = splits_of(d, num_sms);
   DecQ8Args a{d.qkv, d.ldq, d.Hq, d.Hkv, d.Hq / d.Hkv, d.prefix, reinterpret_cast<const float2*>(d.prefix_scales), d.P,
               d.own, reinterpret_cast<const float2*>(d.own_scales), d.T, d.seq_start, d.gen,
               reinterpret_cast<float2*>(d.gen_scales), d.gen_cap / kTileKeys, d.tail, d.slot,
               1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, err};
   switch (d.hd) {
-    case 32: return launch_q8<32>(a, d.R, s);
-    case 64: return launch_q8<64>(a, d.R, s);
-    case 128: return launch_q8<128>(a, d.R, s);
+    case 32: return launch_q8<32>(a, d.R, splits, partial, num_sms, s);
+    case 64: return launch_q8<64>(a, d.R, splits, partial, num_sms, s);
+    case 128: return launch_q8<128>(a, d.R, splits, partial, num_sms, s);
     default: return cudaErrorInvalidValue;
   }
 }

@@ -300,7 +300,9 @@ struct DecodeQ8 {
   int slot;
   __half* out;
 };
-int launch_decode_attention_q8(const DecodeQ8& d, int* err, int num_sms, cudaStream_t s);
+// Workspace that the call takes, in floats (few rows: partial states of ranges of keys).
+size_t decode_q8_floats(const DecodeQ8& d, int num_sms);
+int launch_decode_attention_q8(const DecodeQ8& d, float* partial, int* err, int num_sms, cudaStream_t s);
 
 // -------------------------------------------------------------- sampling ---
 enum LogitType : int { LOGITS_F32 = 0, LOGITS_F16 = 1, LOGITS_BF16 = 2 };

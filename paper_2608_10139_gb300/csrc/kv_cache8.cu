@@ -61,8 +61,8 @@ __global__ void __launch_bounds__(kTileWarps * 32) k_kv_quantize(Cache8Args a, c
   const __half* k = kv + at.token * ld + h * HD;
   const __half* v = k + a.Hkv * HD;
   uint8_t* tile = cache + u * tile8_bytes(HD);
-  const float ak = tile8_quantize_keys<HD>([&](int key) { return k + key * ld; }, at.n, tile);
-  const float av = tile8_quantize_values<HD>([&](int key) { return v + key * ld; }, at.n, tile);
+  const float ak = tile8_quantize_keys<HD, false>([&](int key) { return k + key * ld; }, at.n, tile);
+  const float av = tile8_quantize_values<HD, false>([&](int key) { return v + key * ld; }, at.n, tile);
   if ((threadIdx.x & 31) == 0) {
     scales[u] = make_float2(__fdiv_rn(ak, 127.f), __fdiv_rn(av, 127.f));
     if (!(ak <= 65504.f && av <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);

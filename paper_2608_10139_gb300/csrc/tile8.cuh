@@ -82,94 +82,98 @@ __device__ __forceinline__ float warp_max_abs(__half2 m) {
 
 // The keys (row(key) points at a token's HD elements, 16-byte aligned; only keys
 // < n are read, the others are zeros) into the first half of a tile.  Returns the
-// largest magnitude: the block's scale is it / 127.
-template <int HD, typename Row>
+// largest magnitude: the block's scale is it / 127.  AGAIN reads the rows a second
+// time instead of holding them (32 * HD / 64 registers), for rows in shared memory.
+template <int HD, bool AGAIN, typename Row>
 __device__ __forceinline__ float tile8_quantize_keys(Row row, int n, uint8_t* tile) {
-  constexpr int PER = HD == 32 ? 8 : 16;      // a lane's elements of a key
   constexpr int C = HD == 32 ? 1 : HD / 64;
-  constexpr int W = PER / 2;                  // their fp16 pairs
+  constexpr int W = HD == 32 ? 4 : 8;  // fp16 pairs of a key that a lane holds
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint32_t x[4][C][W];
-  __half2 m = as_h2(0u);
+  const auto load = [&](int j, int c) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bool live = 8 * j + g < n;
-    const __half* p = live ? row(8 * j + g) : nullptr;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int w = 0; w < W; w += 4) {
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (live) v = *reinterpret_cast<const uint4*>(p + 64 * c + PER * t + 2 * w);
-        x[j][c][w] = v.x, x[j][c][w + 1] = v.y, x[j][c][w + 2] = v.z, x[j][c][w + 3] = v.w;
-      }
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int w = 0; w < W; ++w) m = __hmax2_nan(m, __habs2(as_h2(x[j][c][w])));
-  const float a = warp_max_abs(m), inv = tile8_inverse(a);
-  uint4* out = reinterpret_cast<uint4*>(tile);
-  if constexpr (HD == 32) {
-#pragma unroll
-    for (int j = 0; j < 4; j += 2) {
-      uint4 v;
-      v.x = tile8_from_half(x[j][0][0], x[j][0][1], inv);
-      v.y = tile8_from_half(x[j][0][2], x[j][0][3], inv);
-      v.z = tile8_from_half(x[j + 1][0][0], x[j + 1][0][1], inv);
-      v.w = tile8_from_half(x[j + 1][0][2], x[j + 1][0][3], inv);
-      out[(j / 2) * 32 + lane] = v;
+    for (int w = 0; w < W; w += 4) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (8 * j + g < n) v = *reinterpret_cast<const uint4*>(row(8 * j + g) + 64 * c + 2 * W * t + 2 * w);
+      x[j][c][w] = v.x, x[j][c][w + 1] = v.y, x[j][c][w + 2] = v.z, x[j][c][w + 3] = v.w;
     }
-  } else {
+  };
+  if constexpr (!AGAIN) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        uint4 v;
-        v.x = tile8_from_half(x[j][c][0], x[j][c][1], inv);
-        v.y = tile8_from_half(x[j][c][2], x[j][c][3], inv);
-        v.z = tile8_from_half(x[j][c][4], x[j][c][5], inv);
-        v.w = tile8_from_half(x[j][c][6], x[j][c][7], inv);
-        out[(j * C + c) * 32 + lane] = v;
-      }
+      for (int c = 0; c < C; ++c) load(j, c);
   }
+  __half2 m = as_h2(0u);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if constexpr (AGAIN) load(j, c);
+#pragma unroll
+      for (int w = 0; w < W; ++w) m = __hmax2_nan(m, __habs2(as_h2(x[j][c][w])));
+    }
+  const float a = warp_max_abs(m), inv = tile8_inverse(a);
+  if constexpr (AGAIN) asm volatile("" ::: "memory");
+  uint4* out = reinterpret_cast<uint4*>(tile);
+#pragma unroll
+  for (int j = 0; j < 4; j += HD == 32 ? 2 : 1)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if constexpr (AGAIN) {
+        load(j, c);
+        if constexpr (HD == 32) load(j + 1, c);
+      }
+      uint32_t v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t* p = HD == 32 ? &x[j + i / 2][c][2 * (i % 2)] : &x[j][c][2 * i];
+        v[i] = tile8_from_half(p[0], p[1], inv);
+      }
+      out[(HD == 32 ? j / 2 : j * C + c) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
   return a;
 }
 
 // The values into the second half of a tile, as tile8_quantize_keys.  A lane
 // loads eight elements of one key; the transposed 8 x 8 matrices give it two
 // keys of four elements.
-template <int HD, typename Row>
+template <int HD, bool AGAIN, typename Row>
 __device__ __forceinline__ float tile8_quantize_values(Row row, int n, uint8_t* tile) {
   constexpr int C = HD / 32;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint32_t x[4][C][4];
-  __half2 m = as_h2(0u);
+  const auto load = [&](int j, int c) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (8 * j + g < n) v = *reinterpret_cast<const uint4*>(row(8 * j + g) + 32 * c + 8 * t);
+    x[j][c][0] = v.x, x[j][c][1] = v.y, x[j][c][2] = v.z, x[j][c][3] = v.w;
+  };
+  if constexpr (!AGAIN) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bool live = 8 * j + g < n;
-    const __half* p = live ? row(8 * j + g) : nullptr;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (live) v = *reinterpret_cast<const uint4*>(p + 32 * c + 8 * t);
-      x[j][c][0] = v.x, x[j][c][1] = v.y, x[j][c][2] = v.z, x[j][c][3] = v.w;
-    }
+      for (int c = 0; c < C; ++c) load(j, c);
   }
+  __half2 m = as_h2(0u);
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      if constexpr (AGAIN) load(j, c);
 #pragma unroll
       for (int i = 0; i < 4; ++i) m = __hmax2_nan(m, __habs2(as_h2(x[j][c][i])));
+    }
   const float a = warp_max_abs(m), inv = tile8_inverse(a);
+  if constexpr (AGAIN) asm volatile("" ::: "memory");
   uint4* out = reinterpret_cast<uint4*>(tile + kTileKeys * HD);
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      if constexpr (AGAIN) {
+        load(2 * k, c);
+        load(2 * k + 1, c);
+      }
       uint32_t v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
