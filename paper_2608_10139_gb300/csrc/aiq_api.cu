@@ -2230,14 +2230,18 @@ aiq_status aiq_op_sample(aiq_ctx* c, const void* logits, int32_t type, int64_t l
   if (!c || !logits || !uniforms || !s || !tokens || R < 0 || V < 1 || ldl < V)
     return fail(AIQ_ERR_INVALID_ARG, "bad args");
   if (type < AIQ_LOGITS_F32 || type > AIQ_LOGITS_BF16) return fail(AIQ_ERR_INVALID_ARG, "unknown logit type");
+  if (V > (1 << 30)) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^30 logits a row");
   AIQ_TRY(check_sampling(*s, V));
   if (!aligned(logits, type == AIQ_LOGITS_F32 ? 4 : 2) || !aligned(uniforms, 4) || !aligned(tokens, 4) ||
       !aligned(probs, 4))
     return fail(AIQ_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
   if (R == 0) return AIQ_OK;
   CUDA_TRY(cudaSetDevice(c->device));
+  uint8_t* scratch = nullptr;
+  if (const size_t bytes = sample_bytes(R, V, s->top_k, c->num_sms))
+    AIQ_TRY(with_room(c, [&] { return ws(c, "op.sample", bytes, &scratch); }));
   const int e = launch_sample(logits, type, ldl, R, V, uniforms, s->temperature, s->top_k, s->top_p, s->min_p, tokens,
-                              probs, c->d_err, c->stream);
+                              probs, scratch, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("sampling launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);

@@ -309,8 +309,10 @@ enum LogitType : int { LOGITS_F32 = 0, LOGITS_F16 = 1, LOGITS_BF16 = 2 };
 constexpr int kSampleKeepMax = 1024;  // the largest top_k
 // tokens[r] of R rows of V logits (row pitch ld elements) for the uniforms u[r]; probs
 // may be null.  Returns 0 or a cudaError_t value.
+size_t sample_bytes(int R, int V, int top_k, int num_sms);  // scratch that the call takes (16-byte aligned)
 int launch_sample(const void* logits, int type, int64_t ld, int R, int V, const float* u, double temperature, int top_k,
-                  double top_p, double min_p, int32_t* tokens, float* probs, int* err, cudaStream_t s);
+                  double top_p, double min_p, int32_t* tokens, float* probs, void* scratch, int* err, int num_sms,
+                  cudaStream_t s);
 
 // ---------------------------------------------------------------- pairs ---
 // Device scratch of the Q4 self-join over S candidates (sizes in elements):

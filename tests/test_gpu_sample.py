@@ -102,7 +102,7 @@ def test_tokens_ruled_out_are_never_drawn(ctx):
     assert np.isfinite(z[np.arange(64), t]).all() and t[0] == 2999 and t[1] == 7
 
 
-@pytest.mark.parametrize("temperature", [1e-300, 1e-3, 1e3, 1e300])
+@pytest.mark.parametrize("temperature", [1e-310, 1e-300, 1e-3, 1e3, 1e300])
 def test_extreme_temperatures(ctx, temperature):
     rng = np.random.default_rng(4)
     z = rng.standard_normal((8, 777)).astype(np.float32) * 50
