@@ -14,6 +14,7 @@
 // shared memory, and the list is cut back to little more than k, raising the
 // bound, where it grows long.  What is left is sorted.
 #include <algorithm>
+#include <cmath>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -23,15 +24,16 @@ namespace {
 
 using Key = unsigned long long;  // a logit's order bits, then ~index: descending keys are the order of the draw
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 128;
+constexpr int kRowCtas = 9;                           // per SM
 constexpr int kPerThread = 16;                        // elements of a chunk
-constexpr int kChunk = kRowThreads * kPerThread;
+constexpr int kRowChunk = kRowThreads * kPerThread;
 constexpr int kMergeThreads = 1024;
-constexpr int kMergePerThread = 4;
-static_assert(kMergeThreads * kMergePerThread == kChunk, "one list size");
 // What a list is cut back to at most, and a chunk more, and a row's unaligned ends.
 __host__ __device__ constexpr int list_most(int k) { return k + (k / 4 > 32 ? k / 4 : 32); }
-constexpr int kList = list_most(kSampleKeepMax) + kChunk + 32;
+__host__ __device__ constexpr int list_size(int k, int threads) { return list_most(k) + threads * kPerThread + 32; }
+// The merge of slices lists that many before it cuts them back.
+constexpr int kMergeList = 22 * 1024;
 
 struct SampleArgs {
   const void* logits;
@@ -40,9 +42,11 @@ struct SampleArgs {
   const float* u;
   double inv_temperature, top_p, min_p;
   int k;
-  int slices;         // CTAs per row; above 1 each leaves its list in keys / counts
-  int slice_len;      // a multiple of kChunk
-  Key* keys;          // [R][slices][list_most(k)]
+  int slices;         // CTAs per row; above 1 each leaves its list in keys, froms and counts
+  int slice_len;      // elements
+  int slice_k;        // of which so many are listed at least (k where there is one slice)
+  Key* keys;          // [R][slices][list_most(slice_k)]
+  Key* froms;         // [R][slices]: from which key on nothing is missing
   int* counts;        // [R][slices]; -1: a NaN or +inf
   int32_t* tokens;
   float* probs;       // may be null
@@ -56,7 +60,7 @@ __device__ __forceinline__ float logit(__nv_bfloat16 v) { return __bfloat162floa
 // Bits in the order of the values; -0 and +0 alike (the sum is +0).
 __device__ __forceinline__ uint32_t order_bits(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float order_value(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
@@ -71,16 +75,27 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return m;
 }
 
+// c ? a : b, as one instruction: a chain of ?: would become an indexed array, in memory.
+__device__ __forceinline__ float pick(bool c, float a, float b) {
+  float x;
+  asm("{ .reg .pred p; setp.ne.b32 p, %1, 0; selp.f32 %0, %2, %3, p; }" : "=f"(x) : "r"(static_cast<int>(c)), "f"(a), "f"(b));
+  return x;
+}
+
 // Shared memory of a block.
 struct Shared {
-  Key list[kList];
   Key top, bottom;
   double sums[32];
   double total;
   int n;         // entries of the list
   int count[3];  // of the rounds of block_count
-  int bad;
+  unsigned int highest, lowest;
+  int size;      // of the list, which lies behind this
+  int unused;
+  __device__ __forceinline__ Key* list() { return reinterpret_cast<Key*>(this + 1); }
 };
+static_assert(sizeof(Shared) % sizeof(Key) == 0, "the list is aligned");
+constexpr int shared_bytes(int list) { return static_cast<int>(sizeof(Shared)) + list * static_cast<int>(sizeof(Key)); }
 
 // The sum over the block; `round` counts the calls (one barrier each: a call's
 // sum is cleared during the one before it).
@@ -95,7 +110,17 @@ __device__ __forceinline__ int block_count(Shared& s, int& round, int v) {
   return s.count[at];
 }
 
-__device__ __forceinline__ void push(Shared& s, Key key) { s.list[atomicAdd(&s.n, 1)] = key; }
+// Lists the keys of the lanes that want it; the whole warp calls.
+template <typename F>
+__device__ __forceinline__ void push(Shared& s, bool want, F key) {
+  const uint32_t all = __ballot_sync(0xffffffffu, want);
+  if (!all) return;
+  const int lane = threadIdx.x & 31;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&s.n, __popc(all));
+  at = __shfl_sync(0xffffffffu, at, 0) + __popc(all & ((1u << lane) - 1));
+  if (want) s.list()[at] = key();
+}
 
 // Cuts a list of more than `most` entries back to its largest ones, k to `most` of
 // them, by bisection; returns the key from which they were kept (0: all).  Ends
@@ -109,7 +134,7 @@ __device__ __forceinline__ Key cut(Shared& s, int& round, int k, int most) {
   __syncthreads();
   Key top = 0, bottom = ~0ull;
   for (int i = threadIdx.x; i < n; i += NT) {
-    const Key x = s.list[i];
+    const Key x = s.list()[i];
     top = x > top ? x : top;
     bottom = x < bottom ? x : bottom;
   }
@@ -128,7 +153,7 @@ __device__ __forceinline__ Key cut(Shared& s, int& round, int k, int most) {
   while (true) {
     mid = lo + (hi - lo) / 2;
     int c = 0;
-    for (int i = threadIdx.x; i < n; i += NT) c += s.list[i] >= mid;
+    for (int i = threadIdx.x; i < n; i += NT) c += s.list()[i] >= mid;
     c = block_count<NT>(s, round, c);
     if (c > most)
       lo = mid;
@@ -140,35 +165,58 @@ __device__ __forceinline__ Key cut(Shared& s, int& round, int k, int most) {
   // a piece at a time: what is kept lands no further than where it came from
   if (threadIdx.x == 0) s.n = 0;
   for (int base = 0; base < n; base += NT) {
-    const Key x = base + threadIdx.x < n ? s.list[base + threadIdx.x] : 0;
+    const Key x = base + threadIdx.x < n ? s.list()[base + threadIdx.x] : 0;
     __syncthreads();
-    if (x >= mid) push(s, x);
+    push(s, x >= mid, [&] { return x; });
     __syncthreads();
   }
   return mid;
 }
 
-// Inclusive sum over the block's threads.
-template <int NT>
-__device__ __forceinline__ double block_scan(double v, double* warp_sums) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const double w = __shfl_up_sync(0xffffffffu, v, d);
-    if (lane >= d) v += w;
-  }
-  if (lane == 31) warp_sums[warp] = v;
-  __syncthreads();
-  double before = 0;
-  for (int w = 0; w < warp; ++w) before += warp_sums[w];
-  __syncthreads();
-  return v + before;
+// 2^(j / 64).
+__device__ const double kExp2[64] = {
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0,
+};
+// e^x for x <= 0, to about a unit in the last of 64 bits; 0 below -700.  x = (64 e +
+// j) ln 2 / 64 + r, |r| <= ln 2 / 128, and the Taylor series of e^r to r^5 (the next
+// term is below 2^-54).  Eleven 64-bit instructions, of which an SM issues one a
+// warp every 16 clocks: they, not the reads, bound rows of many candidates.
+__device__ __forceinline__ double exp_neg(double x) {
+  if (x < -700.0) return 0.0;
+  const double magic = 0x1.8p52;  // the sum's low bits hold the nearest whole number
+  const double t = fma(x, 0x1.71547652b82fep+6, magic);
+  const int n = __double2loint(t);
+  const double w = t - magic;
+  const double r = fma(w, -0x1.a39ef35793c76p-39, fma(w, -0x1.62e42fee00000p-7, x));
+  const double s = fma(fma(fma(r, 1.0 / 120, 1.0 / 24), r, 1.0 / 6), r, 0.5);
+  const double p = fma(r * r, s, r);
+  const double base = kExp2[n & 63];
+  const double y = fma(base, p, base);
+  return __hiloint2double(__double2hiint(y) + (n >> 6) * (1 << 20), __double2loint(y));
 }
 
 // The draw from a complete list.
 template <int NT>
 __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round, int64_t r, bool bad) {
-  cut<NT>(s, round, a.k, list_most(a.k));
+  // what is sorted: a power of two, and NT entries (one a thread) as they are
+  int size = NT;
+  while (size < a.k) size <<= 1;
+  cut<NT>(s, round, a.k, size);
   __syncthreads();
   const int n_all = s.n, tid = threadIdx.x;
   const float u = a.u[r];
@@ -180,249 +228,431 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
     }
     return;
   }
-  Key* sorted = s.list;
-  if (n_all <= NT) {
-    // an entry's place is the number of larger ones
-    sorted = s.list + kList - NT;
-    const Key mine = tid < n_all ? s.list[tid] : 0;
-    int place = 0;
-    if (tid < n_all)
-      for (int i = 0; i < n_all; ++i) place += s.list[i] > mine;
+  // descending, bitonic
+  Key* sorted = s.list();
+  if (size == NT) {
+    Key mine = tid < n_all ? sorted[tid] : 0;
+    for (int run = 2; run <= NT; run <<= 1) {
+      for (int step = run >> 1; step; step >>= 1) {
+        Key other;
+        if (step >= 32) {
+          __syncthreads();
+          sorted[tid] = mine;
+          __syncthreads();
+          other = sorted[tid ^ step];
+        } else {
+          other = __shfl_xor_sync(0xffffffffu, mine, step);
+        }
+        // the lower place of a pair takes the larger key in a descending run
+        mine = ((tid & step) == 0) == ((tid & run) == 0) ? max(mine, other) : min(mine, other);
+      }
+    }
     __syncthreads();
-    if (tid < n_all) sorted[place] = mine;
+    sorted[tid] = mine;
     __syncthreads();
   } else {
-    int size = 1;
-    while (size < n_all) size <<= 1;
-    for (int i = n_all + tid; i < size; i += NT) s.list[i] = 0;
+    for (int i = n_all + tid; i < size; i += NT) sorted[i] = 0;
     __syncthreads();
     for (int run = 2; run <= size; run <<= 1)
       for (int step = run >> 1; step; step >>= 1) {
         for (int i = tid; i < size / 2; i += NT) {
-          const int x = 2 * step * (i / step) + i % step, y = x + step;
-          const Key kx = s.list[x], ky = s.list[y];
+          const int x = (i & -step) << 1 | (i & (step - 1)), y = x + step;
+          const Key kx = sorted[x], ky = sorted[y];
           if ((x & run) == 0 ? kx < ky : kx > ky) {
-            s.list[x] = ky;
-            s.list[y] = kx;
+            sorted[x] = ky;
+            sorted[y] = kx;
           }
         }
-        __syncthreads();
+        // pairs up to 32 apart stay within the 64 entries that a warp has
+        if (step > 32 || step == 1)
+          __syncthreads();
+        else
+          __syncwarp();
       }
   }
   const int k = n_all < a.k ? n_all : a.k;
-  // a thread's run of consecutive places
+  // A thread's run of consecutive places; warps without any stay out of the 64-bit arithmetic.
   constexpr int MOST = (kSampleKeepMax + NT - 1) / NT;
-  const int per = (k + NT - 1) / NT;
-  const double z0 = order_value(static_cast<uint32_t>(sorted[0] >> 32));
-  double e[MOST], c[MOST], sum = 0;
+  const int per = (k + NT - 1) / NT, lane = tid & 31, warp = tid >> 5;
+  const bool busy = warp * 32 * per < k;
+  double e[MOST], c[MOST];
+  if (busy) {
+    const double z0 = order_value(static_cast<uint32_t>(sorted[0] >> 32));
+    double sum = 0;
 #pragma unroll
-  for (int j = 0; j < MOST; ++j) {
-    const int i = tid * per + j;
-    e[j] = c[j] = 0;
-    if (j < per && i < k) {
-      const double z = order_value(static_cast<uint32_t>(sorted[i] >> 32));
-      e[j] = z == z0 ? 1.0 : exp((z - z0) * a.inv_temperature);  // 1 / T may be infinite
+    for (int j = 0; j < MOST; ++j) {
+      if (j >= per) break;
+      const int i = tid * per + j;
+      e[j] = 0;
+      if (i < k) {
+        const double z = order_value(static_cast<uint32_t>(sorted[i] >> 32));
+        e[j] = z == z0 ? 1.0 : exp_neg((z - z0) * a.inv_temperature);  // 1 / T may be infinite
+      }
+      sum += e[j];
+      c[j] = sum;
     }
-    sum += e[j];
-    c[j] = sum;
-  }
-  const double before = block_scan<NT>(sum, s.sums) - sum;
+    double upto = sum;
 #pragma unroll
-  for (int j = 0; j < MOST; ++j) {
-    c[j] += before;
-    if (j < per && tid * per + j == k - 1) s.total = c[j];
+    for (int d = 1; d < 32; d <<= 1) {
+      const double x = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += x;
+    }
+    if (lane == 31) s.sums[warp] = upto;
+    upto -= sum;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+      if (j >= per) break;
+      c[j] += upto;
+    }
   }
   __syncthreads();
-  const double all = s.total;
-  int in_m = 0, in_p = 0;
+  if constexpr (NT > 256) {  // the sums' own prefix sums, by one warp
+    if (warp == 0) {
+      double x = lane * 32 * per < k ? s.sums[lane] : 0;
 #pragma unroll
-  for (int j = 0; j < MOST; ++j)
-    if (j < per && tid * per + j < k) {
-      in_m += e[j] >= a.min_p;
-      in_p += c[j] < a.top_p * all;
+      for (int d = 1; d < 32; d <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      s.sums[lane] = x;
     }
-  int n = block_count<NT>(s, round, in_m);
-  if (a.top_p < 1.0) n = min(n, 1 + block_count<NT>(s, round, in_p));
+    __syncthreads();
+  }
+  if (busy && warp) {
+    double before = 0;
+    if constexpr (NT > 256)
+      before = s.sums[warp - 1];
+    else
+      for (int w = 0; w < warp; ++w) before += s.sums[w];
 #pragma unroll
-  for (int j = 0; j < MOST; ++j)
-    if (j < per && tid * per + j == n - 1) s.total = c[j];
-  __syncthreads();
-  const double kept = s.total, target = static_cast<double>(u) * kept;
-  int below = 0;
-#pragma unroll
-  for (int j = 0; j < MOST; ++j) below += j < per && tid * per + j < n && c[j] <= target;
-  const int at = min(n - 1, block_count<NT>(s, round, below));
-#pragma unroll
-  for (int j = 0; j < MOST; ++j)
-    if (j < per && tid * per + j == at) {
-      a.tokens[r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(sorted[at]));
-      if (a.probs) a.probs[r] = static_cast<float>(e[j] / kept);
+    for (int j = 0; j < MOST; ++j) {
+      if (j >= per) break;
+      c[j] += before;
     }
+  }
+  // places with e >= min_p: a prefix
+  int n = k;
+  if (a.min_p > 0) {
+    int in = 0;
+    if (busy) {
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) {
+        if (j >= per) break;
+        in += tid * per + j < k && e[j] >= a.min_p;
+      }
+    }
+    n = block_count<NT>(s, round, in);
+  }
+  const auto sum_to = [&](int place) {  // C of a place, for all threads
+    if (busy) {
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) {
+        if (j >= per) break;
+        if (tid * per + j == place) s.total = c[j];
+      }
+    }
+    __syncthreads();
+    return s.total;
+  };
+  const auto places_where = [&](auto f, int end) {
+    int in = 0;
+    if (busy) {
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) {
+        if (j >= per) break;
+        in += tid * per + j < end && f(c[j]);
+      }
+    }
+    return block_count<NT>(s, round, in);
+  };
+  if (a.top_p < 1.0) {
+    const double enough = a.top_p * sum_to(k - 1);
+    n = min(n, 1 + places_where([&](double x) { return x < enough; }, k));
+  }
+  const double kept = sum_to(n - 1), target = static_cast<double>(u) * kept;
+  const int at = min(n - 1, places_where([&](double x) { return x <= target; }, n));
+  if (busy) {
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+      if (j >= per) break;
+      if (tid * per + j == at) {
+        a.tokens[r] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(sorted[at]));
+        if (a.probs) a.probs[r] = static_cast<float>(e[j] / kept);
+      }
+    }
+  }
 }
 
-template <int NT>
-__device__ __forceinline__ void begin(Shared& s) {
+__device__ __forceinline__ void begin(Shared& s, int list) {
   if (threadIdx.x == 0) {
-    s.n = s.bad = 0;
+    s.n = 0;
+    s.size = list;
+    s.top = 0;
+    s.highest = 0, s.lowest = ~0u;
     s.count[0] = s.count[1] = s.count[2] = 0;
   }
   __syncthreads();
 }
 
-// A CTA per slice of a row.
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 4) k_sample_rows(SampleArgs a) {
-  grid_launch_next();
-  grid_wait();
-  constexpr int NT = kRowThreads, VEC = 16 / sizeof(T), GROUPS = kPerThread / VEC;
-  extern __shared__ __align__(16) uint8_t smem[];
-  Shared& s = *reinterpret_cast<Shared*>(smem);
-  begin<NT>(s);
+// Lists the candidates of elements s0 .. s1 - 1 of a row: at least the k largest
+// (all that are finite, where there are fewer).  Returns the key from which
+// nothing is missing (0: nothing at all is), and whether a NaN or +inf came by.
+template <typename T, int NT>
+__device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0, int s1, int k, bool& bad) {
+  constexpr int VEC = 16 / sizeof(T), GROUPS = kPerThread / VEC, CHUNK = NT * kPerThread;
   const int tid = threadIdx.x;
-  const int64_t r = blockIdx.x / a.slices;
-  const int slice = blockIdx.x % a.slices;
-  const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-  const int s0 = slice * a.slice_len, s1 = min(a.V, s0 + a.slice_len);
-  // 16-byte loads between the slice's first and last 16-byte boundary
+  // 16-byte loads between the first and the last 16-byte boundary
   const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row + s0) / sizeof(T) % VEC);
   const int v0 = min(s1, s0 + (skew ? VEC - skew : 0)), v1 = v0 + (s1 - v0) / VEC * VEC;
 
   const auto index = [&](int base, int j) { return base + (j / VEC * NT + tid) * VEC + j % VEC; };
   const auto load = [&](int base, float (&v)[kPerThread]) {
+    const T* from = row + index(base, 0);
+    if (base + CHUNK <= v1) {
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      const int at = index(base, i * VEC);
-      if (at < v1) {
-        const uint4 w = *reinterpret_cast<const uint4*>(row + at);
+      for (int i = 0; i < GROUPS; ++i) {
+        const uint4 w = *reinterpret_cast<const uint4*>(from + i * NT * VEC);
         const T* x = reinterpret_cast<const T*>(&w);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[i * VEC + e] = logit(x[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[i * VEC + e] = -INFINITY;
       }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      const bool in = index(base, i * VEC) < v1;
+      if (in) w = *reinterpret_cast<const uint4*>(from + i * NT * VEC);
+      const T* x = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[i * VEC + e] = in ? logit(x[e]) : -INFINITY;
     }
   };
-  int round = 0;
   float seen = -INFINITY;    // NaN or +inf where one came by
-  float bound = -INFINITY;   // candidates are larger: k listed ones are as large
-  const auto single = [&](int at) {
-    const float v = logit(row[at]);
-    seen = max_nan(seen, v);
-    if (v > bound) push(s, key_of(v, at));
+  float bound = -INFINITY;   // candidates are larger
+  Key from = 0;
+  const auto single = [&](int at, int end) {
+    float x = -INFINITY;
+    if (at < end) x = logit(row[at]);
+    seen = max_nan(seen, x);
+    push(s, x > bound, [&] { return key_of(x, at); });
   };
-  if (s0 + tid < v0) single(s0 + tid);
-  float v[kPerThread], next[kPerThread];
-  load(v0, v);
-  for (int base = v0; base < v1; base += kChunk) {
-    load(base + kChunk, next);
-    if (base == v0) {
-      // the k-th largest of the threads' own maxima, or a little less: k elements reach it
-      float mx = v[0];
+  // The bound: with it the first two chunks list `want` elements or a few more,
+  // found by bisection over the counts of the threads' own maxima where there are
+  // threads enough, of all elements where not.  Where the rest of the row is like
+  // its beginning, the k-th largest of the row is about the (k * share)-th largest
+  // there; three standard deviations more are taken, and a row that then lists too
+  // few (one that begins with its largest elements) is read once more with a bound
+  // that k elements of its beginning reach.
+  const float share = fminf(1.f, 2.f * CHUNK / static_cast<float>(s1 - s0));
+  int want = min(k, static_cast<int>(k * share + 3.f * sqrtf(k * share) + 2.f));
+  while (true) {
+    float v[kPerThread], next[kPerThread];
+    load(v0, v);
+    load(v0 + CHUNK, next);
+    bound = -INFINITY;
+    from = 0;
+    if (tid < 32) single(s0 + tid, v0);
+    const bool by_threads = want <= NT * 3 / 4;
+    float mx = max_nan(v[0], next[0]);
 #pragma unroll
-      for (int j = 1; j < kPerThread; ++j) mx = max_nan(mx, v[j]);
-      seen = max_nan(seen, mx);
-      float least = -INFINITY;
-      if (a.k <= NT * 3 / 4) {
-        const uint32_t mine = order_bits(mx);
-        uint32_t lo = 0, hi = 0xff800001u;  // all threads reach lo, none (but NaN) hi
-        for (int i = 0; i < 32 && hi - lo > 1; ++i) {
-          const uint32_t mid = lo + (hi - lo) / 2;
-          const int c = block_count<NT>(s, round, mine >= mid);
-          if (c < a.k) {
-            hi = mid;
-          } else {
-            lo = mid;
-            if (c <= a.k + a.k / 8 + 4) break;
-          }
-        }
-        if (lo > 0x007fffffu) least = order_value(lo);
-      }
-#pragma unroll
-      for (int j = 0; j < kPerThread; ++j)
-        if (v[j] >= least && v[j] > -INFINITY) push(s, key_of(v[j], index(base, j)));
-      bound = least;
-    } else {
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i) {
-        float mx = v[i * VEC];
-#pragma unroll
-        for (int e = 1; e < VEC; ++e) mx = max_nan(mx, v[i * VEC + e]);
-        seen = max_nan(seen, mx);
-        if (!(mx <= bound)) {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e)
-            if (v[i * VEC + e] > bound) push(s, key_of(v[i * VEC + e], index(base, i * VEC + e)));
-        }
+    for (int j = 1; j < kPerThread; ++j) mx = max_nan(mx, max_nan(v[j], next[j]));
+    const uint32_t mine = order_bits(mx);
+    {
+      const uint32_t high = __reduce_max_sync(0xffffffffu, mine), low = __reduce_min_sync(0xffffffffu, mine);
+      if ((tid & 31) == 0) {
+        atomicMax(&s.highest, high);
+        atomicMin(&s.lowest, low);
       }
     }
     __syncthreads();
-    if (s.n > kList - kChunk - 32) bound = order_value(static_cast<uint32_t>(cut<NT>(s, round, a.k, list_most(a.k)) >> 32));
-    __syncthreads();  // nobody lists more before all have read the number
+    uint32_t lo = 0x007fffffu, hi = min(s.highest, 0xff800000u) + 1;  // -inf; the largest and one more
+    if (by_threads) lo = max(lo, s.lowest);
+    const int most = by_threads ? want + want / 8 + 4 : list_most(want);
+    while (hi - lo > 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      int c;
+      if (by_threads) {
+        c = mine >= mid;
+      } else {
+        const float f = order_value(mid);
+        c = 0;
 #pragma unroll
-    for (int j = 0; j < kPerThread; ++j) v[j] = next[j];
+        for (int j = 0; j < kPerThread; ++j) c += (v[j] >= f) + (next[j] >= f);
+      }
+      c = block_count<NT>(s, round, c);
+      if (c < want) {
+        hi = mid;
+      } else {
+        lo = mid;
+        if (c <= most) break;
+      }
+    }
+    if (lo > 0x007fffffu) {
+      // the number before it, so that what equals it is listed; of 0 that is -2^-149, not -0
+      bound = order_value(lo - (lo == 0x80000000u ? 2 : 1));
+      from = static_cast<Key>(lo) << 32;
+    }
+    for (int base = v0; base < v1; base += CHUNK) {
+#pragma unroll
+      for (int w = 0; w < GROUPS; ++w) {
+        float top = v[w * VEC];
+#pragma unroll
+        for (int e = 1; e < VEC; ++e) top = max_nan(top, v[w * VEC + e]);
+        seen = max_nan(seen, top);
+        // a lane lists its elements one after the other: most that list any have one
+        uint32_t hits = 0;
+        if (__any_sync(0xffffffffu, top > bound)) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) hits |= v[w * VEC + e] > bound ? 1u << e : 0u;
+          while (__any_sync(0xffffffffu, hits)) {
+            const int e = __ffs(hits) - 1;
+            float x = 0.f;
+#pragma unroll
+            for (int f = 0; f < VEC; ++f) x = pick(e == f, v[w * VEC + f], x);
+            push(s, hits, [&] { return key_of(x, index(base, w * VEC) + e); });
+            hits &= hits - 1;
+          }
+        }
+      }
+      load(base + CHUNK, v);
+      // (whoever lists last sees its own entries counted)
+      if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > list_most(k))) {
+        // of what follows, only larger values can be among the k largest: equal ones come later
+        const uint32_t least = static_cast<uint32_t>(cut<NT>(s, round, k, list_most(k)) >> 32);
+        bound = fmaxf(bound, order_value(least));
+        from = max(from, static_cast<Key>(least + 1) << 32);
+        __syncthreads();
+      }
+    }
+    if (tid < 32) single(v1 + tid, s1);
+    __syncthreads();
+    if (want == k || s.n >= k || from == 0) break;
+    want = k;
+    __syncthreads();
+    if (tid == 0) s.n = 0, s.highest = 0, s.lowest = ~0u;
+    __syncthreads();
   }
-  if (v1 + tid < s1) single(v1 + tid);
-  if (!(seen < INFINITY)) s.bad = 1;
-  __syncthreads();
-  const bool bad = s.bad;
+  bad = __syncthreads_or(!(seen < INFINITY));
+  return from;
+}
+
+// A CTA per slice of a row.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) k_sample_rows(SampleArgs a) {
+  grid_launch_next();
+  grid_wait();
+  constexpr int NT = kRowThreads;
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared& s = *reinterpret_cast<Shared*>(smem);
+  begin(s, list_size(a.slice_k, NT));
+  const int64_t r = blockIdx.x / a.slices;
+  const int s0 = static_cast<int>(blockIdx.x % a.slices) * a.slice_len;
+  int round = 0;
+  bool bad;
+  Key from = scan<T, NT>(s, round, static_cast<const T*>(a.logits) + r * a.ld, s0, min(a.V, s0 + a.slice_len), a.slice_k, bad);
   if (a.slices == 1) {
     draw<NT>(a, s, round, r, bad);
     return;
   }
-  const int most = list_most(a.k);
-  cut<NT>(s, round, a.k, most);
+  const int most = list_most(a.slice_k);
+  from = max(from, cut<NT>(s, round, a.slice_k, most));
   __syncthreads();
   const int n = s.n;
   Key* out = a.keys + blockIdx.x * static_cast<int64_t>(most);
-  for (int i = tid; i < n; i += NT) out[i] = s.list[i];
-  if (tid == 0) a.counts[blockIdx.x] = bad ? -1 : n;
+  for (int i = threadIdx.x; i < n; i += NT) out[i] = s.list()[i];
+  if (threadIdx.x == 0) {
+    a.counts[blockIdx.x] = bad ? -1 : n;
+    a.froms[blockIdx.x] = from;
+  }
 }
 
-// A CTA per row: the slices' lists, in their order, and the draw.
+// A CTA per row: the slices' lists and the draw.  A slice lists as many as it
+// should have of the row's k largest, and four standard deviations more; where it
+// has even more of them, the row is listed again as one.
+template <typename T>
 __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
   grid_launch_next();
   grid_wait();
   constexpr int NT = kMergeThreads;
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& s = *reinterpret_cast<Shared*>(smem);
-  begin<NT>(s);
+  begin(s, kMergeList);
   const int64_t r = blockIdx.x;
-  const int most = list_most(a.k);
+  const int most = list_most(a.slice_k);
   int round = 0;
   bool bad = false;
-  Key from = 0;
-  for (int i = 0; i < a.slices; ++i) {
-    const int n = a.counts[r * a.slices + i];
-    bad = bad || n < 0;
-    const Key* in = a.keys + (r * a.slices + i) * most;
-    for (int j = threadIdx.x; j < n; j += NT)
-      if (in[j] >= from) push(s, in[j]);
+  Key from = 0, all = 0;  // what is listed; from where on nothing is missing
+  for (int i = threadIdx.x; i < a.slices; i += NT) {
+    bad = bad || a.counts[r * a.slices + i] < 0;
+    all = max(all, a.froms[r * a.slices + i]);
+  }
+  if (all) atomicMax(&s.top, all);
+  bad = __syncthreads_or(bad);
+  all = s.top;
+  // a warp per slice, as many slices at a time as the list has room for
+  const int batch = (kMergeList - list_most(a.k)) / most;
+  for (int first = 0; first < a.slices; first += batch) {
+    const int end = min(a.slices, first + batch);
+    for (int i = first + (threadIdx.x >> 5); i < end; i += NT / 32) {
+      const int64_t at = r * a.slices + i;
+      const int n = a.counts[at];
+      for (int j = threadIdx.x & 31; j - static_cast<int>(threadIdx.x & 31) < n; j += 32) {
+        const Key x = j < n ? a.keys[at * most + j] : 0;
+        push(s, x >= from && x, [&] { return x; });
+      }
+    }
     __syncthreads();
-    if (s.n > kList - kChunk - 32) from = cut<NT>(s, round, a.k, most);
+    if (end < a.slices) {
+      from = max(from, cut<NT>(s, round, a.k, list_most(a.k)));
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+  int in = 0;
+  for (int i = threadIdx.x; i < s.n; i += NT) in += s.list()[i] >= all;
+  if (!bad && all && block_count<NT>(s, round, in) < a.k) {
     __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    scan<T, NT>(s, round, static_cast<const T*>(a.logits) + r * a.ld, 0, a.V, a.k, bad);
   }
   draw<NT>(a, s, round, r, bad);
 }
-static_assert(list_most(kSampleKeepMax) <= kChunk, "a slice's list fits behind a cut one");
+static_assert(kMergeList >= list_size(kSampleKeepMax, kMergeThreads), "a row's list fits too");
 
 struct Plan {
-  int slices, slice_len;
+  int slices, slice_len, slice_k;
 };
-Plan plan_of(int R, int V, int num_sms) {
-  // few rows: as many slices as fill the GPU, of whole chunks
-  const int64_t chunks = (static_cast<int64_t>(V) + kChunk - 1) / kChunk;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(chunks, static_cast<int64_t>(num_sms) * 4 / R));
-  const int64_t per = (chunks + want - 1) / want;
-  return Plan{static_cast<int>((chunks + per - 1) / per), static_cast<int>(std::min<int64_t>(per * kChunk, INT32_MAX))};
+Plan plan_of(int R, int V, int top_k, int num_sms) {
+  // few rows: as many slices as fill the GPU, of two chunks at least
+  const int64_t pairs = (static_cast<int64_t>(V) + 2 * kRowChunk - 1) / (2 * kRowChunk);
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(pairs, static_cast<int64_t>(num_sms) * kRowCtas / R));
+  const int64_t len = (pairs + want - 1) / want * 2 * kRowChunk;
+  if (len >= V) return Plan{1, V, top_k};
+  const double mean = static_cast<double>(top_k) * len / V;
+  const int k = static_cast<int>(std::min<double>(top_k, std::ceil(mean + 4 * std::sqrt(mean) + 8)));
+  return Plan{static_cast<int>((V + len - 1) / len), static_cast<int>(len), k};
+}
+
+template <typename T>
+int launch_rows(const SampleArgs& a, int R, cudaStream_t s) {
+  static_assert(shared_bytes(list_size(kSampleKeepMax, kRowThreads)) <= 48 * 1024, "no larger shared memory to ask for");
+  cudaError_t e = launch_chained(k_sample_rows<T>, dim3(static_cast<unsigned>(R) * a.slices), kRowThreads,
+                                 shared_bytes(list_size(a.slice_k, kRowThreads)), s, 1, a);
+  if (e != cudaSuccess || a.slices == 1) return e;
+  constexpr int smem = shared_bytes(kMergeList);
+  e = cudaFuncSetAttribute(k_sample_merge<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_chained(k_sample_merge<T>, dim3(static_cast<unsigned>(R)), kMergeThreads, smem, s, 1, a);
 }
 
 }  // namespace
 
 size_t sample_bytes(int R, int V, int top_k, int num_sms) {
   if (R <= 0) return 0;
-  const Plan p = plan_of(R, V, num_sms);
-  return p.slices < 2 ? 0 : static_cast<size_t>(R) * p.slices * (list_most(top_k) * sizeof(Key) + sizeof(int));
+  const Plan p = plan_of(R, V, top_k, num_sms);
+  return p.slices < 2 ? 0 : static_cast<size_t>(R) * p.slices * ((list_most(p.slice_k) + 1) * sizeof(Key) + sizeof(int));
 }
 
 int launch_sample(const void* logits, int type, int64_t ld, int R, int V, const float* u, double temperature, int top_k,
@@ -430,19 +660,18 @@ int launch_sample(const void* logits, int type, int64_t ld, int R, int V, const 
                   cudaStream_t s) {
   if (R <= 0) return 0;
   if (V < 1 || top_k < 1 || top_k > V || top_k > kSampleKeepMax) return cudaErrorInvalidValue;
-  const Plan p = plan_of(R, V, num_sms);
+  const Plan p = plan_of(R, V, top_k, num_sms);
+  const size_t lists = static_cast<size_t>(R) * p.slices;
   Key* keys = static_cast<Key*>(scratch);
-  int* counts = reinterpret_cast<int*>(keys + static_cast<size_t>(R) * p.slices * list_most(top_k));
-  const SampleArgs a{logits, ld,       V, u,    1.0 / temperature, top_p, min_p, top_k, p.slices, p.slice_len,
-                     keys,   counts, tokens, probs, err};
-  const int smem = sizeof(Shared);
-  void (*kernel)(SampleArgs) = type == LOGITS_F32   ? k_sample_rows<float>
-                               : type == LOGITS_F16 ? k_sample_rows<__half>
-                                                    : k_sample_rows<__nv_bfloat16>;
-  static_assert(sizeof(Shared) <= 48 * 1024, "no larger shared memory to ask for");
-  const cudaError_t e = launch_chained(kernel, dim3(static_cast<unsigned>(R) * p.slices), kRowThreads, smem, s, 1, a);
-  if (e != cudaSuccess || p.slices == 1) return e;
-  return launch_chained(k_sample_merge, dim3(static_cast<unsigned>(R)), kMergeThreads, smem, s, 1, a);
+  Key* froms = keys + lists * list_most(p.slice_k);
+  const SampleArgs a{logits, ld,    V, u, 1.0 / temperature, top_p, min_p, top_k, p.slices, p.slice_len, p.slice_k,
+                     keys,   froms, reinterpret_cast<int*>(froms + lists), tokens, probs, err};
+  switch (type) {
+    case LOGITS_F32: return launch_rows<float>(a, R, s);
+    case LOGITS_F16: return launch_rows<__half>(a, R, s);
+    case LOGITS_BF16: return launch_rows<__nv_bfloat16>(a, R, s);
+    default: return cudaErrorInvalidValue;
+  }
 }
 
 }  // namespace aiq
