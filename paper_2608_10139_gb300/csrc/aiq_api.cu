@@ -179,7 +179,8 @@ struct aiq_ctx {
   int64_t* h_pin = nullptr;  // pinned staging for control scalars
   int64_t* d_pin = nullptr;  // its device address
   bool tight = false;        // a call's second try: the routes that need the least device memory
-  unsigned int* d_arrived = nullptr;  // arrival counter of the tile-count scans (zero between launches)
+  // arrival counters, zero between launches: the tile-count scans', then those of kSplitTasksMax attention tasks
+  unsigned int* d_arrived = nullptr;
   size_t bytes_max = SIZE_MAX;
   size_t bytes_used = 0;
   int64_t next_handle = 1;
@@ -1684,8 +1685,8 @@ aiq_status aiq_init(int device, aiq_ctx** out) {
   }
   if (e == cudaSuccess) e = cudaHostAlloc(&c->h_pin, 64 * sizeof(int64_t), cudaHostAllocMapped);
   if (e == cudaSuccess) e = cudaHostGetDevicePointer(&c->d_pin, c->h_pin, 0);
-  if (e == cudaSuccess) e = cudaMalloc(&c->d_arrived, sizeof(unsigned int));
-  if (e == cudaSuccess) e = cudaMemsetAsync(c->d_arrived, 0, sizeof(unsigned int), c->stream);
+  if (e == cudaSuccess) e = cudaMalloc(&c->d_arrived, (1 + kSplitTasksMax) * sizeof(unsigned int));
+  if (e == cudaSuccess) e = cudaMemsetAsync(c->d_arrived, 0, (1 + kSplitTasksMax) * sizeof(unsigned int), c->stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -2219,7 +2220,7 @@ aiq_status aiq_op_decode_attention_q8(aiq_ctx* c, const void* qkv, int32_t R, in
   float* partial = nullptr;
   if (const size_t floats = decode_q8_floats(d, c->num_sms))
     AIQ_TRY(with_room(c, [&] { return ws(c, "op.q8_partial", floats, &partial); }));
-  const int e = launch_decode_attention_q8(d, partial, c->d_err, c->num_sms, c->stream);
+  const int e = launch_decode_attention_q8(d, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);

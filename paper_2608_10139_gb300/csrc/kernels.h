@@ -302,7 +302,10 @@ struct DecodeQ8 {
 };
 // Workspace that the call takes, in floats (few rows: partial states of ranges of keys).
 size_t decode_q8_floats(const DecodeQ8& d, int num_sms);
-int launch_decode_attention_q8(const DecodeQ8& d, float* partial, int* err, int num_sms, cudaStream_t s);
+constexpr int kSplitTasksMax = 1024;
+// arrived: kSplitTasksMax counters, zero between launches.
+int launch_decode_attention_q8(const DecodeQ8& d, float* partial, unsigned int* arrived, int* err, int num_sms,
+                               cudaStream_t s);
 
 // -------------------------------------------------------------- sampling ---
 enum LogitType : int { LOGITS_F32 = 0, LOGITS_F16 = 1, LOGITS_BF16 = 2 };
