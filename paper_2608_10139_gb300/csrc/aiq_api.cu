@@ -304,6 +304,8 @@ aiq_status sync_and_check(aiq_ctx* c) {
   const int err = *c->h_err;
   if (err) {
     *c->h_err = 0;  // no kernel is in flight
+    // a kernel that gave up, or was given sequences that do not ascend, may have left counts behind
+    CUDA_TRY(cudaMemsetAsync(c->d_arrived, 0, (1 + kSplitTasksMax) * sizeof(unsigned int), c->stream));
     if (err & (DEVERR_DUP_BUILD_KEY | DEVERR_SENTINEL_KEY))
       return fail(AIQ_ERR_INVALID_ARG, "join build keys must be unique and differ from INT64_MIN");
     if (err & DEVERR_HASH_FULL) return fail(AIQ_ERR_CAPACITY, "hash table probe sequence exhausted");

@@ -562,10 +562,14 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
 }
 
 // ------------------------------------------- few rows: a CTA or more per task
-// The tiles of a (row, KV head) are cut into `splits` ranges, a CTA each, whose
-// warps take a range's tiles in turns; they merge their (maximum, sum, output) in
-// shared memory.  The ranges' are merged, in their order, by the task's CTA that
-// comes last: a kernel for it took ten microseconds of the four documents' 81.
+// The tiles of a (row, KV head) are cut into ranges, a CTA each, whose warps take a
+// range's tiles in turns; they merge their (maximum, sum, output) in shared memory.
+// The ranges' are merged, in their order, by the task's CTA that comes last: a
+// kernel for it took ten microseconds of the four documents' 81.
+//
+// A KV head has `units` CTAs, at least one a row, the others shared out by the
+// rows' lengths, which only the device knows: row r's are share(r) .. share(r + 1) - 1.
+constexpr int kMaxRanges = 512;  // of a row
 template <int HD>
 struct Split8 {
   static constexpr int NW = 4;
@@ -574,8 +578,14 @@ struct Split8 {
   static constexpr int RING = NW * STAGES * tile8_bytes(HD);
   static constexpr int SMEM = RING + NW * STAGES * 8;
   static_assert(NW * 8 * (HD + 2) * 4 <= RING, "the merge reuses the ring");
+  static_assert(NW * kMaxRanges * 4 <= RING, "and so do the ranges' weights");
 };
-constexpr int kMaxSplits = 64;
+__device__ __forceinline__ int64_t share(const DecQ8Args& a, int64_t R, int64_t units, int64_t r) {
+  // keys before row r, and something for each row's start, prefix and generated tokens
+  const int64_t more = a.P + a.slot + 48;
+  const int64_t before = a.seq_start[r] + r * more, all = a.seq_start[R] + R * more;
+  return r + (units - R) * before / (all > 0 ? all : 1);
+}
 
 // Tile e of a task: its bytes, scales and number of keys.
 template <int HD>
@@ -600,7 +610,7 @@ __device__ __forceinline__ void tile_at(const DecQ8Args& a, const Task8& w, int 
 
 template <int HD>
 __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
-    k_decode_q8_split(DecQ8Args a, int64_t n_tasks, int splits, float* partial, unsigned int* arrived) {
+    k_decode_q8_split(DecQ8Args a, int R, int units, float* partial, unsigned int* arrived) {
   using C = Split8<HD>;
   constexpr int TB = tile8_bytes(HD);
   extern __shared__ __align__(128) uint8_t smem[];
@@ -617,11 +627,35 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
 
   Ring8<HD, C::STAGES> ring;
   ring.begin(smem + warp * C::STAGES * TB, bars, &abort_word, a.err);
-  const int split = blockIdx.x % splits;
-  const int64_t i = blockIdx.x / splits;
-  const Task8 w = task_of(a, i, n_tasks);
-  const int e1 = static_cast<int>(static_cast<int64_t>(w.tiles) * (split + 1) / splits);
-  int e = static_cast<int>(static_cast<int64_t>(w.tiles) * split / splits) + warp, pe = e;
+  const int h = blockIdx.x % a.Hkv, unit = blockIdx.x / a.Hkv;
+  int64_t row = unit, first = unit;
+  int ranges = 1;
+  if (units > R) {
+    // the last row whose share begins at `unit` or before, 32 probes at a time
+    int64_t lo = 0, hi = R;
+    while (hi - lo > 1) {
+      const int64_t step = (hi - lo + 31) / 32, x = lo + lane * step;
+      const uint32_t found = __ballot_sync(0xffffffffu, x < hi && share(a, R, units, x) <= unit);
+      if (found) lo += (31 - __clz(found)) * step;
+      hi = lo + step < hi ? lo + step : hi;
+    }
+    row = lo;
+    first = share(a, R, units, row);
+    // where the starts do not ascend (below), anything within bounds will do
+    ranges = static_cast<int>(min(max(share(a, R, units, row + 1) - first, int64_t(1)),
+                                  static_cast<int64_t>(min(units, kMaxRanges))));
+    first = min(max(first, int64_t(0)), static_cast<int64_t>(units - ranges));
+    // a row may then have no CTA, which would have reported it
+    if (blockIdx.x == 0)
+      for (int k = threadIdx.x; k < R; k += C::NW * 32)
+        if (a.seq_start[k + 1] < a.seq_start[k]) set_dev_error(a.err, DEVERR_BOUNDS);
+  }
+  const int range = static_cast<int>(min(max(unit - first, int64_t(0)), static_cast<int64_t>(ranges - 1)));
+  const int64_t i = row * a.Hkv + h;
+  const Task8 w = task_of(a, i, static_cast<int64_t>(R) * a.Hkv);
+  const int e0 = static_cast<int>(static_cast<int64_t>(w.tiles) * range / ranges);
+  const int e1 = static_cast<int>(static_cast<int64_t>(w.tiles) * (range + 1) / ranges);
+  int e = e0 + warp, pe = e;
   const auto produce = [&] {
     if (pe >= e1) return;
     const uint8_t* tile;
@@ -648,7 +682,7 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
     produce();
   }
   // the open block goes to the warp whose turn it would be, behind its tiles
-  if (ok && split == splits - 1 && warp == (e1 - static_cast<int>(static_cast<int64_t>(w.tiles) * split / splits)) % C::NW) {
+  if (ok && range == ranges - 1 && warp == (e1 - e0) % C::NW) {
     const int kd = a.Hkv * HD, open = a.slot % kTileKeys;
     const __half* sk = reinterpret_cast<const __half*>(ring.slots + ring.put * TB);
     const __half* sv = reinterpret_cast<const __half*>(ring.slots + (ring.put + 1) % C::STAGES * TB);
@@ -682,9 +716,9 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
   }
   __syncthreads();
   __half* orow = a.out + (static_cast<int64_t>(w.r) * a.Hq + w.h * a.G) * HD;
-  // [task][split]: G maxima, G sums, G x HD outputs
+  // [head][unit]: G maxima, G sums, G x HD outputs
   const int size = a.G * (HD + 2);
-  float* mine = partial + blockIdx.x * static_cast<int64_t>(size);
+  float* mine = partial + (static_cast<int64_t>(h) * units + unit) * size;
   for (int k = threadIdx.x; k < a.G * HD; k += C::NW * 32) {
     const int head = k / HD;
     float M = -INFINITY, L = 0.f, O = 0.f;
@@ -696,7 +730,7 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
       L += sl[j * 8 + head] * f;
       O += so[j * 8 * HD + k] * f;
     }
-    if (splits == 1) {
+    if (ranges == 1) {
       const float v = O / L;
       if (!(fabsf(v) <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);
       orow[k] = __float2half_rn(v);
@@ -708,43 +742,38 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
       }
     }
   }
-  if (splits == 1) return;
+  if (ranges == 1) return;
   __threadfence();
   __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(&arrived[i], 1u) == static_cast<unsigned>(splits) - 1;
+  if (threadIdx.x == 0) last = atomicAdd(&arrived[i], 1u) == static_cast<unsigned>(ranges) - 1;
   __syncthreads();
   if (!last) return;
   __threadfence();
   if (threadIdx.x == 0) arrived[i] = 0;  // for the next launch
-  // a warp per head: the ranges' weights (two ranges a lane), then the weighted sums
-  const float* p = partial + i * splits * static_cast<int64_t>(size);
+  // a warp per head: the ranges' weights, then the weighted sums
+  const float* p = partial + (static_cast<int64_t>(h) * units + first) * size;
+  float* weight = sm + warp * kMaxRanges;  // (nobody reads the warps' states any more)
   for (int head = warp; head < a.G; head += C::NW) {
-    float m[2], f[2], M = -INFINITY, L = 0.f;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int j = lane + 32 * k;
-      m[k] = j < splits ? __ldcg(p + j * size + head) : -INFINITY;
-      f[k] = j < splits ? __ldcg(p + j * size + a.G + head) : 0.f;
-      M = fmaxf(M, m[k]);
-    }
+    float M = -INFINITY, L = 0.f;
+    for (int j = lane; j < ranges; j += 32) M = fmaxf(M, __ldcg(p + j * size + head));
 #pragma unroll
     for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      m[k] = exp2_approx(m[k] - M);  // 0 for a range without tiles
-      L += f[k] * m[k];
+    for (int j = lane; j < ranges; j += 32) {
+      const float f = exp2_approx(__ldcg(p + j * size + head) - M);  // 0 for a range without tiles
+      weight[j] = f;
+      L += __ldcg(p + j * size + a.G + head) * f;
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+    __syncwarp();
     float O[HD / 32];
 #pragma unroll
     for (int k = 0; k < HD / 32; ++k) O[k] = 0.f;
 #pragma unroll 8
-    for (int j = 0; j < splits; ++j) {
-      const float w8 = __shfl_sync(0xffffffffu, j < 32 ? m[0] : m[1], j & 31);
+    for (int j = 0; j < ranges; ++j)
 #pragma unroll
-      for (int k = 0; k < HD / 32; ++k) O[k] = fmaf(__ldcg(p + j * size + 2 * a.G + head * HD + 32 * k + lane), w8, O[k]);
-    }
+      for (int k = 0; k < HD / 32; ++k)
+        O[k] = fmaf(__ldcg(p + j * size + 2 * a.G + head * HD + 32 * k + lane), weight[j], O[k]);
     bool fine = true;
 #pragma unroll
     for (int k = 0; k < HD / 32; ++k) {
@@ -753,67 +782,67 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
       orow[head * HD + 32 * k + lane] = __float2half_rn(v);
     }
     if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+    __syncwarp();
   }
 }
-static_assert(kMaxSplits == 64, "two ranges a lane");
 
-// Ranges that a task's tiles are cut into; 0: a warp per task.
+// CTAs per KV head (one a row at least); 0: a warp per task.
 template <int HD>
-int splits_of(int64_t tasks, double tiles, int num_sms) {
+int units_of(int64_t R, int64_t Hkv, double tiles, int num_sms) {
   using C = Stream8<HD>;
-  const int64_t ctas = static_cast<int64_t>(num_sms) * C::CTAS;
+  const int64_t ctas = static_cast<int64_t>(num_sms) * C::CTAS, tasks = R * Hkv;
   if (tasks >= 2 * ctas * C::NW) return 0;
-  if (tasks > kSplitTasksMax) return 1;
-  const int64_t most = static_cast<int64_t>(tiles / (2 * Split8<HD>::NW));  // two tiles a warp at least
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({ctas / tasks, most, kMaxSplits})));
+  if (tasks > kSplitTasksMax) return static_cast<int>(R);
+  // four tiles a warp: shorter ranges cost more in the merge than they save (24 rows of
+  // about 200 keys, 32/8 heads, head_dim 64: 8.5 us with a CTA a task, 11.3 with 1.8)
+  const int64_t most = static_cast<int64_t>(tiles / (4 * Split8<HD>::NW));
+  return static_cast<int>(std::max<int64_t>(R, std::min<int64_t>({ctas / Hkv, most, R + kMaxRanges - 1})));
 }
-int splits_of(const DecodeQ8& d, int num_sms) {
-  const int64_t tasks = static_cast<int64_t>(d.R) * d.Hkv;
-  const double tiles = d.P / 32 + static_cast<double>(d.T) / d.R / 32 + d.slot / 32;  // of a task, on average
+int units_of(const DecodeQ8& d, int num_sms) {
+  const double tiles = d.T / 32.0 + static_cast<double>(d.R) * (d.P / 32 + d.slot / 32);  // of a KV head
   switch (d.hd) {
-    case 32: return splits_of<32>(tasks, tiles, num_sms);
-    case 64: return splits_of<64>(tasks, tiles, num_sms);
-    default: return splits_of<128>(tasks, tiles, num_sms);
+    case 32: return units_of<32>(d.R, d.Hkv, tiles, num_sms);
+    case 64: return units_of<64>(d.R, d.Hkv, tiles, num_sms);
+    default: return units_of<128>(d.R, d.Hkv, tiles, num_sms);
   }
 }
 
 template <int HD>
-int launch_q8(const DecQ8Args& a, int R, int splits, float* partial, unsigned int* arrived, int num_sms, cudaStream_t s) {
-  const int64_t tasks = static_cast<int64_t>(R) * a.Hkv;
-  if (splits == 0) {
+int launch_q8(const DecQ8Args& a, int R, int units, float* partial, unsigned int* arrived, int num_sms, cudaStream_t s) {
+  if (units == 0) {
     using C = Stream8<HD>;
     const cudaError_t e = cudaFuncSetAttribute(k_decode_q8_stream<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     return launch_chained(k_decode_q8_stream<HD>, dim3(static_cast<unsigned>(num_sms * C::CTAS)), C::NW * 32, C::SMEM, s, 1,
-                          a, tasks);
+                          a, static_cast<int64_t>(R) * a.Hkv);
   }
   using C = Split8<HD>;
   const cudaError_t e = cudaFuncSetAttribute(k_decode_q8_split<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
-  return launch_chained(k_decode_q8_split<HD>, dim3(static_cast<unsigned>(tasks * splits)), C::NW * 32, C::SMEM, s, 1, a,
-                        tasks, splits, partial, arrived);
+  return launch_chained(k_decode_q8_split<HD>, dim3(static_cast<unsigned>(units) * a.Hkv), C::NW * 32, C::SMEM, s, 1, a, R,
+                        units, partial, arrived);
 }
 
 }  // namespace
 
 size_t decode_q8_floats(const DecodeQ8& d, int num_sms) {
   if (d.R <= 0) return 0;
-  const int splits = splits_of(d, num_sms);
-  return splits < 2 ? 0 : static_cast<size_t>(d.R) * d.Hkv * splits * (d.Hq / d.Hkv) * (d.hd + 2);
+  const int units = units_of(d, num_sms);
+  return units <= d.R ? 0 : static_cast<size_t>(units) * d.Hkv * (d.Hq / d.Hkv) * (d.hd + 2);
 }
 
 int launch_decode_attention_q8(const DecodeQ8& d, float* partial, unsigned int* arrived, int* err, int num_sms,
                                cudaStream_t s) {
   if (d.R <= 0) return 0;
-  const int splits = splits_of(d, num_sms);
+  const int units = units_of(d, num_sms);
   DecQ8Args a{d.qkv, d.ldq, d.Hq, d.Hkv, d.Hq / d.Hkv, d.prefix, reinterpret_cast<const float2*>(d.prefix_scales), d.P,
               d.own, reinterpret_cast<const float2*>(d.own_scales), d.T, d.seq_start, d.gen,
               reinterpret_cast<float2*>(d.gen_scales), d.gen_cap / kTileKeys, d.tail, d.slot,
               1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, err};
   switch (d.hd) {
-    case 32: return launch_q8<32>(a, d.R, splits, partial, arrived, num_sms, s);
-    case 64: return launch_q8<64>(a, d.R, splits, partial, arrived, num_sms, s);
-    case 128: return launch_q8<128>(a, d.R, splits, partial, arrived, num_sms, s);
+    case 32: return launch_q8<32>(a, d.R, units, partial, arrived, num_sms, s);
+    case 64: return launch_q8<64>(a, d.R, units, partial, arrived, num_sms, s);
+    case 128: return launch_q8<128>(a, d.R, units, partial, arrived, num_sms, s);
     default: return cudaErrorInvalidValue;
   }
 }
