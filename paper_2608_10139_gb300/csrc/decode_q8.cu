@@ -193,7 +193,8 @@ struct Attn8 {
         }
       }
     uint32_t hi[2][2], lo[2][2];
-    softmax(sc, scale_log2 * s.x, n, hi, lo);
+    // (keys that are all 0 have scale 0; their scores are 0 by any, and a masked one stays -infinity)
+    softmax(sc, s.x == 0.f ? scale_log2 : scale_log2 * s.x, n, hi, lo);
 #pragma unroll
     for (int c = 0; c < C32; ++c) {
       float acc[2][4];

@@ -285,6 +285,30 @@ def test_a_rows_bits_do_not_depend_on_the_rows_beside_it(ctx):
     assert np.array_equal(moved, first)
 
 
+@pytest.mark.parametrize("heads", [(4, 4, 32), (8, 2, 64), (4, 1, 128)], ids=str)
+@pytest.mark.parametrize("part", ["keys", "values", "both"])
+def test_blocks_of_zeros(ctx, heads, part):
+    """A block whose keys (or values) are all 0 has scale 0."""
+    Hq, Hkv, hd = heads
+    s = Step(6, *heads, [33, 0, 5, 64], 7, 64)
+    kd = Hkv * hd
+    c = slice(0, kd) if part == "keys" else slice(kd, 2 * kd) if part == "values" else slice(0, 2 * kd)
+    own, pre = _rows(s.rng, s.T, 2 * kd), _rows(s.rng, s.P, 2 * kd)
+    own[:, c], pre[:, c] = 0, 0
+    s.own_c, s.own_s, q, sc = kv8.build_cache(own, s.lens, Hkv, hd)
+    s.own = q * sc[..., None]
+    s.pre_c, s.pre_s, q, sc = kv8.build_cache(pre, [7], Hkv, hd)
+    s.pre = q * sc[..., None]
+    s.d[:4] = [_d(a) for a in (s.own_c, s.own_s, s.pre_c, s.pre_s)]
+    for slot in range(2):
+        qkv = s.qkv()
+        if part == "both":
+            qkv[:, Hq * hd:] = 0
+        out = s.call(ctx, qkv, slot)
+        s.append(qkv)
+        s.check(out, qkv)
+
+
 @pytest.mark.parametrize("scale", [1e-4, 30.0])
 def test_small_and_large_scores(ctx, scale):
     """Scores that are all alike, and scores where one key has all the weight."""
@@ -329,6 +353,116 @@ def test_attention_reports_what_is_not_finite(ctx):
         with pytest.raises(aiq.AiqError) as e:
             s.call(ctx, qkv, 0)
         assert e.value.status == aiq.ERR_DEVICE_CHECK
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """1.2 million tokens of 2,048 values: bytes and elements past 2^31, and rows past 2^32 bytes."""
+    Hkv, hd, T = 8, 128, 1_200_000
+    w = 2 * Hkv * hd
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    kv = torch.empty((T, w), dtype=torch.float16, device="cuda")
+    for i in range(0, T, 100_000):
+        kv[i:i + 100_000].normal_(generator=g)
+    lens = [T - 50, 50]
+    st = _d(kv8.starts(lens))
+    nb = kv8.blocks(T, 2)
+    cache = torch.zeros((nb, Hkv, 64 * hd), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros((nb, Hkv, 2), device="cuda")
+    torch.cuda.synchronize()
+    ctx.op_kv_quantize(kv.data_ptr(), w, T, st.data_ptr(), 2, Hkv, hd, cache.data_ptr(), scales.data_ptr())
+    tail = kv[-50:].cpu().numpy()
+    ref, ref_s, q, s = kv8.build_cache(tail, [50], Hkv, hd)
+    b = kv8.first_block(T - 50, 1)
+    assert np.array_equal(cache[b:b + 2].cpu().numpy(), ref[:2]) and np.array_equal(scales[b:b + 2].cpu().numpy(), ref_s[:2])
+    j = (2 ** 31 // w) // 32 * 32  # a block of the first sequence around 2^31 elements
+    ref, ref_s, _, _ = kv8.build_cache(kv[j:j + 32].cpu().numpy(), [32], Hkv, hd)
+    assert np.array_equal(cache[j // 32].cpu().numpy(), ref[0])
+    back = torch.zeros_like(kv)
+    torch.cuda.synchronize()
+    ctx.op_kv_dequantize(cache.data_ptr(), scales.data_ptr(), T, st.data_ptr(), 2, Hkv, hd, back.data_ptr(), w)
+    assert np.array_equal(back[-50:].cpu().numpy(), kv8.read_back(q, s))
+    assert float((back[j - 64:j + 64].float() - kv[j - 64:j + 64].float()).abs().max()) < 0.03
+    del back
+    Hq = 16
+    qkv = torch.empty((2, (Hq + 2 * Hkv) * hd), dtype=torch.float16, device="cuda").normal_(generator=g)
+    gt = torch.zeros((2, 32, w), dtype=torch.float16, device="cuda")
+    out = torch.zeros((2, Hq * hd), dtype=torch.float16, device="cuda")
+    torch.cuda.synchronize()
+    ctx.op_decode_attention_q8(qkv.data_ptr(), 2, Hq, Hkv, hd, cache.data_ptr(), scales.data_ptr(), T, st.data_ptr(), 0, 0,
+                               gt.data_ptr(), 8, 0, out.data_ptr())
+    x = qkv.cpu().numpy()
+    rows = np.concatenate([(q * s[..., None]), x[1, Hq * hd:].astype(np.float64).reshape(1, 2, Hkv, hd)])
+    want, bound = kv8.attend(x[1, :Hq * hd].astype(np.float64).reshape(Hq, hd), rows[:, 0], rows[:, 1])
+    got = out.cpu().numpy().astype(np.float64)
+    assert (np.abs(got[1].reshape(Hq, hd) - want) <= bound).all()
+    # the long row: 64-bit sums on the GPU, a KV head at a time, of the values the cache holds
+    for h in (0, Hkv - 1):
+        c = cache[:(T - 50 + 31) // 32, h].view(-1, 64 * hd)
+        mk, mv = (torch.as_tensor(m).cuda() for m in kv8.tile_maps(hd))
+        parts = []
+        for m, k in ((mk, 0), (mv, 1)):
+            v = (c[:, m.reshape(-1)].double().view(-1, 32, hd) - 128) * scales[:len(c), h, k].double()[:, None, None]
+            parts.append(v.reshape(-1, hd)[:T - 50])
+        new = qkv[0, Hq * hd:].double().view(2, Hkv, hd)[:, h]
+        k, v = torch.cat([parts[0], new[:1]]), torch.cat([parts[1], new[1:]])
+        qh = qkv[0, :Hq * hd].double().view(Hkv, 2, hd)[h]
+        p = torch.softmax(qh @ k.T / hd ** 0.5, 1)
+        ref, A = p @ v, p @ v.abs()
+        err = (out[0].double().view(Hkv, 2, hd)[h] - ref).abs()
+        # as kv8.attend's bound: 2^-11 of the output, 2^-11 + 2^-18 and the scores' part of A
+        S = float((qh.abs() @ k.abs().T / hd ** 0.5).max())
+        rel = 2.0 ** -11 + 2.0 ** -18 + 2 * (hd + 8) * 2.0 ** -23 * S
+        assert bool((err <= A * rel + ref.abs() * 2.0 ** -11 + 2.0 ** -25).all())
+
+
+def test_two_contexts_at_once():
+    """Each has its own stream, workspace and counters."""
+    import threading
+    made, outs, fails = [], {}, []
+
+    def work(i):
+        try:
+            c = made[i]
+            s = Step(40 + i, 8, 2, 64, [900, 30, 2500], 10, 64)
+            s.fill_generated(20)
+            qkv = s.qkv()
+            first = s.call(c, qkv, 20)
+            for _ in range(40):
+                assert np.array_equal(s.call(c, qkv, 20), first)
+            s.append(qkv)
+            s.check(first, qkv)
+            outs[i] = first
+        except Exception as e:  # reported by the main thread
+            fails.append(e)
+
+    made = [gpu_ctx(), gpu_ctx()]
+    try:
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        for c in made:
+            c.close()
+    assert not fails, fails
+    assert len(outs) == 2
+
+
+def test_a_call_after_a_reported_one_is_right(ctx):
+    """Starts that do not ascend, in a call whose rows share CTAs, leave nothing behind."""
+    s = Step(50, 4, 1, 64, [4000, 3000], 0, 32)
+    qkv = s.qkv()
+    first = s.call(ctx, qkv, 0)
+    good = s.d[4]
+    for starts in ([0, 7000, 10], [0, -1, 7000], [5000, 10, 7000], [0, 4000, 8000]):
+        s.d[4] = _d(np.array(starts, np.int32))
+        with pytest.raises(aiq.AiqError) as e:
+            s.call(ctx, qkv, 0)
+        assert e.value.status == aiq.ERR_DEVICE_CHECK
+        s.d[4] = good
+        assert np.array_equal(s.call(ctx, qkv, 0), first)
 
 
 def test_refusals(ctx):
