@@ -232,6 +232,9 @@ typedef struct {
  * appends the first index of the largest full-vocabulary logit (final RMSNorm,
  * LM head, bias) at the row's last position.  After a row emits eos_id, its
  * remaining positions hold pad_id; eos_id < 0 disables the stop.
+ * With AIQ_GEN_SAMPLE a step draws its token from the full vocabulary's fp32 logits
+ * by the given uniform numbers instead (top_k = 1 gives the greedy tokens); a number
+ * outside [0, 1) that a candidate row takes gives AIQ_ERR_DEVICE_CHECK.
  * like_len > 0 adds Q5's filter: a row matches when the pattern occurs as a
  * contiguous run of its generated tokens before the eos (SQL LIKE '%...%' on
  * token ids); like_len == 0 with a non-NULL like_tokens matches every row. */
@@ -242,10 +245,16 @@ typedef struct {
   const int32_t* like_tokens; /* host; NULL: no LIKE filter (Q3 form) */
   int32_t like_len;           /* 0..256 */
   int32_t flags;              /* AIQ_GEN_* */
+  /* read with AIQ_GEN_SAMPLE only */
+  const aiq_sampling* sampling;
+  const float* uniforms;      /* host, [the table's rows][max_new_tokens], in [0, 1): step t of table row i takes
+                                 uniforms[i * max_new_tokens + t], whichever rows are selected and however they
+                                 run together */
 } aiq_generate;
 
 enum {
-  AIQ_GEN_MATCH_TOKENS = 1 /* with LIKE: also return the matching rows' tokens (the "debug outputs") */
+  AIQ_GEN_MATCH_TOKENS = 1, /* with LIKE: also return the matching rows' tokens (the "debug outputs") */
+  AIQ_GEN_SAMPLE = 2        /* draw each token (aiq_sampling) instead of taking the largest logit */
 };
 
 /* Table 2 Q3: SELECT AI_TRANSFORM(text, prefix) FROM table WHERE <preds>:
@@ -306,7 +315,11 @@ const char* aiq_last_error(void);
  * drift past the 2e-2 margin tolerance on a few rows),
  * "decode_rows" (aiq_run_transform: rows per prefill chunk, which
  * decode together, default 4096; the chunk's token budget grows to fit them,
- * up to 2^20 tokens and 32 GB of cached prompt keys/values), "device_bytes_max"
+ * up to 2^20 tokens and 32 GB of cached prompt keys/values), "kv_bits"
+ * (aiq_run_transform: 16, the default, or 8: cached keys and values as bytes with
+ * a scale per 32 tokens, KV head and keys / values, the layout and rounding that
+ * aiq_ops.h states; about half the cache's memory and reads, for logits that differ
+ * by the rounding; up to 8 query heads per KV head), "device_bytes_max"
  * (the context's device byte cap, as AIQ_DEVICE_BYTES_MAX at aiq_init; <= 0
  * lifts it; tables and models already held stay; a load or a query that finds no
  * room takes back the context's workspace, and a query runs again in the least

@@ -22,7 +22,7 @@ INT32, INT64, FLOAT32, TOKENS = 0, 1, 2, 3
 LT, LE, GT, GE, EQ, NE = 0, 1, 2, 3, 4, 5
 AGG_COUNT, AGG_ROW_IDS, AGG_GROUP_LABEL, AGG_GROUP_BUILD_KEY, AGG_SUM = 0, 1, 2, 3, 4
 FLAG_LOGITS, FLAG_RELATIONAL_ONLY = 1, 2
-GEN_MATCH_TOKENS = 1
+GEN_MATCH_TOKENS, GEN_SAMPLE = 1, 2
 LOGITS_F32, LOGITS_F16, LOGITS_BF16 = 0, 1, 2
 KV_BLOCK = 32          # tokens of an 8-bit cache that share a scale
 SAMPLE_MAX_K = 1024    # the largest top_k
@@ -74,13 +74,14 @@ class _View(C.Structure):
                 ("sum_int", C.c_int64), ("sum_float", C.c_double)]
 
 
-class _Generate(C.Structure):
-    _fields_ = [("max_new_tokens", C.c_int32), ("eos_id", C.c_int32), ("pad_id", C.c_int32),
-                ("like_tokens", C.POINTER(C.c_int32)), ("like_len", C.c_int32), ("flags", C.c_int32)]
-
-
 class _Sampling(C.Structure):
     _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32)]
+
+
+class _Generate(C.Structure):
+    _fields_ = [("max_new_tokens", C.c_int32), ("eos_id", C.c_int32), ("pad_id", C.c_int32),
+                ("like_tokens", C.POINTER(C.c_int32)), ("like_len", C.c_int32), ("flags", C.c_int32),
+                ("sampling", C.POINTER(_Sampling)), ("uniforms", C.POINTER(C.c_float))]
 
 
 class _Term(C.Structure):
@@ -175,6 +176,10 @@ def filter_compact_static(terms, n_rows: int, ids_out: int, count_out: int, stre
     ts = [_Term(p, t, op, int(v) if t != FLOAT32 else 0, float(v)) for p, t, op, v in terms]
     arr = (_Term * max(len(ts), 1))(*ts)
     _check(lib.aiq_filter_compact_static(arr, len(ts), n_rows, ids_out or None, count_out or None, stream or None))
+
+
+def _sampling(temperature: float = 1.0, top_k: int = 50, top_p: float = 1.0, min_p: float = 0.0) -> _Sampling:
+    return _Sampling(temperature, top_p, min_p, top_k)
 
 
 def kv_cache_blocks(T: int, n_seqs: int) -> int:
@@ -407,15 +412,26 @@ class Context:
 
     def run_transform(self, table: TableRef, model: int, preds, prefix, max_new: int, eos: int = -1,
                       pad: int = 0, like=None, match_tokens: bool = False,
-                      text_name: str = "text") -> TransformResult:
-        """AI_TRANSFORM (greedy) of every candidate row; with ``like`` (a token
-        sequence) only the COUNT / ids of the rows whose output contains it."""
+                      text_name: str = "text", sampling: Optional[dict] = None,
+                      uniforms: Optional[np.ndarray] = None) -> TransformResult:
+        """AI_TRANSFORM of every candidate row; with ``like`` (a token sequence)
+        only the COUNT / ids of the rows whose output contains it.  Greedy, or, with
+        ``sampling`` (temperature, top_k, top_p, min_p as in op_sample), drawn by
+        ``uniforms`` [table rows, max_new], numbers in [0, 1)."""
         sel, keep = self._select(table, preds, prefix, [], AGG_COUNT, 0, text_name)
         pat = _i32(like if like is not None else [])
         buf = pat if pat.size else np.zeros(1, np.int32)   # a non-NULL pointer for the empty pattern
         g = _Generate(max_new, eos, pad,
                       buf.ctypes.data_as(C.POINTER(C.c_int32)) if like is not None else None,
                       len(pat), GEN_MATCH_TOKENS if match_tokens else 0)
+        if sampling is not None:
+            sp = _sampling(**sampling)
+            u = np.ascontiguousarray(uniforms, dtype=np.float32)
+            if u.shape != (table.n_rows, max_new):
+                raise ValueError(f"uniforms must be [{table.n_rows}, {max_new}], not {list(u.shape)}")
+            g.flags |= GEN_SAMPLE
+            g.sampling = C.pointer(sp)
+            g.uniforms = u.ctypes.data_as(C.POINTER(C.c_float))
         h = C.c_int64()
         _check(self.lib.aiq_run_transform(self.h, table.handle, model, C.byref(sel), C.byref(g), C.byref(h)))
         v = _View()
@@ -500,6 +516,6 @@ class Context:
     def op_sample(self, logits: int, type: int, ldl: int, R: int, V: int, uniforms: int, tokens: int,
                   temperature: float = 1.0, top_k: int = 50, top_p: float = 1.0, min_p: float = 0.0, probs: int = 0):
         """A token per row of logits (LOGITS_*) from the uniforms in [0, 1) and, optionally, its probability."""
-        s = _Sampling(temperature, top_p, min_p, top_k)
+        s = _sampling(temperature, top_k, top_p, min_p)
         _check(self.lib.aiq_op_sample(self.h, logits or None, type, ldl, R, V, uniforms or None, C.byref(s),
                                       tokens or None, probs or None))

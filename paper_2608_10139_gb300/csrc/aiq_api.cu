@@ -21,6 +21,7 @@
 #include "aiq_ops.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "tile8.cuh"
 
 using namespace aiq;
 
@@ -197,6 +198,7 @@ struct aiq_ctx {
   // fp16 path's label-logit error reaches the 2e-2 parity tolerance
   int mlp_split = -1;
   int64_t decode_rows = 4096;  // generation: target rows per prefill chunk (= decode batch)
+  int kv_bits = 16;            // generation: bits of the cached keys and values
   std::vector<ProfRec> prof;
   std::vector<cudaEvent_t> ev_pool;
   std::map<std::string, StatAcc> stats;
@@ -588,16 +590,36 @@ aiq_status prefill_bufs(aiq_ctx* c, const ModelD& m, int64_t B, int64_t max_rows
   return AIQ_OK;
 }
 
+// An 8-bit cache of every layer: [L][blocks][Hkv] tiles and pairs of scales.
+struct Kv8 {
+  uint8_t* cache = nullptr;
+  float* scales = nullptr;
+  int64_t blocks = 0;
+  uint8_t* tiles(int l, const aiq_model_config& g) const {
+    return cache + l * blocks * g.n_kv_heads * tile8_bytes(g.head_dim);
+  }
+  float* pairs(int l, const aiq_model_config& g) const { return scales + l * blocks * g.n_kv_heads * 2; }
+};
+aiq_status kv8_bufs(aiq_ctx* c, const aiq_model_config& g, const char* cache, const char* scales, int64_t blocks, Kv8* k) {
+  const int64_t units = std::max<int64_t>(blocks, 1) * g.n_layers * g.n_kv_heads;
+  AIQ_TRY(ws(c, cache, units * tile8_bytes(g.head_dim), &k->cache));
+  AIQ_TRY(ws(c, scales, units * 2, &k->scales));
+  k->blocks = blocks;
+  return AIQ_OK;
+}
+
 // Decoder forward over one packed chunk of n_seqs sequences / T tokens.
 // The shared prefix that every sequence attends: its per-layer keys/values
 // pkv_in [L][P_in][2 Hkv hd], or, with prefix_first, the chunk's own first
 // sequence of P_in tokens.  kv_out (optional): where this pass stores the
-// keys/values of its first kv_rows tokens per layer.
+// keys/values of its first kv_rows tokens per layer; kv8_out (optional): the
+// 8-bit cache that takes those of all its tokens.
 // rows_only_last: the final layer's O-projection and MLP run only on each
 // sequence's last token (the only position whose output reaches the label
 // head); the result lands in b.resid_last, rows in sequence order.
 aiq_status run_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, int64_t T, int64_t n_seqs, const __half* pkv_in,
-                      int P_in, bool prefix_first, __half* kv_out, int64_t kv_rows, bool rows_only_last) {
+                      int P_in, bool prefix_first, __half* kv_out, int64_t kv_rows, bool rows_only_last,
+                      const Kv8* kv8_out = nullptr) {
   const aiq_model_config& g = m.cfg;
   const int d = g.d_model, hd = g.head_dim, Hq = g.n_heads, Hkv = g.n_kv_heads, f = g.d_ffn;
   const int nqkv = (Hq + 2 * Hkv) * hd;
@@ -637,6 +659,15 @@ aiq_status run_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, int64_t T, in
     e1.d_norm = static_cast<float>(d);
     e1.eps = g.rms_eps;
     AIQ_TRY(gemm(c, "gemm_qkv_rope", b.xn, d, L.wqkv, d, M, nqkv, d, m.bn_qkv, e1));
+    if (kv8_out) {
+      ProfScope p(c, "kv_quantize", 0, 3.0 * double(T) * ldkv);
+      const int e = launch_kv_quantize(b.qkv + Hq * hd, nqkv, T, b.seq_start, static_cast<int>(n_seqs), Hkv, hd,
+                                       kv8_out->tiles(l, g), kv8_out->pairs(l, g), c->d_err, c->stream);
+      counted(c, T > 0);
+      if (e != 0)
+        return fail(AIQ_ERR_CUDA, std::string("cache quantisation launch: ") +
+                                      cudaGetErrorString(static_cast<cudaError_t>(e)));
+    }
     if (kv_out && kv_rows > 0)
       CUDA_TRY(cudaMemcpy2DAsync(kv_out + l * kv_rows * ldkv, ldkv * sizeof(__half), b.qkv + Hq * hd,
                                  nqkv * sizeof(__half), ldkv * sizeof(__half), kv_rows, cudaMemcpyDeviceToDevice,
@@ -728,6 +759,9 @@ struct GenPlan {
   std::vector<std::pair<cudaEvent_t, cudaEvent_t>> spans;  // decode time per chunk
   double flops = 0;
   int64_t steps = 0;
+  const aiq_sampling* sampling = nullptr;  // nullptr: greedy
+  const float* uniforms = nullptr;         // [table rows][max_new] (device)
+  const int32_t* ids = nullptr;            // [S] the candidates' table rows (device)
 };
 
 // Full-vocabulary LM head in the GEMM's operand format, made once per model.
@@ -766,19 +800,66 @@ struct DecodeBufs {
   int gcap;
   unsigned long long* best;
   int32_t *done, *next, *pos;
+  // instead of kvc and gkv, the 8-bit cache: the prefix's, the prompts' and the generated tokens', and the
+  // open blocks [L][R][32][2 kd]
+  bool bits8;
+  Kv8 prefix8, own8, gen8;
+  __half* tail;
 };
 
-// Greedy tokens of the LM head for R rows of normalised hidden states in b.xn.
-aiq_status lm_argmax_select(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const DecodeBufs& d, int R, int t,
-                            GenPlan* gp, int64_t r0, int P) {
-  GemmEpilogue e;
-  e.kind = EPI_ARGMAX;
-  e.bias = m.lm_bias_f32;
-  e.best = d.best;
-  e.err = c->d_err;
-  AIQ_TRY(gemm(c, "gemm_lm_argmax", b.xn, m.cfg.d_model, m.lm_f16, m.cfg.d_model, R, m.vpad, m.cfg.d_model, 256, e));
+// Sampled tokens for R rows of normalised hidden states in b.xn: their logits, as
+// many rows at a time as 1 GB holds, then the draw.
+aiq_status lm_sample(aiq_ctx* c, ModelD& m, const PrefillBufs& b, int R, int t, const GenPlan* gp, int64_t r0,
+                     int32_t** tokens) {
+  const int dm = m.cfg.d_model, V = m.cfg.vocab;
+  const aiq_sampling& sp = *gp->sampling;
+  const int rows = std::max(1, std::min<int>(R, (1 << 28) / m.vpad));
+  float *logits, *u;
+  uint8_t* scratch = nullptr;
+  AIQ_TRY(ws(c, "g.logits", static_cast<int64_t>(rows) * m.vpad, &logits));
+  AIQ_TRY(ws(c, "g.u", R, &u));
+  AIQ_TRY(ws(c, "g.sampled", R, tokens));
+  const size_t bytes = std::max(sample_bytes(rows, V, sp.top_k, c->num_sms),
+                                sample_bytes((R - 1) % rows + 1, V, sp.top_k, c->num_sms));
+  if (bytes) AIQ_TRY(ws(c, "op.sample", bytes, &scratch));
+  launch_gather_uniforms(gp->uniforms, gp->ids + r0, gp->max_new, t, R, u, c->stream);
+  counted(c, 1);
+  for (int r = 0; r < R; r += rows) {
+    const int n = std::min(rows, R - r);
+    launch_fill_rows(m.lm_bias_f32, n, m.vpad, logits, c->stream);
+    counted(c, 1);
+    GemmEpilogue e;
+    e.kind = EPI_RESID_F32;
+    e.out = logits;
+    e.ldo = m.vpad;
+    e.err = c->d_err;
+    AIQ_TRY(gemm(c, "gemm_lm_logits", b.xn + static_cast<int64_t>(r) * dm, dm, m.lm_f16, dm, n, m.vpad, dm, 256, e));
+    ProfScope p(c, "sample", 0, 4.0 * double(n) * V);
+    const int err = launch_sample(logits, LOGITS_F32, m.vpad, n, V, u + r, sp.temperature, sp.top_k, sp.top_p, sp.min_p,
+                                  *tokens + r, nullptr, scratch, c->d_err, c->num_sms, c->stream);
+    counted(c, 1);
+    if (err != 0)
+      return fail(AIQ_ERR_CUDA, std::string("sampling launch: ") + cudaGetErrorString(static_cast<cudaError_t>(err)));
+  }
+  return AIQ_OK;
+}
+
+// The next tokens (greedy, or sampled) for R rows of normalised hidden states in b.xn.
+aiq_status lm_select(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const DecodeBufs& d, int R, int t, GenPlan* gp,
+                     int64_t r0, int P) {
+  int32_t* sampled = nullptr;
+  if (gp->sampling) {
+    AIQ_TRY(lm_sample(c, m, b, R, t, gp, r0, &sampled));
+  } else {
+    GemmEpilogue e;
+    e.kind = EPI_ARGMAX;
+    e.bias = m.lm_bias_f32;
+    e.best = d.best;
+    e.err = c->d_err;
+    AIQ_TRY(gemm(c, "gemm_lm_argmax", b.xn, m.cfg.d_model, m.lm_f16, m.cfg.d_model, R, m.vpad, m.cfg.d_model, 256, e));
+  }
   ProfScope p(c, "decode_select", 0, 0);
-  launch_decode_select(d.best, R, t, gp->max_new, gp->eos, gp->pad, m.cfg.vocab, d.done,
+  launch_decode_select(d.best, sampled, R, t, gp->max_new, gp->eos, gp->pad, m.cfg.vocab, d.done,
                        gp->tok + r0 * gp->max_new, gp->len + r0, d.next, d.pos, b.seq_start, P, c->d_err, c->stream);
   counted(c, 1);
   return AIQ_OK;
@@ -818,12 +899,24 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
     {
       // keys read per row: P + len + slot + 1; summed over the rows: R (P + slot + 1) + Tc
       const double keys = double(R) * (P + slot + 1) + double(Tc);
+      const double per_key = d.bits8 ? ldkv * 1.0 : ldkv * 2.0;
       ProfScope p(c, "decode_attention", 4.0 * Hq * hd * keys,
-                  keys * ldkv * 2.0 + double(R) * (nqkv + Hq * hd + ldkv) * 2.0);
-      const int e = launch_decode_attention(b.qkv, nqkv, R, Hq, Hkv, hd, pkv ? pkv + l * P * ldkv : nullptr, P,
-                                            d.kvc + l * Tc * ldkv, b.seq_start,
-                                            d.gkv + static_cast<int64_t>(l) * R * d.gcap * ldkv, d.gcap, slot, b.att,
-                                            c->d_err, c->num_sms, c->stream);
+                  keys * per_key + double(R) * (nqkv + Hq * hd + ldkv) * 2.0);
+      int e;
+      if (d.bits8) {
+        const DecodeQ8 q{b.qkv, nqkv, R, Hq, Hkv, hd, P ? d.prefix8.tiles(l, g) : nullptr,
+                         P ? d.prefix8.pairs(l, g) : nullptr, P, d.own8.tiles(l, g), d.own8.pairs(l, g), Tc, b.seq_start,
+                         d.gen8.tiles(l, g), d.gen8.pairs(l, g), d.gcap,
+                         d.tail + static_cast<int64_t>(l) * R * AIQ_KV_BLOCK * ldkv, slot, b.att};
+        float* partial = nullptr;
+        if (const size_t floats = decode_q8_floats(q, c->num_sms)) AIQ_TRY(ws(c, "op.q8_partial", floats, &partial));
+        e = launch_decode_attention_q8(q, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
+      } else {
+        e = launch_decode_attention(b.qkv, nqkv, R, Hq, Hkv, hd, pkv ? pkv + l * P * ldkv : nullptr, P,
+                                    d.kvc + l * Tc * ldkv, b.seq_start,
+                                    d.gkv + static_cast<int64_t>(l) * R * d.gcap * ldkv, d.gcap, slot, b.att, c->d_err,
+                                    c->num_sms, c->stream);
+      }
       counted(c, 1);
       if (e != 0)
         return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
@@ -870,7 +963,7 @@ aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Decod
     launch_rmsnorm(b.resid_last, R, g.d_model, m.final_norm, g.rms_eps, b.xn, c->d_err, c->stream);
     counted(c, 2);
   }
-  AIQ_TRY(lm_argmax_select(c, m, b, d, R, 0, gp, r0, P));
+  AIQ_TRY(lm_select(c, m, b, d, R, 0, gp, r0, P));
   for (int t = 1; t < gp->max_new; ++t) {
     AIQ_TRY(decode_layers(c, m, b, d, R, Tc, pkv, P, t - 1));
     {
@@ -878,7 +971,7 @@ aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Decod
       launch_rmsnorm(b.resid, R, g.d_model, m.final_norm, g.rms_eps, b.xn, c->d_err, c->stream);
       counted(c, 1);
     }
-    AIQ_TRY(lm_argmax_select(c, m, b, d, R, t, gp, r0, P));
+    AIQ_TRY(lm_select(c, m, b, d, R, t, gp, r0, P));
   }
   // executed FLOPs: full LM head every step; decoder passes with attention over
   // P + len + t keys per row (sum over rows: R (P + t) + Tc)
@@ -953,10 +1046,16 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
     // fill the decode GEMMs' last tile wave measured slower: more launches.)
     const int64_t per_row = T / S + 1;
     const int64_t kv_row = 2 * int64_t(m.cfg.n_layers) * 2 * m.cfg.n_kv_heads * m.cfg.head_dim;  // bytes/token
-    const int64_t kv_cap = (int64_t(32) << 30) / kv_row;
-    const int64_t gen_rows_cap = std::max<int64_t>(1, (int64_t(32) << 30) / (kv_row * std::max(gp->max_new - 1, 1)));
-    const int64_t row_cap = std::max<int64_t>(
-        1, std::min<int64_t>({c->decode_rows, (int64_t(1) << 20) / per_row, kv_cap / per_row, gen_rows_cap}));
+    int64_t prompt_row = kv_row * per_row, gen_row = kv_row * std::max(gp->max_new - 1, 1);
+    if (c->kv_bits == 8) {
+      // a block more per row than its tokens need, and the open block in fp16
+      const int64_t block = int64_t(m.cfg.n_layers) * m.cfg.n_kv_heads * (tile8_bytes(m.cfg.head_dim) + 8);
+      prompt_row = block * (per_row / AIQ_KV_BLOCK + 1);
+      gen_row = block * (gp->max_new / AIQ_KV_BLOCK) + kv_row * AIQ_KV_BLOCK;
+    }
+    const int64_t room = int64_t(32) << 30;
+    const int64_t row_cap = std::max<int64_t>(1, std::min<int64_t>({c->decode_rows, (int64_t(1) << 20) / per_row,
+                                                                    room / prompt_row, room / gen_row}));
     n_chunks = (S + row_cap - 1) / row_cap;
     rows_per_chunk = (S + n_chunks - 1) / n_chunks;
   } else {
@@ -1000,8 +1099,16 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
   if (gp) {
     AIQ_TRY(ensure_lm_f16(c, m));
     db.gcap = std::max(gp->max_new - 1, 1);
-    AIQ_TRY(ws(c, "g.kvc", static_cast<int64_t>(g.n_layers) * std::max<int64_t>(Bmax, 1) * ldkv, &db.kvc));
-    AIQ_TRY(ws(c, "g.gkv", static_cast<int64_t>(g.n_layers) * Rmax * db.gcap * ldkv, &db.gkv));
+    db.bits8 = c->kv_bits == 8;
+    if (db.bits8) {
+      AIQ_TRY(kv8_bufs(c, g, "g.own8", "g.own8s", tile8_blocks(Bmax, Rmax), &db.own8));
+      AIQ_TRY(kv8_bufs(c, g, "g.gen8", "g.gen8s", Rmax * (db.gcap / AIQ_KV_BLOCK), &db.gen8));
+      AIQ_TRY(kv8_bufs(c, g, "g.prefix8", "g.prefix8s", tile8_blocks(P, 1), &db.prefix8));
+      AIQ_TRY(ws(c, "g.tail", static_cast<int64_t>(g.n_layers) * Rmax * AIQ_KV_BLOCK * ldkv, &db.tail));
+    } else {
+      AIQ_TRY(ws(c, "g.kvc", static_cast<int64_t>(g.n_layers) * std::max<int64_t>(Bmax, 1) * ldkv, &db.kvc));
+      AIQ_TRY(ws(c, "g.gkv", static_cast<int64_t>(g.n_layers) * Rmax * db.gcap * ldkv, &db.gkv));
+    }
     AIQ_TRY(ws(c, "g.best", Rmax, &db.best));
     AIQ_TRY(ws(c, "g.done", Rmax, &db.done));
     AIQ_TRY(ws(c, "g.next", Rmax, &db.next));
@@ -1018,7 +1125,7 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
     NvtxPhase pr("prefix");
     launch_pack_prefix(prefix_d, P, pb.tok, pb.pos, pb.seq_start, pb.last_idx, c->stream);
     counted(c, 1);
-    AIQ_TRY(run_layers(c, m, pb, P, 1, nullptr, 0, false, pkv, P, false));
+    AIQ_TRY(run_layers(c, m, pb, P, 1, nullptr, 0, false, pkv, P, false, db.bits8 ? &db.prefix8 : nullptr));
     CUDA_TRY(cudaMemcpyAsync(prefix_last, pb.resid + static_cast<int64_t>(P - 1) * g.d_model, g.d_model * sizeof(float),
                              cudaMemcpyDeviceToDevice, c->stream));
   }
@@ -1039,7 +1146,7 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
     // generation keeps every layer's prompt keys/values of the chunk for the decode
     // steps; a first chunk keeps the prefix's for the chunks after it
     AIQ_TRY(run_layers(c, m, pb, tok0 + Tc, seq0 + r1 - r0, first ? nullptr : pkv, static_cast<int>(P), first,
-                       gp ? db.kvc : (first ? pkv : nullptr), gp ? Tc : P, true));
+                       gp ? db.kvc : (first ? pkv : nullptr), gp ? Tc : P, true, db.bits8 ? &db.own8 : nullptr));
     if (first)  // the final hidden state of the prefix's last token, for rows without text
       CUDA_TRY(cudaMemcpyAsync(prefix_last, pb.resid_last, g.d_model * sizeof(float), cudaMemcpyDeviceToDevice, c->stream));
     if (gp) {
@@ -1361,6 +1468,33 @@ aiq_status run_query(aiq_ctx* c, const TableD* build, int32_t build_key, const a
   return AIQ_OK;
 }
 
+bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// What the two copies between fp16 rows and the 8-bit cache ask of their arguments.
+aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                            int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache, const float* scales) {
+  if (!c || !kv || !seq_start || !cache || !scales || T < 0 || T > INT32_MAX || n_seqs < 0 || Hkv <= 0)
+    return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (!(hd == 32 || hd == 64 || hd == 128)) return fail(AIQ_ERR_UNSUPPORTED, "hd must be 32, 64 or 128");
+  if (ldkv < 2 * int64_t(Hkv) * hd || ldkv % 8)
+    return fail(AIQ_ERR_INVALID_ARG, "ldkv must be at least 2 Hkv hd and a multiple of 8");
+  if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(seq_start, 4))
+    return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
+  if ((T / AIQ_KV_BLOCK + n_seqs) * Hkv > (int64_t(1) << 33))
+    return fail(AIQ_ERR_UNSUPPORTED, "more than 2^33 (block, KV head) pairs");
+  return AIQ_OK;
+}
+
+aiq_status check_sampling(const aiq_sampling& s, int V) {
+  if (!(s.temperature > 0) || std::isinf(s.temperature))
+    return fail(AIQ_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (s.top_k < 1 || s.top_k > V) return fail(AIQ_ERR_INVALID_ARG, "top_k must be 1..vocab");
+  if (s.top_k > AIQ_SAMPLE_MAX_K) return fail(AIQ_ERR_UNSUPPORTED, "top_k above 1024");
+  if (!(s.top_p > 0 && s.top_p <= 1)) return fail(AIQ_ERR_INVALID_ARG, "top_p must be in (0, 1]");
+  if (!(s.min_p >= 0 && s.min_p <= 1)) return fail(AIQ_ERR_INVALID_ARG, "min_p must be in [0, 1]");
+  return AIQ_OK;
+}
+
 // Table 2 Q3 / Q5: relational phase, prefill + greedy decoding per chunk,
 // then the LIKE filter and the result arrays.
 aiq_status run_transform(aiq_ctx* c, const TableD& t, ModelD* m, const aiq_select* q, const aiq_generate* gen,
@@ -1376,6 +1510,13 @@ aiq_status run_transform(aiq_ctx* c, const TableD& t, ModelD* m, const aiq_selec
   for (int i = 0; like && i < gen->like_len; ++i)
     if (gen->like_tokens[i] < 0 || gen->like_tokens[i] >= V)
       return fail(AIQ_ERR_INVALID_ARG, "LIKE pattern token id out of range");
+  const bool sampled = gen->flags & AIQ_GEN_SAMPLE;
+  if (sampled) {
+    if (!gen->sampling || !gen->uniforms) return fail(AIQ_ERR_INVALID_ARG, "AIQ_GEN_SAMPLE needs sampling and uniforms");
+    AIQ_TRY(check_sampling(*gen->sampling, V));
+  }
+  if (c->kv_bits == 8 && m->cfg.n_heads / m->cfg.n_kv_heads > 8)
+    return fail(AIQ_ERR_UNSUPPORTED, "the 8-bit cache takes up to 8 query heads per KV head");
   PredSet ps{};
   AIQ_TRY(make_pred_set(t, q->preds, q->n_preds, &ps));
 
@@ -1397,6 +1538,15 @@ aiq_status run_transform(aiq_ctx* c, const TableD& t, ModelD* m, const aiq_selec
   gp.pad = gen->pad_id;
   AIQ_TRY(ws(c, "g.tok", std::max<int64_t>(S * W, 1), &gp.tok));
   AIQ_TRY(ws(c, "g.len", std::max<int64_t>(S, 1), &gp.len));
+  if (sampled) {
+    float* u;
+    AIQ_TRY(ws(c, "g.uniforms", std::max<int64_t>(t.n_rows * W, 1), &u));
+    if (S > 0)
+      CUDA_TRY(cudaMemcpyAsync(u, gen->uniforms, t.n_rows * W * sizeof(float), cudaMemcpyHostToDevice, c->stream));
+    gp.sampling = gen->sampling;
+    gp.uniforms = u;
+    gp.ids = st.ids;
+  }
   AIQ_TRY(prefill_phase(c, t, *m, q, &st, &gp));
   CUDA_TRY(cudaEventRecord(ev[2], c->stream));
   phase.begin("aggregate");
@@ -1624,33 +1774,6 @@ aiq_status model_alloc(aiq_ctx* c, ModelD& m, size_t count, T** out) {
   AIQ_TRY(dalloc_kept(c, &p, count * sizeof(T)));
   m.allocs.push_back(DevBuf{p, std::max<size_t>(count * sizeof(T), 256)});
   *out = static_cast<T*>(p);
-  return AIQ_OK;
-}
-
-bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
-// What the two copies between fp16 rows and the 8-bit cache ask of their arguments.
-aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
-                            int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache, const float* scales) {
-  if (!c || !kv || !seq_start || !cache || !scales || T < 0 || T > INT32_MAX || n_seqs < 0 || Hkv <= 0)
-    return fail(AIQ_ERR_INVALID_ARG, "bad args");
-  if (!(hd == 32 || hd == 64 || hd == 128)) return fail(AIQ_ERR_UNSUPPORTED, "hd must be 32, 64 or 128");
-  if (ldkv < 2 * int64_t(Hkv) * hd || ldkv % 8)
-    return fail(AIQ_ERR_INVALID_ARG, "ldkv must be at least 2 Hkv hd and a multiple of 8");
-  if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(seq_start, 4))
-    return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
-  if ((T / AIQ_KV_BLOCK + n_seqs) * Hkv > (int64_t(1) << 33))
-    return fail(AIQ_ERR_UNSUPPORTED, "more than 2^33 (block, KV head) pairs");
-  return AIQ_OK;
-}
-
-aiq_status check_sampling(const aiq_sampling& s, int V) {
-  if (!(s.temperature > 0) || std::isinf(s.temperature))
-    return fail(AIQ_ERR_INVALID_ARG, "temperature must be positive and finite");
-  if (s.top_k < 1 || s.top_k > V) return fail(AIQ_ERR_INVALID_ARG, "top_k must be 1..vocab");
-  if (s.top_k > AIQ_SAMPLE_MAX_K) return fail(AIQ_ERR_UNSUPPORTED, "top_k above 1024");
-  if (!(s.top_p > 0 && s.top_p <= 1)) return fail(AIQ_ERR_INVALID_ARG, "top_p must be in (0, 1]");
-  if (!(s.min_p >= 0 && s.min_p <= 1)) return fail(AIQ_ERR_INVALID_ARG, "min_p must be in [0, 1]");
   return AIQ_OK;
 }
 
@@ -2047,6 +2170,11 @@ aiq_status aiq_set_option(aiq_ctx* c, const char* name, int64_t value) {
   if (!std::strcmp(name, "decode_rows")) {
     if (value < 1 || value > (int64_t(1) << 20)) return fail(AIQ_ERR_INVALID_ARG, "decode_rows must be 1..2^20");
     c->decode_rows = value;
+    return AIQ_OK;
+  }
+  if (!std::strcmp(name, "kv_bits")) {
+    if (value != 8 && value != 16) return fail(AIQ_ERR_INVALID_ARG, "kv_bits must be 8 or 16");
+    c->kv_bits = static_cast<int>(value);
     return AIQ_OK;
   }
   if (!std::strcmp(name, "attention_tc")) {

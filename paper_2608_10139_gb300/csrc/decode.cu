@@ -478,21 +478,26 @@ __global__ void __launch_bounds__(DecStream<HD>::NW * 32, DecStream<HD>::CTAS)
   cp_async_wait_all();
 }
 
-// Next token of each row from the LM head's packed (max, first index), the
-// pad mask after an eos, and the position the token takes when fed back.
-__global__ void k_decode_select(unsigned long long* best, int R, int t, int max_new, int eos, int pad, int V,
+// Next token of each row from the LM head's packed (max, first index), or as
+// sampled, the pad mask after an eos, and the position the token takes when fed back.
+__global__ void k_decode_select(unsigned long long* best, const int32_t* sampled, int R, int t, int max_new, int eos, int pad, int V,
                                 int32_t* done, int32_t* gen_tok, int32_t* gen_len, int32_t* next_tok, int32_t* pos,
                                 const int32_t* seq_start, int P, int* err) {
   grid_launch_next();
   grid_wait();
   const int r = blockIdx.x * blockDim.x + threadIdx.x;
   if (r >= R) return;
-  const unsigned long long key = best[r];
-  best[r] = 0ull;  // ready for the next step's atomicMax
-  int tok = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(key & 0xFFFFFFFFull));
-  if (key == 0ull || tok < 0 || tok >= V) {
-    set_dev_error(err, DEVERR_BOUNDS);
-    tok = 0;
+  int tok;
+  if (sampled) {
+    tok = sampled[r];  // within the vocabulary
+  } else {
+    const unsigned long long key = best[r];
+    best[r] = 0ull;  // ready for the next step's atomicMax
+    tok = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(key & 0xFFFFFFFFull));
+    if (key == 0ull || tok < 0 || tok >= V) {
+      set_dev_error(err, DEVERR_BOUNDS);
+      tok = 0;
+    }
   }
   const int was_done = t == 0 ? 0 : done[r];
   if (t == 0) gen_len[r] = max_new;
@@ -501,6 +506,22 @@ __global__ void k_decode_select(unsigned long long* best, int R, int t, int max_
   done[r] = was_done || tok == eos;
   next_tok[r] = tok;
   pos[r] = P + (seq_start[r + 1] - seq_start[r]) + t;
+}
+
+// u[r] = step t's number of row r's table row, uniforms [table rows][max_new].
+__global__ void k_gather_uniforms(const float* uniforms, const int32_t* ids, int max_new, int t, int R, float* u) {
+  grid_launch_next();
+  grid_wait();
+  const int r = blockIdx.x * blockDim.x + threadIdx.x;
+  if (r < R) u[r] = uniforms[static_cast<int64_t>(ids[r]) * max_new + t];
+}
+
+// out[r] = src[0 .. width) in every row (width a multiple of 4, 16-byte aligned).
+__global__ void k_fill_rows(const float* src, int width, float* out) {
+  grid_launch_next();
+  grid_wait();
+  float4* dst = reinterpret_cast<float4*>(out + blockIdx.x * static_cast<int64_t>(width));
+  for (int i = threadIdx.x; i < width / 4; i += blockDim.x) dst[i] = reinterpret_cast<const float4*>(src)[i];
 }
 
 // Rows of a chunk whose text is empty take the shared prefix's last hidden state.
@@ -588,12 +609,23 @@ int launch_decode_attention(const __half* qkv, int64_t ldq, int R, int Hq, int H
   }
 }
 
-void launch_decode_select(unsigned long long* best, int R, int t, int max_new, int eos, int pad, int V, int32_t* done,
+void launch_decode_select(unsigned long long* best, const int32_t* sampled, int R, int t, int max_new, int eos, int pad, int V, int32_t* done,
                           int32_t* gen_tok, int32_t* gen_len, int32_t* next_tok, int32_t* pos,
                           const int32_t* seq_start, int P, int* err, cudaStream_t s) {
   if (R <= 0) return;
-  launch_chained(k_decode_select, dim3((R + 255) / 256), 256, 0, s, 1, best, R, t, max_new, eos, pad, V, done, gen_tok, gen_len, next_tok,
+  launch_chained(k_decode_select, dim3((R + 255) / 256), 256, 0, s, 1, best, sampled, R, t, max_new, eos, pad, V, done, gen_tok, gen_len, next_tok,
                                                   pos, seq_start, P, err);
+}
+
+void launch_gather_uniforms(const float* uniforms, const int32_t* ids, int max_new, int t, int R, float* u,
+                            cudaStream_t s) {
+  if (R <= 0) return;
+  launch_chained(k_gather_uniforms, dim3((R + 255) / 256), 256, 0, s, 1, uniforms, ids, max_new, t, R, u);
+}
+
+void launch_fill_rows(const float* src, int rows, int width, float* out, cudaStream_t s) {
+  if (rows <= 0) return;
+  launch_chained(k_fill_rows, dim3(rows), 256, 0, s, 1, src, width, out);
 }
 
 void launch_patch_empty_rows(float* resid, const int32_t* last_idx, const float* prefix_last, int R, int d,

@@ -258,10 +258,15 @@ int launch_decode_attention(const __half* qkv, int64_t ldq, int R, int Hq, int H
                             const __half* kvc, const int32_t* seq_start, __half* gkv, int gcap, int slot, __half* out,
                             int* err, int num_sms, cudaStream_t s);
 // Token of step t for every row from the packed LM-head argmax (best[] is reset
-// to 0), pad after an eos, and the fed-back position P + len + t.
-void launch_decode_select(unsigned long long* best, int R, int t, int max_new, int eos, int pad, int V, int32_t* done,
+// to 0) or, where sampled is given, from it, pad after an eos, and the fed-back
+// position P + len + t.
+void launch_decode_select(unsigned long long* best, const int32_t* sampled, int R, int t, int max_new, int eos, int pad, int V, int32_t* done,
                           int32_t* gen_tok, int32_t* gen_len, int32_t* next_tok, int32_t* pos,
                           const int32_t* seq_start, int P, int* err, cudaStream_t s);
+void launch_gather_uniforms(const float* uniforms, const int32_t* ids, int max_new, int t, int R, float* u,
+                            cudaStream_t s);
+// out [rows][width] = src [width] in every row (width a multiple of 4, 16-byte aligned).
+void launch_fill_rows(const float* src, int rows, int width, float* out, cudaStream_t s);
 void launch_patch_empty_rows(float* resid, const int32_t* last_idx, const float* prefix_last, int R, int d,
                              cudaStream_t s);
 void launch_bias_f32(const uint16_t* b, int V, int Vpad, float* out, cudaStream_t s);

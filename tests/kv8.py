@@ -132,3 +132,43 @@ def sample(z, u, temperature, top_k, top_p, min_p):
         n = min(n, 1 + int((c < top_p * c[-1]).sum()))
     i = min(n - 1, int((c[:n] <= float(np.float32(u)) * c[n - 1]).sum()))
     return int(order[i]), e[i] / c[n - 1]
+
+
+def logits_on_8_bits(m, prefix, text, generated):
+    """Vocabulary logits [len(generated) + 1, V] of an oracle model for the steps that
+    follow prefix ++ text, teacher-forced on `generated`, where generated tokens attend
+    the 8-bit cache: prefix and text quantised block by block, earlier tokens in
+    whole blocks too, the open block as it is.  (Keys and values are rounded to fp16
+    first, as they are stored before they are quantised.)"""
+    from oracle import transformer as tf
+    s, n0 = m.s, len(prefix) + len(text)
+    ids = np.concatenate([prefix, text, generated]).astype(np.int64)
+    n, pos = len(ids), np.arange(len(ids))
+    x = m.embed_rows(ids)
+    kd = s.n_kv_heads * s.head_dim
+
+    def held(rows):  # whole sequences, as the cache holds them
+        if len(rows) == 0:
+            return np.zeros((0, 2, s.n_kv_heads, s.head_dim))
+        _, _, q, sc = build_cache(rows.reshape(len(rows), 2 * kd).astype(np.float16), [len(rows)], s.n_kv_heads, s.head_dim)
+        return q * sc[..., None]
+
+    for l in range(s.n_layers):
+        w = {name: m.get(f"l{l}.{name}") for name in tf.LAYER_TENSORS}
+        h = tf.rmsnorm(x, w["attn_norm"], s.rms_eps)
+        q = tf.rope((h @ w["wq"].T).reshape(n, s.n_heads, s.head_dim), pos, s.rope_theta)
+        k = tf.rope((h @ w["wk"].T).reshape(n, s.n_kv_heads, s.head_dim), pos, s.rope_theta)
+        v = (h @ w["wv"].T).reshape(n, s.n_kv_heads, s.head_dim)
+        a = np.zeros((n, s.n_heads, s.head_dim))
+        a[:n0] = tf.causal_attention(q[:n0], k[:n0], v[:n0])
+        kv = np.stack([k, v], 1)
+        prompt = np.concatenate([held(kv[:len(prefix)]), held(kv[len(prefix):n0])])
+        for i in range(n0, n):
+            whole = n0 + (i - n0) // BLOCK * BLOCK
+            see = np.concatenate([prompt, held(kv[n0:whole]), kv[whole:i + 1]])
+            a[i], _ = attend(q[i], see[:, 0], see[:, 1])
+        x = x + a.reshape(n, -1) @ w["wo"].T
+        h = tf.rmsnorm(x, w["mlp_norm"], s.rms_eps)
+        x = x + (tf.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
+    h = tf.rmsnorm(x[n0 - 1:], m.get("final_norm"), s.rms_eps)
+    return h @ tf.bf16_to_f64(m.w["lm_head"]).T + tf.bf16_to_f64(m.w["lm_bias"])
