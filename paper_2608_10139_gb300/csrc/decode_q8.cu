@@ -295,7 +295,7 @@ struct Task8 {
   int len;
   int tiles;
 };
-__device__ __forceinline__ int tiles_of(int keys) { return (keys + kTileKeys - 1) / kTileKeys; }
+__device__ __forceinline__ int tiles_of(int keys) { return keys / kTileKeys + (keys % kTileKeys != 0); }
 __device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int64_t i, int64_t n_tasks) {
   Task8 t{0, 0, 0, 0, 0};
   if (i >= n_tasks) return t;
@@ -583,7 +583,7 @@ struct Split8 {
 };
 __device__ __forceinline__ int64_t share(const DecQ8Args& a, int64_t R, int64_t units, int64_t r) {
   // keys before row r, and something for each row's start, prefix and generated tokens
-  const int64_t more = a.P + a.slot + 48;
+  const int64_t more = static_cast<int64_t>(a.P) + a.slot + 48;
   const int64_t before = a.seq_start[r] + r * more, all = a.seq_start[R] + R * more;
   return r + (units - R) * before / (all > 0 ? all : 1);
 }

@@ -257,6 +257,24 @@ def test_attention_sizes(ctx, heads, lens):
     s.check(out, qkv)
 
 
+@pytest.mark.parametrize("heads,rows", [((8, 8, 32), 700), ((8, 8, 64), 700), ((8, 2, 64), 2500), ((4, 4, 128), 1000)], ids=str)
+@pytest.mark.parametrize("slot", [0, 31, 40])
+def test_many_rows(ctx, heads, rows, slot):
+    """Batches in which a warp takes whole tasks, one after the other; rows of every small length."""
+    Hq, Hkv, hd = heads
+    s = Step(slot, *heads, [i % 71 for i in range(rows)], 33 if slot else 0, 64)
+    s.fill_generated(slot)
+    qkv = s.qkv()
+    out = s.call(ctx, qkv, slot)
+    s.append(qkv)
+    s.check(out, qkv)
+    if slot == 31:
+        gc, gs = s.gc.cpu().numpy(), s.gs.cpu().numpy()
+        for r in range(0, rows, 7):
+            c, sc, _, _ = kv8.build_cache(s.gen[r], [32], Hkv, hd)
+            assert np.array_equal(gc[2 * r], c[0]) and np.array_equal(gs[2 * r], sc[0])
+
+
 @pytest.mark.parametrize("heads", [(4, 4, 32), (6, 2, 64), (8, 1, 128)], ids=str)
 def test_steps_build_the_cache(ctx, heads):
     """70 steps: each output, and the cache that they leave, equal to the tokens quantised at once."""
