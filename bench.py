@@ -73,6 +73,8 @@ def parse():
                    help="AI_TRANSFORM: greedy tokens per candidate row (0: the AI_IF query)")
     p.add_argument("--like", default="", help="AI_TRANSFORM ... LIKE pattern, comma-separated token ids")
     p.add_argument("--decode-rows", type=int, default=0, help="AI_TRANSFORM rows per decode batch (0: library default)")
+    p.add_argument("--kv-bits", type=int, default=16, choices=[8, 16], help="AI_TRANSFORM: bits of cached keys and values")
+    p.add_argument("--top-k", type=int, default=0, help="AI_TRANSFORM: draw tokens from that many (0: greedy)")
     p.add_argument("--pairs", action="store_true", help="Table 2 Q4: AI_IF over the reviews self-joined on movie id")
     return p.parse_args()
 
@@ -695,10 +697,16 @@ def transform_bench(args):
     like = [int(x) for x in args.like.split(",")] if args.like else None
     if args.decode_rows:
         ctx.set_option("decode_rows", args.decode_rows)
+    ctx.set_option("kv_bits", args.kv_bits)
+    draws = {}
+    if args.top_k:
+        u = np.random.default_rng(w.data_seed).random((w.n_rows, args.transform), dtype=np.float32)
+        draws = dict(sampling=dict(temperature=0.8, top_k=args.top_k, top_p=0.95),
+                     uniforms=np.minimum(u, np.float32(1 - 2.0 ** -24)))
     flush = torch.empty(2 * L2_BYTES // 4, dtype=torch.float32, device="cuda")
 
     def run():
-        return ctx.run_transform(table, model, preds, q.prefix, args.transform, like=like)
+        return ctx.run_transform(table, model, preds, q.prefix, args.transform, like=like, **draws)
 
     for _ in range(args.warmup):
         run()
@@ -721,7 +729,7 @@ def transform_bench(args):
     pk, src = peaks()
     att = stats.get("decode_attention", {"total_ms": 0, "bytes": 0, "launches": 0})
     att_gbs = att["bytes"] / (att["total_ms"] / 1000.0) / 1e9 if att["total_ms"] else None
-    dg = [v for k, v in stats.items() if k.startswith("dec_gemm_") or k == "gemm_lm_argmax"]
+    dg = [v for k, v in stats.items() if k.startswith("dec_gemm_") or k in ("gemm_lm_argmax", "gemm_lm_logits")]
     dg_ms = sum(v["total_ms"] for v in dg)
     dg_tf = sum(v["flops"] for v in dg) / (dg_ms / 1000.0) / 1e12 if dg_ms else None
     line = {"metric": "AI_TRANSFORM generated tokens/s", "value": gen_tokens / (ms / 1000.0), "unit": "tokens/s",
@@ -729,7 +737,7 @@ def transform_bench(args):
             "data": "synthetic",
             "config": {"workload": w.name, "rows": w.n_rows, "candidates": r.n_candidates,
                        "max_new_tokens": args.transform, "like": like, "chunks": r.n_chunks,
-                       "decode_rows": args.decode_rows or 4096},
+                       "decode_rows": args.decode_rows or 4096, "kv_bits": args.kv_bits, "top_k": args.top_k},
             "input_rows_per_s": w.n_rows / (ms / 1000.0), "p50_latency_ms": ms, "decode_ms_p50": dec_ms,
             "prefill_ms_p50": statistics.median([x.ms_prefill - x.ms_decode for x in res]),
             "decode_tflops": r.decode_flops / (dec_ms / 1000.0) / 1e12 if dec_ms else None,
