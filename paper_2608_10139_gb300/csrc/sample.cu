@@ -25,10 +25,12 @@ namespace {
 using Key = unsigned long long;  // a logit's order bits, then ~index: descending keys are the order of the draw
 
 constexpr int kRowThreads = 128;
-constexpr int kRowCtas = 9;                           // per SM
+constexpr int kRowCtas = 8;                           // per SM
 constexpr int kPerThread = 16;                        // elements of a chunk
 constexpr int kRowChunk = kRowThreads * kPerThread;
 constexpr int kMergeThreads = 1024;
+// As many as that are counted by the threads' own maxima, and sorted one a thread.
+__host__ __device__ constexpr int few(int threads) { return threads * 3 / 4; }
 // What a list is cut back to at most, and a chunk more, and a row's unaligned ends.
 __host__ __device__ constexpr int list_most(int k) { return k + (k / 4 > 32 ? k / 4 : 32); }
 __host__ __device__ constexpr int list_size(int k, int threads) { return list_most(k) + threads * kPerThread + 32; }
@@ -75,13 +77,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return m;
 }
 
-// c ? a : b, as one instruction: a chain of ?: would become an indexed array, in memory.
-__device__ __forceinline__ float pick(bool c, float a, float b) {
-  float x;
-  asm("{ .reg .pred p; setp.ne.b32 p, %1, 0; selp.f32 %0, %2, %3, p; }" : "=f"(x) : "r"(static_cast<int>(c)), "f"(a), "f"(b));
-  return x;
-}
-
 // Shared memory of a block.
 struct Shared {
   Key top, bottom;
@@ -120,6 +115,14 @@ __device__ __forceinline__ void push(Shared& s, bool want, F key) {
   if (lane == 0) at = atomicAdd(&s.n, __popc(all));
   at = __shfl_sync(0xffffffffu, at, 0) + __popc(all & ((1u << lane) - 1));
   if (want) s.list()[at] = key();
+}
+
+// A place on the list for one lane.  (An atomicAdd of 1 would be gathered from the
+// warp's lanes by the compiler, three times the instructions for one or two of them.)
+__device__ __forceinline__ int place(Shared& s) {
+  int at;
+  asm volatile("atom.shared.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(smem_u32(&s.n)) : "memory");
+  return at;
 }
 
 // Cuts a list of more than `most` entries back to its largest ones, k to `most` of
@@ -211,11 +214,12 @@ __device__ __forceinline__ double exp_neg(double x) {
 }
 
 // The draw from a complete list.
-template <int NT>
+template <int NT, bool FEW>
 __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round, int64_t r, bool bad) {
   // what is sorted: a power of two, and NT entries (one a thread) as they are
   int size = NT;
-  while (size < a.k) size <<= 1;
+  if constexpr (!FEW)
+    while (size < a.k) size <<= 1;
   cut<NT>(s, round, a.k, size);
   __syncthreads();
   const int n_all = s.n, tid = threadIdx.x;
@@ -230,7 +234,7 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
   }
   // descending, bitonic
   Key* sorted = s.list();
-  if (size == NT) {
+  if (FEW || size == NT) {
     Key mine = tid < n_all ? sorted[tid] : 0;
     for (int run = 2; run <= NT; run <<= 1) {
       for (int step = run >> 1; step; step >>= 1) {
@@ -272,8 +276,8 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
   }
   const int k = n_all < a.k ? n_all : a.k;
   // A thread's run of consecutive places; warps without any stay out of the 64-bit arithmetic.
-  constexpr int MOST = (kSampleKeepMax + NT - 1) / NT;
-  const int per = (k + NT - 1) / NT, lane = tid & 31, warp = tid >> 5;
+  constexpr int MOST = FEW ? 1 : (kSampleKeepMax + NT - 1) / NT;
+  const int per = FEW ? 1 : (k + NT - 1) / NT, lane = tid & 31, warp = tid >> 5;
   const bool busy = warp * 32 * per < k;
   double e[MOST], c[MOST];
   if (busy) {
@@ -397,7 +401,7 @@ __device__ __forceinline__ void begin(Shared& s, int list) {
 // Lists the candidates of elements s0 .. s1 - 1 of a row: at least the k largest
 // (all that are finite, where there are fewer).  Returns the key from which
 // nothing is missing (0: nothing at all is), and whether a NaN or +inf came by.
-template <typename T, int NT>
+template <typename T, int NT, bool FEW>
 __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0, int s1, int k, bool& bad) {
   constexpr int VEC = 16 / sizeof(T), GROUPS = kPerThread / VEC, CHUNK = NT * kPerThread;
   const int tid = threadIdx.x;
@@ -453,7 +457,7 @@ __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0,
     bound = -INFINITY;
     from = 0;
     if (tid < 32) single(s0 + tid, v0);
-    const bool by_threads = want <= NT * 3 / 4;
+    const bool by_threads = FEW || want <= few(NT);
     float mx = max_nan(v[0], next[0]);
 #pragma unroll
     for (int j = 1; j < kPerThread; ++j) mx = max_nan(mx, max_nan(v[j], next[j]));
@@ -500,19 +504,11 @@ __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0,
 #pragma unroll
         for (int e = 1; e < VEC; ++e) top = max_nan(top, v[w * VEC + e]);
         seen = max_nan(seen, top);
-        // a lane lists its elements one after the other: most that list any have one
-        uint32_t hits = 0;
-        if (__any_sync(0xffffffffu, top > bound)) {
+        // Few lanes list anything, and most of those one element: each takes its place by itself.
+        if (top > bound) {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) hits |= v[w * VEC + e] > bound ? 1u << e : 0u;
-          while (__any_sync(0xffffffffu, hits)) {
-            const int e = __ffs(hits) - 1;
-            float x = 0.f;
-#pragma unroll
-            for (int f = 0; f < VEC; ++f) x = pick(e == f, v[w * VEC + f], x);
-            push(s, hits, [&] { return key_of(x, index(base, w * VEC) + e); });
-            hits &= hits - 1;
-          }
+          for (int e = 0; e < VEC; ++e)
+            if (v[w * VEC + e] > bound) s.list()[place(s)] = key_of(v[w * VEC + e], index(base, w * VEC + e));
         }
       }
       load(base + CHUNK, v);
@@ -537,8 +533,10 @@ __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0,
   return from;
 }
 
-// A CTA per slice of a row.
-template <typename T>
+// A CTA per slice of a row.  FEW: k <= few(kRowThreads), which most draws are; the
+// code for more would take twice the instructions' room, and an SM's eight rows
+// are at as many places in it.
+template <typename T, bool FEW>
 __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_sample_rows(SampleArgs a) {
   grid_launch_next();
   grid_wait();
@@ -550,9 +548,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_sample_rows(SampleArg
   const int s0 = static_cast<int>(blockIdx.x % a.slices) * a.slice_len;
   int round = 0;
   bool bad;
-  Key from = scan<T, NT>(s, round, static_cast<const T*>(a.logits) + r * a.ld, s0, min(a.V, s0 + a.slice_len), a.slice_k, bad);
+  Key from = scan<T, NT, FEW>(s, round, static_cast<const T*>(a.logits) + r * a.ld, s0, min(a.V, s0 + a.slice_len), a.slice_k, bad);
   if (a.slices == 1) {
-    draw<NT>(a, s, round, r, bad);
+    draw<NT, FEW>(a, s, round, r, bad);
     return;
   }
   const int most = list_most(a.slice_k);
@@ -615,9 +613,9 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
     __syncthreads();
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    scan<T, NT>(s, round, static_cast<const T*>(a.logits) + r * a.ld, 0, a.V, a.k, bad);
+    scan<T, NT, false>(s, round, static_cast<const T*>(a.logits) + r * a.ld, 0, a.V, a.k, bad);
   }
-  draw<NT>(a, s, round, r, bad);
+  draw<NT, false>(a, s, round, r, bad);
 }
 static_assert(kMergeList >= list_size(kSampleKeepMax, kMergeThreads), "a row's list fits too");
 
@@ -638,7 +636,9 @@ Plan plan_of(int R, int V, int top_k, int num_sms) {
 template <typename T>
 int launch_rows(const SampleArgs& a, int R, cudaStream_t s) {
   static_assert(shared_bytes(list_size(kSampleKeepMax, kRowThreads)) <= 48 * 1024, "no larger shared memory to ask for");
-  cudaError_t e = launch_chained(k_sample_rows<T>, dim3(static_cast<unsigned>(R) * a.slices), kRowThreads,
+  // (a slice's draw is the merge's)
+  void (*rows)(SampleArgs) = a.slice_k <= few(kRowThreads) ? k_sample_rows<T, true> : k_sample_rows<T, false>;
+  cudaError_t e = launch_chained(rows, dim3(static_cast<unsigned>(R) * a.slices), kRowThreads,
                                  shared_bytes(list_size(a.slice_k, kRowThreads)), s, 1, a);
   if (e != cudaSuccess || a.slices == 1) return e;
   constexpr int smem = shared_bytes(kMergeList);
