@@ -29,11 +29,14 @@ constexpr int kRowCtas = 8;                           // per SM
 constexpr int kPerThread = 16;                        // elements of a chunk
 constexpr int kRowChunk = kRowThreads * kPerThread;
 constexpr int kMergeThreads = 1024;
+constexpr int kDrawThreads = 256;
 // As many as that are counted by the threads' own maxima, and sorted one a thread.
 __host__ __device__ constexpr int few(int threads) { return threads * 3 / 4; }
-// What a list is cut back to at most, and a chunk more, and a row's unaligned ends.
-__host__ __device__ constexpr int list_most(int k) { return k + (k / 4 > 32 ? k / 4 : 32); }
-__host__ __device__ constexpr int list_size(int k, int threads) { return list_most(k) + threads * kPerThread + 32; }
+// What a list is cut back to at most; what it may hold before it is; and a chunk
+// more, and a row's unaligned ends.
+__host__ __device__ constexpr int list_most(int k) { return k + (k / 4 > 8 ? k / 4 : 8); }
+__host__ __device__ constexpr int list_hold(int k, int threads) { return list_most(k) > 2 * threads ? list_most(k) : 2 * threads; }
+__host__ __device__ constexpr int list_size(int k, int threads) { return list_hold(k, threads) + threads * kPerThread + 32; }
 // The merge of slices lists that many before it cuts them back.
 constexpr int kMergeList = 22 * 1024;
 
@@ -79,30 +82,49 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 // Shared memory of a block.
 struct Shared {
-  Key top, bottom;
+  Key top;
   double sums[32];
   double total;
   int n;         // entries of the list
-  int count[3];  // of the rounds of block_count
+  int part[2][32];  // of the rounds of block_count: the warps' sums
   unsigned int highest, lowest;
   int size;      // of the list, which lies behind this
-  int unused;
   __device__ __forceinline__ Key* list() { return reinterpret_cast<Key*>(this + 1); }
 };
 static_assert(sizeof(Shared) % sizeof(Key) == 0, "the list is aligned");
 constexpr int shared_bytes(int list) { return static_cast<int>(sizeof(Shared)) + list * static_cast<int>(sizeof(Key)); }
 
-// The sum over the block; `round` counts the calls (one barrier each: a call's
-// sum is cleared during the one before it).
+// Barrier of the first NT threads, which may be all that are left of a block.
+template <int NT>
+__device__ __forceinline__ void sync() {
+  asm volatile("barrier.sync 1, %0;" ::"n"(NT) : "memory");
+}
+
+// The sum over the block, one barrier; `round` counts the calls, which take the
+// two rows of sums in turns.
 template <int NT>
 __device__ __forceinline__ int block_count(Shared& s, int& round, int v) {
-  const int at = round % 3;
+  int* part = s.part[round++ & 1];
   v = __reduce_add_sync(0xffffffffu, v);
-  if ((threadIdx.x & 31) == 0) atomicAdd(&s.count[at], v);
-  if (threadIdx.x == 0) s.count[(at + 1) % 3] = 0;
-  __syncthreads();
-  ++round;
-  return s.count[at];
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  sync<NT>();
+  const int lane = threadIdx.x & 31;
+  return __reduce_add_sync(0xffffffffu, lane < NT / 32 ? part[lane] : 0);
+}
+
+// The next bound to count at between lo, which more reach than wanted, and hi,
+// which fewer do (by two at least): where `want` would lie on the line between
+// their counts, and halfway in every other round, so that 64 rounds always do.
+template <typename U>
+__device__ __forceinline__ U between(U lo, U hi, int count_lo, int count_hi, int want, int i) {
+  const U width = hi - lo;
+  U step = width / 2;
+  if (!(i & 1)) {
+    const float part = __fdividef(static_cast<float>(count_lo - want), static_cast<float>(count_lo - count_hi));
+    step = static_cast<U>(static_cast<float>(width) * part);
+  }
+  step = step < 1 ? 1 : step;
+  return lo + (step < width ? step : width - 1);
 }
 
 // Lists the keys of the lanes that want it; the whole warp calls.
@@ -126,42 +148,41 @@ __device__ __forceinline__ int place(Shared& s) {
 }
 
 // Cuts a list of more than `most` entries back to its largest ones, k to `most` of
-// them, by bisection; returns the key from which they were kept (0: all).  Ends
-// after 64 rounds at most: keys are all different.
+// them, by counting; returns the key from which they were kept (0: all).  Ends: keys
+// are all different.
 template <int NT>
 __device__ __forceinline__ Key cut(Shared& s, int& round, int k, int most) {
-  __syncthreads();
+  sync<NT>();
   const int n = s.n;
   if (n <= most) return 0;
-  if (threadIdx.x == 0) s.top = 0, s.bottom = ~0ull;
-  __syncthreads();
-  Key top = 0, bottom = ~0ull;
+  // the keys' range by their upper halves (64-bit maxima in shared memory are slow)
+  if (threadIdx.x == 0) s.highest = 0, s.lowest = ~0u;
+  sync<NT>();
+  uint32_t high = 0, low = ~0u;
   for (int i = threadIdx.x; i < n; i += NT) {
-    const Key x = s.list()[i];
-    top = x > top ? x : top;
-    bottom = x < bottom ? x : bottom;
+    const uint32_t x = static_cast<uint32_t>(s.list()[i] >> 32);
+    high = max(high, x);
+    low = min(low, x);
   }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    const Key x = __shfl_xor_sync(0xffffffffu, top, d), y = __shfl_xor_sync(0xffffffffu, bottom, d);
-    top = x > top ? x : top;
-    bottom = y < bottom ? y : bottom;
-  }
+  high = __reduce_max_sync(0xffffffffu, high);
+  low = __reduce_min_sync(0xffffffffu, low);
   if ((threadIdx.x & 31) == 0) {
-    atomicMax(&s.top, top);
-    atomicMin(&s.bottom, bottom);
+    atomicMax(&s.highest, high);
+    atomicMin(&s.lowest, low);
   }
-  __syncthreads();
-  Key lo = s.bottom, hi = s.top + 1, mid;  // n > most entries reach lo, none (< k) reaches hi
-  while (true) {
-    mid = lo + (hi - lo) / 2;
+  sync<NT>();
+  // n > most entries reach lo, none (< k) reaches hi
+  Key lo = static_cast<Key>(s.lowest) << 32, hi = static_cast<Key>(s.highest + 1) << 32, mid;
+  int count_lo = n, count_hi = 0;
+  for (int r = 0;; ++r) {
+    mid = between(lo, hi, count_lo, count_hi, (k + most) / 2, r);
     int c = 0;
     for (int i = threadIdx.x; i < n; i += NT) c += s.list()[i] >= mid;
     c = block_count<NT>(s, round, c);
     if (c > most)
-      lo = mid;
+      lo = mid, count_lo = c;
     else if (c < k)
-      hi = mid;
+      hi = mid, count_hi = c;
     else
       break;
   }
@@ -169,9 +190,9 @@ __device__ __forceinline__ Key cut(Shared& s, int& round, int k, int most) {
   if (threadIdx.x == 0) s.n = 0;
   for (int base = 0; base < n; base += NT) {
     const Key x = base + threadIdx.x < n ? s.list()[base + threadIdx.x] : 0;
-    __syncthreads();
+    sync<NT>();
     push(s, x >= mid, [&] { return x; });
-    __syncthreads();
+    sync<NT>();
   }
   return mid;
 }
@@ -221,7 +242,7 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
   if constexpr (!FEW)
     while (size < a.k) size <<= 1;
   cut<NT>(s, round, a.k, size);
-  __syncthreads();
+  sync<NT>();
   const int n_all = s.n, tid = threadIdx.x;
   const float u = a.u[r];
   if (bad || n_all == 0 || !(u >= 0.f && u < 1.f)) {
@@ -240,9 +261,9 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       for (int step = run >> 1; step; step >>= 1) {
         Key other;
         if (step >= 32) {
-          __syncthreads();
+          sync<NT>();
           sorted[tid] = mine;
-          __syncthreads();
+          sync<NT>();
           other = sorted[tid ^ step];
         } else {
           other = __shfl_xor_sync(0xffffffffu, mine, step);
@@ -251,12 +272,12 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
         mine = ((tid & step) == 0) == ((tid & run) == 0) ? max(mine, other) : min(mine, other);
       }
     }
-    __syncthreads();
+    sync<NT>();
     sorted[tid] = mine;
-    __syncthreads();
+    sync<NT>();
   } else {
     for (int i = n_all + tid; i < size; i += NT) sorted[i] = 0;
-    __syncthreads();
+    sync<NT>();
     for (int run = 2; run <= size; run <<= 1)
       for (int step = run >> 1; step; step >>= 1) {
         for (int i = tid; i < size / 2; i += NT) {
@@ -269,7 +290,7 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
         }
         // pairs up to 32 apart stay within the 64 entries that a warp has
         if (step > 32 || step == 1)
-          __syncthreads();
+          sync<NT>();
         else
           __syncwarp();
       }
@@ -309,7 +330,7 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       c[j] += upto;
     }
   }
-  __syncthreads();
+  sync<NT>();
   if constexpr (NT > 256) {  // the sums' own prefix sums, by one warp
     if (warp == 0) {
       double x = lane * 32 * per < k ? s.sums[lane] : 0;
@@ -320,7 +341,7 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       }
       s.sums[lane] = x;
     }
-    __syncthreads();
+    sync<NT>();
   }
   if (busy && warp) {
     double before = 0;
@@ -334,19 +355,6 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       c[j] += before;
     }
   }
-  // places with e >= min_p: a prefix
-  int n = k;
-  if (a.min_p > 0) {
-    int in = 0;
-    if (busy) {
-#pragma unroll
-      for (int j = 0; j < MOST; ++j) {
-        if (j >= per) break;
-        in += tid * per + j < k && e[j] >= a.min_p;
-      }
-    }
-    n = block_count<NT>(s, round, in);
-  }
   const auto sum_to = [&](int place) {  // C of a place, for all threads
     if (busy) {
 #pragma unroll
@@ -355,26 +363,29 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
         if (tid * per + j == place) s.total = c[j];
       }
     }
-    __syncthreads();
+    sync<NT>();
     return s.total;
   };
-  const auto places_where = [&](auto f, int end) {
+  // Two counts of places in one round.
+  const auto places_where = [&](int end, auto f, auto g) {
     int in = 0;
     if (busy) {
 #pragma unroll
       for (int j = 0; j < MOST; ++j) {
         if (j >= per) break;
-        in += tid * per + j < end && f(c[j]);
+        if (tid * per + j < end) in += (f(j) ? 1 : 0) + (g(j) ? 1 << 16 : 0);
       }
     }
     return block_count<NT>(s, round, in);
   };
-  if (a.top_p < 1.0) {
-    const double enough = a.top_p * sum_to(k - 1);
-    n = min(n, 1 + places_where([&](double x) { return x < enough; }, k));
+  int n = k;
+  if (a.top_p < 1.0 || a.min_p > 0) {
+    const double enough = a.top_p < 1.0 ? a.top_p * sum_to(k - 1) : INFINITY;
+    const int both = places_where(k, [&](int j) { return e[j] >= a.min_p; }, [&](int j) { return c[j] < enough; });
+    n = a.top_p < 1.0 ? min(both & 0xffff, 1 + (both >> 16)) : both & 0xffff;
   }
   const double kept = sum_to(n - 1), target = static_cast<double>(u) * kept;
-  const int at = min(n - 1, places_where([&](double x) { return x <= target; }, n));
+  const int at = min(n - 1, places_where(n, [&](int j) { return c[j] <= target; }, [](int) { return false; }));
   if (busy) {
 #pragma unroll
     for (int j = 0; j < MOST; ++j) {
@@ -393,7 +404,6 @@ __device__ __forceinline__ void begin(Shared& s, int list) {
     s.size = list;
     s.top = 0;
     s.highest = 0, s.lowest = ~0u;
-    s.count[0] = s.count[1] = s.count[2] = 0;
   }
   __syncthreads();
 }
@@ -473,8 +483,9 @@ __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0,
     uint32_t lo = 0x007fffffu, hi = min(s.highest, 0xff800000u) + 1;  // -inf; the largest and one more
     if (by_threads) lo = max(lo, s.lowest);
     const int most = by_threads ? want + want / 8 + 4 : list_most(want);
-    while (hi - lo > 1) {
-      const uint32_t mid = lo + (hi - lo) / 2;
+    int count_lo = by_threads ? NT : 2 * CHUNK, count_hi = 0;
+    for (int i = 0; hi - lo > 1; ++i) {
+      const uint32_t mid = between(lo, hi, count_lo, count_hi, (want + most) / 2, i);
       int c;
       if (by_threads) {
         c = mine >= mid;
@@ -486,9 +497,9 @@ __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0,
       }
       c = block_count<NT>(s, round, c);
       if (c < want) {
-        hi = mid;
+        hi = mid, count_hi = c;
       } else {
-        lo = mid;
+        lo = mid, count_lo = c;
         if (c <= most) break;
       }
     }
@@ -513,7 +524,7 @@ __device__ __forceinline__ Key scan(Shared& s, int& round, const T* row, int s0,
       }
       load(base + CHUNK, v);
       // (whoever lists last sees its own entries counted)
-      if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > list_most(k))) {
+      if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > list_hold(k, NT))) {
         // of what follows, only larger values can be among the k largest: equal ones come later
         const uint32_t least = static_cast<uint32_t>(cut<NT>(s, round, k, list_most(k)) >> 32);
         bound = fmaxf(bound, order_value(least));
@@ -611,11 +622,18 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
   for (int i = threadIdx.x; i < s.n; i += NT) in += s.list()[i] >= all;
   if (!bad && all && block_count<NT>(s, round, in) < a.k) {
     __syncthreads();
-    if (threadIdx.x == 0) s.n = 0;
+    if (threadIdx.x == 0) s.n = 0, s.highest = 0, s.lowest = ~0u;
     __syncthreads();
     scan<T, NT, false>(s, round, static_cast<const T*>(a.logits) + r * a.ld, 0, a.V, a.k, bad);
   }
-  draw<NT, false>(a, s, round, r, bad);
+  if (a.k <= kDrawThreads) {
+    // eight warps are enough, and their barriers cheaper
+    cut<NT>(s, round, a.k, 8 * kDrawThreads);
+    sync<NT>();
+    if (threadIdx.x < kDrawThreads) draw<kDrawThreads, true>(a, s, round, r, bad);
+  } else {
+    draw<NT, false>(a, s, round, r, bad);
+  }
 }
 static_assert(kMergeList >= list_size(kSampleKeepMax, kMergeThreads), "a row's list fits too");
 
@@ -629,7 +647,7 @@ Plan plan_of(int R, int V, int top_k, int num_sms) {
   const int64_t len = (pairs + want - 1) / want * 2 * kRowChunk;
   if (len >= V) return Plan{1, V, top_k};
   const double mean = static_cast<double>(top_k) * len / V;
-  const int k = static_cast<int>(std::min<double>(top_k, std::ceil(mean + 4 * std::sqrt(mean) + 8)));
+  const int k = static_cast<int>(std::min<double>(top_k, std::ceil(mean + 4 * std::sqrt(mean) + 4)));
   return Plan{static_cast<int>((V + len - 1) / len), static_cast<int>(len), k};
 }
 
