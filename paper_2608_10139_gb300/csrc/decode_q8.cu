@@ -2,6 +2,13 @@
 // row r's new token against the shared prefix, its own prompt, the generated
 // tokens in whole blocks (all 8 bits) and the open block of fewer than 32
 // generated tokens, which stays fp16 until the step that fills it quantises it.
+//
+// out = sum_j p_j v_j / sum_j p_j, p_j = 2^(s_j - m), in one pass over the keys with
+// the running maximum m, sum and output of a softmax in fp32.  Of a tile, scores are
+// s_k log2(e) / sqrt(hd) * (q . k) and the output's share is s_v * (p . v), products
+// of fp16 numbers with whole ones, so that the scales cost one multiplication per
+// score and per output element, and nothing is rounded before the products but the
+// probabilities.
 #include <algorithm>
 
 #include "kernels.h"
@@ -455,7 +462,15 @@ struct Stream8 {
 };
 
 // Many rows: a persistent warp per (row, KV head) task, the entries of all its
-// tasks as one stream through its ring.
+// tasks as one stream through its ring.  Long rows run at the memory's rate (2,432
+// rows of about 720 keys, 32/8 heads, head_dim 64, 1.53 GB: 245 us, 0.92 of the
+// copy); short ones at the issue slots' (some 355 instructions a tile, 128 of them
+// bytes to fp16, and 1,000 a task): 3,263 rows of about 217 keys, 592 MB, take 139 us,
+// 0.63 of the copy.  The fp16 cache's kernel takes 225 us for the same rows.  Not
+// kept: two tiles at a time with one softmax (177 us: short rows have few pairs),
+// tasks drawn from a counter (139), heads as the rows of the A tile, half of it
+// padding (154); 20 or 24 warps an SM with two slots each (the call 156 and 164 us
+// against 155).
 template <int HD>
 __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_decode_q8_stream(DecQ8Args a, int64_t n_tasks) {
   using C = Stream8<HD>;
@@ -566,7 +581,9 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
 // The tiles of a (row, KV head) are cut into ranges, a CTA each, whose warps take a
 // range's tiles in turns; they merge their (maximum, sum, output) in shared memory.
 // The ranges' are merged, in their order, by the task's CTA that comes last: a
-// kernel for it took ten microseconds of the four documents' 81.
+// kernel for it took ten microseconds of the four documents' 81.  Those (24,439,
+// 33,879, 18,661 and 65,536 tokens, 32/8 heads, head_dim 128, 292 MB) take 53 us, 0.81 of
+// the copy; 24 rows of about 200 keys, head_dim 64, 8.5 us.
 //
 // A KV head has `units` CTAs, at least one a row, the others shared out by the
 // rows' lengths, which only the device knows: row r's are share(r) .. share(r + 1) - 1.
@@ -792,6 +809,10 @@ template <int HD>
 int units_of(int64_t R, int64_t Hkv, double tiles, int num_sms) {
   using C = Stream8<HD>;
   const int64_t ctas = static_cast<int64_t>(num_sms) * C::CTAS, tasks = R * Hkv;
+  // A warp per task once every warp has two (a CTA per task against that, 32/8 heads,
+  // the call with 43 us around it: head_dim 64, 500 rows of about 200 keys 102 and 101 us,
+  // 1,000 rows 145 and 131; head_dim 128, 500 rows 134 and 125, but 178 and 206 where
+  // they have about 500 keys).
   if (tasks >= 2 * ctas * C::NW) return 0;
   if (tasks > kSplitTasksMax) return static_cast<int>(R);
   // four tiles a warp: shorter ranges cost more in the merge than they save (24 rows of

@@ -9,10 +9,16 @@
 // exponentials and sums are 64 bits wide, so that a row's token hangs on no
 // rounding of 32 bits.
 //
-// A row is read once.  Its first chunk gives a bound that at least k of its
-// elements reach; the row's candidates, what lies above the bound, are listed in
-// shared memory, and the list is cut back to little more than k, raising the
-// bound, where it grows long.  What is left is sorted.
+// A row is read once.  Its first two chunks give a bound; the row's candidates, what
+// lies above the bound, are listed in shared memory, and the list is cut back to
+// little more than k, raising the bound, where it grows long.  What is left is
+// sorted.
+//
+// 3,263 rows of 32,000 fp32 logits (418 MB) with 50 candidates take 89 us, 0.69 of the
+// copy: a row's own steps one after the other (bound, sort, sums) take as long as
+// its read, and eight rows an SM overlap them.  128 threads a row measured best (108
+// us when 256 took 134 and 64 took 129); loading a chunk ahead into registers or the
+// whole row into L2 does not pay (the call 102 us, then 106 and 120).
 #include <algorithm>
 #include <cmath>
 
@@ -32,8 +38,10 @@ constexpr int kMergeThreads = 1024;
 constexpr int kDrawThreads = 256;
 // As many as that are counted by the threads' own maxima, and sorted one a thread.
 __host__ __device__ constexpr int few(int threads) { return threads * 3 / 4; }
-// What a list is cut back to at most; what it may hold before it is; and a chunk
-// more, and a row's unaligned ends.
+// What a list is cut back to at most; what it may hold before it is; and its size.
+// Whoever lists a chunk begins with list_hold entries at most, an unaligned start's
+// (up to 7) among them, and lists threads * kPerThread more; the list is then cut where
+// it holds more than list_hold; the unaligned end adds up to 7 after the last chunk.
 __host__ __device__ constexpr int list_most(int k) { return k + (k / 4 > 8 ? k / 4 : 8); }
 __host__ __device__ constexpr int list_hold(int k, int threads) { return list_most(k) > 2 * threads ? list_most(k) : 2 * threads; }
 __host__ __device__ constexpr int list_size(int k, int threads) { return list_hold(k, threads) + threads * kPerThread + 32; }
