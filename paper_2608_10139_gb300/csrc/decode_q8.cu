@@ -464,7 +464,7 @@ struct Stream8 {
 // Many rows: a persistent warp per (row, KV head) task, the entries of all its
 // tasks as one stream through its ring.  Long rows run at the memory's rate (2,432
 // rows of about 720 keys, 32/8 heads, head_dim 64, 1.53 GB: 245 us, 0.92 of the
-// copy); short ones at the issue slots' (some 355 instructions a tile, 128 of them
+// copy); short ones at the issue slots' (some 360 instructions a tile, 128 of them
 // bytes to fp16, and 1,000 a task): 3,263 rows of about 217 keys, 592 MB, take 139 us,
 // 0.63 of the copy.  The fp16 cache's kernel takes 225 us for the same rows.  Not
 // kept: two tiles at a time with one softmax (177 us: short rows have few pairs),
