@@ -599,9 +599,9 @@ struct Split8 {
   static_assert(NW * kMaxRanges * 4 <= RING, "and so do the ranges' weights");
 };
 __device__ __forceinline__ int64_t share(const DecQ8Args& a, int64_t R, int64_t units, int64_t r) {
-  // keys before row r, and something for each row's start, prefix and generated tokens
-  const int64_t more = static_cast<int64_t>(a.P) + a.slot + 48;
-  const int64_t before = a.seq_start[r] + r * more, all = a.seq_start[R] + R * more;
+  // own keys before row r, and something for each row's start, prefix and generated tokens
+  const int64_t more = static_cast<int64_t>(a.P) + a.slot + 48, none = a.seq_start[0];
+  const int64_t before = a.seq_start[r] - none + r * more, all = a.seq_start[R] - none + R * more;
   return r + (units - R) * before / (all > 0 ? all : 1);
 }
 

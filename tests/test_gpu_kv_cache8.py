@@ -483,6 +483,30 @@ def test_a_call_after_a_reported_one_is_right(ctx):
         assert np.array_equal(s.call(ctx, qkv, 0), first)
 
 
+@pytest.mark.parametrize("rows,length", [(3, 40), (2, 6000), (700, 20)])
+def test_the_first_sequence_need_not_begin_at_the_first_token(ctx, rows, length):
+    """As aiq_op_kv_quantize lays out sequences that begin at token 77 of the rows at hand."""
+    Hq, Hkv, hd, first = 8, 8 if rows == 700 else 2, 32, 77
+    s = Step(rows, Hq, Hkv, hd, [length + i % 5 for i in range(rows)], 0, 32)
+    starts = kv8.starts(s.lens)
+    nb = kv8.blocks(s.T + first, rows)
+    cache, scales = np.full((nb, Hkv, 64 * hd), 9, np.uint8), np.full((nb, Hkv, 2), np.float32(9))
+    for r in range(rows):
+        n = -(-s.lens[r] // 32)
+        a, b = kv8.first_block(int(starts[r]), r), kv8.first_block(int(starts[r]) + first, r)
+        cache[b:b + n], scales[b:b + n] = s.own_c[a:a + n], s.own_s[a:a + n]
+    qkv = s.qkv()
+    want = s.call(ctx, qkv, 0)
+    s.d[0], s.d[1], s.d[4] = _d(cache), _d(scales), _d(starts + np.int32(first))
+    s.T += first
+    for _ in range(3):
+        out = s.call(ctx, qkv, 0)
+        assert np.abs(out.astype(np.float64) - want).max() <= 2.0 ** -10 * np.abs(want).max()  # (ranges may be cut elsewhere)
+    s.append(qkv)
+    s.T -= first
+    s.check(out, qkv)
+
+
 def test_refusals(ctx):
     buf = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
     p = buf.data_ptr()
