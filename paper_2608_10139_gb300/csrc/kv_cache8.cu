@@ -31,7 +31,10 @@ __device__ __forceinline__ Block8 block_of(const Cache8Args& a, int64_t b) {
     const int64_t step = (hi - lo + 31) / 32, i = lo + lane * step;
     const bool here = i < hi && tile8_first_block(a.seq_start[i], i) <= b;
     const uint32_t found = __ballot_sync(0xffffffffu, here);
-    if (!found) return Block8{0, 0};
+    if (!found) {  // before the first sequence, which may lie behind the last block
+      if (lane == 0 && a.seq_start[0] > a.T) set_dev_error(a.err, DEVERR_BOUNDS);
+      return Block8{0, 0};
+    }
     lo += (31 - __clz(found)) * step;
     hi = lo + step < hi ? lo + step : hi;
     if (step == 1) break;

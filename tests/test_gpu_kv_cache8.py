@@ -148,6 +148,11 @@ def test_sequences_outside_the_rows_are_reported(ctx, starts):
         assert e.value.status == aiq.ERR_DEVICE_CHECK
 
 
+def test_a_first_sequence_behind_the_last_block_is_reported(ctx):
+    test_sequences_outside_the_rows_are_reported(ctx, [1000, 1005])
+    test_sequences_outside_the_rows_are_reported(ctx, [2 ** 31 - 40, 2 ** 31 - 9])
+
+
 # ------------------------------------------------------------------ attention
 
 class Step:
