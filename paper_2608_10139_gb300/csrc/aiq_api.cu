@@ -1470,6 +1470,8 @@ aiq_status run_query(aiq_ctx* c, const TableD* build, int32_t build_key, const a
 
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
+constexpr int32_t kHeadsMax = 1 << 20;  // a row's elements are counted in 32 bits
+
 // What the two copies between fp16 rows and the 8-bit cache ask of their arguments.
 aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
                             int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache, const float* scales) {
@@ -1480,6 +1482,7 @@ aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T,
     return fail(AIQ_ERR_INVALID_ARG, "ldkv must be at least 2 Hkv hd and a multiple of 8");
   if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(seq_start, 4))
     return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
+  if (Hkv > kHeadsMax) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^20 heads");
   if ((T / AIQ_KV_BLOCK + n_seqs) * Hkv > (int64_t(1) << 33))
     return fail(AIQ_ERR_UNSUPPORTED, "more than 2^33 (block, KV head) pairs");
   return AIQ_OK;
@@ -2340,6 +2343,7 @@ aiq_status aiq_op_decode_attention_q8(aiq_ctx* c, const void* qkv, int32_t R, in
       !aligned(gen_tail, 16) || !aligned(out, 16) || !aligned(prefix_scales, 8) || !aligned(own_scales, 8) ||
       !aligned(gen_scales, 8) || !aligned(seq_start, 4))
     return fail(AIQ_ERR_INVALID_ARG, "qkv, caches, gen_tail and out must be 16-byte aligned, scales 8-byte aligned");
+  if (Hq > kHeadsMax) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^20 heads");
   if (int64_t(R) * Hkv > INT32_MAX) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^31 - 1 (row, KV head) pairs");
   if (R == 0) return AIQ_OK;
   CUDA_TRY(cudaSetDevice(c->device));

@@ -545,3 +545,14 @@ def test_refusals(ctx):
             ctx.op_decode_attention_q8(**{**good, **b})
         assert e.value.status == aiq.ERR_UNSUPPORTED, b
     ctx.op_decode_attention_q8(**{**good, "R": 0})
+
+
+def test_more_heads_than_a_row_can_count_are_refused(ctx):
+    p = torch.zeros(1 << 12, dtype=torch.uint8, device="cuda").data_ptr()
+    heads = (1 << 20) + 1
+    for call in (lambda: ctx.op_kv_quantize(p, 2 * 32 * heads, 4, p, 1, heads, 32, p, p),
+                 lambda: ctx.op_kv_dequantize(p, p, 4, p, 1, heads, 32, p, 2 * 32 * heads),
+                 lambda: ctx.op_decode_attention_q8(p, 1, heads, heads, 32, p, p, 4, p, 0, 0, p, 1, 0, p)):
+        with pytest.raises(aiq.AiqError) as e:
+            call()
+        assert e.value.status == aiq.ERR_UNSUPPORTED
