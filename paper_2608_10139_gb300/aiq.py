@@ -424,6 +424,8 @@ class Context:
         g = _Generate(max_new, eos, pad,
                       buf.ctypes.data_as(C.POINTER(C.c_int32)) if like is not None else None,
                       len(pat), GEN_MATCH_TOKENS if match_tokens else 0)
+        if sampling is None and uniforms is not None:
+            raise ValueError("uniforms need sampling")
         if sampling is not None:
             sp = _sampling(**sampling)
             u = np.ascontiguousarray(uniforms, dtype=np.float32)

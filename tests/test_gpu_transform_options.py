@@ -200,6 +200,13 @@ def test_refusals(ctx):
     assert e.value.status == aiq.ERR_UNSUPPORTED
 
 
+def test_uniforms_alone_are_refused(ctx):
+    shape, W, _ = _zero_model()
+    table, prefix = _inputs(shape, 3, 12)
+    with pytest.raises(ValueError):
+        _run(ctx, shape, W, table, prefix, [], 3, uniforms=np.zeros((3, 3), np.float32))
+
+
 def test_the_flag_needs_its_arguments(ctx):
     shape, W, _ = _zero_model()
     table, prefix = _inputs(shape, 3, 12)
