@@ -83,7 +83,7 @@ struct Attn8 {
   float m[2], l[2];
 
   // k-step k takes elements 64 c + 16 t + 4 kk .. + 3 (HD 32: 8 t + 4 k .. + 3) of every lane's key
-  __device__ __forceinline__ void begin(const __half* qrow, int G) {
+  __device__ __forceinline__ void load(const __half* qrow, int G) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -93,6 +93,8 @@ struct Attn8 {
       q[k][0] = v.x;
       q[k][1] = v.y;
     }
+  }
+  __device__ __forceinline__ void begin() {
 #pragma unroll
     for (int c = 0; c < C32; ++c)
 #pragma unroll
@@ -120,14 +122,14 @@ struct Attn8 {
     float mb[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
-#pragma unroll
-    for (int d = 4; d < 32; d <<= 1) {
-      mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
-      mb[1] = fmaxf(mb[1], __shfl_xor_sync(0xffffffffu, mb[1], d));
-    }
-    mb[0] *= scale;  // finite: a block has a key, and products of finite numbers do not overflow
+    mb[0] *= scale;
     mb[1] *= scale;
     if (__any_sync(0xffffffffu, mb[0] > m[0] + 8.f || mb[1] > m[1] + 8.f)) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {  // to finite maxima: a block has a key
+        mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
+        mb[1] = fmaxf(mb[1], __shfl_xor_sync(0xffffffffu, mb[1], d));
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float mn = fmaxf(m[e], mb[e]), f = exp2_approx(m[e] - mn);
@@ -540,9 +542,10 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
   for (int i = 0; i < C::STAGES; ++i) produce();
 
   Attn8<HD> at;
+  Task8 w = task_of(a, first, n_tasks);
+  at.load(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
   for (int64_t i = first; i < n_tasks; i += step) {
-    const Task8 w = task_of(a, i, n_tasks);
-    at.begin(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
+    at.begin();
     for (int e = 0; e < w.tiles; ++e) {
       if (!ring.wait()) return;
       const float2 s = make_float2(__shfl_sync(0xffffffffu, ring.scale.x, ring.get),
@@ -553,12 +556,15 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
       __syncwarp();  // every lane is done with the slot before it is refilled
       produce();
     }
+    const Task8 next = task_of(a, i + step, n_tasks);
     ring.wait_rows();
     const __half* sk = reinterpret_cast<const __half*>(ring.slot());
     ring.used();
     const __half* sv = reinterpret_cast<const __half*>(ring.slot());
     ring.used();
     open_block<HD>(a, w, at, sk, sv);
+    // the next task's queries are on their way while this one's output is written
+    at.load(a.qkv + next.r * a.ldq + next.h * a.G * HD, a.G);
     __syncwarp();
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) produce();
@@ -574,6 +580,7 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
       if (head < a.G) fine = store_eight(orow + 32 * c, v, inv) && fine;
     }
     if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+    w = next;
   }
 }
 
@@ -686,7 +693,8 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
 #pragma unroll 1
   for (int k = 0; k < C::STAGES; ++k) produce();
   Attn8<HD> at;
-  at.begin(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
+  at.load(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
+  at.begin();
   bool ok = true;
   for (; e < e1 && ok; e += C::NW) {
     ok = ring.wait();
