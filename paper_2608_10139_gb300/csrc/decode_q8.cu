@@ -60,6 +60,14 @@ __device__ __forceinline__ void cp_async16(uint32_t saddr, const void* gmem) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(saddr), "l"(gmem) : "memory");
 }
 
+__device__ __forceinline__ void cp_async8(uint32_t saddr, const void* gmem) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(saddr), "l"(gmem) : "memory");
+}
+// The thread's copies so far arrive at the barrier (as one arrival) when they are complete.
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 // 2^x to 2^-22 of it; 0 for -infinity.
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -337,10 +345,15 @@ __device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int64_t i, int64_t 
   return t;
 }
 
-// A warp's ring of tile-sized slots in shared memory, filled by bulk copies an
-// entry each: a tile, the open block's keys or its values (32 fp16 rows are as
-// many bytes as a tile).  Lane s keeps slot s's scales and number of keys, so that
-// they are on their way as early as the tile.
+// A warp's ring of tile-sized slots in shared memory, filled by asynchronous copies
+// an entry each: a tile, the open block's keys or its values (32 fp16 rows are as
+// many bytes as a tile).  A tile's scales come along as a copy of eight bytes, which
+// arrives at the same barrier (in a register, any entry's would be waited for where
+// one is read).
+struct __align__(16) Head8 {
+  float2 scale;
+  int keys;
+};
 __device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t phase, volatile int* abort_flag, int* err) {
   return mbar_wait_bounded(bar, phase, abort_flag, err);
 }
@@ -348,21 +361,19 @@ template <int HD, int STAGES>
 struct Ring8 {
   static constexpr int TB = tile8_bytes(HD);
   uint8_t* slots;
+  Head8* heads;
   uint64_t* full;
   volatile int* abort_flag;
   int* err;
   int put, get;            // slots
   uint32_t phases;         // bit s: the phase of slot s's barrier that is waited for next
   uint32_t busy;           // bit s: a tile is on its way to slot s or there
-  float2 scale;            // lane s: slot s's
-  int keys;
 
-  __device__ __forceinline__ void begin(uint8_t* slots_, uint64_t* full_, volatile int* abort_, int* err_) {
-    slots = slots_, full = full_, abort_flag = abort_, err = err_;
-    put = get = keys = 0;
+  __device__ __forceinline__ void begin(uint8_t* slots_, Head8* heads_, uint64_t* full_, volatile int* abort_, int* err_) {
+    slots = slots_, heads = heads_, full = full_, abort_flag = abort_, err = err_;
+    put = get = 0;
     busy = 0;
     phases = 0;
-    scale = make_float2(0.f, 0.f);
   }
   // All lanes call; the slot must have been used up by every lane before.
   __device__ __forceinline__ void issue_tile(const uint8_t* at, const float2* s, int n) {
@@ -371,6 +382,9 @@ struct Ring8 {
       // a block's first keys are a prefix of both halves (8 or 16 keys at a time)
       constexpr int KSTEP = HD == 32 ? 16 : 8;
       uint8_t* dst = slots + put * TB;
+      heads[put].keys = n;
+      cp_async8(smem_u32(&heads[put].scale), s);
+      cp_async_arrive(&full[put]);
       if (n == kTileKeys) {
         mbar_arrive_expect_tx(&full[put], TB);
         bulk_copy_g2s(dst, at, TB, &full[put]);
@@ -380,10 +394,6 @@ struct Ring8 {
         bulk_copy_g2s(dst, at, kb, &full[put]);
         bulk_copy_g2s(dst + kTileKeys * HD, at + kTileKeys * HD, vb, &full[put]);
       }
-    }
-    if (lane == put) {
-      scale = *s;
-      keys = n;
     }
     busy |= 1u << put;
     issued();
@@ -403,6 +413,8 @@ struct Ring8 {
   __device__ __forceinline__ void issued() {
     put = put + 1 == STAGES ? 0 : put + 1;
   }
+  // After each entry, and instead of one: wait_rows counts them.
+  __device__ __forceinline__ void entry_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
   // The next entry, a tile, has arrived.  False: a wait ran out somewhere; the
   // warp's copies are then awaited.
   __device__ __forceinline__ bool wait() {
@@ -413,14 +425,19 @@ struct Ring8 {
       phases ^= 1u << get;
       return true;
     }
-    wait_rows();
+    wait_rows<0>();
     volatile int never = 0;
     for (int i = 0; i < STAGES; ++i)  // a barrier without copies in flight stands at the phase before
       if (busy >> i & 1) mbar_wait_bounded(&full[i], phases >> i & 1, &never, nullptr, 200000000ull);
     return false;
   }
+  // The rows of all entries but the last LATER have arrived.
+  template <int LATER>
   __device__ __forceinline__ void wait_rows() {
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    if constexpr (LATER == 0)
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    else
+      asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory");
     __syncwarp();
   }
   __device__ __forceinline__ void used() {
@@ -428,6 +445,7 @@ struct Ring8 {
     get = get + 1 == STAGES ? 0 : get + 1;
   }
   __device__ __forceinline__ const uint8_t* slot() const { return slots + get * TB; }
+  __device__ __forceinline__ const Head8& head() const { return heads[get]; }
 };
 
 // The open block's products, this step's key and value into it, and, where that
@@ -474,7 +492,7 @@ struct Stream8 {
   static constexpr int STAGES = HD == 128 ? 2 : 3;
   static constexpr int CTAS = HD == 128 ? 3 : 4;   // per SM
   static constexpr int RING = NW * STAGES * tile8_bytes(HD);
-  static constexpr int SMEM = RING + NW * STAGES * 8;
+  static constexpr int SMEM = RING + NW * STAGES * (16 + 8);
   static_assert(CTAS * (SMEM + 1024 + 64) <= 233472, "shared memory per SM");
 };
 
@@ -495,9 +513,10 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING) + warp * C::STAGES;
+  Head8* heads = reinterpret_cast<Head8*>(smem + C::RING) + warp * C::STAGES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::NW * C::STAGES * sizeof(Head8)) + warp * C::STAGES;
   if (lane == 0)
-    for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 1);
+    for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 2);  // the tile, its scales
   if (threadIdx.x == 0) abort_word = 0;
   fence_mbar_init();
   __syncthreads();
@@ -505,7 +524,7 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
   grid_wait();
 
   Ring8<HD, C::STAGES> ring;
-  ring.begin(smem + warp * C::STAGES * TB, bars, &abort_word, a.err);
+  ring.begin(smem + warp * C::STAGES * TB, heads, bars, &abort_word, a.err);
   const int kd = a.Hkv * HD, open = a.slot % kTileKeys;
   const int64_t stride = static_cast<int64_t>(a.Hkv) * TB;
   const int64_t step = static_cast<int64_t>(gridDim.x) * C::NW;
@@ -532,7 +551,7 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
     else
       run_of(a.gc, a.gs, pt.r * a.gen_blocks, a.slot - open);
   };
-  const auto produce = [&] {
+  const auto next_entry = [&] {
     if (pi >= n_tasks) return;
     if (pe < pt.tiles) {
       if (left <= 0) next_run();
@@ -553,6 +572,10 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
       pe = left = 0;
     }
   };
+  const auto produce = [&] {
+    next_entry();
+    ring.entry_done();
+  };
 #pragma unroll 1
   for (int i = 0; i < C::STAGES; ++i) produce();
 
@@ -563,16 +586,13 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
     at.begin();
     for (int e = 0; e < w.tiles; ++e) {
       if (!ring.wait()) return;
-      const float2 s = make_float2(__shfl_sync(0xffffffffu, ring.scale.x, ring.get),
-                                   __shfl_sync(0xffffffffu, ring.scale.y, ring.get));
-      const int n = __shfl_sync(0xffffffffu, ring.keys, ring.get);
-      at.tile(ring.slot(), s, n, a.scale_log2);
+      at.tile(ring.slot(), ring.head().scale, ring.head().keys, a.scale_log2);
       ring.used();
       __syncwarp();  // every lane is done with the slot before it is refilled
       produce();
     }
     const Task8 next = task_of(a, i + step, n_tasks);
-    ring.wait_rows();
+    ring.template wait_rows<C::STAGES - 2>();
     const __half* sk = reinterpret_cast<const __half*>(ring.slot());
     ring.used();
     const __half* sv = reinterpret_cast<const __half*>(ring.slot());
@@ -616,7 +636,7 @@ struct Split8 {
   static constexpr int STAGES = Stream8<HD>::STAGES;
   static constexpr int CTAS = Stream8<HD>::CTAS;
   static constexpr int RING = NW * STAGES * tile8_bytes(HD);
-  static constexpr int SMEM = RING + NW * STAGES * 8;
+  static constexpr int SMEM = RING + NW * STAGES * (16 + 8);
   static_assert(NW * 8 * (HD + 2) * 4 <= RING, "the merge reuses the ring");
   static_assert(NW * kMaxRanges * 4 <= RING, "and so do the ranges' weights");
 };
@@ -656,9 +676,10 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int abort_word, last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING) + warp * C::STAGES;
+  Head8* heads = reinterpret_cast<Head8*>(smem + C::RING) + warp * C::STAGES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::NW * C::STAGES * sizeof(Head8)) + warp * C::STAGES;
   if (lane == 0)
-    for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 1);
+    for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 2);  // the tile, its scales
   if (threadIdx.x == 0) abort_word = 0;
   fence_mbar_init();
   __syncthreads();
@@ -666,7 +687,7 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
   grid_wait();
 
   Ring8<HD, C::STAGES> ring;
-  ring.begin(smem + warp * C::STAGES * TB, bars, &abort_word, a.err);
+  ring.begin(smem + warp * C::STAGES * TB, heads, bars, &abort_word, a.err);
   const int h = blockIdx.x % a.Hkv, unit = blockIdx.x / a.Hkv;
   int64_t row = unit, first = unit;
   int ranges = 1;
@@ -714,10 +735,7 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
   for (; e < e1 && ok; e += C::NW) {
     ok = ring.wait();
     if (!ok) break;
-    const float2 s = make_float2(__shfl_sync(0xffffffffu, ring.scale.x, ring.get),
-                                 __shfl_sync(0xffffffffu, ring.scale.y, ring.get));
-    const int n = __shfl_sync(0xffffffffu, ring.keys, ring.get);
-    at.tile(ring.slot(), s, n, a.scale_log2);
+    at.tile(ring.slot(), ring.head().scale, ring.head().keys, a.scale_log2);
     ring.used();
     __syncwarp();
     produce();
@@ -731,7 +749,7 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
     for (int v = 0; v < 2; ++v)
       ring.issue_rows(a.tail + static_cast<int64_t>(w.r) * kTileKeys * 2 * kd + w.h * HD + v * kd,
                       2 * static_cast<int64_t>(kd), a.qkv + w.r * a.ldq + (a.Hq + w.h) * HD + v * kd, open + 1);
-    ring.wait_rows();
+    ring.template wait_rows<0>();
     open_block<HD, PAIRS>(a, w, at, sk, sv);
   }
   at.sum_keys();
