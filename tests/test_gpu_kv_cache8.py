@@ -473,6 +473,36 @@ def test_two_contexts_at_once():
     assert len(outs) == 2
 
 
+@pytest.mark.parametrize("rows,heads", [(700, (8, 8, 32)), (5200, (4, 1, 64)), (700, (8, 8, 128))], ids=str)
+def test_many_rows_of_very_different_lengths(ctx, rows, heads):
+    """The longest rows are taken first; the output is that of the rows as they came."""
+    rng = np.random.default_rng(rows)
+    lens = np.where(rng.random(rows) < 0.3, 0, rng.integers(1, 70, rows))
+    lens[rows // 2], lens[rows - 1], lens[3] = 33_100, 1_500, 700
+    s = Step(rows, *heads, [int(n) for n in lens], 5, 32)
+    s.fill_generated(2)
+    qkv = s.qkv()
+    out = s.call(ctx, qkv, 2)
+    s.append(qkv)
+    s.check(out, qkv)
+
+
+def test_many_rows_with_one_outside_the_tokens(ctx):
+    rows = 700
+    s = Step(1, 8, 8, 32, [20] * rows, 0, 32)
+    qkv = s.qkv()
+    first = s.call(ctx, qkv, 0)
+    good = s.d[4]
+    starts = kv8.starts(s.lens)
+    starts[300] += 30  # behind the next one
+    s.d[4] = _d(starts)
+    with pytest.raises(aiq.AiqError) as e:
+        s.call(ctx, qkv, 0)
+    assert e.value.status == aiq.ERR_DEVICE_CHECK
+    s.d[4] = good
+    assert np.array_equal(s.call(ctx, qkv, 0), first)
+
+
 def test_a_call_after_a_reported_one_is_right(ctx):
     """Starts that do not ascend, in a call whose rows share CTAs, leave nothing behind."""
     s = Step(50, 4, 1, 64, [4000, 3000], 0, 32)
