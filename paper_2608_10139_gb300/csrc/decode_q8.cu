@@ -328,13 +328,9 @@ struct Task8 {
   int tiles;
 };
 __device__ __forceinline__ int tiles_of(int keys) { return keys / kTileKeys + (keys % kTileKeys != 0); }
-__device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int64_t i, int64_t n_tasks) {
-  Task8 t{0, 0, 0, 0, 0};
-  if (i >= n_tasks) return t;
-  t.r = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(a.Hkv));
-  t.h = static_cast<int>(i) - t.r * a.Hkv;
-  t.st = a.seq_start[t.r];
-  const int64_t end = a.seq_start[t.r + 1];
+__device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int r, int h) {
+  Task8 t{r, h, a.seq_start[r], 0, 0};
+  const int64_t end = a.seq_start[r + 1];
   if (t.st < 0 || end < t.st || end > a.T) {
     set_dev_error(a.err, DEVERR_BOUNDS);
     t.st = 0;
@@ -527,12 +523,13 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
   ring.begin(smem + warp * C::STAGES * TB, heads, bars, &abort_word, a.err);
   const int kd = a.Hkv * HD, open = a.slot % kTileKeys;
   const int64_t stride = static_cast<int64_t>(a.Hkv) * TB;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * C::NW;
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * C::NW + warp;
+  const int step = gridDim.x * C::NW, first = blockIdx.x * C::NW + warp;
+  const int rows_on = step / a.Hkv, heads_on = step % a.Hkv;  // from a warp's task to its next
 
   // the copies run ahead of the products by the ring's length, over the tasks' borders
   int64_t pi = first;
-  Task8 pt = task_of(a, pi, n_tasks);
+  Task8 pt{0, 0, 0, 0, 0};
+  if (pi < n_tasks) pt = task_of(a, first / a.Hkv, first % a.Hkv);
   const uint8_t* tile = nullptr;
   const float2* scale = nullptr;
   int pe = 0, left = 0;  // the task's next entry; keys left in the run of tiles that `tile` is in
@@ -568,7 +565,10 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
     ++pe;
     if (v) {
       pi += step;
-      pt = task_of(a, pi, n_tasks);
+      if (pi < n_tasks) {
+        const bool carry = pt.h + heads_on >= a.Hkv;
+        pt = task_of(a, pt.r + rows_on + carry, pt.h + heads_on - (carry ? a.Hkv : 0));
+      }
       pe = left = 0;
     }
   };
@@ -576,11 +576,11 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
     next_entry();
     ring.entry_done();
   };
+  Task8 w = pt;
 #pragma unroll 1
   for (int i = 0; i < C::STAGES; ++i) produce();
 
   Attn8<HD, PAIRS> at;
-  Task8 w = task_of(a, first, n_tasks);
   at.load(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
   for (int64_t i = first; i < n_tasks; i += step) {
     at.begin();
@@ -591,7 +591,9 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
       __syncwarp();  // every lane is done with the slot before it is refilled
       produce();
     }
-    const Task8 next = task_of(a, i + step, n_tasks);
+    // the producer's: it is past this task's entries, and not past two of the next one's
+    static_assert(C::STAGES <= 3);
+    const Task8 next = pt;
     ring.template wait_rows<C::STAGES - 2>();
     const __half* sk = reinterpret_cast<const __half*>(ring.slot());
     ring.used();
@@ -713,7 +715,7 @@ __global__ void __launch_bounds__(Split8<HD>::NW * 32, Split8<HD>::CTAS)
   }
   const int range = static_cast<int>(min(max(unit - first, int64_t(0)), static_cast<int64_t>(ranges - 1)));
   const int64_t i = row * a.Hkv + h;
-  const Task8 w = task_of(a, i, static_cast<int64_t>(R) * a.Hkv);
+  const Task8 w = task_of(a, static_cast<int>(row), h);
   const int e0 = static_cast<int>(static_cast<int64_t>(w.tiles) * range / ranges);
   const int e1 = static_cast<int>(static_cast<int64_t>(w.tiles) * (range + 1) / ranges);
   int e = e0 + warp, pe = e;
