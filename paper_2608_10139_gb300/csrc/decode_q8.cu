@@ -852,11 +852,14 @@ template <int HD>
 int units_of(int64_t R, int64_t Hkv, double tiles, int num_sms) {
   using C = Stream8<HD>;
   const int64_t ctas = static_cast<int64_t>(num_sms) * C::CTAS, tasks = R * Hkv;
-  // A warp per task once every warp has two (a CTA per task against that, 32/8 heads,
-  // the call with 43 us around it: head_dim 64, 500 rows of about 200 keys 102 and 101 us,
-  // 1,000 rows 145 and 131; head_dim 128, 500 rows 134 and 125, but 178 and 206 where
-  // they have about 500 keys).
-  if (tasks >= 2 * ctas * C::NW) return 0;
+  // A CTA per task costs its start and its merge, a warp per task the time of the longest
+  // ones' tiles: the warp where a task has fewer tiles than 2.25 times the CTAs' rounds
+  // (tasks per CTA that the GPU holds).  Calls, CTA and warp, 8 KV heads, prefix of 64,
+  // texts of about so many keys; head_dim 64: 130 rows of 60 56 and 53 us, of 200 60 and
+  // 63; 260 rows of 200 72 and 68, of 350 78 and 83; 500 rows of 200 99 and 83, of 500 122
+  // and 124; 1,500 rows of 200 183 and 141.  head_dim 128: 200 rows of 200 85 and 77, of 350
+  // 93 and 105; 450 rows of 200 122 and 99, of 500 159 and 182; 3,000 rows of 120 467 and 245.
+  if ((tiles + 0.5 * R) * ctas <= 2.25 * R * tasks) return 0;
   if (tasks > kSplitTasksMax) return static_cast<int>(R);
   // four tiles a warp: shorter ranges cost more in the merge than they save (24 rows of
   // about 200 keys, 32/8 heads, head_dim 64: 8.5 us with a CTA a task, 11.3 with 1.8)

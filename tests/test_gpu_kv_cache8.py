@@ -473,6 +473,19 @@ def test_two_contexts_at_once():
     assert len(outs) == 2
 
 
+@pytest.mark.parametrize("rows,heads", [(140, (8, 8, 64)), (1100, (4, 1, 32)), (150, (56, 8, 128)), (40, (16, 8, 64)),
+                                        (3, (4, 2, 32))], ids=str)
+@pytest.mark.parametrize("length", [10, 150, 700])
+def test_tasks_and_tiles(ctx, rows, heads, length):
+    """Few and many tasks of few and many tiles: a warp, a CTA and several CTAs for one."""
+    s = Step(rows, *heads, [length - i % 9 for i in range(rows)], 20, 64)
+    s.fill_generated(33)
+    qkv = s.qkv()
+    out = s.call(ctx, qkv, 33)
+    s.append(qkv)
+    s.check(out, qkv)
+
+
 @pytest.mark.parametrize("rows,heads", [(700, (8, 8, 32)), (5200, (4, 1, 64)), (700, (8, 8, 128))], ids=str)
 def test_many_rows_of_very_different_lengths(ctx, rows, heads):
     """The longest rows are taken first; the output is that of the rows as they came."""
