@@ -205,6 +205,62 @@ __device__ __forceinline__ Key cut(Shared& s, int& round, int k, int most) {
   return mid;
 }
 
+// As cut, by the whole block and in one pass: the entries are counted in bins of equal
+// width, and kept are the first bins that have k of them.  Where those have more than
+// `most` (values that are alike), nothing is done.
+__device__ __forceinline__ void cut_by_bins(Shared& s, int k, int most) {
+  constexpr int NT = kMergeThreads;
+  __shared__ int bins[NT], sums[NT / 32], last;
+  __syncthreads();
+  const int n = s.n, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (n <= most) return;
+  bins[tid] = 0;
+  if (tid == 0) s.highest = 0, s.lowest = ~0u, last = NT;
+  __syncthreads();
+  uint32_t high = 0, low = ~0u;
+  for (int i = tid; i < n; i += NT) {
+    const uint32_t x = static_cast<uint32_t>(s.list()[i] >> 32);
+    high = max(high, x);
+    low = min(low, x);
+  }
+  high = __reduce_max_sync(0xffffffffu, high);
+  low = __reduce_min_sync(0xffffffffu, low);
+  if (lane == 0) {
+    atomicMax(&s.highest, high);
+    atomicMin(&s.lowest, low);
+  }
+  __syncthreads();
+  const float top = order_value(s.highest), scale = NT / (top - order_value(s.lowest));
+  // never larger for a larger value (NaN, of an infinite difference or of no width, counts as 0)
+  const auto bin_of = [&](Key x) {
+    return min(NT - 1, static_cast<int>((top - order_value(static_cast<uint32_t>(x >> 32))) * scale));
+  };
+  for (int i = tid; i < n; i += NT) atomicAdd(&bins[bin_of(s.list()[i])], 1);
+  __syncthreads();
+  const int mine = bins[tid];
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 31) sums[warp] = upto;
+  __syncthreads();
+  upto += __reduce_add_sync(0xffffffffu, lane < warp ? sums[lane] : 0);
+  if (upto >= k && upto - mine < k && upto <= most) last = tid;
+  __syncthreads();
+  const int end = last;
+  if (end == NT) return;
+  // a piece at a time: what is kept lands no further than where it came from
+  if (tid == 0) s.n = 0;
+  for (int base = 0; base < n; base += NT) {
+    const Key x = base + tid < n ? s.list()[base + tid] : 0;
+    __syncthreads();
+    push(s, base + tid < n && bin_of(x) <= end, [&] { return x; });
+    __syncthreads();
+  }
+}
+
 // 2^(j / 64).
 __device__ const double kExp2[64] = {
     0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
@@ -242,9 +298,10 @@ __device__ __forceinline__ double exp_neg(double x) {
   return __hiloint2double(__double2hiint(y) + (n >> 6) * (1 << 20), __double2loint(y));
 }
 
-// The draw from a complete list.
+// The first step of the draw from a complete list: its largest entries, k at least, in
+// descending order.  False: the row has no token.
 template <int NT, bool FEW>
-__device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round, int64_t r, bool bad) {
+__device__ __forceinline__ bool sort_list(const SampleArgs& a, Shared& s, int& round, int64_t r, bool bad) {
   // what is sorted: a power of two, and NT entries (one a thread) as they are
   int size = NT;
   if constexpr (!FEW)
@@ -259,7 +316,7 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       a.tokens[r] = 0;
       if (a.probs) a.probs[r] = 0.f;
     }
-    return;
+    return false;
   }
   // descending, bitonic
   Key* sorted = s.list();
@@ -303,6 +360,15 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
           __syncwarp();
       }
   }
+  return true;
+}
+
+// The token of a sorted list.
+template <int NT, bool FEW>
+__device__ __forceinline__ void pick(const SampleArgs& a, Shared& s, int& round, int64_t r) {
+  const int n_all = s.n, tid = threadIdx.x;
+  const float u = a.u[r];
+  const Key* sorted = s.list();
   const int k = n_all < a.k ? n_all : a.k;
   // A thread's run of consecutive places; warps without any stay out of the 64-bit arithmetic.
   constexpr int MOST = FEW ? 1 : (kSampleKeepMax + NT - 1) / NT;
@@ -310,7 +376,8 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
   const bool busy = warp * 32 * per < k;
   double e[MOST], c[MOST];
   if (busy) {
-    const double z0 = order_value(static_cast<uint32_t>(sorted[0] >> 32));
+    const float z0f = order_value(static_cast<uint32_t>(sorted[0] >> 32));
+    const double z0 = z0f;
     double sum = 0;
 #pragma unroll
     for (int j = 0; j < MOST; ++j) {
@@ -318,8 +385,8 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       const int i = tid * per + j;
       e[j] = 0;
       if (i < k) {
-        const double z = order_value(static_cast<uint32_t>(sorted[i] >> 32));
-        e[j] = z == z0 ? 1.0 : exp_neg((z - z0) * a.inv_temperature);  // 1 / T may be infinite
+        const float zf = order_value(static_cast<uint32_t>(sorted[i] >> 32));
+        e[j] = zf == z0f ? 1.0 : exp_neg((zf - z0) * a.inv_temperature);  // 1 / T may be infinite
       }
       sum += e[j];
       c[j] = sum;
@@ -374,6 +441,8 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
     sync<NT>();
     return s.total;
   };
+  // (numbers that are not negative, and -0, are in the order of their bits, which takes no 64-bit arithmetic)
+  const auto bits = [](double x) { return __double_as_longlong(x); };
   // Two counts of places in one round.
   const auto places_where = [&](int end, auto f, auto g) {
     int in = 0;
@@ -389,11 +458,12 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
   int n = k;
   if (a.top_p < 1.0 || a.min_p > 0) {
     const double enough = a.top_p < 1.0 ? a.top_p * sum_to(k - 1) : INFINITY;
-    const int both = places_where(k, [&](int j) { return e[j] >= a.min_p; }, [&](int j) { return c[j] < enough; });
+    const int both = places_where(k, [&](int j) { return bits(e[j]) >= bits(a.min_p); },
+                                  [&](int j) { return bits(c[j]) < bits(enough); });
     n = a.top_p < 1.0 ? min(both & 0xffff, 1 + (both >> 16)) : both & 0xffff;
   }
   const double kept = sum_to(n - 1), target = static_cast<double>(u) * kept;
-  const int at = min(n - 1, places_where(n, [&](int j) { return c[j] <= target; }, [](int) { return false; }));
+  const int at = min(n - 1, places_where(n, [&](int j) { return bits(c[j]) <= bits(target); }, [](int) { return false; }));
   if (busy) {
 #pragma unroll
     for (int j = 0; j < MOST; ++j) {
@@ -404,6 +474,11 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
       }
     }
   }
+}
+
+template <int NT, bool FEW>
+__device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round, int64_t r, bool bad) {
+  if (sort_list<NT, FEW>(a, s, round, r, bad)) pick<NT, FEW>(a, s, round, r);
 }
 
 __device__ __forceinline__ void begin(Shared& s, int list) {
@@ -613,10 +688,14 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
     const int end = min(a.slices, first + batch);
     for (int i = first + (threadIdx.x >> 5); i < end; i += NT / 32) {
       const int64_t at = r * a.slices + i;
-      const int n = a.counts[at];
-      for (int j = threadIdx.x & 31; j - static_cast<int>(threadIdx.x & 31) < n; j += 32) {
-        const Key x = j < n ? a.keys[at * most + j] : 0;
-        push(s, x >= from && x, [&] { return x; });
+      const int n = a.counts[at], lane = threadIdx.x & 31;
+      for (int base = 0; base < most; base += 4 * 32) {
+        Key x[4];  // on their way before their number is known
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = base + 32 * j + lane < most ? a.keys[at * most + base + 32 * j + lane] : 0;
+        if (base >= n) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) push(s, base + 32 * j + lane < n && x[j] >= from, [&] { return x[j]; });
       }
     }
     __syncthreads();
@@ -640,7 +719,8 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
     sync<NT>();
     if (threadIdx.x < kDrawThreads) draw<kDrawThreads, true>(a, s, round, r, bad);
   } else {
-    draw<NT, false>(a, s, round, r, bad);
+    cut_by_bins(s, a.k, kSampleKeepMax);
+    if (sort_list<NT, false>(a, s, round, r, bad) && threadIdx.x < kDrawThreads) pick<kDrawThreads, false>(a, s, round, r);
   }
 }
 static_assert(kMergeList >= list_size(kSampleKeepMax, kMergeThreads), "a row's list fits too");

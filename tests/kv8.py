@@ -125,7 +125,8 @@ def sample(z, u, temperature, top_k, top_p, min_p):
     """(token, probability) of one row of logits (exact in 32 bits) for the uniform u."""
     z = z.astype(np.float64)
     order = np.argsort(-z, kind="stable")[:top_k]
-    e = np.exp((z[order] - z[order[0]]) / temperature)
+    with np.errstate(over="ignore"):  # a difference divided by next to nothing
+        e = np.exp((z[order] - z[order[0]]) / temperature)
     c = np.cumsum(e)
     n = int((e >= min_p).sum())
     if top_p < 1:

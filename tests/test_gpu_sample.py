@@ -121,6 +121,24 @@ def test_ascending_descending_and_peaked_rows(ctx):
         _check(held, u, t, p, top_k=k)
 
 
+@pytest.mark.parametrize("k", [300, 1000, 1024])
+def test_long_rows_of_uneven_values(ctx, k):
+    """The slices' lists in one: values far apart, the whole range of the type, most of them alike."""
+    rng = np.random.default_rng(k)
+    z = rng.standard_normal((6, 90000)).astype(np.float32)
+    z[0, ::7] = 1e30
+    z[1] = np.where(rng.random(90000) < 0.5, 3.4e38, -3.4e38)
+    z[2, rng.integers(0, 90000, 900)] = 5.0
+    z[2, 4567] = 3.3e38
+    z[3] = np.where(rng.random(90000) < 0.02, z[3], -np.inf)
+    z[4] = np.float32(1) + z[4] * 2.0 ** -22
+    z[5, 100:] *= 1e-40
+    u = np.array([0.4, 0.1, 0.999, 0.6, 0.8, 0.3], np.float32)
+    for top_p in (1.0, 0.7):
+        held, t, p = _run(ctx, z, u, top_k=k, top_p=top_p)
+        _check(held, u, t, p, top_k=k, top_p=top_p)
+
+
 def test_greedy_is_top_k_1(ctx):
     rng = np.random.default_rng(9)
     z = rng.standard_normal((50, 5000)).astype(np.float32)
