@@ -805,6 +805,7 @@ struct DecodeBufs {
   bool bits8;
   Kv8 prefix8, own8, gen8;
   __half* tail;
+  const int4* order;  // of the chunk's rows, for the attention; may be null
 };
 
 // Sampled tokens for R rows of normalised hidden states in b.xn: their logits, as
@@ -907,7 +908,7 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
         const DecodeQ8 q{b.qkv, nqkv, R, Hq, Hkv, hd, P ? d.prefix8.tiles(l, g) : nullptr,
                          P ? d.prefix8.pairs(l, g) : nullptr, P, d.own8.tiles(l, g), d.own8.pairs(l, g), Tc, b.seq_start,
                          d.gen8.tiles(l, g), d.gen8.pairs(l, g), d.gcap,
-                         d.tail + static_cast<int64_t>(l) * R * AIQ_KV_BLOCK * ldkv, slot, b.att};
+                         d.tail + static_cast<int64_t>(l) * R * AIQ_KV_BLOCK * ldkv, slot, b.att, d.order};
         float* partial = nullptr;
         if (const size_t floats = decode_q8_floats(q, c->num_sms)) AIQ_TRY(ws(c, "op.q8_partial", floats, &partial));
         e = launch_decode_attention_q8(q, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
@@ -952,11 +953,31 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
   return AIQ_OK;
 }
 
+// The order of a batch's rows for the attention over an 8-bit cache, or null.
+aiq_status q8_order(aiq_ctx* c, const DecodeQ8& d, bool once, const int4** order) {
+  *order = nullptr;
+  const int rows = decode_q8_order_rows(d, once, c->num_sms);
+  if (!rows) return AIQ_OK;
+  int4* o;
+  AIQ_TRY(ws(c, "op.q8_order", rows, &o));
+  const int e = launch_decode_q8_order(d.seq_start, rows, d.T, o, c->d_err, c->stream);
+  counted(c, 1);
+  if (e != 0)
+    return fail(AIQ_ERR_CUDA, std::string("row order launch: ") + cudaGetErrorString(static_cast<cudaError_t>(e)));
+  *order = o;
+  return AIQ_OK;
+}
+
 // max_new greedy steps for the R rows of one chunk whose prefill just ran
 // (final hidden state of each row's last prompt token in b.resid_last).
-aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const DecodeBufs& d, int R, int64_t Tc,
+aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, DecodeBufs d, int R, int64_t Tc,
                         const __half* pkv, int P, const float* prefix_last, int64_t r0, GenPlan* gp) {
   const aiq_model_config& g = m.cfg;
+  if (d.bits8 && gp->max_new > 1) {
+    DecodeQ8 q{};
+    q.R = R, q.Hq = g.n_heads, q.Hkv = g.n_kv_heads, q.hd = g.head_dim, q.P = P, q.T = Tc, q.seq_start = b.seq_start;
+    AIQ_TRY(q8_order(c, q, false, &d.order));
+  }
   launch_patch_empty_rows(b.resid_last, b.last_compact, prefix_last, R, g.d_model, c->stream);
   {
     ProfScope p(c, "rmsnorm", 0, 6.0 * double(R) * g.d_model);
@@ -2347,10 +2368,11 @@ aiq_status aiq_op_decode_attention_q8(aiq_ctx* c, const void* qkv, int32_t R, in
   if (int64_t(R) * Hkv > INT32_MAX) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^31 - 1 (row, KV head) pairs");
   if (R == 0) return AIQ_OK;
   CUDA_TRY(cudaSetDevice(c->device));
-  const DecodeQ8 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, Hq, Hkv, hd,
+  DecodeQ8 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, Hq, Hkv, hd,
                    static_cast<const uint8_t*>(prefix_cache), prefix_scales, P, static_cast<const uint8_t*>(own_cache),
                    own_scales, T, seq_start, static_cast<uint8_t*>(gen_cache), gen_scales, gen_cap,
-                   static_cast<__half*>(gen_tail), slot, static_cast<__half*>(out)};
+                   static_cast<__half*>(gen_tail), slot, static_cast<__half*>(out), nullptr};
+  AIQ_TRY(with_room(c, [&] { return q8_order(c, d, true, &d.order); }));
   float* partial = nullptr;
   if (const size_t floats = decode_q8_floats(d, c->num_sms))
     AIQ_TRY(with_room(c, [&] { return ws(c, "op.q8_partial", floats, &partial); }));

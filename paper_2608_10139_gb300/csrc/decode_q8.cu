@@ -36,6 +36,7 @@ struct DecQ8Args {
   float scale_log2;   // log2(e) / sqrt(HD)
   __half* out;        // [R][Hq HD]
   int* err;
+  const int4* order;  // rows, first tokens and lengths, long ones first; null: as they come
 };
 
 // d (+)= A B.
@@ -322,20 +323,32 @@ struct Attn8 {
 // A (row, KV head): its prompt's place and its number of tiles (prefix, own
 // prompt, generated).  The open block's keys and its values come after them.
 struct Task8 {
+  int at;  // the row's place
   int r, h;
   int64_t st;  // first prompt token
   int len;
   int tiles;
 };
 __device__ __forceinline__ int tiles_of(int keys) { return keys / kTileKeys + (keys % kTileKeys != 0); }
-__device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int r, int h) {
-  Task8 t{r, h, a.seq_start[r], 0, 0};
-  const int64_t end = a.seq_start[r + 1];
-  if (t.st < 0 || end < t.st || end > a.T) {
+// False, and no tokens: the row's prompt is not within the T tokens.
+__device__ __forceinline__ bool prompt_of(const int32_t* seq_start, int r, int64_t T, int64_t& st, int& len) {
+  st = seq_start[r], len = 0;
+  const int64_t end = seq_start[r + 1];
+  if (st < 0 || end < st || end > T) {
+    st = 0;
+    return false;
+  }
+  len = static_cast<int>(end - st);
+  return true;
+}
+// KV head h of the row at place `at`.
+__device__ __forceinline__ Task8 task_of(const DecQ8Args& a, int at, int h) {
+  Task8 t{at, at, h, 0, 0, 0};
+  if (a.order) {
+    const int4 x = a.order[at];
+    t.r = x.x, t.st = x.y, t.len = x.z;
+  } else if (!prompt_of(a.seq_start, at, a.T, t.st, t.len)) {
     set_dev_error(a.err, DEVERR_BOUNDS);
-    t.st = 0;
-  } else {
-    t.len = static_cast<int>(end - t.st);
   }
   t.tiles = tiles_of(a.P) + tiles_of(t.len) + a.slot / kTileKeys;
   return t;
@@ -492,6 +505,56 @@ struct Stream8 {
   static_assert(CTAS * (SMEM + 1024 + 64) <= 233472, "shared memory per SM");
 };
 
+// The rows by the tiles of their prompts, the longest first: a counting sort by one CTA.
+// (Rows of equally many tiles come in any order, on which no result depends: a task's
+// numbers are the same whichever warp has it.)  With it the warps of k_decode_q8_stream
+// have about equally much to do: 3,263 rows of about 217 keys 122 us after 129.
+constexpr int kOrderThreads = 1024;
+constexpr int kOrderBins = 1024;
+__global__ void __launch_bounds__(kOrderThreads) k_decode_q8_order(const int32_t* seq_start, int R, int64_t T, int4* order,
+                                                                   int* err) {
+  __shared__ int at[kOrderBins], sums[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  at[tid] = 0;
+  grid_launch_next();
+  grid_wait();
+  __syncthreads();
+  // f(row, first token, length, how many rows of its bin were counted before), for all rows
+  const auto count = [&](auto f) {
+    for (int base = 0; base < R; base += kOrderThreads) {
+      const int r = base + tid;
+      int64_t st = 0;
+      int len = 0, bin = -1, before = 0;
+      if (r < R) {
+        if (!prompt_of(seq_start, r, T, st, len)) set_dev_error(err, DEVERR_BOUNDS);
+        bin = kOrderBins - 1 - min(tiles_of(len), kOrderBins - 1);
+      }
+      // a warp's rows of one bin at once: most rows fall into a few bins
+      const uint32_t same = __match_any_sync(0xffffffffu, bin);
+      const int leader = __ffs(same) - 1;
+      if (lane == leader && bin >= 0) before = atomicAdd(&at[bin], __popc(same));
+      before = __shfl_sync(0xffffffffu, before, leader) + __popc(same & ((1u << lane) - 1));
+      if (r < R) f(r, st, len, before);
+    }
+  };
+  count([](int, int64_t, int, int) {});
+  __syncthreads();
+  const int mine = at[tid];
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 31) sums[warp] = upto;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) upto += sums[w];
+  at[tid] = upto - mine;
+  __syncthreads();
+  count([&](int r, int64_t st, int len, int place) { order[place] = make_int4(r, static_cast<int>(st), len, 0); });
+}
+static_assert(kOrderBins == kOrderThreads, "a thread per bin");
+
 // Many rows: a persistent warp per (row, KV head) task, the entries of all its
 // tasks as one stream through its ring.  Long rows run at the memory's rate (2,432
 // rows of about 720 keys, 32/8 heads, head_dim 64, 1.53 GB: 245 us, 0.92 of the
@@ -523,12 +586,16 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
   ring.begin(smem + warp * C::STAGES * TB, heads, bars, &abort_word, a.err);
   const int kd = a.Hkv * HD, open = a.slot % kTileKeys;
   const int64_t stride = static_cast<int64_t>(a.Hkv) * TB;
-  const int step = gridDim.x * C::NW, first = blockIdx.x * C::NW + warp;
-  const int rows_on = step / a.Hkv, heads_on = step % a.Hkv;  // from a warp's task to its next
+  const int first = blockIdx.x * C::NW + warp;
+  // from a warp's task to its next: every other round of tasks is dealt out backwards, so that
+  // whoever had the longest gets the shortest
+  const int up = 2 * (static_cast<int>(gridDim.x) * C::NW - first) - 1, down = 2 * first + 1;
+  const int up_rows = up / a.Hkv, up_heads = up % a.Hkv, down_rows = down / a.Hkv, down_heads = down % a.Hkv;
+  bool p_odd = false, odd = false;
 
   // the copies run ahead of the products by the ring's length, over the tasks' borders
   int64_t pi = first;
-  Task8 pt{0, 0, 0, 0, 0};
+  Task8 pt{0, 0, 0, 0, 0, 0};
   if (pi < n_tasks) pt = task_of(a, first / a.Hkv, first % a.Hkv);
   const uint8_t* tile = nullptr;
   const float2* scale = nullptr;
@@ -564,11 +631,11 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
                     2 * static_cast<int64_t>(kd), a.qkv + pt.r * a.ldq + (a.Hq + pt.h) * HD + v * kd, open + 1);
     ++pe;
     if (v) {
-      pi += step;
-      if (pi < n_tasks) {
-        const bool carry = pt.h + heads_on >= a.Hkv;
-        pt = task_of(a, pt.r + rows_on + carry, pt.h + heads_on - (carry ? a.Hkv : 0));
-      }
+      pi += p_odd ? down : up;
+      const int h = pt.h + (p_odd ? down_heads : up_heads);
+      const bool carry = h >= a.Hkv;
+      if (pi < n_tasks) pt = task_of(a, pt.at + (p_odd ? down_rows : up_rows) + carry, h - (carry ? a.Hkv : 0));
+      p_odd = !p_odd;
       pe = left = 0;
     }
   };
@@ -582,7 +649,7 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
 
   Attn8<HD, PAIRS> at;
   at.load(a.qkv + w.r * a.ldq + w.h * a.G * HD, a.G);
-  for (int64_t i = first; i < n_tasks; i += step) {
+  for (int64_t i = first; i < n_tasks; i += odd ? down : up, odd = !odd) {
     at.begin();
     for (int e = 0; e < w.tiles; ++e) {
       if (!ring.wait()) return;
@@ -866,8 +933,9 @@ int units_of(int64_t R, int64_t Hkv, double tiles, int num_sms) {
   const int64_t most = static_cast<int64_t>(tiles / (4 * Split8<HD>::NW));
   return static_cast<int>(std::max<int64_t>(R, std::min<int64_t>({ctas / Hkv, most, R + kMaxRanges - 1})));
 }
+double tiles_of_head(const DecodeQ8& d) { return d.T / 32.0 + static_cast<double>(d.R) * (d.P / 32 + d.slot / 32); }
 int units_of(const DecodeQ8& d, int num_sms) {
-  const double tiles = d.T / 32.0 + static_cast<double>(d.R) * (d.P / 32 + d.slot / 32);  // of a KV head
+  const double tiles = tiles_of_head(d);
   switch (d.hd) {
     case 32: return units_of<32>(d.R, d.Hkv, tiles, num_sms);
     case 64: return units_of<64>(d.R, d.Hkv, tiles, num_sms);
@@ -897,6 +965,28 @@ int launch_q8(const DecQ8Args& a, int R, int units, float* partial, unsigned int
 
 }  // namespace
 
+int decode_q8_order_rows(const DecodeQ8& d, bool once, int num_sms) {
+  if (d.R <= 0 || units_of(d, num_sms) != 0) return 0;
+  const double warps = static_cast<double>(num_sms) * (d.hd == 128 ? Stream8<128>::CTAS * Stream8<128>::NW
+                                                                    : Stream8<64>::CTAS * Stream8<64>::NW);
+  const double per_warp = d.R * static_cast<double>(d.Hkv) / warps;
+  const double own = d.T / 32.0 / d.R;
+  // The fewer tasks a warp has the more uneven they are.  The sort takes 4 to 10 us: it
+  // pays for one call where a text has 1.2 times as many tiles as a warp has tasks (calls,
+  // ordered and as they come, 8 KV heads; head_dim 64: 2,432 rows of about 200 keys 182 and
+  // 181 us, of 570 364 and 390, 6,000 rows of 120 276 and 266; 128: 700 rows of 200 132 and
+  // 145, 4,000 rows of 200 426 and 421, of 600 980 and 1,057; 32: 3,000 rows of 400 214 and
+  // 249) and the texts, in which alone the rows differ, are most of the keys (of 12 tiles 7,
+  // the call with the cache's read-back 227 and 224); for many calls over the same rows up
+  // to some 24 tasks.
+  return per_warp > 1 && (once ? own >= 1.2 * per_warp && own >= tiles_of_head(d) / d.R * 2 / 3 : per_warp <= 24) ? d.R : 0;
+}
+
+int launch_decode_q8_order(const int32_t* seq_start, int R, int64_t T, int4* order, int* err, cudaStream_t s) {
+  if (R <= 0) return 0;
+  return launch_chained(k_decode_q8_order, dim3(1), kOrderThreads, 0, s, 1, seq_start, R, T, order, err);
+}
+
 size_t decode_q8_floats(const DecodeQ8& d, int num_sms) {
   if (d.R <= 0) return 0;
   const int units = units_of(d, num_sms);
@@ -910,7 +1000,8 @@ int launch_decode_attention_q8(const DecodeQ8& d, float* partial, unsigned int* 
   DecQ8Args a{d.qkv, d.ldq, d.Hq, d.Hkv, d.Hq / d.Hkv, d.prefix, reinterpret_cast<const float2*>(d.prefix_scales), d.P,
               d.own, reinterpret_cast<const float2*>(d.own_scales), d.T, d.seq_start, d.gen,
               reinterpret_cast<float2*>(d.gen_scales), d.gen_cap / kTileKeys, d.tail, d.slot,
-              1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, err};
+              1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, err,
+              units ? nullptr : d.order};
   switch (d.hd) {
     case 32: return launch_q8<32>(a, d.R, units, partial, arrived, num_sms, s);
     case 64: return launch_q8<64>(a, d.R, units, partial, arrived, num_sms, s);

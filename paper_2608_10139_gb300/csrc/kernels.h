@@ -304,10 +304,16 @@ struct DecodeQ8 {
   __half* tail;
   int slot;
   __half* out;
+  const int4* order;  // as launch_decode_q8_order writes it, or null
 };
 // Workspace that the call takes, in floats (few rows: partial states of ranges of keys).
 size_t decode_q8_floats(const DecodeQ8& d, int num_sms);
 constexpr int kSplitTasksMax = 1024;
+// The order in which many rows of different lengths keep the GPU evenly busy: an int4
+// per row, as many as decode_q8_order_rows says (0: the call does without).  once: it is
+// made for one call, not for all layers and steps of a batch.
+int decode_q8_order_rows(const DecodeQ8& d, bool once, int num_sms);
+int launch_decode_q8_order(const int32_t* seq_start, int R, int64_t T, int4* order, int* err, cudaStream_t s);
 // arrived: kSplitTasksMax counters, zero between launches.
 int launch_decode_attention_q8(const DecodeQ8& d, float* partial, unsigned int* arrived, int* err, int num_sms,
                                cudaStream_t s);

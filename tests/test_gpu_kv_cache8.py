@@ -487,10 +487,11 @@ def test_tasks_and_tiles(ctx, rows, heads, length):
 
 
 @pytest.mark.parametrize("rows,heads", [(700, (8, 8, 32)), (5200, (4, 1, 64)), (700, (8, 8, 128))], ids=str)
-def test_many_rows_of_very_different_lengths(ctx, rows, heads):
-    """The longest rows are taken first; the output is that of the rows as they came."""
+@pytest.mark.parametrize("longest", [70, 300])
+def test_many_rows_of_very_different_lengths(ctx, rows, heads, longest):
+    """The longest rows may be taken first; the output is that of the rows as they came."""
     rng = np.random.default_rng(rows)
-    lens = np.where(rng.random(rows) < 0.3, 0, rng.integers(1, 70, rows))
+    lens = np.where(rng.random(rows) < 0.3, 0, rng.integers(1, longest, rows))
     lens[rows // 2], lens[rows - 1], lens[3] = 33_100, 1_500, 700
     s = Step(rows, *heads, [int(n) for n in lens], 5, 32)
     s.fill_generated(2)
@@ -500,14 +501,15 @@ def test_many_rows_of_very_different_lengths(ctx, rows, heads):
     s.check(out, qkv)
 
 
-def test_many_rows_with_one_outside_the_tokens(ctx):
+@pytest.mark.parametrize("length", [20, 200])
+def test_many_rows_with_one_outside_the_tokens(ctx, length):
     rows = 700
-    s = Step(1, 8, 8, 32, [20] * rows, 0, 32)
+    s = Step(1, 8, 8, 32, [length] * rows, 0, 32)
     qkv = s.qkv()
     first = s.call(ctx, qkv, 0)
     good = s.d[4]
     starts = kv8.starts(s.lens)
-    starts[300] += 30  # behind the next one
+    starts[300] += length + 10  # behind the next one
     s.d[4] = _d(starts)
     with pytest.raises(aiq.AiqError) as e:
         s.call(ctx, qkv, 0)
