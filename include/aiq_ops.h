@@ -107,7 +107,7 @@ enum { AIQ_KV_BLOCK = 32 };
  * rows of kv that no sequence holds are not read, and blocks of the cache that no
  * token falls into are left as they were.  A NaN or an infinity gives
  * AIQ_ERR_DEVICE_CHECK, and so does a sequence outside the T rows.  hd in
- * {32, 64, 128}.  The call synchronises its stream. */
+ * {32, 64, 128}, at most 2^20 KV heads.  The call synchronises its stream. */
 aiq_status aiq_op_kv_quantize(aiq_ctx* ctx, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
                               int32_t n_seqs, int32_t Hkv, int32_t hd, void* cache, float* scales);
 
@@ -131,7 +131,7 @@ aiq_status aiq_op_kv_dequantize(aiq_ctx* ctx, const void* cache, const float* sc
  * where that is the last place the block's tiles and scales to gen_cache and
  * gen_scales: steps 0, 1, 2, ... build the cache, and a block is quantised once,
  * from what the tail holds.  out fp16 [R, Hq * hd].  hd in {32, 64, 128},
- * Hq / Hkv <= 8.  qkv, caches, gen_tail and out 16-byte aligned, scales 8-byte.
+ * Hq / Hkv <= 8, at most 2^20 heads.  qkv, caches, gen_tail and out 16-byte aligned, scales 8-byte.
  * A sequence outside the T tokens, or an output that is not finite in fp16,
  * gives AIQ_ERR_DEVICE_CHECK.  The call synchronises its stream. */
 aiq_status aiq_op_decode_attention_q8(aiq_ctx* ctx, const void* qkv, int32_t R, int32_t Hq, int32_t Hkv, int32_t hd,

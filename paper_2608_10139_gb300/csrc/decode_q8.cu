@@ -557,14 +557,14 @@ static_assert(kOrderBins == kOrderThreads, "a thread per bin");
 
 // Many rows: a persistent warp per (row, KV head) task, the entries of all its
 // tasks as one stream through its ring.  Long rows run at the memory's rate (2,432
-// rows of about 720 keys, 32/8 heads, head_dim 64, 1.53 GB: 245 us, 0.92 of the
-// copy); short ones at the issue slots' (some 360 instructions a tile, 128 of them
-// bytes to fp16, and 1,000 a task): 3,263 rows of about 217 keys, 592 MB, take 139 us,
-// 0.63 of the copy.  The fp16 cache's kernel takes 225 us for the same rows.  Not
-// kept: two tiles at a time with one softmax (177 us: short rows have few pairs),
-// tasks drawn from a counter (139), heads as the rows of the A tile, half of it
-// padding (154); 20 or 24 warps an SM with two slots each (the call 156 and 164 us
-// against 155).
+// rows of about 725 keys, 32/8 heads, head_dim 64, 1.72 GB: 267 us, 0.95 of the
+// copy; 299 in the order in which they come); short ones at the issue slots' and their latency (some 350 instructions a
+// tile, 128 of them bytes to fp16, and 1,000 a task): 3,263 rows of about 217 keys, 592
+// MB, take 123 us, 0.71 of the copy.  The fp16 cache's kernel takes 225 us for the same
+// rows.  Not kept, when it took 139: two tiles at a time with one softmax (177 us: short
+// rows have few pairs), tasks drawn from a counter (139), heads as the rows of the A
+// tile, half of it padding (154); 20 or 24 warps an SM with two slots each (the call
+// 156 and 164 us against 155).
 template <int HD, bool PAIRS>
 __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_decode_q8_stream(DecQ8Args a, int64_t n_tasks) {
   using C = Stream8<HD>;
@@ -694,7 +694,7 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
 // The ranges' are merged, in their order, by the task's CTA that comes last: a
 // kernel for it took ten microseconds of the four documents' 81.  Those (24,439,
 // 33,879, 18,661 and 65,536 tokens, 32/8 heads, head_dim 128, 292 MB) take 53 us, 0.81 of
-// the copy; 24 rows of about 200 keys, head_dim 64, 8.5 us.
+// the copy; 24 rows of about 200 keys, head_dim 64, 8 us.
 //
 // A KV head has `units` CTAs, at least one a row, the others shared out by the
 // rows' lengths, which only the device knows: row r's are share(r) .. share(r + 1) - 1.

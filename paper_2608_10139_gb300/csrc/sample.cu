@@ -723,6 +723,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
     if (sort_list<NT, false>(a, s, round, r, bad) && threadIdx.x < kDrawThreads) pick<kDrawThreads, false>(a, s, round, r);
   }
 }
+static_assert(kMergeThreads >= kSampleKeepMax, "the candidates are sorted one a thread");
 static_assert(kMergeList >= list_size(kSampleKeepMax, kMergeThreads), "a row's list fits too");
 
 struct Plan {
