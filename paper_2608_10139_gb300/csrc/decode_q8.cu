@@ -453,6 +453,13 @@ struct Ring8 {
     busy &= ~(1u << get);
     get = get + 1 == STAGES ? 0 : get + 1;
   }
+  // Every lane is done with the rows' slots before a bulk copy refills them: the rows came
+  // by cp.async, which writes shared memory as ordinary stores do, and a bulk copy's writes
+  // are ordered behind those by a proxy fence only.
+  __device__ __forceinline__ void rows_used() {
+    fence_proxy_async_smem();
+    __syncwarp();
+  }
   __device__ __forceinline__ const uint8_t* slot() const { return slots + get * TB; }
   __device__ __forceinline__ const Head8& head() const { return heads[get]; }
 };
@@ -669,7 +676,7 @@ __global__ void __launch_bounds__(Stream8<HD>::NW * 32, Stream8<HD>::CTAS) k_dec
     open_block<HD, PAIRS>(a, w, at, sk, sv);
     // the next task's queries are on their way while this one's output is written
     at.load(a.qkv + next.r * a.ldq + next.h * a.G * HD, a.G);
-    __syncwarp();
+    ring.rows_used();
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) produce();
     at.sum_keys();
