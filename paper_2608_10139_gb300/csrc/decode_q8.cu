@@ -90,6 +90,7 @@ struct Attn8 {
   static constexpr int C32 = HD / 32;
   static constexpr int C64 = HD == 32 ? 1 : HD / 64;
   static constexpr int PER = HD == 32 ? 8 : 16;  // a lane's consecutive elements of a key
+  static constexpr float kAbove = 11.f, kLag = 4.f;
   uint32_t q[KS][2];
   // [c][i / 2][2 (i % 2) + head]: element 32 c + 8 (g / 2) + 2 i + g % 2 of heads 2 t, 2 t + 1
   float o[C32][2][4];
@@ -117,12 +118,15 @@ struct Attn8 {
     l[0] = l[1] = 0.f;
   }
 
-  // Scores of keys 16 k + 8 h + g ([k][2 h + head], keys >= n masked) times scale,
-  // in log2 units, to probabilities relative to m, the largest score so far.  m
-  // follows only when it is left behind by more than 8, and then the output is
-  // scaled down: a probability is at most 256, and the running output need not be
-  // touched for most tiles.  hi is a probability rounded to fp16, lo what the
-  // rounding left: the two keep the output's error at that of its own rounding.
+  // Scores of keys 16 k + 8 h + g ([k][2 h + head], keys >= n masked) times scale, in
+  // log2 units, to probabilities relative to m, which lies kAbove to kAbove + kLag below
+  // the largest score so far: it follows, and the output is scaled down, only where that
+  // would come to lie higher, so that the running output need not be touched for most
+  // tiles and a probability is at most 2^15, within fp16.  hi is a probability rounded to
+  // fp16, lo what the rounding left: the two are off by 2^-22 of it, or by half of fp16's
+  // last place, 2^-25, where that is more, which is 2^-36 of the largest.  That is what
+  // kAbove is for: relative to the largest score itself, keys that one outweighs by 2^25
+  // would be lost, however many they are.
   __device__ __forceinline__ void softmax(float (&sc)[2][4], float scale, int n, uint32_t (&hi)[2][2],
                                           uint32_t (&lo)[2][2]) {
     const int g = (threadIdx.x & 31) >> 2;
@@ -139,7 +143,7 @@ struct Attn8 {
     for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
     mb[0] *= scale;
     mb[1] *= scale;
-    if (__any_sync(0xffffffffu, mb[0] > m[0] + 8.f || mb[1] > m[1] + 8.f)) {
+    if (__any_sync(0xffffffffu, mb[0] > m[0] + (kAbove + kLag) || mb[1] > m[1] + (kAbove + kLag))) {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) {  // to finite maxima: a block has a key
         mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
@@ -147,7 +151,7 @@ struct Attn8 {
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float mn = fmaxf(m[e], mb[e]), f = exp2_approx(m[e] - mn);
+        const float mn = fmaxf(m[e], mb[e] - kAbove), f = exp2_approx(m[e] - mn);
         m[e] = mn;
         l[e] *= f;
 #pragma unroll
