@@ -809,12 +809,12 @@ struct DecodeBufs {
 };
 
 // Sampled tokens for R rows of normalised hidden states in b.xn: their logits, as
-// many rows at a time as 1 GB holds, then the draw.
+// many rows at a time as 1 GB holds (32 MB where memory is short), then the draw.
 aiq_status lm_sample(aiq_ctx* c, ModelD& m, const PrefillBufs& b, int R, int t, const GenPlan* gp, int64_t r0,
                      int32_t** tokens) {
   const int dm = m.cfg.d_model, V = m.cfg.vocab;
   const aiq_sampling& sp = *gp->sampling;
-  const int rows = std::max(1, std::min<int>(R, (1 << 28) / m.vpad));
+  const int rows = std::max(1, std::min<int>(R, (c->tight ? 1 << 23 : 1 << 28) / m.vpad));
   float *logits, *u;
   uint8_t* scratch = nullptr;
   AIQ_TRY(ws(c, "g.logits", static_cast<int64_t>(rows) * m.vpad, &logits));

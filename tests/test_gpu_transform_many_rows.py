@@ -8,7 +8,8 @@ import kv8
 import synth
 from helpers import MARGIN_RTOL, gpu_ctx, weights_list
 from oracle import transformer as tf
-from test_gpu_transform_options import SHAPES, _inputs, _run
+from paper_2608_10139_gb300 import aiq
+from test_gpu_transform_options import SHAPES, _inputs, _run, _zero_model
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,31 @@ def test_many_rows_on_the_8_bit_cache(ctx, name, rows, new):
         for t in range(new):
             gap = z[t].max() - z[t][r.gen_tokens[row, t]]
             assert gap <= MARGIN_RTOL * max(1.0, abs(z[t].max())), f"row {row} step {t}: {gap:.4g} below the largest"
+
+
+def test_draws_in_little_memory():
+    """115 MB of logits a step under a cap that leaves 40 MB beside the greedy query's least."""
+    shape, W, bias = _zero_model(vocab=32000)
+    rows = 900
+    table, prefix = _inputs(shape, rows, 14, lens=np.full(rows, 3))
+    u = np.random.default_rng(3).random((rows, 2)).astype(np.float32) * np.float32(0.999)
+    c = gpu_ctx()
+    try:
+        m = c.load_model(shape, weights_list(shape, W))
+        t = c.load_table(table.cols, (table.offsets, table.tokens))
+        loaded = sum(v.nbytes for v in weights_list(shape, W))
+        for cap in range(loaded, loaded + (1 << 29), 4 << 20):
+            c.set_option("device_bytes_max", cap)
+            try:
+                c.run_transform(t, m, [], prefix, 2)
+                break
+            except aiq.AiqError as e:
+                assert e.status == aiq.ERR_OOM
+        assert cap < loaded + (1 << 28)
+        sampling = dict(temperature=0.9, top_k=40, top_p=0.9)
+        c.set_option("device_bytes_max", cap + (40 << 20))
+        r = c.run_transform(t, m, [], prefix, 2, sampling=sampling, uniforms=u)
+        want = [[kv8.sample(bias, u[i, s], 0.9, 40, 0.9, 0.0)[0] for s in range(2)] for i in range(rows)]
+        assert np.array_equal(r.gen_tokens, want)
+    finally:
+        c.close()
