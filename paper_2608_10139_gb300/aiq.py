@@ -182,6 +182,14 @@ def _sampling(temperature: float = 1.0, top_k: int = 50, top_p: float = 1.0, min
     return _Sampling(temperature, top_p, min_p, top_k)
 
 
+def _uniforms(u) -> np.ndarray:
+    """Numbers in [0, 1) as fp32: those below 1 whose nearest fp32 number is 1 become the largest below it."""
+    u = np.asarray(u)
+    f = np.ascontiguousarray(u, dtype=np.float32)
+    up = (f == 1) & (u < 1)
+    return np.where(up, np.float32(1 - 2.0 ** -24), f) if up.any() else f
+
+
 def kv_cache_blocks(T: int, n_seqs: int) -> int:
     """Blocks of an 8-bit cache for T tokens in n_seqs sequences: it holds
     blocks * Hkv * 64 * hd bytes, and 2 fp32 scales per block and KV head."""
@@ -417,18 +425,19 @@ class Context:
         """AI_TRANSFORM of every candidate row; with ``like`` (a token sequence)
         only the COUNT / ids of the rows whose output contains it.  Greedy, or, with
         ``sampling`` (temperature, top_k, top_p, min_p as in op_sample), drawn by
-        ``uniforms`` [table rows, max_new], numbers in [0, 1)."""
+        ``uniforms`` [table rows, max_new], numbers in [0, 1) (64-bit ones are rounded
+        to fp32, never to 1)."""
         sel, keep = self._select(table, preds, prefix, [], AGG_COUNT, 0, text_name)
         pat = _i32(like if like is not None else [])
         buf = pat if pat.size else np.zeros(1, np.int32)   # a non-NULL pointer for the empty pattern
         g = _Generate(max_new, eos, pad,
                       buf.ctypes.data_as(C.POINTER(C.c_int32)) if like is not None else None,
                       len(pat), GEN_MATCH_TOKENS if match_tokens else 0)
-        if sampling is None and uniforms is not None:
-            raise ValueError("uniforms need sampling")
+        if (sampling is None) != (uniforms is None):
+            raise ValueError("sampling and uniforms need each other")
         if sampling is not None:
             sp = _sampling(**sampling)
-            u = np.ascontiguousarray(uniforms, dtype=np.float32)
+            u = _uniforms(uniforms)
             if u.shape != (table.n_rows, max_new):
                 raise ValueError(f"uniforms must be [{table.n_rows}, {max_new}], not {list(u.shape)}")
             g.flags |= GEN_SAMPLE

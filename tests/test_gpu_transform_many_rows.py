@@ -64,3 +64,26 @@ def test_draws_in_little_memory():
         assert np.array_equal(r.gen_tokens, want)
     finally:
         c.close()
+
+
+def test_numbers_of_64_bits_below_1_stay_below_1(ctx):
+    """The largest 64-bit numbers below 1 are in [0, 1), though their nearest 32-bit number is 1."""
+    shape, W, bias = _zero_model()
+    table, prefix = _inputs(shape, 5, 15)
+    u = np.full((5, 3), 1 - 2.0 ** -53)
+    u[1] = 1 - 2.0 ** -25
+    r = _run(ctx, shape, W, table, prefix, [], 3, sampling=dict(temperature=1.3, top_k=400), uniforms=u)
+    want = kv8.sample(bias, np.float32(1 - 2.0 ** -24), 1.3, 400, 1.0, 0.0)[0]
+    assert (r.gen_tokens == want).all()
+    for bad in (1.0, -1e-9, float("nan")):  # these are not
+        u[2, 1] = bad
+        with pytest.raises(aiq.AiqError) as e:
+            _run(ctx, shape, W, table, prefix, [], 3, sampling=dict(top_k=5), uniforms=u)
+        assert e.value.status == aiq.ERR_DEVICE_CHECK
+
+
+def test_sampling_without_numbers_is_refused(ctx):
+    shape, W, _ = _zero_model()
+    table, prefix = _inputs(shape, 5, 15)
+    with pytest.raises(ValueError):
+        _run(ctx, shape, W, table, prefix, [], 3, sampling=dict(top_k=5))
