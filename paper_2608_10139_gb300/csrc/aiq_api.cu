@@ -315,6 +315,9 @@ aiq_status sync_and_check(aiq_ctx* c) {
     if (err & DEVERR_FP16_RANGE) return fail(AIQ_ERR_DEVICE_CHECK, "an activation left the fp16 range (or was NaN)");
     if (err & DEVERR_BOUNDS)
       return fail(AIQ_ERR_DEVICE_CHECK, "an index failed its bounds check (e.g. no finite logit for a greedy step)");
+    if (err & DEVERR_LOGIT)
+      return fail(AIQ_ERR_DEVICE_CHECK, "a row of logits holds a NaN or +infinity, or nothing finite to draw from");
+    if (err & DEVERR_UNIFORM) return fail(AIQ_ERR_DEVICE_CHECK, "a uniform number is outside [0, 1)");
     return fail(AIQ_ERR_DEVICE_CHECK, "device check failed (code " + std::to_string(err) + ")");
   }
   return AIQ_OK;

@@ -19,6 +19,8 @@ enum : int {
   DEVERR_DUP_BUILD_KEY = 1 << 3, // join build key not unique
   DEVERR_SENTINEL_KEY = 1 << 4,  // build key equals the empty-slot sentinel
   DEVERR_BOUNDS = 1 << 5,        // an index failed its bounds check
+  DEVERR_LOGIT = 1 << 6,         // a row of logits to draw from holds a NaN or +inf, or nothing finite
+  DEVERR_UNIFORM = 1 << 7,       // a uniform number outside [0, 1)
 };
 
 // The word is host memory that the device maps (read by the host once the

@@ -312,7 +312,7 @@ __device__ __forceinline__ bool sort_list(const SampleArgs& a, Shared& s, int& r
   const float u = a.u[r];
   if (bad || n_all == 0 || !(u >= 0.f && u < 1.f)) {
     if (tid == 0) {
-      set_dev_error(a.err, bad ? DEVERR_FP16_RANGE : DEVERR_BOUNDS);
+      set_dev_error(a.err, bad || n_all == 0 ? DEVERR_LOGIT : DEVERR_UNIFORM);
       a.tokens[r] = 0;
       if (a.probs) a.probs[r] = 0.f;
     }
