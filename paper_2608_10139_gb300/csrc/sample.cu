@@ -45,7 +45,8 @@ __host__ __device__ constexpr int few(int threads) { return threads * 3 / 4; }
 __host__ __device__ constexpr int list_most(int k) { return k + (k / 4 > 8 ? k / 4 : 8); }
 __host__ __device__ constexpr int list_hold(int k, int threads) { return list_most(k) > 2 * threads ? list_most(k) : 2 * threads; }
 __host__ __device__ constexpr int list_size(int k, int threads) { return list_hold(k, threads) + threads * kPerThread + 32; }
-// The merge of slices lists that many before it cuts them back.
+// The merge lists all of its slices' entries at once: the more slices, the more they are,
+// 1,216 slices (eight a row of each of 152 SMs) of 17 at most, 20,672.
 constexpr int kMergeList = 22 * 1024;
 
 struct SampleArgs {
@@ -96,7 +97,7 @@ struct Shared {
   int n;         // entries of the list
   int part[2][32];  // of the rounds of block_count: the warps' sums
   unsigned int highest, lowest;
-  int size;      // of the list, which lies behind this
+  // (the list lies behind this)
   __device__ __forceinline__ Key* list() { return reinterpret_cast<Key*>(this + 1); }
 };
 static_assert(sizeof(Shared) % sizeof(Key) == 0, "the list is aligned");
@@ -122,7 +123,8 @@ __device__ __forceinline__ int block_count(Shared& s, int& round, int v) {
 
 // The next bound to count at between lo, which more reach than wanted, and hi,
 // which fewer do (by two at least): where `want` would lie on the line between
-// their counts, and halfway in every other round, so that 64 rounds always do.
+// their counts, and halfway in every other round, so that twice U's bits of rounds
+// always do.
 template <typename U>
 __device__ __forceinline__ U between(U lo, U hi, int count_lo, int count_hi, int want, int i) {
   const U width = hi - lo;
@@ -481,10 +483,9 @@ __device__ __forceinline__ void draw(const SampleArgs& a, Shared& s, int& round,
   if (sort_list<NT, FEW>(a, s, round, r, bad)) pick<NT, FEW>(a, s, round, r);
 }
 
-__device__ __forceinline__ void begin(Shared& s, int list) {
+__device__ __forceinline__ void begin(Shared& s) {
   if (threadIdx.x == 0) {
     s.n = 0;
-    s.size = list;
     s.top = 0;
     s.highest = 0, s.lowest = ~0u;
   }
@@ -637,7 +638,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_sample_rows(SampleArg
   constexpr int NT = kRowThreads;
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& s = *reinterpret_cast<Shared*>(smem);
-  begin(s, list_size(a.slice_k, NT));
+  begin(s);
   const int64_t r = blockIdx.x / a.slices;
   const int s0 = static_cast<int>(blockIdx.x % a.slices) * a.slice_len;
   int round = 0;
@@ -669,12 +670,12 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
   constexpr int NT = kMergeThreads;
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& s = *reinterpret_cast<Shared*>(smem);
-  begin(s, kMergeList);
+  begin(s);
   const int64_t r = blockIdx.x;
   const int most = list_most(a.slice_k);
   int round = 0;
   bool bad = false;
-  Key from = 0, all = 0;  // what is listed; from where on nothing is missing
+  Key all = 0;  // from where on nothing is missing
   for (int i = threadIdx.x; i < a.slices; i += NT) {
     bad = bad || a.counts[r * a.slices + i] < 0;
     all = max(all, a.froms[r * a.slices + i]);
@@ -682,26 +683,17 @@ __global__ void __launch_bounds__(kMergeThreads) k_sample_merge(SampleArgs a) {
   if (all) atomicMax(&s.top, all);
   bad = __syncthreads_or(bad);
   all = s.top;
-  // a warp per slice, as many slices at a time as the list has room for
-  const int batch = (kMergeList - list_most(a.k)) / most;
-  for (int first = 0; first < a.slices; first += batch) {
-    const int end = min(a.slices, first + batch);
-    for (int i = first + (threadIdx.x >> 5); i < end; i += NT / 32) {
-      const int64_t at = r * a.slices + i;
-      const int n = a.counts[at], lane = threadIdx.x & 31;
-      for (int base = 0; base < most; base += 4 * 32) {
-        Key x[4];  // on their way before their number is known
+  // a warp per slice
+  for (int i = threadIdx.x >> 5; i < a.slices; i += NT / 32) {
+    const int64_t at = r * a.slices + i;
+    const int n = a.counts[at], lane = threadIdx.x & 31;
+    for (int base = 0; base < most; base += 4 * 32) {
+      Key x[4];  // on their way before their number is known
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = base + 32 * j + lane < most ? a.keys[at * most + base + 32 * j + lane] : 0;
-        if (base >= n) break;
+      for (int j = 0; j < 4; ++j) x[j] = base + 32 * j + lane < most ? a.keys[at * most + base + 32 * j + lane] : 0;
+      if (base >= n) break;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) push(s, base + 32 * j + lane < n && x[j] >= from, [&] { return x[j]; });
-      }
-    }
-    __syncthreads();
-    if (end < a.slices) {
-      from = max(from, cut<NT>(s, round, a.k, list_most(a.k)));
-      __syncthreads();
+      for (int j = 0; j < 4; ++j) push(s, base + 32 * j + lane < n, [&] { return x[j]; });
     }
   }
   __syncthreads();
@@ -768,6 +760,7 @@ int launch_sample(const void* logits, int type, int64_t ld, int R, int V, const 
   if (R <= 0) return 0;
   if (V < 1 || top_k < 1 || top_k > V || top_k > kSampleKeepMax) return cudaErrorInvalidValue;
   const Plan p = plan_of(R, V, top_k, num_sms);
+  if (p.slices > 1 && p.slices * list_most(p.slice_k) > kMergeList) return cudaErrorInvalidValue;  // a GPU of more SMs
   const size_t lists = static_cast<size_t>(R) * p.slices;
   Key* keys = static_cast<Key*>(scratch);
   Key* froms = keys + lists * list_most(p.slice_k);
