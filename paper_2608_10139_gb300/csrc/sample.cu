@@ -282,10 +282,13 @@ __device__ const double kExp2[64] = {
     0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
     0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0,
 };
-// e^x for x <= 0, to about a unit in the last of 64 bits; 0 below -700.  x = (64 e +
-// j) ln 2 / 64 + r, |r| <= ln 2 / 128, and the Taylor series of e^r to r^5 (the next
-// term is below 2^-54).  Eleven 64-bit instructions, of which an SM issues one a
-// warp every 16 clocks: they, not the reads, bound rows of many candidates.
+// e^x for x <= 0, to 2.4 * 2^-53 of it; 0 below -700.  Tang's table-driven method (ACM
+// TOMS 15, 1989): x = (64 e + j) ln 2 / 64 + r, |r| <= ln 2 / 128, with ln 2 / 64 in two
+// parts, the first of 33 bits, whose product with 64 e + j is exact (Cody and Waite);
+// 2^(j / 64) from the table and the Taylor series of e^r to r^5.  Errors: the table's
+// rounding and the last fma's, 2^-53 each, the series' next term, 2^-54.6, and 2^-7 of a
+// rounding or two in r and the series.  Eleven 64-bit instructions, of which an SM issues
+// one a warp every 16 clocks: they, not the reads, bound rows of many candidates.
 __device__ __forceinline__ double exp_neg(double x) {
   if (x < -700.0) return 0.0;
   const double magic = 0x1.8p52;  // the sum's low bits hold the nearest whole number
