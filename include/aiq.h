@@ -138,7 +138,7 @@ typedef struct {
   int32_t gen_max_new;        /* columns of gen_tokens: the generate spec's max_new_tokens */
   int64_t n_gen_rows;         /* rows of gen_tokens */
   const int32_t* gen_row_ids; /* [n_gen_rows] ascending table rows */
-  const int32_t* gen_tokens;  /* [n_gen_rows, gen_max_new]: greedy tokens, the eos, then pad_id */
+  const int32_t* gen_tokens;  /* [n_gen_rows, gen_max_new]: the tokens, the eos, then pad_id */
   const int32_t* gen_text_len; /* [n_gen_rows]: generated tokens before the eos (max_new without one) */
   float ms_decode;            /* device time of the decode steps (inside ms_prefill) */
   double decode_flops;        /* 2*params per decoded token + attention over cached keys + full LM head */
@@ -318,8 +318,10 @@ const char* aiq_last_error(void);
  * up to 2^20 tokens and 32 GB of cached prompt keys/values), "kv_bits"
  * (aiq_run_transform: 16, the default, or 8: cached keys and values as bytes with
  * a scale per 32 tokens, KV head and keys / values, the layout and rounding that
- * aiq_ops.h states; about half the cache's memory and reads, for logits that differ
- * by the rounding; up to 8 query heads per KV head), "device_bytes_max"
+ * aiq_ops.h states; about half the reads of a decode step, and of the memory half for
+ * whole blocks, while a row's open block takes 32 fp16 tokens a layer however few are
+ * generated (texts of 137 tokens and 32 new ones: a third less, 2 new ones: a sixth);
+ * logits differ by the rounding; up to 8 query heads per KV head), "device_bytes_max"
  * (the context's device byte cap, as AIQ_DEVICE_BYTES_MAX at aiq_init; <= 0
  * lifts it; tables and models already held stay; a load or a query that finds no
  * room takes back the context's workspace, and a query runs again in the least

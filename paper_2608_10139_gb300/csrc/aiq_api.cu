@@ -753,7 +753,7 @@ struct QueryState {
   bool merged_prefix = false;               // ... as the first chunk's first sequence
 };
 
-// Generation state of an AI_TRANSFORM query (Table 1): greedy decoding of
+// Generation state of an AI_TRANSFORM query (Table 1): decoding, greedy or by draws, of
 // every candidate row after its chunk's prefill.
 struct GenPlan {
   int max_new = 0, eos = -1, pad = 0;
@@ -971,7 +971,7 @@ aiq_status q8_order(aiq_ctx* c, const DecodeQ8& d, bool once, const int4** order
   return AIQ_OK;
 }
 
-// max_new greedy steps for the R rows of one chunk whose prefill just ran
+// max_new steps for the R rows of one chunk whose prefill just ran
 // (final hidden state of each row's last prompt token in b.resid_last).
 aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, DecodeBufs d, int R, int64_t Tc,
                         const __half* pkv, int P, const float* prefix_last, int64_t r0, GenPlan* gp) {
@@ -1522,7 +1522,7 @@ aiq_status check_sampling(const aiq_sampling& s, int V) {
   return AIQ_OK;
 }
 
-// Table 2 Q3 / Q5: relational phase, prefill + greedy decoding per chunk,
+// Table 2 Q3 / Q5: relational phase, prefill + decoding (greedy or by draws) per chunk,
 // then the LIKE filter and the result arrays.
 aiq_status run_transform(aiq_ctx* c, const TableD& t, ModelD* m, const aiq_select* q, const aiq_generate* gen,
                          aiq_result_h* out) {

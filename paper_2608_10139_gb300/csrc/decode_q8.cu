@@ -987,9 +987,13 @@ int decode_q8_order_rows(const DecodeQ8& d, bool once, int num_sms) {
   // ordered and as they come, 8 KV heads; head_dim 64: 2,432 rows of about 200 keys 182 and
   // 181 us, of 570 364 and 390, 6,000 rows of 120 276 and 266; 128: 700 rows of 200 132 and
   // 145, 4,000 rows of 200 426 and 421, of 600 980 and 1,057; 32: 3,000 rows of 400 214 and
-  // 249) and the texts, in which alone the rows differ, are most of the keys (of 12 tiles 7,
-  // the call with the cache's read-back 227 and 224); for many calls over the same rows up
-  // to some 24 tasks.
+  // 249) and the texts, in which alone the rows differ, are two thirds of the keys (more:
+  // head_dim 64, 700 rows of 200 behind 64 96 and 94, 1,500 of 300 behind 128 162 and 179,
+  // 2,432 of 570 behind 320 370 and 386; 128, 700 of 200 behind 64 127 and 134.  Fewer: 64,
+  // 700 of 200 behind 192 104 and 99, 1,500 of 300 behind 256 183 and 181, behind 512 221 and
+  // 230; 128, 700 of 200 behind 192 139 and 149, 1,500 of 300 behind 512 344 and 334; 32,
+  // 3,000 of 400 behind 512 317 and 335: either way, so nothing is spent); for many calls
+  // over the same rows up to some 24 tasks.
   return per_warp > 1 && (once ? own >= 1.2 * per_warp && own >= tiles_of_head(d) / d.R * 2 / 3 : per_warp <= 24) ? d.R : 0;
 }
 

@@ -2,19 +2,19 @@
 //
 // A tile holds 32 tokens' keys and then values of one KV head, one unsigned
 // byte u = q + 128 per element, 64 * HD bytes.  With s the largest magnitude of
-// the block's 32 * HD keys (or values) divided by 127, q = 127 x / (127 s)
+// the block's 32 * HD keys (or values) divided by 127, q = 127 x / that magnitude
 // rounded to the nearest whole number, halves away from zero, and q * s is the
 // value that the byte stands for.  A tile lies in the order in which the lanes
 // of a warp feed mma.sync.m16n8k16 from it: lane = 4 g + t reads 16 consecutive
-// bytes per load, and a word's four bytes are the two registers of one B
-// fragment, two keys by two elements.
+// bytes per load, and a word's four bytes become two registers of an A fragment's
+// row: four elements of a key, or an element of two keys and of the two 8 behind them.
 //
 //   keys,   HD 64 / 128: [key / 8][c][lane g = key % 8, t][b], element 64 c + 16 t + b
 //           HD 32:       [key / 16][lane g = key % 8, t][key / 8 % 2][b], element 8 t + b
 //   values: [key / 16][c][lane g, t][i][key / 8 % 2][e], element 32 c + 8 (g / 2) + 2 i + g % 2,
 //           key % 8 = 2 t + e
 //
-// The element that a lane's k index stands for is the same in the queries'
+// The element that a lane's k index stands for is the same in the queries' B
 // fragments, and the output's columns come out as eight consecutive elements
 // per lane.  A block's first keys are a prefix of both halves (in steps of 8 and
 // 16 keys), so that a partly filled block need not be read whole.
