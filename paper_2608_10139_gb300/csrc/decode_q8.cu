@@ -122,7 +122,7 @@ struct Attn8 {
   // log2 units, to probabilities relative to m, which lies kAbove to kAbove + kLag below
   // the largest score so far: it follows, and the output is scaled down, only where that
   // would come to lie higher, so that the running output need not be touched for most
-  // tiles and a probability is at most 2^15, within fp16.  hi is a probability rounded to
+  // tiles and a probability is at most 2^15.25, within fp16.  hi is a probability rounded to
   // fp16, lo what the rounding left: the two are off by 2^-22 of it, or by half of fp16's
   // last place, 2^-25, where that is more, which is 2^-36 of the largest.  That is what
   // kAbove is for: relative to the largest score itself, keys that one outweighs by 2^25
@@ -143,7 +143,18 @@ struct Attn8 {
     for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
     mb[0] *= scale;
     mb[1] *= scale;
-    if (__any_sync(0xffffffffu, mb[0] > m[0] + (kAbove + kLag) || mb[1] > m[1] + (kAbove + kLag))) {
+    if (fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f) {
+      // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
+      // score that is not rounded (in the fma below) could lie so far above a rounded m that
+      // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
+      // most, and the largest probability stays between 1 and 2^15 whatever the last place.
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[k][e] *= scale;
+      scale = 1.f;
+    }
+    if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag))) {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) {  // to finite maxima: a block has a key
         mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
@@ -151,7 +162,7 @@ struct Attn8 {
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float mn = fmaxf(m[e], mb[e] - kAbove), f = exp2_approx(m[e] - mn);
+        const float mn = fmaxf(m[e], __fsub_ru(mb[e], kAbove)), f = exp2_approx(m[e] - mn);
         m[e] = mn;
         l[e] *= f;
 #pragma unroll
