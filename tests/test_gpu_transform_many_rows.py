@@ -38,7 +38,8 @@ def test_many_rows_on_the_8_bit_cache(ctx, name, rows, new):
             assert gap <= MARGIN_RTOL * max(1.0, abs(z[t].max())), f"row {row} step {t}: {gap:.4g} below the largest"
 
 
-def test_draws_in_little_memory():
+@pytest.mark.parametrize("bits", [16, 8])
+def test_draws_in_little_memory(bits):
     """115 MB of logits a step under a cap that leaves 40 MB beside the greedy query's least."""
     shape, W, bias = _zero_model(vocab=32000)
     rows = 900
@@ -48,6 +49,7 @@ def test_draws_in_little_memory():
     try:
         m = c.load_model(shape, weights_list(shape, W))
         t = c.load_table(table.cols, (table.offsets, table.tokens))
+        c.set_option("kv_bits", bits)
         loaded = sum(v.nbytes for v in weights_list(shape, W))
         for cap in range(loaded, loaded + (1 << 29), 4 << 20):
             c.set_option("device_bytes_max", cap)
