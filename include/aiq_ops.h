@@ -140,6 +140,66 @@ aiq_status aiq_op_decode_attention_q8(aiq_ctx* ctx, const void* qkv, int32_t R, 
                                       const int32_t* seq_start, void* gen_cache, float* gen_scales, void* gen_tail,
                                       int32_t gen_cap, int32_t slot, void* out);
 
+/* The 4-bit key/value cache: a quarter of the fp16 one's bytes and what the scales
+ * take.  (The paper has no counterpart, as with the 8-bit cache.)
+ *
+ * A group is min(hd, 64) consecutive elements of one token's key, or value, of one
+ * KV head.  Its smallest element is m (fp16), its scale s the difference of the
+ * largest and the smallest / 15, rounded up to fp16, and x is held as the whole number
+ * n = floor((x - m) / s + 1/2), 0 .. 15 (0 where s is 0); it stands for m + n s, which is
+ * within s / 2 of x.
+ * Tiles of AIQ_KV_BLOCK = 32 tokens of one KV head hold the codes n and the pairs
+ * (s, m); sequence i of a packed batch begins at block seq_start[i] / 32 + i, as in the
+ * 8-bit cache.
+ *
+ *   cache   [blocks][Hkv][32 hd + 256 C] bytes, C = 2 where hd is 128 and else 1, 16-byte
+ *           aligned.  A tile: 16 hd bytes of keys, 16 hd of values, C * 256 of pairs, in
+ *           the order in which the attention reads them; a byte holds two elements of
+ *           one token, the first in its low four bits:
+ *             keys, hd 64 and 128:   [k 2][c C][g 8][t 4][h 2][b 8]
+ *                 = key 16 k + 8 h + g, elements 64 c + 16 t + 2 b and + 1
+ *             keys, hd 32:           [g 8][t 4][j 4][b 4]
+ *                 = key 8 j + g, elements 8 t + 2 b and + 1
+ *             values, hd 64 and 128: [k 2][c C][g 8][t 4][i 4][e 2][h 2]
+ *                 = key 16 k + 8 h + 2 t + e, elements 64 c + 8 g + 2 i and + 1
+ *             values, hd 32:         [g 8][t 4][k 2][i 2][e 2][h 2]
+ *                 = key 16 k + 8 h + 2 t + e, elements 4 g + 2 i and + 1
+ *             pairs:                 [c C][keys, values][g 8][j 4][s, m] fp16
+ *                 = key 8 j + g, elements 64 c and on
+ *           Bytes of keys that a block does not hold count for nothing. */
+
+/* Quantises packed keys and values as they are written: kv, ldkv, seq_start and their
+ * limits as for aiq_op_kv_quantize.  Blocks of the cache that no token falls into are left
+ * as they were.  A NaN or an infinity gives AIQ_ERR_DEVICE_CHECK, and so does a sequence
+ * outside the T rows.  The call synchronises its stream. */
+aiq_status aiq_op_kv_quantize4(aiq_ctx* ctx, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                               int32_t n_seqs, int32_t Hkv, int32_t hd, void* cache);
+
+/* Reads such a cache back into fp16 rows: m + n s rounded once, at most 65504; rows that no
+ * sequence holds are left as they were.  A cache of whole blocks (generated tokens', below)
+ * is one sequence of 32 * blocks tokens. */
+aiq_status aiq_op_kv_dequantize4(aiq_ctx* ctx, const void* cache, int64_t T, const int32_t* seq_start, int32_t n_seqs,
+                                 int32_t Hkv, int32_t hd, void* kv, int64_t ldkv);
+
+/* aiq_op_decode_attention over 4-bit caches, for rows of which `beams` share a prompt.  Row
+ * r's token of qkv fp16 [R, (Hq + 2 Hkv) * hd] attends
+ *   the prefix: P tokens, one sequence (NULL when P == 0);
+ *   a prompt: sequence r / beams of a packed cache of R / beams sequences, seq_start int32
+ *     [R / beams + 1] (device), its last at most T (NULL cache when T == 0);
+ *   its generated tokens 0 .. slot, gen_cache [R][(gen_cap + 31) / 32 blocks], where this
+ *     step's key and value are first written, in 4 bits, to token `slot`.
+ * All are taken as the cache holds them, m + n s without another rounding, the step's own
+ * token among them.  held (optional) fp16 [R, 2 Hkv hd]: the step's keys, then its values, as
+ * aiq_op_kv_dequantize4 would read them back.  out fp16 [R, Hq * hd].  hd in {32, 64, 128},
+ * Hq / Hkv <= 8, at most 2^20 heads, beams >= 1 and a divisor of R.  qkv, caches, out and
+ * held 16-byte aligned.  A sequence outside the T tokens, a key or value of this step that is
+ * not finite and an output that is not finite in fp16 give AIQ_ERR_DEVICE_CHECK.  The call
+ * synchronises its stream. */
+aiq_status aiq_op_decode_attention_q4(aiq_ctx* ctx, const void* qkv, int32_t R, int32_t beams, int32_t Hq, int32_t Hkv,
+                                      int32_t hd, const void* prefix_cache, int32_t P, const void* own_cache, int64_t T,
+                                      const int32_t* seq_start, void* gen_cache, int32_t gen_cap, int32_t slot, void* out,
+                                      void* held);
+
 typedef enum { AIQ_LOGITS_F32 = 0, AIQ_LOGITS_F16 = 1, AIQ_LOGITS_BF16 = 2 } aiq_logit_type;
 
 /* The next token of R rows of V logits (row pitch ldl elements) for the given
@@ -152,6 +212,47 @@ typedef enum { AIQ_LOGITS_F32 = 0, AIQ_LOGITS_F16 = 1, AIQ_LOGITS_BF16 = 2 } aiq
  * the call synchronises its stream. */
 aiq_status aiq_op_sample(aiq_ctx* ctx, const void* logits, int32_t type, int64_t ldl, int32_t R, int32_t V,
                          const float* uniforms, const aiq_sampling* sampling, int32_t* tokens, float* probs);
+
+/* One step of beam search: the best continuations of n groups of `beams` hypotheses
+ * each.  (The paper decodes greedily; this is its generative decoding, Table 1, over
+ * several hypotheses.)  Row g * beams + b of the logits (n * beams rows of V, pitch ldl
+ * elements) belongs to hypothesis b of group g, of score C = scores[g][b] (fp32, a sum of
+ * log probabilities; -infinity: the place holds none, its row is not read).  It offers
+ * every token t at
+ *     s = C + z_t - log sum_i exp(z_i),
+ * computed in 64 bits, where z_t is finite (-infinity rules a token out, a row of
+ * -infinity alone offers nothing); a hypothesis that has ended (done[g][b] != 0; done may be
+ * NULL: none has) offers itself, pad_id at s = C, and its row is not read.
+ * The first `keep` of a group's offers, by s descending, equal ones by hypothesis, those of
+ * one hypothesis by logit descending and then by token, go to parents, tokens (int32
+ * [n][keep], a parent being a hypothesis of the group, 0 .. beams - 1), scores_out (fp32) and
+ * done_out (int32, optional): 1 where the parent had ended or the token is eos_id
+ * (eos_id < 0: none).  Places beyond the offers get parent 0, pad_id, score -infinity and
+ * done 1.  beams 1 .. AIQ_BEAMS_MAX, keep 1 .. 2 * AIQ_BEAMS_MAX; keep = beams continues with the
+ * outputs as the next step's inputs, keep = 2 * beams leaves ended hypotheses to the caller.
+ * A NaN or +infinity among the logits of a row that is read, or among the scores, gives
+ * AIQ_ERR_DEVICE_CHECK; that group's places are as if there were no offers, the other
+ * groups' are written.  Outputs must not overlap inputs.  All pointers are device memory,
+ * aligned to their elements; the call synchronises its stream. */
+enum { AIQ_BEAMS_MAX = 16 };
+aiq_status aiq_op_beam_select(aiq_ctx* ctx, const void* logits, int32_t type, int64_t ldl, int32_t n, int32_t beams,
+                              int32_t V, const float* scores, const int32_t* done, int32_t eos_id, int32_t pad_id,
+                              int32_t keep, int32_t* parents, int32_t* tokens, float* scores_out, int32_t* done_out);
+
+/* Moves the state of hypotheses to the places that selection gave them: of each of
+ * `layers` layers, row g * beams + i becomes what row g * beams + parents[g][i] was
+ * (parents int32 [n][beams], device).  Row r of layer l is `bytes` bytes at
+ * src + l * layer_pitch + r * pitch, and at dst likewise.  dst == src reorders in place:
+ * rows whose parent is their own place are neither read nor written.  Otherwise every row
+ * is written and the two may not overlap.  What lies between rows is left as it was.  It
+ * moves any state of the hypotheses, the caches of generated tokens (fp16, 8 bits and
+ * their tails, 4 bits: the blocks in use, rows pitch apart) as well as token histories.
+ * Pointers, sizes and pitches that are multiples of 16 (or 4) bytes move by as much.
+ * beams 1 .. AIQ_BEAMS_MAX.  pitch >= bytes where there is more than one row; layers must not
+ * overlap.  A parent outside the group gives AIQ_ERR_DEVICE_CHECK and leaves the group's rows as
+ * they were.  The call synchronises its stream. */
+aiq_status aiq_op_beam_reorder(aiq_ctx* ctx, const void* src, void* dst, int64_t bytes, int64_t pitch, int32_t n,
+                               int32_t beams, const int32_t* parents, int32_t layers, int64_t layer_pitch);
 
 /* One relational term for aiq_filter_compact_static: `column op constant` on a
  * caller-owned device column of n_rows values (16-byte aligned).  INT32 and

@@ -24,7 +24,8 @@ AGG_COUNT, AGG_ROW_IDS, AGG_GROUP_LABEL, AGG_GROUP_BUILD_KEY, AGG_SUM = 0, 1, 2,
 FLAG_LOGITS, FLAG_RELATIONAL_ONLY = 1, 2
 GEN_MATCH_TOKENS, GEN_SAMPLE = 1, 2
 LOGITS_F32, LOGITS_F16, LOGITS_BF16 = 0, 1, 2
-KV_BLOCK = 32          # tokens of an 8-bit cache that share a scale
+KV_BLOCK = 32          # tokens of a block of the 8-bit cache (which share a scale) and of the 4-bit one
+BEAMS_MAX = 16         # the most hypotheses of a group
 SAMPLE_MAX_K = 1024    # the largest top_k
 EPI_F16, EPI_ROPE_F16, EPI_RESID_F32, EPI_SWIGLU_F16, EPI_RESID_ADD_F32 = 0, 1, 2, 3, 5
 
@@ -133,6 +134,17 @@ _SIGS = {
     "aiq_op_decode_attention_q8": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                    C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                    C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p],
+    "aiq_op_kv_quantize4": [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                            C.c_void_p],
+    "aiq_op_kv_dequantize4": [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                              C.c_int64],
+    "aiq_op_decode_attention_q4": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                   C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                                   C.c_int32, C.c_void_p, C.c_void_p],
+    "aiq_op_beam_select": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                           C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
+    "aiq_op_beam_reorder": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
+                            C.c_int32, C.c_int64],
     "aiq_op_sample": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
                       C.POINTER(_Sampling), C.c_void_p, C.c_void_p],
     "aiq_filter_compact_static": [C.POINTER(_Term), C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p],
@@ -194,6 +206,12 @@ def kv_cache_blocks(T: int, n_seqs: int) -> int:
     """Blocks of an 8-bit cache for T tokens in n_seqs sequences: it holds
     blocks * Hkv * 64 * hd bytes, and 2 fp32 scales per block and KV head."""
     return T // KV_BLOCK + n_seqs
+
+
+def kv4_tile_bytes(hd: int) -> int:
+    """Bytes of a block and KV head of the 4-bit cache, which holds kv_cache_blocks(T, n_seqs)
+    blocks of Hkv of them; the generated tokens' holds (gen_cap + 31) // 32 blocks per row."""
+    return KV_BLOCK * hd + 256 * max(1, hd // 64)
 
 
 def _i32(a) -> np.ndarray:
@@ -523,6 +541,38 @@ class Context:
                                                    prefix_scales or None, P, own_cache or None, own_scales or None, T,
                                                    seq_start or None, gen_cache or None, gen_scales or None,
                                                    gen_tail or None, gen_cap, slot, out or None))
+
+    def op_kv_quantize4(self, kv: int, ldkv: int, T: int, seq_start: int, n_seqs: int, Hkv: int, hd: int, cache: int):
+        """fp16 keys / values into the 4-bit cache (kv4_tile_bytes; see aiq_ops.h)."""
+        _check(self.lib.aiq_op_kv_quantize4(self.h, kv or None, ldkv, T, seq_start or None, n_seqs, Hkv, hd, cache or None))
+
+    def op_kv_dequantize4(self, cache: int, T: int, seq_start: int, n_seqs: int, Hkv: int, hd: int, kv: int, ldkv: int):
+        """The 4-bit cache back to fp16 rows."""
+        _check(self.lib.aiq_op_kv_dequantize4(self.h, cache or None, T, seq_start or None, n_seqs, Hkv, hd, kv or None,
+                                              ldkv))
+
+    def op_decode_attention_q4(self, qkv: int, R: int, Hq: int, Hkv: int, hd: int, own_cache: int, T: int, seq_start: int,
+                               gen_cache: int, gen_cap: int, slot: int, out: int, beams: int = 1, prefix: int = 0,
+                               P: int = 0, held: int = 0):
+        """op_decode_attention over 4-bit caches, rows r of a prompt r // beams; the step's key and
+        value become token ``slot`` of gen_cache."""
+        _check(self.lib.aiq_op_decode_attention_q4(self.h, qkv or None, R, beams, Hq, Hkv, hd, prefix or None, P,
+                                                   own_cache or None, T, seq_start or None, gen_cache or None, gen_cap,
+                                                   slot, out or None, held or None))
+
+    def op_beam_select(self, logits: int, type: int, ldl: int, n: int, beams: int, V: int, scores: int, keep: int,
+                       parents: int, tokens: int, scores_out: int, done: int = 0, done_out: int = 0, eos: int = -1,
+                       pad: int = 0):
+        """The best ``keep`` continuations of n groups of beams from their rows of logits (LOGITS_*) and scores."""
+        _check(self.lib.aiq_op_beam_select(self.h, logits or None, type, ldl, n, beams, V, scores or None, done or None,
+                                           eos, pad, keep, parents or None, tokens or None, scores_out or None,
+                                           done_out or None))
+
+    def op_beam_reorder(self, src: int, dst: int, bytes: int, pitch: int, n: int, beams: int, parents: int,
+                        layers: int = 1, layer_pitch: int = 0):
+        """Rows of state to the places that op_beam_select gave their hypotheses (src == dst: in place)."""
+        _check(self.lib.aiq_op_beam_reorder(self.h, src or None, dst or None, bytes, pitch, n, beams, parents or None,
+                                            layers, layer_pitch))
 
     def op_sample(self, logits: int, type: int, ldl: int, R: int, V: int, uniforms: int, tokens: int,
                   temperature: float = 1.0, top_k: int = 50, top_p: float = 1.0, min_p: float = 0.0, probs: int = 0):

@@ -1498,17 +1498,25 @@ constexpr int32_t kHeadsMax = 1 << 20;  // a row's elements are counted in 32 bi
 
 // What the two copies between fp16 rows and the 8-bit cache ask of their arguments.
 aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
-                            int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache, const float* scales) {
-  if (!c || !kv || !seq_start || !cache || !scales || T < 0 || T > INT32_MAX || n_seqs < 0 || Hkv <= 0)
+                            int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache) {
+  if (!c || !kv || !seq_start || !cache || T < 0 || T > INT32_MAX || n_seqs < 0 || Hkv <= 0)
     return fail(AIQ_ERR_INVALID_ARG, "bad args");
   if (!(hd == 32 || hd == 64 || hd == 128)) return fail(AIQ_ERR_UNSUPPORTED, "hd must be 32, 64 or 128");
   if (ldkv < 2 * int64_t(Hkv) * hd || ldkv % 8)
     return fail(AIQ_ERR_INVALID_ARG, "ldkv must be at least 2 Hkv hd and a multiple of 8");
-  if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(seq_start, 4))
+  if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(seq_start, 4))
     return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
   if (Hkv > kHeadsMax) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^20 heads");
   if ((T / AIQ_KV_BLOCK + n_seqs) * Hkv > (int64_t(1) << 33))
     return fail(AIQ_ERR_UNSUPPORTED, "more than 2^33 (block, KV head) pairs");
+  return AIQ_OK;
+}
+aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                            int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache, const float* scales) {
+  if (!scales) return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  AIQ_TRY(check_cache_rows(c, kv, ldkv, T, seq_start, n_seqs, Hkv, hd, cache));
+  if (!aligned(scales, 8))
+    return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
   return AIQ_OK;
 }
 
@@ -2381,6 +2389,107 @@ aiq_status aiq_op_decode_attention_q8(aiq_ctx* c, const void* qkv, int32_t R, in
     AIQ_TRY(with_room(c, [&] { return ws(c, "op.q8_partial", floats, &partial); }));
   const int e = launch_decode_attention_q8(d, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_kv_quantize4(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
+                               int32_t n_seqs, int32_t Hkv, int32_t hd, void* cache) {
+  AIQ_TRY(check_cache_rows(c, kv, ldkv, T, seq_start, n_seqs, Hkv, hd, cache));
+  if (T == 0 || n_seqs == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const int e = launch_kv_quantize4(static_cast<const __half*>(kv), ldkv, T, seq_start, n_seqs, Hkv, hd,
+                                    static_cast<uint8_t*>(cache), c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("cache quantisation launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_kv_dequantize4(aiq_ctx* c, const void* cache, int64_t T, const int32_t* seq_start, int32_t n_seqs,
+                                 int32_t Hkv, int32_t hd, void* kv, int64_t ldkv) {
+  AIQ_TRY(check_cache_rows(c, kv, ldkv, T, seq_start, n_seqs, Hkv, hd, cache));
+  if (T == 0 || n_seqs == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const int e = launch_kv_dequantize4(static_cast<const uint8_t*>(cache), T, seq_start, n_seqs, Hkv, hd,
+                                      static_cast<__half*>(kv), ldkv, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("cache read-back launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_decode_attention_q4(aiq_ctx* c, const void* qkv, int32_t R, int32_t beams, int32_t Hq, int32_t Hkv,
+                                      int32_t hd, const void* prefix_cache, int32_t P, const void* own_cache, int64_t T,
+                                      const int32_t* seq_start, void* gen_cache, int32_t gen_cap, int32_t slot, void* out,
+                                      void* held) {
+  if (!c || !qkv || !seq_start || !gen_cache || !out || R < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || P < 0 ||
+      (P > 0 && !prefix_cache) || T < 0 || T > INT32_MAX || (T > 0 && !own_cache) || gen_cap < 1 || slot < 0 ||
+      slot >= gen_cap)
+    return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (beams < 1 || R % beams) return fail(AIQ_ERR_INVALID_ARG, "beams must be at least 1 and divide R");
+  if (!(hd == 32 || hd == 64 || hd == 128) || Hq / Hkv > 8)
+    return fail(AIQ_ERR_UNSUPPORTED, "hd must be 32, 64 or 128 and Hq / Hkv <= 8");
+  if (!aligned(qkv, 16) || !aligned(prefix_cache, 16) || !aligned(own_cache, 16) || !aligned(gen_cache, 16) ||
+      !aligned(out, 16) || !aligned(held, 16) || !aligned(seq_start, 4))
+    return fail(AIQ_ERR_INVALID_ARG, "qkv, caches, out and held must be 16-byte aligned");
+  if (Hq > kHeadsMax) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^20 heads");
+  if (int64_t(R) * Hq > INT32_MAX) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^31 - 1 (row, head) pairs");
+  if (R == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  const DecodeQ4 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, beams, Hq, Hkv,
+                   hd, static_cast<const uint8_t*>(prefix_cache), P, static_cast<const uint8_t*>(own_cache), T, seq_start,
+                   static_cast<uint8_t*>(gen_cache), gen_cap, slot, static_cast<__half*>(out), static_cast<__half*>(held)};
+  const int e = launch_decode_attention_q4(d, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_beam_select(aiq_ctx* c, const void* logits, int32_t type, int64_t ldl, int32_t n, int32_t beams,
+                              int32_t V, const float* scores, const int32_t* done, int32_t eos_id, int32_t pad_id,
+                              int32_t keep, int32_t* parents, int32_t* tokens, float* scores_out, int32_t* done_out) {
+  if (!c || !logits || !scores || !parents || !tokens || !scores_out || n < 0 || V < 1 || ldl < V)
+    return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (type < AIQ_LOGITS_F32 || type > AIQ_LOGITS_BF16) return fail(AIQ_ERR_INVALID_ARG, "unknown logit type");
+  if (beams < 1 || keep < 1) return fail(AIQ_ERR_INVALID_ARG, "beams and keep must be at least 1");
+  if (beams > AIQ_BEAMS_MAX || keep > 2 * AIQ_BEAMS_MAX)
+    return fail(AIQ_ERR_UNSUPPORTED, "beams above 16 or keep above 32");
+  if (V > (1 << 30)) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^30 logits a row");
+  if (int64_t(n) * beams > (1 << 24)) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^24 rows of logits");
+  if (!aligned(logits, type == AIQ_LOGITS_F32 ? 4 : 2) || !aligned(scores, 4) || !aligned(done, 4) ||
+      !aligned(parents, 4) || !aligned(tokens, 4) || !aligned(scores_out, 4) || !aligned(done_out, 4))
+    return fail(AIQ_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+  if (n == 0) return AIQ_OK;
+  CUDA_TRY(cudaSetDevice(c->device));
+  uint8_t* scratch = nullptr;
+  AIQ_TRY(with_room(c, [&] { return ws(c, "op.beam", beam_select_bytes(n, beams, keep), &scratch); }));
+  const BeamSelect b{logits, type, ldl, n, beams, V, scores, done, eos_id, pad_id, keep, parents, tokens, scores_out, done_out};
+  const int e = launch_beam_select(b, scratch, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("beam selection launch: ") +
+                                            cudaGetErrorString(static_cast<cudaError_t>(e)));
+  return sync_and_check(c);
+}
+
+aiq_status aiq_op_beam_reorder(aiq_ctx* c, const void* src, void* dst, int64_t bytes, int64_t pitch, int32_t n,
+                               int32_t beams, const int32_t* parents, int32_t layers, int64_t layer_pitch) {
+  if (!c || !src || !dst || !parents || bytes < 0 || n < 0 || layers < 0) return fail(AIQ_ERR_INVALID_ARG, "bad args");
+  if (beams < 1) return fail(AIQ_ERR_INVALID_ARG, "beams must be at least 1");
+  if (beams > AIQ_BEAMS_MAX) return fail(AIQ_ERR_UNSUPPORTED, "beams above 16");
+  if (!aligned(parents, 4)) return fail(AIQ_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+  if (bytes == 0 || n == 0 || layers == 0) return AIQ_OK;
+  const int64_t rows = int64_t(n) * beams, most = int64_t(1) << 46;
+  if (bytes > most || (rows > 1 && (pitch < bytes || pitch > most / rows)) ||
+      (layers > 1 && (layer_pitch < bytes || layer_pitch > most / layers)))
+    return fail(AIQ_ERR_INVALID_ARG, "pitch and layer_pitch must be at least bytes and within the address space");
+  const int64_t span = (rows - 1) * (rows > 1 ? pitch : 0) + bytes;  // of a layer
+  const int64_t deep = (layers - 1) * (layers > 1 ? layer_pitch : 0) + bytes;  // of a row's layers
+  if (rows > 1 && layers > 1 && layer_pitch < span && pitch < deep)
+    return fail(AIQ_ERR_INVALID_ARG, "layers overlap");
+  const uintptr_t a = reinterpret_cast<uintptr_t>(src), b = reinterpret_cast<uintptr_t>(dst);
+  const uint64_t all = static_cast<uint64_t>(span) + (deep - bytes);
+  if (a != b && (a < b ? b - a < all : a - b < all)) return fail(AIQ_ERR_INVALID_ARG, "src and dst overlap");
+  CUDA_TRY(cudaSetDevice(c->device));
+  const int e = launch_beam_reorder(src, dst, bytes, pitch, n, beams, parents, layers, layer_pitch, c->d_err, c->stream);
+  if (e != 0) return fail(AIQ_ERR_CUDA, std::string("beam reordering launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);
 }

@@ -318,6 +318,49 @@ int launch_decode_q8_order(const int32_t* seq_start, int R, int64_t T, int4* ord
 int launch_decode_attention_q8(const DecodeQ8& d, float* partial, unsigned int* arrived, int* err, int num_sms,
                                cudaStream_t s);
 
+// ------------------------------------------------------- 4-bit K/V cache ---
+// As the 8-bit cache's, with tiles that hold their scales (tile4.cuh).
+int launch_kv_quantize4(const __half* kv, int64_t ld, int64_t T, const int32_t* seq_start, int n_seqs, int Hkv, int hd,
+                        uint8_t* cache, int* err, cudaStream_t s);
+int launch_kv_dequantize4(const uint8_t* cache, int64_t T, const int32_t* seq_start, int n_seqs, int Hkv, int hd,
+                          __half* kv, int64_t ld, int* err, cudaStream_t s);
+// launch_decode_attention over that cache: rows r share the prompt of sequence r / beams;
+// generated tokens in (gen_cap + 31) / 32 tiles per row, the step's own among them.
+struct DecodeQ4 {
+  const __half* qkv;
+  int64_t ldq;
+  int R, beams, Hq, Hkv, hd;
+  const uint8_t* prefix;
+  int P;
+  const uint8_t* own;
+  int64_t T;
+  const int32_t* seq_start;
+  uint8_t* gen;
+  int gen_cap, slot;
+  __half* out;
+  __half* held;  // [R][2 Hkv hd] the step's key and value as the cache holds them, or null
+};
+int launch_decode_attention_q4(const DecodeQ4& d, int* err, cudaStream_t s);
+
+// ----------------------------------------------------------- beam search ---
+constexpr int kBeamsMax = 16;
+struct BeamSelect {
+  const void* logits;
+  int type;  // LogitType
+  int64_t ld;
+  int groups, beams, V;
+  const float* scores;
+  const int32_t* done;  // or null
+  int eos, pad, keep;
+  int32_t *parents, *tokens;
+  float* scores_out;
+  int32_t* done_out;    // or null
+};
+size_t beam_select_bytes(int groups, int beams, int keep);  // scratch that the call takes (16-byte aligned)
+int launch_beam_select(const BeamSelect& b, void* scratch, int* err, cudaStream_t s);
+int launch_beam_reorder(const void* src, void* dst, int64_t bytes, int64_t pitch, int groups, int beams,
+                        const int32_t* parents, int layers, int64_t layer_pitch, int* err, cudaStream_t s);
+
 // -------------------------------------------------------------- sampling ---
 enum LogitType : int { LOGITS_F32 = 0, LOGITS_F16 = 1, LOGITS_BF16 = 2 };
 constexpr int kSampleKeepMax = 1024;  // the largest top_k
