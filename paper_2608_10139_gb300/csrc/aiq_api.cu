@@ -2437,8 +2437,12 @@ aiq_status aiq_op_decode_attention_q4(aiq_ctx* c, const void* qkv, int32_t R, in
   CUDA_TRY(cudaSetDevice(c->device));
   const DecodeQ4 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, beams, Hq, Hkv,
                    hd, static_cast<const uint8_t*>(prefix_cache), P, static_cast<const uint8_t*>(own_cache), T, seq_start,
-                   static_cast<uint8_t*>(gen_cache), gen_cap, slot, static_cast<__half*>(out), static_cast<__half*>(held)};
-  const int e = launch_decode_attention_q4(d, c->d_err, c->stream);
+                   static_cast<uint8_t*>(gen_cache), gen_cap, slot, static_cast<__half*>(out), static_cast<__half*>(held),
+                   nullptr};
+  float* partial = nullptr;
+  if (const size_t floats = decode_q4_floats(d, c->num_sms))
+    AIQ_TRY(with_room(c, [&] { return ws(c, "op.q4_partial", floats, &partial); }));
+  const int e = launch_decode_attention_q4(d, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("decode attention launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);

@@ -1,9 +1,17 @@
 // One generation step's attention over the 4-bit key/value cache (tile4.cuh):
 // row r's new token against the shared prefix, the prompt of its sequence (rows
 // r / beams share it), its generated tokens and itself, all as the cache holds them;
-// the step's key and value are appended first.
+// the step's key and value are appended on the way.
 //
-// out = sum_j p_j v_j / sum_j p_j, p_j = exp((q . k_j) / sqrt(hd) - m).
+// out = sum_j p_j v_j / sum_j p_j, p_j = 2^(z_j - M), in one pass over the keys with the
+// running maximum, sum and output of a softmax in fp32.  A key is m + n s for a token's
+// (s, m) and the codes n of its elements, so that
+//     q . k = s (q . n) + m sum(q),      sum_j p_j v_j = sum_j (p_j s_j) n_j + sum_j p_j m_j:
+// the products take the codes alone, which fp16 holds exactly, and the scales cost a few
+// multiplications per score.  Nothing is rounded before the products but p_j s_j, to two
+// fp16 numbers.
+#include <algorithm>
+
 #include "kernels.h"
 #include "tile4.cuh"
 
@@ -14,6 +22,8 @@ struct DecQ4Args {
   const __half* qkv;  // [R][(Hq + 2 Hkv) HD]
   int64_t ldq;
   int Hq, Hkv, G, beams;
+  int wide;           // beams of a task
+  int inner;          // tasks of a sequence: Hkv * ceil(beams / wide)
   const uint8_t* pc;  // prefix tiles
   int P;
   const uint8_t* oc;  // prompt tiles (packed: tile8_first_block)
@@ -22,144 +32,907 @@ struct DecQ4Args {
   uint8_t* gc;        // generated tokens: gen_blocks tiles per row
   int64_t gen_blocks;
   int slot;
-  float scale;        // 1 / sqrt(HD)
+  float scale_log2;   // log2(e) / sqrt(HD)
   __half* out;        // [R][Hq HD]
   __half* held;       // [R][2 Hkv HD] or null
   int* err;
+  const int4* order;  // sequences, first tokens and lengths, long ones first; null: as they come
 };
 
-constexpr int kThreads = 128;
-
-template <int HD>
-__device__ __forceinline__ float element4(const uint8_t* tile, int key, int d, bool value) {
-  const int at = value ? tile4_value_at<HD>(key, d & ~1) : tile4_key_at<HD>(key, d & ~1);
-  const uint32_t pair = *reinterpret_cast<const uint32_t*>(tile + tile4_pair_at<HD>(key, value, d / 64));
-  const float n = static_cast<float>(tile[at] >> (d & 1 ? 4 : 0) & 15);
-  return fmaf(n, __low2float(as_h2(pair)), __high2float(as_h2(pair)));
+// d (+)= A B.
+template <bool FIRST>
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         const uint32_t (&b)[2]) {
+  if constexpr (FIRST)  // the addend is a constant, which takes no register to be cleared
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]), "f"(0.f));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 
-// A CTA per (row, query head): 128 keys at a time, a score per thread, then an
-// output element per thread.
+// 2^x to 2^-22 of it; 0 for -infinity.
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float power2(int e) { return __int_as_float((127 + e) << 23); }  // -126 .. 127
+
+// A step's elements of one row and KV head that a lane quantises: of the key where
+// lane < 16, else of the value.
 template <int HD>
-__global__ void __launch_bounds__(kThreads) k_decode_q4(DecQ4Args a) {
+struct Token4 {
+  static constexpr int E = HD / 16;
+  uint32_t x[E / 2];
+  __device__ __forceinline__ void load(const __half* key, int64_t to_value) {
+    const int lane = threadIdx.x & 31;
+    const __half* from = key + (lane & 16 ? to_value : 0) + (lane & 15) * E;
+    if constexpr (E == 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(from);
+      x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    } else if constexpr (E == 4) {
+      const uint2 v = *reinterpret_cast<const uint2*>(from);
+      x[0] = v.x, x[1] = v.y;
+    } else {
+      x[0] = *reinterpret_cast<const uint32_t*>(from);
+    }
+  }
+  // Into token `key` of a tile: the copy in shared memory and the cache's own.  held: the
+  // row's keys of this head, or null.  False: an element is not finite.
+  __device__ __forceinline__ bool append(uint8_t* copy, uint8_t* tile, int key, __half* held, int64_t to_value) const {
+    const int lane = threadIdx.x & 31, d = (lane & 15) * E, c = d / 64;
+    const bool value = lane & 16;
+    __half2 e = extent4<E / 2>(x);
+#pragma unroll
+    for (int s = 1; s < (HD == 128 ? 8 : 16); s <<= 1) e = __hmin2_nan(e, as_h2(__shfl_xor_sync(0xffffffffu, as_u32(e), s)));
+    const Group4 g = group4(e);
+    const uint32_t code = codes4<E>(x, g), pair = g.pair();
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+      const int at = value ? tile4_value_at<HD>(key, d + 2 * i) : tile4_key_at<HD>(key, d + 2 * i);
+      copy[at] = tile[at] = static_cast<uint8_t>(code >> (8 * i));
+    }
+    if (d % 64 == 0) {
+      const int at = tile4_pair_at<HD>(key, value, c);
+      *reinterpret_cast<uint32_t*>(copy + at) = *reinterpret_cast<uint32_t*>(tile + at) = pair;
+    }
+    if (held) {
+      uint32_t* to = reinterpret_cast<uint32_t*>(held + (value ? to_value : 0) + d);
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) to[i] = byte4(code, i, pair);
+    }
+    return g.finite();
+  }
+};
+
+// A warp's running softmax of a task: `wide` beams' G query heads of one KV head, up to
+// eight columns in all.  Keys and values are the A operands (16 keys, or 16 elements of
+// the output, as rows): no row of a product is padding, and a lane's numbers all belong to
+// columns 2 t and 2 t + 1 (lane = 4 g + t).
+// PAIRS, for up to four columns: 4 .. 7 are 0 .. 3 again, so that one product takes a
+// weight's hi (below) in the first four and its lo in the others, and their outputs are
+// added at the end.
+template <int HD, bool PAIRS>
+struct Attn4 {
+  static constexpr int C = tile4_groups(HD);
+  static constexpr int KS = HD / 16;
+  static constexpr int FR = KS / C;      // 16-element fragments of a group
+  static constexpr int NQ = HD / 32;     // 16-byte loads of a lane's query elements
+  static constexpr float kAbove = 11.f, kLag = 4.f, kLow = -1e30f;
+  uint32_t q[KS][2];
+  float scale[2], sum[C][2];  // of columns 2 t, 2 t + 1
+  // [c][i][2 r + column]: element 64 c + 8 g + 2 i + r (HD 32: 4 g + 2 i + r) of columns 2 t, 2 t + 1
+  float o[C][FR][4];
+  float low[C][2];  // sums of p m over the lane's keys
+  float m[2], l[2];
+
+  static __device__ __forceinline__ int column() {
+    const int g = (threadIdx.x & 31) >> 2;
+    return PAIRS ? g & 3 : g;
+  }
+  // The query elements of the lane's column (null: none): 16 t .. + 15 of each 64 (HD 32: 8 t .. + 7).
+  static __device__ __forceinline__ void fetch(uint4 (&raw)[NQ], const __half* query) {
+    const int t = threadIdx.x & 3;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      raw[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (query) raw[i] = *reinterpret_cast<const uint4*>(query + (HD == 32 ? 8 * t : 64 * (i / 2) + 16 * t + 8 * (i % 2)));
+    }
+  }
+  // The B fragments: k-step 4 c + 2 w + f takes elements 2 f, 2 f + 4 and 2 f + 1, 2 f + 5 of the
+  // eight of word w, as a word of codes gives them.  Its second register meets codes 16 times too
+  // large, and all codes are 2^-24 too small.  A column is scaled by the power of two that brings its
+  // largest element to 2^10 .. 2^11, so that a sixteenth of any that counts is exact.
+  __device__ __forceinline__ void begin(const uint4 (&raw)[NQ], float scale_log2) {
+    const int lane = threadIdx.x & 31, t = lane & 3;
+    __half2 big = as_h2(0u);
+    float own[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) own[c] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const uint32_t x[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        big = __hmax2(big, __habs2(as_h2(x[j])));
+        const float2 v = __half22float2(as_h2(x[j]));
+        own[i / (HD == 32 ? 1 : 2)] += v.x + v.y;
+      }
+    }
+    uint32_t top = as_u32(__hmax2(big, __lowhigh2highlow(big))) & 0xffffu;
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+#pragma unroll
+      for (int c = 0; c < C; ++c) own[c] += __shfl_xor_sync(0xffffffffu, own[c], d);
+    }
+    const int e = max(static_cast<int>(top >> 10), 1);  // elements are below 2^(e - 14)
+    const float f = power2(25 - e), f16 = power2(21 - e);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const uint32_t b[4] = {__byte_perm(raw[i].x, raw[i].z, 0x5410), __byte_perm(raw[i].x, raw[i].z, 0x7632),
+                             __byte_perm(raw[i].y, raw[i].w, 0x5410), __byte_perm(raw[i].y, raw[i].w, 0x7632)};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 v = __half22float2(as_h2(b[j]));
+        const float by = j & 1 ? f16 : f;
+        q[2 * i + j / 2][j & 1] = as_u32(__floats2half2_rn(v.x * by, v.y * by));
+      }
+    }
+    const float unit = power2(e - 1), rest = power2(1 - e);  // 2^24 / f, and sum(q) in its units
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int from = 4 * (2 * t + j);  // a lane of the column
+      scale[j] = scale_log2 * __shfl_sync(0xffffffffu, unit, from);
+#pragma unroll
+      for (int c = 0; c < C; ++c) sum[c][j] = __shfl_sync(0xffffffffu, own[c] * rest, from);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int i = 0; i < FR; ++i) o[c][i][0] = o[c][i][1] = o[c][i][2] = o[c][i][3] = 0.f;
+      low[c][0] = low[c][1] = 0.f;
+    }
+    m[0] = m[1] = kLow;  // (below any score)
+    l[0] = l[1] = 0.f;
+  }
+
+  // One tile: n keys (1 .. 32); see0, see1: whether columns 2 t and 2 t + 1 attend it.
+  __device__ __forceinline__ void tile(const uint8_t* tile, int n, bool see0, bool see1) {
+    const int lane = threadIdx.x & 31, g = lane >> 2;
+    const uint4* kin = reinterpret_cast<const uint4*>(tile);
+    const uint4* vin = reinterpret_cast<const uint4*>(tile + kTileKeys * HD / 2);
+    const uint4* pairs = reinterpret_cast<const uint4*>(tile + tile4_pairs(HD));
+    constexpr uint32_t kLo = 0x000f000fu, kHi = 0x00f000f0u;
+    float sc[2][4];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint4 kp = pairs[16 * c + g];
+      const uint32_t p[4] = {kp.x, kp.y, kp.z, kp.w};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {  // keys 16 k + g and + 8
+        float acc[4];
+        const uint4 v = kin[HD == 32 ? lane : (k * C + c) * 32 + lane];
+        uint32_t a[FR / 2], b[FR / 2];
+        if constexpr (HD == 32) {
+          a[0] = k ? v.z : v.x, b[0] = k ? v.w : v.y;
+        } else {
+          a[0] = v.x, a[1] = v.y, b[0] = v.z, b[1] = v.w;
+        }
+#pragma unroll
+        for (int w = 0; w < FR / 2; ++w) {
+          const uint32_t(&q0)[2] = q[c * FR + 2 * w];
+          if (w == 0)
+            mma16816<true>(acc, a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
+          else
+            mma16816<false>(acc, a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
+          const uint32_t a8 = a[w] >> 8, b8 = b[w] >> 8;
+          mma16816<false>(acc, a8 & kLo, b8 & kLo, a8 & kHi, b8 & kHi, q[c * FR + 2 * w + 1]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float2 sm = __half22float2(as_h2(p[2 * k + h]));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float base = c ? fmaf(sm.y, sum[c][e], sc[k][2 * h + e]) : sm.y * sum[c][e];
+            sc[k][2 * h + e] = fmaf(sm.x, acc[2 * h + e], base);
+          }
+        }
+      }
+    }
+    if (n < kTileKeys) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * k + 8 * (e / 2) + g >= n) sc[k][e] = -INFINITY;
+    }
+    if (!see0) sc[0][0] = sc[0][2] = sc[1][0] = sc[1][2] = -INFINITY;
+    if (!see1) sc[0][1] = sc[0][3] = sc[1][1] = sc[1][3] = -INFINITY;
+
+    // Probabilities relative to m, which lies kAbove to kAbove + kLag below the largest score so
+    // far: it follows, and the output is scaled down, only where that would come to lie higher,
+    // so that the running output need not be touched for most tiles.
+    float mb[2], by[2] = {scale[0], scale[1]};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e])) * by[e];
+    if (fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f) {
+      // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
+      // score that is not rounded (in the fma below) could lie so far above a rounded m that
+      // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
+      // most, and the largest probability stays between 1 and 2^15 whatever the last place.
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[k][e] *= by[e & 1];
+      by[0] = by[1] = 1.f;
+    }
+    if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag))) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
+        mb[1] = fmaxf(mb[1], __shfl_xor_sync(0xffffffffu, mb[1], d));
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float mn = fmaxf(m[e], __fsub_ru(mb[e], kAbove)), f = exp2_approx(m[e] - mn);
+        m[e] = mn;
+        l[e] *= f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          low[c][e] *= f;
+#pragma unroll
+          for (int i = 0; i < FR; ++i) o[c][i][e] *= f, o[c][i][2 + e] *= f;
+        }
+      }
+    }
+    float pr[4][2];  // of keys 8 j + g
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        pr[j][e] = exp2_approx(fmaf(sc[j / 2][2 * (j & 1) + e], by[e], -m[e]));
+        l[e] += pr[j][e];  // a lane's sums cover its own keys only; finish adds them
+      }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint4 vp = pairs[16 * c + 8 + g];
+      uint32_t p[4] = {vp.x, vp.y, vp.z, vp.w};
+      if (n < kTileKeys) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (8 * j + g >= n) p[j] = 0u;  // 0 times anything may be NaN
+      }
+      // A weight p s is at most p where the scales are brought below 1 by the power of two that
+      // the tile's largest asks for; a probability is at most 2^15.25, within fp16.
+      const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(p[0] & 0xffffu, p[1] & 0xffffu), max(p[2] & 0xffffu, p[3] & 0xffffu)));
+      const int ex = max(static_cast<int>(top >> 10), 1);  // scales are below 2^(ex - 14)
+      const float down = power2(14 - ex);
+      // hi is a weight rounded to fp16, lo what the rounding left: the two are off by 2^-22 of it,
+      // or by 2^-25, where that is more, which is 2^-36 of the largest there can be.  That is what
+      // kAbove is for: relative to the largest score itself, keys that one outweighs by 2^25 would
+      // be lost, however many they are.
+      uint32_t hi[2][2], lo[2][2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 sm = __half22float2(as_h2(p[j]));
+        const float s = sm.x * down;
+        low[c][0] = fmaf(pr[j][0], sm.y, low[c][0]);
+        low[c][1] = fmaf(pr[j][1], sm.y, low[c][1]);
+        const float w0 = pr[j][0] * s, w1 = pr[j][1] * s;
+        const __half2 w = __floats2half2_rn(w0, w1);
+        const float2 back = __half22float2(w);
+        const uint32_t rest = as_u32(__floats2half2_rn(w0 - back.x, w1 - back.y));
+        // key 8 h + g's two columns become column g's two keys
+        hi[j / 2][j & 1] = movmatrix_t(PAIRS && (lane & 2) ? rest : as_u32(w));
+        if constexpr (!PAIRS) lo[j / 2][j & 1] = movmatrix_t(rest);
+      }
+      const float up = power2(10 + ex), up16 = power2(6 + ex);
+      uint4 v[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (HD != 32 || k == 0) v[k] = vin[HD == 32 ? lane : (k * C + c) * 32 + lane];
+#pragma unroll
+      for (int i = 0; i < FR; ++i) {
+        float acc[4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w;
+          if constexpr (HD == 32)
+            w = k ? (i ? v[0].w : v[0].z) : (i ? v[0].y : v[0].x);
+          else
+            w = i == 0 ? v[k].x : i == 1 ? v[k].y : i == 2 ? v[k].z : v[k].w;
+          const uint32_t a0 = w & kLo, a1 = w & kHi, w8 = w >> 8, a2 = w8 & kLo, a3 = w8 & kHi;
+          if (k == 0)
+            mma16816<true>(acc, a0, a1, a2, a3, hi[k]);
+          else
+            mma16816<false>(acc, a0, a1, a2, a3, hi[k]);
+          if constexpr (!PAIRS) mma16816<false>(acc, a0, a1, a2, a3, lo[k]);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          o[c][i][e] = fmaf(acc[e], up, o[c][i][e]);
+          o[c][i][2 + e] = fmaf(acc[2 + e], up16, o[c][i][2 + e]);
+        }
+      }
+    }
+  }
+
+  // The sums over all keys; the output with its share of the smallest values.
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
+#pragma unroll
+        for (int c = 0; c < C; ++c) low[c][e] += __shfl_xor_sync(0xffffffffu, low[c][e], d);
+      }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < FR; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (PAIRS) o[c][i][e] += __shfl_xor_sync(0xffffffffu, o[c][i][e], 2);
+          o[c][i][e] += low[c][e & 1];
+        }
+  }
+};
+
+// A sequence's KV head and up to `wide` of its beams: its tiles are the prefix's, the
+// prompt's and, beam by beam, the generated tokens'.
+struct Task4 {
+  int at;     // the sequence's place
+  int seq, inner;
+  int64_t st;  // first prompt token
+  int len;
+  int tiles;
+};
+__device__ __forceinline__ int tiles_of(int keys) { return keys / kTileKeys + (keys % kTileKeys != 0); }
+__device__ __forceinline__ int head_of(const DecQ4Args& a, int inner) { return inner % a.Hkv; }
+__device__ __forceinline__ int beam_of(const DecQ4Args& a, int inner) { return inner / a.Hkv * a.wide; }  // the first
+__device__ __forceinline__ int beams_of(const DecQ4Args& a, int inner) { return min(a.wide, a.beams - beam_of(a, inner)); }
+__device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int at, int inner) {
+  Task4 t{at, at, inner, 0, 0, 0};
+  if (a.order) {
+    const int4 x = a.order[at];
+    t.seq = x.x, t.st = x.y, t.len = x.z;
+  } else {
+    const int64_t st = a.seq_start[at], end = a.seq_start[at + 1];
+    if (st < 0 || end < st || end > a.T)
+      set_dev_error(a.err, DEVERR_BOUNDS);
+    else
+      t.st = st, t.len = static_cast<int>(end - st);
+  }
+  t.tiles = tiles_of(a.P) + tiles_of(t.len) + beams_of(a, inner) * (a.slot / kTileKeys + 1);
+  return t;
+}
+
+// What a tile is to its task.
+constexpr int kKeys = 63, kGenerated = 64, kAppend = 128, kBeamShift = 8, kFirst = 1 << 12, kLast = 1 << 13;
+template <int HD>
+__device__ __forceinline__ void tile_at(const DecQ4Args& a, const Task4& w, int e, const uint8_t*& tile, int& info) {
+  const int np = tiles_of(a.P), no = tiles_of(w.len), h = head_of(a, w.inner);
+  int64_t block;
+  int n = kTileKeys, flags = 0;
+  if (e < np) {
+    tile = a.pc, block = e;
+    n = min(n, a.P - e * kTileKeys);
+  } else if (e < np + no) {
+    tile = a.oc, block = tile8_first_block(w.st, w.seq) + (e - np);
+    n = min(n, w.len - (e - np) * kTileKeys);
+  } else {
+    const int ng = a.slot / kTileKeys + 1, b = (e - np - no) / ng, j = (e - np - no) % ng;
+    tile = a.gc, block = (static_cast<int64_t>(w.seq) * a.beams + beam_of(a, w.inner) + b) * a.gen_blocks + j;
+    flags = kGenerated | b << kBeamShift;
+    if (j == ng - 1) n = a.slot % kTileKeys + 1, flags |= kAppend;
+  }
+  tile += (block * a.Hkv + h) * tile4_bytes(HD);
+  info = n | flags | (e == 0 ? kFirst : 0) | (e == w.tiles - 1 ? kLast : 0);
+}
+
+// A warp's ring of tiles in shared memory, filled by bulk copies.
+struct __align__(16) Head4 {
+  int seq, inner, info, unused;
+};
+template <int HD, int STAGES>
+struct Ring4 {
+  static constexpr int TB = tile4_bytes(HD);
+  uint8_t* slots;
+  Head4* heads;
+  uint64_t* full;
+  volatile int* abort_flag;
+  int* err;
+  int put, get;
+  uint32_t phases;  // bit s: the phase of slot s's barrier that is waited for next
+  uint32_t busy;    // bit s: a tile is on its way to slot s or there
+
+  // The whole block calls.  smem: SMEM bytes, 128-byte aligned.
+  static constexpr int smem(int warps) { return warps * STAGES * (TB + static_cast<int>(sizeof(Head4)) + 8); }
+  __device__ __forceinline__ void begin(uint8_t* smem, int warps, int* abort_word, int* err_) {
+    const int warp = threadIdx.x >> 5;
+    slots = smem + warp * STAGES * TB;
+    heads = reinterpret_cast<Head4*>(smem + warps * STAGES * TB) + warp * STAGES;
+    full = reinterpret_cast<uint64_t*>(smem + warps * STAGES * (TB + sizeof(Head4))) + warp * STAGES;
+    abort_flag = abort_word;
+    err = err_;
+    put = get = 0;
+    phases = busy = 0;
+    if ((threadIdx.x & 31) == 0)
+      for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1);
+    if (threadIdx.x == 0) *abort_word = 0;
+    fence_mbar_init();
+    __syncthreads();
+  }
+  // All lanes call; the slot must have been used up by every lane before.
+  __device__ __forceinline__ void issue(const uint8_t* tile, int seq, int inner, int info) {
+    if ((threadIdx.x & 31) == 0) {
+      heads[put] = Head4{seq, inner, info, 0};
+      mbar_arrive_expect_tx(&full[put], TB);
+      bulk_copy_g2s(slots + put * TB, tile, TB, &full[put]);
+    }
+    busy |= 1u << put;
+    put = put + 1 == STAGES ? 0 : put + 1;
+  }
+  // The next tile has arrived.  False: a wait ran out somewhere; the warp's copies are then awaited.
+  __device__ __forceinline__ bool wait() {
+    const uint32_t phase = phases >> get & 1;
+    bool ok = mbar_try_wait(&full[get], phase);
+    if (!ok) ok = longer(&full[get], phase, abort_flag, err);
+    if (__all_sync(0xffffffffu, ok)) {
+      phases ^= 1u << get;
+      return true;
+    }
+    volatile int never = 0;
+    for (int i = 0; i < STAGES; ++i)  // a barrier without copies in flight stands at the phase before
+      if (busy >> i & 1) mbar_wait_bounded(&full[i], phases >> i & 1, &never, nullptr, 200000000ull);
+    return false;
+  }
+  static __device__ __noinline__ bool longer(uint64_t* bar, uint32_t phase, volatile int* abort_flag, int* err) {
+    return mbar_wait_bounded(bar, phase, abort_flag, err);
+  }
+  // Every lane is done with the slot.
+  __device__ __forceinline__ void used() {
+    busy &= ~(1u << get);
+    get = get + 1 == STAGES ? 0 : get + 1;
+  }
+  __device__ __forceinline__ uint8_t* slot() const { return slots + get * TB; }
+  __device__ __forceinline__ const Head4& head() const { return heads[get]; }
+};
+
+// Where a task's rows are: the query of the lane's column (null: it has none), the step's key of beam b.
+template <int HD, bool PAIRS>
+__device__ __forceinline__ const __half* query_of(const DecQ4Args& a, int seq, int inner, int beam, int head) {
+  const int b = beam_of(a, inner) + beam;
+  if (head < 0 || beam >= beams_of(a, inner)) return nullptr;
+  return a.qkv + (static_cast<int64_t>(seq) * a.beams + b) * a.ldq + (head_of(a, inner) * a.G + head) * HD;
+}
+template <int HD>
+__device__ __forceinline__ const __half* key_of(const DecQ4Args& a, int seq, int inner, int beam) {
+  const int64_t row = static_cast<int64_t>(seq) * a.beams + beam_of(a, inner) + beam;
+  return a.qkv + row * a.ldq + (a.Hq + head_of(a, inner)) * HD;
+}
+
+// The step's token into the tile in the ring's slot and the cache's.
+template <int HD>
+__device__ __forceinline__ void append(const DecQ4Args& a, const Token4<HD>& token, uint8_t* copy, int seq, int inner, int beam) {
+  const int64_t row = static_cast<int64_t>(seq) * a.beams + beam_of(a, inner) + beam;
+  const int h = head_of(a, inner);
+  const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
+  uint8_t* tile = a.gc + ((row * a.gen_blocks + a.slot / kTileKeys) * a.Hkv + h) * tile4_bytes(HD);
+  if (!token.append(copy, tile, a.slot % kTileKeys, a.held ? a.held + row * 2 * kd + h * HD : nullptr, kd))
+    set_dev_error(a.err, DEVERR_FP16_RANGE);
+  __syncwarp();
+}
+
+// The two columns of a lane: beam and head (-1: none).
+struct Columns4 {
+  int beam[2], head[2];
+  template <bool PAIRS>
+  static __device__ __forceinline__ void of(const DecQ4Args& a, int column, int& beam, int& head) {
+    if (PAIRS) column &= 3;
+    beam = column / a.G;
+    head = beam < a.wide ? column % a.G : -1;
+  }
+};
+
+template <int HD>
+struct Stream4 {
+  static constexpr int NW = 4;                     // warps per CTA
+  static constexpr int STAGES = HD == 128 ? 3 : 4;
+  static constexpr int CTAS = HD == 128 ? 3 : 4;   // per SM
+  static constexpr int SMEM = Ring4<HD, STAGES>::smem(NW);
+  static_assert(CTAS * (SMEM + 1024 + 64) <= 233472, "shared memory per SM");
+};
+
+// Many tasks: a persistent warp per task, the tiles of all its tasks as one stream
+// through its ring.
+template <int HD, bool PAIRS>
+__global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_decode_q4_stream(DecQ4Args a, int64_t n_tasks) {
+  using S = Stream4<HD>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  Ring4<HD, S::STAGES> ring;
+  ring.begin(smem, S::NW, &abort_word, a.err);
   grid_launch_next();
   grid_wait();
-  __shared__ float q[HD], p[kThreads], nk[HD], nv[HD], red[kThreads / 32];
-  const int tid = threadIdx.x, hq = blockIdx.x % a.Hq, h = hq / a.G;
-  const int64_t r = blockIdx.x / a.Hq, seq = r / a.beams;
-  int64_t st = a.seq_start[seq], end = a.seq_start[seq + 1];
-  if (st < 0 || end < st || end > a.T) {
-    if (tid == 0) set_dev_error(a.err, DEVERR_BOUNDS);
-    st = end = 0;
-  }
-  const __half* row = a.qkv + r * a.ldq;
-  // the step's key and value
-  const int64_t unit = (r * a.gen_blocks + a.slot / kTileKeys) * a.Hkv + h;
-  uint8_t* tile = a.gc + unit * tile4_bytes(HD);
-  const int key = a.slot % kTileKeys;
-  bool fine = true;
-  for (int i = tid; i < HD; i += kThreads) {  // (elements 2 i and 2 i + 1 of the key, then the value)
-    const bool value = i >= HD / 2;
-    const int d = 2 * i % HD, c = d / 64;
-    const __half* x = row + (a.Hq + (value ? a.Hkv : 0) + h) * HD;
-    float mn = INFINITY, mx = -INFINITY;
-    for (int j = 64 * c; j < min(HD, 64 * c + 64); ++j) {
-      const float v = __half2float(x[j]);
-      fine = fine && fabsf(v) <= 65504.f;
-      mn = fminf(mn, v);
-      mx = fmaxf(mx, v);
+
+  const int first = blockIdx.x * S::NW + warp;
+  // from a warp's task to its next: every other round of tasks is dealt out backwards, so that
+  // whoever had the longest gets the shortest
+  const int up = 2 * (static_cast<int>(gridDim.x) * S::NW - first) - 1, down = 2 * first + 1;
+  const int up_rows = up / a.inner, up_inner = up % a.inner, down_rows = down / a.inner, down_inner = down % a.inner;
+  bool odd = false;
+
+  // the copies run ahead of the products by the ring's length, over the tasks' borders
+  int64_t pi = first;
+  Task4 pt{0, 0, 0, 0, 0, 0};
+  if (pi < n_tasks) pt = task_of(a, first / a.inner, first % a.inner);
+  int pe = 0;
+  const auto produce = [&] {
+    if (pi >= n_tasks) return;
+    const uint8_t* tile;
+    int info;
+    tile_at<HD>(a, pt, pe, tile, info);
+    ring.issue(tile, pt.seq, pt.inner, info);
+    if (++pe < pt.tiles) return;
+    pe = 0;
+    pi += odd ? down : up;
+    if (pi < n_tasks) {
+      const int inner = pt.inner + (odd ? down_inner : up_inner);
+      const bool carry = inner >= a.inner;
+      pt = task_of(a, pt.at + (odd ? down_rows : up_rows) + carry, inner - (carry ? a.inner : 0));
     }
-    const Group4 gr = group4(mn, mx);
-    const uint32_t w[2] = {*reinterpret_cast<const uint32_t*>(x + d), *reinterpret_cast<const uint32_t*>(x + d)};
-    const uint32_t code = codes4<4>(w, gr) & 255u;
-    float* to = value ? nv : nk;
-    to[d] = fmaf(static_cast<float>(code & 15), gr.s, gr.m);
-    to[d + 1] = fmaf(static_cast<float>(code >> 4), gr.s, gr.m);
-    if (hq % a.G == 0) {
-      tile[value ? tile4_value_at<HD>(key, d) : tile4_key_at<HD>(key, d)] = static_cast<uint8_t>(code);
-      if (d % 64 == 0) *reinterpret_cast<uint32_t*>(tile + tile4_pair_at<HD>(key, value, c)) = gr.pair();
-      if (a.held) {
-        __half* held = a.held + (r * 2 + (value ? 1 : 0)) * a.Hkv * HD + h * HD + d;
-        const __half2 n = __floats2half2_rn(static_cast<float>(code & 15), static_cast<float>(code >> 4));
-        *reinterpret_cast<uint32_t*>(held) = value4(n, __float2half2_rn(gr.s), __float2half2_rn(gr.m));
-      }
-    }
-  }
-  for (int d = tid; d < HD; d += kThreads) q[d] = __half2float(row[hq * HD + d]) * a.scale;
-  __syncthreads();
-  const int64_t P = a.P, len = end - st, all = P + len + a.slot + 1;
-  const auto place = [&](int64_t j, int& k) -> const uint8_t* {
-    if (j < P) {
-      k = static_cast<int>(j % kTileKeys);
-      return a.pc + (j / kTileKeys * a.Hkv + h) * tile4_bytes(HD);
-    }
-    if (j < P + len) {
-      j -= P;
-      k = static_cast<int>(j % kTileKeys);
-      return a.oc + ((tile8_first_block(st, seq) + j / kTileKeys) * a.Hkv + h) * tile4_bytes(HD);
-    }
-    j -= P + len;
-    k = static_cast<int>(j % kTileKeys);
-    return a.gc + ((r * a.gen_blocks + j / kTileKeys) * a.Hkv + h) * tile4_bytes(HD);
+    odd = !odd;
   };
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int64_t base = 0; base < all; base += kThreads) {
-    const int64_t j = base + tid;
-    float z = -INFINITY;
-    int k = 0;
-    if (j == all - 1) {
-      z = 0.f;
-      for (int d = 0; d < HD; ++d) z = fmaf(q[d], nk[d], z);
-    } else if (j < all) {
-      const uint8_t* t = place(j, k);
-      z = 0.f;
-      for (int d = 0; d < HD; ++d) z = fmaf(q[d], element4<HD>(t, k, d, false), z);
+#pragma unroll 1
+  for (int i = 0; i < S::STAGES; ++i) produce();
+
+  using At = Attn4<HD, PAIRS>;
+  At at;
+  int my_beam, my_head, beam[2], head[2];
+  Columns4::of<PAIRS>(a, g, my_beam, my_head);
+  Columns4::of<PAIRS>(a, 2 * t, beam[0], head[0]);
+  Columns4::of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
+  const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
+  uint4 raw[At::NQ];
+  Token4<HD> token;
+  const auto fetch = [&](const Head4& x) {
+    At::fetch(raw, query_of<HD, PAIRS>(a, x.seq, x.inner, my_beam, my_head));
+    token.load(key_of<HD>(a, x.seq, x.inner, 0), kd);
+  };
+  __syncwarp();  // the heads that lane 0 wrote
+  if (ring.busy) fetch(ring.head());
+  while (ring.busy) {
+    if (!ring.wait()) return;
+    const Head4 x = ring.head();
+    const int info = x.info, n = info & kKeys, b = info >> kBeamShift & 15;
+    if (info & kFirst) at.begin(raw, a.scale_log2);
+    if (info & kAppend) {
+      append<HD>(a, token, ring.slot(), x.seq, x.inner, b);
+      if (!(info & kLast)) token.load(key_of<HD>(a, x.seq, x.inner, b + 1), kd);
     }
-    float top = z;
-    for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-    if (tid % 32 == 0) red[tid / 32] = top;
-    __syncthreads();
-    for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, red[w]);
-    top = fmaxf(top, m);
-    const float f = expf(m - top);
-    m = top;
-    p[tid] = expf(z - m);
-    float lc = 0.f, oc = 0.f;  // (128 at a time: added one by one, many light keys would be rounded away)
-    __syncthreads();
-    const int n = static_cast<int>(all - base < kThreads ? all - base : kThreads);
-    for (int i = 0; i < n; ++i) {
-      lc += p[i];
-      if (tid >= HD) continue;
-      if (base + i == all - 1)
-        oc = fmaf(p[i], nv[tid], oc);
-      else {
-        const uint8_t* t = place(base + i, k);
-        oc = fmaf(p[i], element4<HD>(t, k, tid, true), oc);
+    if (info & kLast) {  // the next task's queries are on their way while this one ends
+      const int after = ring.get + 1 == S::STAGES ? 0 : ring.get + 1;
+      if (ring.busy >> after & 1) fetch(ring.heads[after]);
+    }
+    const bool all = !(info & kGenerated);
+    at.tile(ring.slot(), n, all || beam[0] == b, all || beam[1] == b);
+    ring.used();
+    if (info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
+    __syncwarp();  // every lane is done with the slot before it is refilled
+    produce();
+    if (!(info & kLast)) continue;
+    at.finish();
+    bool fine = true;
+    const auto store = [&](int beam, int head, bool odd, float l) {
+      if (head < 0 || beam >= beams_of(a, x.inner)) return;
+      const float inv = 1.f / l;
+      const int64_t row = static_cast<int64_t>(x.seq) * a.beams + beam_of(a, x.inner) + beam;
+      __half* to = a.out + (row * a.Hq + head_of(a, x.inner) * a.G + head) * HD + 2 * At::FR * g;
+#pragma unroll
+      for (int c = 0; c < At::C; ++c) {
+        uint32_t v[At::FR];
+#pragma unroll
+        for (int i = 0; i < At::FR; ++i) {
+          const float x0 = (odd ? at.o[c][i][1] : at.o[c][i][0]) * inv, x1 = (odd ? at.o[c][i][3] : at.o[c][i][2]) * inv;
+          fine = fine && fabsf(x0) <= 65504.f && fabsf(x1) <= 65504.f;
+          v[i] = as_u32(__floats2half2_rn(x0, x1));
+        }
+        if constexpr (HD == 32)
+          *reinterpret_cast<uint2*>(to) = make_uint2(v[0], v[1]);
+        else
+          *reinterpret_cast<uint4*>(to + 64 * c) = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    };
+    if constexpr (PAIRS) {  // two lanes have the same two columns
+      const bool odd = t >> 1;
+      store(odd ? beam[1] : beam[0], odd ? head[1] : head[0], odd, odd ? at.l[1] : at.l[0]);
+    } else {
+      store(beam[0], head[0], false, at.l[0]);
+      store(beam[1], head[1], true, at.l[1]);
+    }
+    if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+  }
+}
+
+// ------------------------------------------- few tasks: a CTA or more per task
+// The tiles of a task are cut into ranges, a CTA each, whose warps take a range's tiles
+// in turns; they merge their (maximum, sum, output) in shared memory.  The ranges' are
+// merged, in their order, by the task's CTA that comes last.
+//
+// An inner task (KV head, beams) has `units` CTAs, at least one a sequence, the others
+// shared out by the sequences' lengths, which only the device knows: sequence i's are
+// share(i) .. share(i + 1) - 1.
+constexpr int kMaxRanges = 512;  // of a task
+template <int HD>
+struct Split4 {
+  static constexpr int NW = 4;
+  static constexpr int STAGES = Stream4<HD>::STAGES;
+  static constexpr int CTAS = Stream4<HD>::CTAS;
+  static constexpr int MERGE = NW * 8 * (HD + 2) * 4;  // the merge reuses the ring
+  static constexpr int SMEM = std::max(Ring4<HD, STAGES>::smem(NW), std::max(MERGE, NW * kMaxRanges * 4));
+};
+__device__ __forceinline__ int64_t share(const DecQ4Args& a, int64_t S, int64_t units, int64_t i) {
+  // own keys before sequence i, and something for each one's start, prefix and generated tokens
+  const int64_t more = static_cast<int64_t>(a.P) + a.slot * static_cast<int64_t>(a.wide) + 48, none = a.seq_start[0];
+  const int64_t before = a.seq_start[i] - none + i * more, all = a.seq_start[S] - none + S * more;
+  return i + (units - S) * before / (all > 0 ? all : 1);
+}
+
+template <int HD, bool PAIRS>
+__global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
+    k_decode_q4_split(DecQ4Args a, int n_seqs, int units, float* partial, unsigned int* arrived) {
+  using S = Split4<HD>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int abort_word, last;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  Ring4<HD, S::STAGES> ring;
+  ring.begin(smem, S::NW, &abort_word, a.err);
+  grid_launch_next();
+  grid_wait();
+
+  const int inner = blockIdx.x % a.inner, unit = blockIdx.x / a.inner;
+  int64_t seq = unit, first = unit;
+  int ranges = 1;
+  if (units > n_seqs) {
+    // the last sequence whose share begins at `unit` or before, 32 probes at a time
+    int64_t lo = 0, hi = n_seqs;
+    while (hi - lo > 1) {
+      const int64_t step = (hi - lo + 31) / 32, x = lo + lane * step;
+      const uint32_t found = __ballot_sync(0xffffffffu, x < hi && share(a, n_seqs, units, x) <= unit);
+      if (found) lo += (31 - __clz(found)) * step;
+      hi = lo + step < hi ? lo + step : hi;
+    }
+    seq = lo;
+    first = share(a, n_seqs, units, seq);
+    // where the starts do not ascend (below), anything within bounds will do
+    ranges = static_cast<int>(min(max(share(a, n_seqs, units, seq + 1) - first, int64_t(1)),
+                                  static_cast<int64_t>(min(units, kMaxRanges))));
+    first = min(max(first, int64_t(0)), static_cast<int64_t>(units - ranges));
+    // a sequence may then have no CTA, which would have reported it
+    if (blockIdx.x == 0)
+      for (int k = threadIdx.x; k < n_seqs; k += S::NW * 32)
+        if (a.seq_start[k + 1] < a.seq_start[k]) set_dev_error(a.err, DEVERR_BOUNDS);
+  }
+  const int range = static_cast<int>(min(max(unit - first, int64_t(0)), static_cast<int64_t>(ranges - 1)));
+  const int64_t task = seq * a.inner + inner;
+  const Task4 w = task_of(a, static_cast<int>(seq), inner);
+  const int e0 = static_cast<int>(static_cast<int64_t>(w.tiles) * range / ranges);
+  const int e1 = static_cast<int>(static_cast<int64_t>(w.tiles) * (range + 1) / ranges);
+  int e = e0 + warp, pe = e;
+  const auto produce = [&] {
+    if (pe >= e1) return;
+    const uint8_t* tile;
+    int info;
+    tile_at<HD>(a, w, pe, tile, info);
+    ring.issue(tile, w.seq, inner, info);
+    pe += S::NW;
+  };
+#pragma unroll 1
+  for (int k = 0; k < S::STAGES; ++k) produce();
+  using At = Attn4<HD, PAIRS>;
+  At at;
+  int my_beam, my_head, beam[2], head[2];
+  Columns4::of<PAIRS>(a, g, my_beam, my_head);
+  Columns4::of<PAIRS>(a, 2 * t, beam[0], head[0]);
+  Columns4::of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
+  {
+    uint4 raw[At::NQ];
+    At::fetch(raw, query_of<HD, PAIRS>(a, w.seq, inner, my_beam, my_head));
+    at.begin(raw, a.scale_log2);
+  }
+  const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
+  for (; e < e1; e += S::NW) {
+    if (!ring.wait()) break;
+    const int info = ring.head().info, b = info >> kBeamShift & 15;
+    if (info & kAppend) {
+      Token4<HD> token;
+      token.load(key_of<HD>(a, w.seq, inner, b), kd);
+      append<HD>(a, token, ring.slot(), w.seq, inner, b);
+    }
+    const bool all = !(info & kGenerated);
+    at.tile(ring.slot(), info & kKeys, all || beam[0] == b, all || beam[1] == b);
+    ring.used();
+    if (info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
+    __syncwarp();
+    produce();
+  }
+  at.finish();
+  // merge the warps (a wait that ran out leaves wrong numbers and an error)
+  __syncthreads();
+  float* sm = reinterpret_cast<float*>(smem);  // [NW][8] maxima, [NW][8] sums, [NW][8][HD]
+  float* sl = sm + S::NW * 8;
+  float* so = sl + S::NW * 8;
+  if (g == 0) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      sm[warp * 8 + 2 * t + j] = at.m[j];
+      sl[warp * 8 + 2 * t + j] = at.l[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int c = 0; c < At::C; ++c) {
+      float2* dst = reinterpret_cast<float2*>(so + (warp * 8 + 2 * t + j) * HD + 64 * c + 2 * At::FR * g);
+#pragma unroll
+      for (int i = 0; i < At::FR; ++i) dst[i] = make_float2(at.o[c][i][j], at.o[c][i][2 + j]);
+    }
+  __syncthreads();
+  const int columns = beams_of(a, inner) * a.G;
+  const auto row_of = [&](int column) {
+    const int64_t row = static_cast<int64_t>(w.seq) * a.beams + beam_of(a, inner) + column / a.G;
+    return a.out + (row * a.Hq + head_of(a, inner) * a.G + column % a.G) * HD;
+  };
+  // [inner][unit]: maxima, sums, outputs of up to eight columns
+  const int most = a.wide * a.G, size = most * (HD + 2);
+  float* mine = partial + (static_cast<int64_t>(inner) * units + unit) * size;
+  for (int k = threadIdx.x; k < columns * HD; k += S::NW * 32) {
+    const int column = k / HD;
+    float M = At::kLow, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int j = 0; j < S::NW; ++j) M = fmaxf(M, sm[j * 8 + column]);
+#pragma unroll
+    for (int j = 0; j < S::NW; ++j) {
+      const float f = exp2_approx(sm[j * 8 + column] - M);  // 0 for a warp without tiles
+      L += sl[j * 8 + column] * f;
+      O += so[j * 8 * HD + k] * f;
+    }
+    if (ranges == 1) {
+      const float v = O / L;
+      if (!(fabsf(v) <= 65504.f)) set_dev_error(a.err, DEVERR_FP16_RANGE);
+      row_of(column)[k % HD] = __float2half_rn(v);
+    } else {
+      mine[2 * most + k] = O;
+      if (k % HD == 0) {
+        mine[column] = M;
+        mine[most + column] = L;
       }
     }
-    l = fmaf(l, f, lc);
-    o = fmaf(o, f, oc);
-    __syncthreads();
   }
-  if (tid < HD) {
-    const float v = o / l;
-    fine = fine && fabsf(v) <= 65504.f;
-    a.out[(r * a.Hq + hq) * HD + tid] = __float2half_rn(v);
+  if (ranges == 1) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(&arrived[task], 1u) == static_cast<unsigned>(ranges) - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  if (threadIdx.x == 0) arrived[task] = 0;  // for the next launch
+  // a warp per column: the ranges' weights, then the weighted sums
+  const float* p = partial + (static_cast<int64_t>(inner) * units + first) * size;
+  float* weight = sm + warp * kMaxRanges;  // (nobody reads the warps' states any more)
+  for (int column = warp; column < columns; column += S::NW) {
+    float M = At::kLow, L = 0.f;
+    for (int j = lane; j < ranges; j += 32) M = fmaxf(M, __ldcg(p + j * size + column));
+#pragma unroll
+    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+    for (int j = lane; j < ranges; j += 32) {
+      const float f = exp2_approx(__ldcg(p + j * size + column) - M);  // 0 for a range without tiles
+      weight[j] = f;
+      L += __ldcg(p + j * size + most + column) * f;
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+    __syncwarp();
+    float O[HD / 32];
+#pragma unroll
+    for (int k = 0; k < HD / 32; ++k) O[k] = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < ranges; ++j)
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k)
+        O[k] = fmaf(__ldcg(p + j * size + 2 * most + column * HD + 32 * k + lane), weight[j], O[k]);
+    bool fine = true;
+#pragma unroll
+    for (int k = 0; k < HD / 32; ++k) {
+      const float v = O[k] / L;
+      fine = fine && fabsf(v) <= 65504.f;
+      row_of(column)[32 * k + lane] = __float2half_rn(v);
+    }
+    if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+    __syncwarp();
   }
-  if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+}
+
+// How a call runs: beams of a task, tasks of a sequence, and CTAs per inner task (at
+// least one a sequence; 0: a warp per task).
+struct Plan {
+  int wide, inner, units;
+  int64_t seqs;
+  double tiles;  // of an inner task, over all sequences
+};
+template <int HD>
+int units_of(const Plan& p, int num_sms) {
+  using S = Stream4<HD>;
+  const int64_t ctas = static_cast<int64_t>(num_sms) * S::CTAS, tasks = p.seqs * p.inner;
+  if ((p.tiles + 0.5 * p.seqs) * ctas <= 2.25 * p.seqs * tasks) return 0;
+  if (tasks > kSplitTasksMax) return static_cast<int>(p.seqs);
+  const int64_t most = static_cast<int64_t>(p.tiles / (4 * Split4<HD>::NW));
+  return static_cast<int>(std::max<int64_t>(p.seqs, std::min<int64_t>({ctas / p.inner, most, p.seqs + kMaxRanges - 1})));
+}
+Plan plan_of(const DecodeQ4& d, int num_sms) {
+  Plan p;
+  const int G = d.Hq / d.Hkv;
+  p.wide = std::min(d.beams, 8 / G);
+  p.inner = d.Hkv * ((d.beams + p.wide - 1) / p.wide);
+  p.seqs = d.R / d.beams;
+  p.tiles = d.T / 32.0 + 0.5 * p.seqs + static_cast<double>(p.seqs) * (d.P / 32 + p.wide * (d.slot / 32 + 1));
+  p.units = d.hd == 32 ? units_of<32>(p, num_sms) : d.hd == 64 ? units_of<64>(p, num_sms) : units_of<128>(p, num_sms);
+  return p;
+}
+
+template <int HD, bool PAIRS>
+int launch_pairs(const DecQ4Args& a, const Plan& p, float* partial, unsigned int* arrived, int num_sms, cudaStream_t s) {
+  if (p.units == 0) {
+    using S = Stream4<HD>;
+    const cudaError_t e = cudaFuncSetAttribute(k_decode_q4_stream<HD, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e != cudaSuccess) return e;
+    return launch_chained(k_decode_q4_stream<HD, PAIRS>, dim3(static_cast<unsigned>(num_sms * S::CTAS)), S::NW * 32, S::SMEM, s, 1,
+                          a, p.seqs * p.inner);
+  }
+  using S = Split4<HD>;
+  const cudaError_t e = cudaFuncSetAttribute(k_decode_q4_split<HD, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+  if (e != cudaSuccess) return e;
+  return launch_chained(k_decode_q4_split<HD, PAIRS>, dim3(static_cast<unsigned>(p.units) * a.inner), S::NW * 32, S::SMEM, s, 1, a,
+                        static_cast<int>(p.seqs), p.units, partial, arrived);
 }
 
 }  // namespace
 
-int launch_decode_attention_q4(const DecodeQ4& d, int* err, cudaStream_t s) {
+size_t decode_q4_floats(const DecodeQ4& d, int num_sms) {
   if (d.R <= 0) return 0;
-  const DecQ4Args a{d.qkv, d.ldq, d.Hq, d.Hkv, d.Hq / d.Hkv, d.beams, d.prefix, d.P, d.own, d.T, d.seq_start, d.gen,
-                    (d.gen_cap + kTileKeys - 1) / kTileKeys, d.slot, 1.f / sqrtf(static_cast<float>(d.hd)), d.out, d.held, err};
-  const dim3 grid(static_cast<unsigned>(d.R) * d.Hq);
+  const Plan p = plan_of(d, num_sms);
+  return p.units <= p.seqs ? 0 : static_cast<size_t>(p.units) * p.inner * p.wide * (d.Hq / d.Hkv) * (d.hd + 2);
+}
+
+int decode_q4_order_seqs(const DecodeQ4& d, bool once, int num_sms) {
+  (void)once;
+  if (d.R <= 0 || plan_of(d, num_sms).units != 0) return 0;
+  return 0;
+}
+
+int launch_decode_attention_q4(const DecodeQ4& d, float* partial, unsigned int* arrived, int* err, int num_sms,
+                               cudaStream_t s) {
+  if (d.R <= 0) return 0;
+  const Plan p = plan_of(d, num_sms);
+  const DecQ4Args a{d.qkv, d.ldq, d.Hq, d.Hkv, d.Hq / d.Hkv, d.beams, p.wide, p.inner, d.prefix, d.P, d.own, d.T, d.seq_start,
+                    d.gen, (d.gen_cap + kTileKeys - 1) / kTileKeys, d.slot,
+                    1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, d.held, err, p.units ? nullptr : d.order};
+  const bool pairs = p.wide * a.G <= 4;
   switch (d.hd) {
-    case 32: return launch_chained(k_decode_q4<32>, grid, kThreads, 0, s, 1, a);
-    case 64: return launch_chained(k_decode_q4<64>, grid, kThreads, 0, s, 1, a);
-    case 128: return launch_chained(k_decode_q4<128>, grid, kThreads, 0, s, 1, a);
+    case 32: return (pairs ? launch_pairs<32, true> : launch_pairs<32, false>)(a, p, partial, arrived, num_sms, s);
+    case 64: return (pairs ? launch_pairs<64, true> : launch_pairs<64, false>)(a, p, partial, arrived, num_sms, s);
+    case 128: return (pairs ? launch_pairs<128, true> : launch_pairs<128, false>)(a, p, partial, arrived, num_sms, s);
     default: return cudaErrorInvalidValue;
   }
 }

@@ -339,8 +339,13 @@ struct DecodeQ4 {
   int gen_cap, slot;
   __half* out;
   __half* held;  // [R][2 Hkv hd] the step's key and value as the cache holds them, or null
+  const int4* order;  // of the sequences, as launch_decode_q8_order writes it, or null
 };
-int launch_decode_attention_q4(const DecodeQ4& d, int* err, cudaStream_t s);
+// As decode_q8_floats, decode_q8_order_rows (sequences here) and launch_decode_attention_q8.
+size_t decode_q4_floats(const DecodeQ4& d, int num_sms);
+int decode_q4_order_seqs(const DecodeQ4& d, bool once, int num_sms);
+int launch_decode_attention_q4(const DecodeQ4& d, float* partial, unsigned int* arrived, int* err, int num_sms,
+                               cudaStream_t s);
 
 // ----------------------------------------------------------- beam search ---
 constexpr int kBeamsMax = 16;

@@ -92,8 +92,9 @@ __device__ __forceinline__ __half2 extent4(const uint32_t* x) {
     mn = __hmin2_nan(mn, as_h2(x[i]));
     mx = __hmax2_nan(mx, as_h2(x[i]));
   }
-  mx = __hneg2(mx);
-  return __hmin2_nan(__lows2half2(mn, mx), __highs2half2(mn, mx));
+  // (the larger ones' signs turned by hand: of one word alone, __hneg2 left them as they were)
+  const uint32_t neg = as_u32(mx) ^ 0x80008000u;
+  return __hmin2_nan(as_h2(__byte_perm(as_u32(mn), neg, 0x5410)), as_h2(__byte_perm(as_u32(mn), neg, 0x7632)));
 }
 __device__ __forceinline__ Group4 group4(__half2 extent) { return group4(__low2float(extent), -__high2float(extent)); }
 
