@@ -71,6 +71,14 @@ template <int HD>
 struct Token4 {
   static constexpr int E = HD / 16;
   uint32_t x[E / 2];
+  int at, step, pair_at;  // where a tile takes them: a byte for two, `step` apart; the pair, or -1
+  __device__ __forceinline__ void place(int key) {
+    const int lane = threadIdx.x & 31, d = (lane & 15) * E;
+    const bool value = lane & 16;
+    at = value ? tile4_value_at<HD>(key, d) : tile4_key_at<HD>(key, d);
+    step = value ? 4 : 1;
+    pair_at = d % 64 == 0 ? tile4_pair_at<HD>(key, value, d / 64) : -1;
+  }
   __device__ __forceinline__ void load(const __half* key, int64_t to_value) {
     const int lane = threadIdx.x & 31;
     const __half* from = key + (lane & 16 ? to_value : 0) + (lane & 15) * E;
@@ -84,27 +92,20 @@ struct Token4 {
       x[0] = *reinterpret_cast<const uint32_t*>(from);
     }
   }
-  // Into token `key` of a tile: the copy in shared memory and the cache's own.  held: the
-  // row's keys of this head, or null.  False: an element is not finite.
-  __device__ __forceinline__ bool append(uint8_t* copy, uint8_t* tile, int key, __half* held, int64_t to_value) const {
-    const int lane = threadIdx.x & 31, d = (lane & 15) * E, c = d / 64;
-    const bool value = lane & 16;
+  // Into a tile: the copy in shared memory and the cache's own.  held: the row's keys of
+  // this head, or null.  False: an element is not finite.
+  __device__ __forceinline__ bool append(uint8_t* copy, uint8_t* tile, __half* held, int64_t to_value) const {
+    const int lane = threadIdx.x & 31;
     __half2 e = extent4<E / 2>(x);
 #pragma unroll
     for (int s = 1; s < (HD == 128 ? 8 : 16); s <<= 1) e = __hmin2_nan(e, as_h2(__shfl_xor_sync(0xffffffffu, as_u32(e), s)));
     const Group4 g = group4(e);
     const uint32_t code = codes4<E>(x, g), pair = g.pair();
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const int at = value ? tile4_value_at<HD>(key, d + 2 * i) : tile4_key_at<HD>(key, d + 2 * i);
-      copy[at] = tile[at] = static_cast<uint8_t>(code >> (8 * i));
-    }
-    if (d % 64 == 0) {
-      const int at = tile4_pair_at<HD>(key, value, c);
-      *reinterpret_cast<uint32_t*>(copy + at) = *reinterpret_cast<uint32_t*>(tile + at) = pair;
-    }
+    for (int i = 0; i < E / 2; ++i) copy[at + i * step] = tile[at + i * step] = static_cast<uint8_t>(code >> (8 * i));
+    if (pair_at >= 0) *reinterpret_cast<uint32_t*>(copy + pair_at) = *reinterpret_cast<uint32_t*>(tile + pair_at) = pair;
     if (held) {
-      uint32_t* to = reinterpret_cast<uint32_t*>(held + (value ? to_value : 0) + d);
+      uint32_t* to = reinterpret_cast<uint32_t*>(held + (lane & 16 ? to_value : 0) + (lane & 15) * E);
 #pragma unroll
       for (int i = 0; i < E / 2; ++i) to[i] = byte4(code, i, pair);
     }
@@ -204,21 +205,24 @@ struct Attn4 {
     l[0] = l[1] = 0.f;
   }
 
-  // One tile: n keys (1 .. 32); see0, see1: whether columns 2 t and 2 t + 1 attend it.
-  __device__ __forceinline__ void tile(const uint8_t* tile, int n, bool see0, bool see1) {
+  // One tile: n keys (1 .. 32); mine0, mine1: whether columns 2 t and 2 t + 1 attend it, `some`: whether
+  // that need be looked at.
+  __device__ __forceinline__ void tile(const uint8_t* tile, int n, bool some, bool mine0, bool mine1) {
     const int lane = threadIdx.x & 31, g = lane >> 2;
+    const bool second = PAIRS && (lane & 2);
     const uint4* kin = reinterpret_cast<const uint4*>(tile);
     const uint4* vin = reinterpret_cast<const uint4*>(tile + kTileKeys * HD / 2);
     const uint4* pairs = reinterpret_cast<const uint4*>(tile + tile4_pairs(HD));
     constexpr uint32_t kLo = 0x000f000fu, kHi = 0x00f000f0u;
-    float sc[2][4];
+    // Scores of keys 16 k + 8 h + g ([k][2 h + column]).  With PAIRS a column's numbers are in two lanes:
+    // one takes keys 0 .. 15 of the tile on, the other 16 .. 31.
+    constexpr int K = PAIRS ? 1 : 2;
+    float sc[K][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const uint4 kp = pairs[16 * c + g];
-      const uint32_t p[4] = {kp.x, kp.y, kp.z, kp.w};
+      float acc[2][4];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {  // keys 16 k + g and + 8
-        float acc[4];
+      for (int k = 0; k < 2; ++k) {
         const uint4 v = kin[HD == 32 ? lane : (k * C + c) * 32 + lane];
         uint32_t a[FR / 2], b[FR / 2];
         if constexpr (HD == 32) {
@@ -230,53 +234,66 @@ struct Attn4 {
         for (int w = 0; w < FR / 2; ++w) {
           const uint32_t(&q0)[2] = q[c * FR + 2 * w];
           if (w == 0)
-            mma16816<true>(acc, a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
+            mma16816<true>(acc[k], a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
           else
-            mma16816<false>(acc, a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
+            mma16816<false>(acc[k], a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
           const uint32_t a8 = a[w] >> 8, b8 = b[w] >> 8;
-          mma16816<false>(acc, a8 & kLo, b8 & kLo, a8 & kHi, b8 & kHi, q[c * FR + 2 * w + 1]);
+          mma16816<false>(acc[k], a8 & kLo, b8 & kLo, a8 & kHi, b8 & kHi, q[c * FR + 2 * w + 1]);
         }
+      }
+      const uint4 kp = pairs[16 * c + g];
+      const uint32_t p[4] = {second ? kp.z : kp.x, second ? kp.w : kp.y, kp.z, kp.w};
+#pragma unroll
+      for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float2 sm = __half22float2(as_h2(p[2 * k + h]));
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
+            const float x = second ? acc[1][2 * h + e] : acc[k][2 * h + e];
             const float base = c ? fmaf(sm.y, sum[c][e], sc[k][2 * h + e]) : sm.y * sum[c][e];
-            sc[k][2 * h + e] = fmaf(sm.x, acc[2 * h + e], base);
+            sc[k][2 * h + e] = fmaf(sm.x, x, base);
           }
         }
-      }
     }
+    const int from = second ? 16 + g : g;  // the lane's first key
     if (n < kTileKeys) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (16 * k + 8 * (e / 2) + g >= n) sc[k][e] = -INFINITY;
+          if (16 * k + 8 * (e / 2) + from >= n) sc[k][e] = -INFINITY;
     }
-    if (!see0) sc[0][0] = sc[0][2] = sc[1][0] = sc[1][2] = -INFINITY;
-    if (!see1) sc[0][1] = sc[0][3] = sc[1][1] = sc[1][3] = -INFINITY;
+    if (some) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (!mine0) sc[k][2 * h] = -INFINITY;
+          if (!mine1) sc[k][2 * h + 1] = -INFINITY;
+        }
+    }
 
     // Probabilities relative to m, which lies kAbove to kAbove + kLag below the largest score so
     // far: it follows, and the output is scaled down, only where that would come to lie higher,
     // so that the running output need not be touched for most tiles.
     float mb[2], by[2] = {scale[0], scale[1]};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e])) * by[e];
+    for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[K - 1][e], sc[K - 1][2 + e])) * by[e];
     if (fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f) {
       // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
       // score that is not rounded (in the fma below) could lie so far above a rounded m that
       // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
       // most, and the largest probability stays between 1 and 2^15 whatever the last place.
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sc[k][e] *= by[e & 1];
       by[0] = by[1] = 1.f;
     }
     if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag))) {
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) {
+      for (int d = PAIRS ? 2 : 4; d < 32; d <<= 1) {
         mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
         mb[1] = fmaxf(mb[1], __shfl_xor_sync(0xffffffffu, mb[1], d));
       }
@@ -293,9 +310,9 @@ struct Attn4 {
         }
       }
     }
-    float pr[4][2];  // of keys 8 j + g
+    float pr[2 * K][2];  // of keys 16 k + 8 h + g: [2 k + h]
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2 * K; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         pr[j][e] = exp2_approx(fmaf(sc[j / 2][2 * (j & 1) + e], by[e], -m[e]));
@@ -304,16 +321,19 @@ struct Attn4 {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const uint4 vp = pairs[16 * c + 8 + g];
-      uint32_t p[4] = {vp.x, vp.y, vp.z, vp.w};
+      uint32_t p[2 * K];
+      p[0] = second ? vp.z : vp.x, p[1] = second ? vp.w : vp.y;
+      if constexpr (!PAIRS) p[2] = vp.z, p[3] = vp.w;
       if (n < kTileKeys) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (8 * j + g >= n) p[j] = 0u;  // 0 times anything may be NaN
+        for (int j = 0; j < 2 * K; ++j)
+          if (8 * j + from >= n) p[j] = 0u;  // 0 times anything may be NaN
       }
       // A weight p s is at most p where the scales are brought below 1 by the power of two that
       // the tile's largest asks for; a probability is at most 2^15.25, within fp16.
-      const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(p[0] & 0xffffu, p[1] & 0xffffu), max(p[2] & 0xffffu, p[3] & 0xffffu)));
-      const int ex = max(static_cast<int>(top >> 10), 1);  // scales are below 2^(ex - 14)
+      uint32_t top = as_u32(__hmax2(as_h2(p[0]), as_h2(p[1])));
+      if constexpr (!PAIRS) top = as_u32(__hmax2(as_h2(top), __hmax2(as_h2(p[2]), as_h2(p[3]))));
+      const int ex = max(static_cast<int>(__reduce_max_sync(0xffffffffu, top & 0xffffu) >> 10), 1);  // scales are below 2^(ex - 14)
       const float down = power2(14 - ex);
       // hi is a weight rounded to fp16, lo what the rounding left: the two are off by 2^-22 of it,
       // or by 2^-25, where that is more, which is 2^-36 of the largest there can be.  That is what
@@ -321,7 +341,7 @@ struct Attn4 {
       // be lost, however many they are.
       uint32_t hi[2][2], lo[2][2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 2 * K; ++j) {
         const float2 sm = __half22float2(as_h2(p[j]));
         const float s = sm.x * down;
         low[c][0] = fmaf(pr[j][0], sm.y, low[c][0]);
@@ -329,10 +349,17 @@ struct Attn4 {
         const float w0 = pr[j][0] * s, w1 = pr[j][1] * s;
         const __half2 w = __floats2half2_rn(w0, w1);
         const float2 back = __half22float2(w);
-        const uint32_t rest = as_u32(__floats2half2_rn(w0 - back.x, w1 - back.y));
+        const uint32_t whole = as_u32(w), rest = as_u32(__floats2half2_rn(w0 - back.x, w1 - back.y));
         // key 8 h + g's two columns become column g's two keys
-        hi[j / 2][j & 1] = movmatrix_t(PAIRS && (lane & 2) ? rest : as_u32(w));
-        if constexpr (!PAIRS) lo[j / 2][j & 1] = movmatrix_t(rest);
+        if constexpr (PAIRS) {
+          // the first lane's keys 0 .. 15 with their rests in the second, whose 16 .. 31 it gets
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, second ? whole : rest, 2);
+          hi[0][j] = movmatrix_t(second ? other : whole);
+          hi[1][j] = movmatrix_t(second ? rest : other);
+        } else {
+          hi[j / 2][j & 1] = movmatrix_t(whole);
+          lo[j / 2][j & 1] = movmatrix_t(rest);
+        }
       }
       const float up = power2(10 + ex), up16 = power2(6 + ex);
       uint4 v[2];
@@ -368,7 +395,7 @@ struct Attn4 {
   // The sums over all keys; the output with its share of the smallest values.
   __device__ __forceinline__ void finish() {
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1)
+    for (int d = PAIRS ? 2 : 4; d < 32; d <<= 1)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
@@ -390,18 +417,16 @@ struct Attn4 {
 // A sequence's KV head and up to `wide` of its beams: its tiles are the prefix's, the
 // prompt's and, beam by beam, the generated tokens'.
 struct Task4 {
-  int at;     // the sequence's place
-  int seq, inner;
-  int64_t st;  // first prompt token
-  int len;
-  int tiles;
+  int at;        // the sequence's place
+  int inner;     // KV head + Hkv * (the first beam / wide)
+  int seq, len;
+  int64_t st;    // first prompt token
+  int h, beams;  // KV head, number of beams
+  int row;       // the first beam's
 };
 __device__ __forceinline__ int tiles_of(int keys) { return keys / kTileKeys + (keys % kTileKeys != 0); }
-__device__ __forceinline__ int head_of(const DecQ4Args& a, int inner) { return inner % a.Hkv; }
-__device__ __forceinline__ int beam_of(const DecQ4Args& a, int inner) { return inner / a.Hkv * a.wide; }  // the first
-__device__ __forceinline__ int beams_of(const DecQ4Args& a, int inner) { return min(a.wide, a.beams - beam_of(a, inner)); }
 __device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int at, int inner) {
-  Task4 t{at, at, inner, 0, 0, 0};
+  Task4 t{at, inner, at, 0, 0, inner, a.beams, 0};
   if (a.order) {
     const int4 x = a.order[at];
     t.seq = x.x, t.st = x.y, t.len = x.z;
@@ -412,36 +437,23 @@ __device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int at, int inner) 
     else
       t.st = st, t.len = static_cast<int>(end - st);
   }
-  t.tiles = tiles_of(a.P) + tiles_of(t.len) + beams_of(a, inner) * (a.slot / kTileKeys + 1);
+  t.row = t.seq * a.beams;
+  if (a.wide < a.beams) {
+    const int before = inner / a.Hkv * a.wide;
+    t.h = inner % a.Hkv;
+    t.row += before;
+    t.beams = min(a.wide, a.beams - before);
+  }
   return t;
 }
 
-// What a tile is to its task.
+// What a tile is to its task: its number of keys, whether they are generated ones, and of
+// which beam; whether the step's token goes into it; the task's first and last.
 constexpr int kKeys = 63, kGenerated = 64, kAppend = 128, kBeamShift = 8, kFirst = 1 << 12, kLast = 1 << 13;
-template <int HD>
-__device__ __forceinline__ void tile_at(const DecQ4Args& a, const Task4& w, int e, const uint8_t*& tile, int& info) {
-  const int np = tiles_of(a.P), no = tiles_of(w.len), h = head_of(a, w.inner);
-  int64_t block;
-  int n = kTileKeys, flags = 0;
-  if (e < np) {
-    tile = a.pc, block = e;
-    n = min(n, a.P - e * kTileKeys);
-  } else if (e < np + no) {
-    tile = a.oc, block = tile8_first_block(w.st, w.seq) + (e - np);
-    n = min(n, w.len - (e - np) * kTileKeys);
-  } else {
-    const int ng = a.slot / kTileKeys + 1, b = (e - np - no) / ng, j = (e - np - no) % ng;
-    tile = a.gc, block = (static_cast<int64_t>(w.seq) * a.beams + beam_of(a, w.inner) + b) * a.gen_blocks + j;
-    flags = kGenerated | b << kBeamShift;
-    if (j == ng - 1) n = a.slot % kTileKeys + 1, flags |= kAppend;
-  }
-  tile += (block * a.Hkv + h) * tile4_bytes(HD);
-  info = n | flags | (e == 0 ? kFirst : 0) | (e == w.tiles - 1 ? kLast : 0);
-}
 
 // A warp's ring of tiles in shared memory, filled by bulk copies.
 struct __align__(16) Head4 {
-  int seq, inner, info, unused;
+  int row, h, beams, info;
 };
 template <int HD, int STAGES>
 struct Ring4 {
@@ -473,9 +485,9 @@ struct Ring4 {
     __syncthreads();
   }
   // All lanes call; the slot must have been used up by every lane before.
-  __device__ __forceinline__ void issue(const uint8_t* tile, int seq, int inner, int info) {
+  __device__ __forceinline__ void issue(const uint8_t* tile, const Task4& w, int info) {
     if ((threadIdx.x & 31) == 0) {
-      heads[put] = Head4{seq, inner, info, 0};
+      heads[put] = Head4{w.row, w.h, w.beams, info};
       mbar_arrive_expect_tx(&full[put], TB);
       bulk_copy_g2s(slots + put * TB, tile, TB, &full[put]);
     }
@@ -508,28 +520,21 @@ struct Ring4 {
   __device__ __forceinline__ const Head4& head() const { return heads[get]; }
 };
 
-// Where a task's rows are: the query of the lane's column (null: it has none), the step's key of beam b.
-template <int HD, bool PAIRS>
-__device__ __forceinline__ const __half* query_of(const DecQ4Args& a, int seq, int inner, int beam, int head) {
-  const int b = beam_of(a, inner) + beam;
-  if (head < 0 || beam >= beams_of(a, inner)) return nullptr;
-  return a.qkv + (static_cast<int64_t>(seq) * a.beams + b) * a.ldq + (head_of(a, inner) * a.G + head) * HD;
+// The query of a task's beam and head (null: it has none), the step's key of a beam.
+__device__ __forceinline__ const __half* query_of(const DecQ4Args& a, int hd, int row, int h, int beams, int beam, int head) {
+  if (head < 0 || beam >= beams) return nullptr;
+  return a.qkv + static_cast<int64_t>(row + beam) * a.ldq + (h * a.G + head) * hd;
 }
-template <int HD>
-__device__ __forceinline__ const __half* key_of(const DecQ4Args& a, int seq, int inner, int beam) {
-  const int64_t row = static_cast<int64_t>(seq) * a.beams + beam_of(a, inner) + beam;
-  return a.qkv + row * a.ldq + (a.Hq + head_of(a, inner)) * HD;
+__device__ __forceinline__ const __half* key_of(const DecQ4Args& a, int hd, int row, int h) {
+  return a.qkv + row * a.ldq + (a.Hq + h) * hd;
 }
 
 // The step's token into the tile in the ring's slot and the cache's.
 template <int HD>
-__device__ __forceinline__ void append(const DecQ4Args& a, const Token4<HD>& token, uint8_t* copy, int seq, int inner, int beam) {
-  const int64_t row = static_cast<int64_t>(seq) * a.beams + beam_of(a, inner) + beam;
-  const int h = head_of(a, inner);
+__device__ __forceinline__ void append(const DecQ4Args& a, const Token4<HD>& token, uint8_t* copy, int64_t row, int h) {
   const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
   uint8_t* tile = a.gc + ((row * a.gen_blocks + a.slot / kTileKeys) * a.Hkv + h) * tile4_bytes(HD);
-  if (!token.append(copy, tile, a.slot % kTileKeys, a.held ? a.held + row * 2 * kd + h * HD : nullptr, kd))
-    set_dev_error(a.err, DEVERR_FP16_RANGE);
+  if (!token.append(copy, tile, a.held ? a.held + row * 2 * kd + h * HD : nullptr, kd)) set_dev_error(a.err, DEVERR_FP16_RANGE);
   __syncwarp();
 }
 
@@ -575,17 +580,29 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
 
   // the copies run ahead of the products by the ring's length, over the tasks' borders
   int64_t pi = first;
-  Task4 pt{0, 0, 0, 0, 0, 0};
+  Task4 pt{};
   if (pi < n_tasks) pt = task_of(a, first / a.inner, first % a.inner);
-  int pe = 0;
+  const int64_t stride = static_cast<int64_t>(a.Hkv) * tile4_bytes(HD);
+  const uint8_t* tile = nullptr;
+  int run = -1, left = 0;  // prefix, prompt, the beams' tokens; keys left of the run that `tile` is in
+  int flag = kFirst;
   const auto produce = [&] {
     if (pi >= n_tasks) return;
-    const uint8_t* tile;
-    int info;
-    tile_at<HD>(a, pt, pe, tile, info);
-    ring.issue(tile, pt.seq, pt.inner, info);
-    if (++pe < pt.tiles) return;
-    pe = 0;
+    while (left <= 0) {
+      ++run;
+      const uint8_t* from = run == 0 ? a.pc : run == 1 ? a.oc : a.gc;
+      const int64_t block = run == 0 ? 0 : run == 1 ? tile8_first_block(pt.st, pt.seq) : (pt.row + run - 2) * a.gen_blocks;
+      left = run == 0 ? a.P : run == 1 ? pt.len : a.slot + 1;
+      tile = from + (block * a.Hkv + pt.h) * tile4_bytes(HD);
+    }
+    const bool ends = left <= kTileKeys && run >= 2, last = ends && run == pt.beams + 1;
+    ring.issue(tile, pt, min(left, kTileKeys) | (run >= 2 ? kGenerated | (run - 2) << kBeamShift : 0) | (ends ? kAppend : 0) | flag |
+                             (last ? kLast : 0));
+    flag = 0;
+    tile += stride;
+    left -= kTileKeys;
+    if (!last) return;
+    run = -1, left = 0, flag = kFirst;
     pi += odd ? down : up;
     if (pi < n_tasks) {
       const int inner = pt.inner + (odd ? down_inner : up_inner);
@@ -606,9 +623,10 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
   const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
   uint4 raw[At::NQ];
   Token4<HD> token;
+  token.place(a.slot % kTileKeys);
   const auto fetch = [&](const Head4& x) {
-    At::fetch(raw, query_of<HD, PAIRS>(a, x.seq, x.inner, my_beam, my_head));
-    token.load(key_of<HD>(a, x.seq, x.inner, 0), kd);
+    At::fetch(raw, query_of(a, HD, x.row, x.h, x.beams, my_beam, my_head));
+    token.load(key_of(a, HD, x.row, x.h), kd);
   };
   __syncwarp();  // the heads that lane 0 wrote
   if (ring.busy) fetch(ring.head());
@@ -618,15 +636,14 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
     const int info = x.info, n = info & kKeys, b = info >> kBeamShift & 15;
     if (info & kFirst) at.begin(raw, a.scale_log2);
     if (info & kAppend) {
-      append<HD>(a, token, ring.slot(), x.seq, x.inner, b);
-      if (!(info & kLast)) token.load(key_of<HD>(a, x.seq, x.inner, b + 1), kd);
+      append<HD>(a, token, ring.slot(), x.row + b, x.h);
+      if (!(info & kLast)) token.load(key_of(a, HD, x.row + b + 1, x.h), kd);
     }
     if (info & kLast) {  // the next task's queries are on their way while this one ends
       const int after = ring.get + 1 == S::STAGES ? 0 : ring.get + 1;
       if (ring.busy >> after & 1) fetch(ring.heads[after]);
     }
-    const bool all = !(info & kGenerated);
-    at.tile(ring.slot(), n, all || beam[0] == b, all || beam[1] == b);
+    at.tile(ring.slot(), n, (info & kGenerated) && x.beams > 1, beam[0] == b, beam[1] == b);
     ring.used();
     if (info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
     __syncwarp();  // every lane is done with the slot before it is refilled
@@ -635,10 +652,9 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
     at.finish();
     bool fine = true;
     const auto store = [&](int beam, int head, bool odd, float l) {
-      if (head < 0 || beam >= beams_of(a, x.inner)) return;
+      if (head < 0 || beam >= x.beams) return;
       const float inv = 1.f / l;
-      const int64_t row = static_cast<int64_t>(x.seq) * a.beams + beam_of(a, x.inner) + beam;
-      __half* to = a.out + (row * a.Hq + head_of(a, x.inner) * a.G + head) * HD + 2 * At::FR * g;
+      __half* to = a.out + (static_cast<int64_t>(x.row + beam) * a.Hq + x.h * a.G + head) * HD + 2 * At::FR * g;
 #pragma unroll
       for (int c = 0; c < At::C; ++c) {
         uint32_t v[At::FR];
@@ -727,15 +743,24 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
   const int range = static_cast<int>(min(max(unit - first, int64_t(0)), static_cast<int64_t>(ranges - 1)));
   const int64_t task = seq * a.inner + inner;
   const Task4 w = task_of(a, static_cast<int>(seq), inner);
-  const int e0 = static_cast<int>(static_cast<int64_t>(w.tiles) * range / ranges);
-  const int e1 = static_cast<int>(static_cast<int64_t>(w.tiles) * (range + 1) / ranges);
+  const int np = tiles_of(a.P), no = tiles_of(w.len), ng = a.slot / kTileKeys + 1, tiles = np + no + w.beams * ng;
+  const int e0 = static_cast<int>(static_cast<int64_t>(tiles) * range / ranges);
+  const int e1 = static_cast<int>(static_cast<int64_t>(tiles) * (range + 1) / ranges);
   int e = e0 + warp, pe = e;
   const auto produce = [&] {
     if (pe >= e1) return;
-    const uint8_t* tile;
-    int info;
-    tile_at<HD>(a, w, pe, tile, info);
-    ring.issue(tile, w.seq, inner, info);
+    const uint8_t* tile = a.pc;
+    int64_t block = pe;
+    int info = min(kTileKeys, a.P - pe * kTileKeys);
+    if (pe >= np + no) {
+      const int b = (pe - np - no) / ng, j = (pe - np - no) % ng;
+      tile = a.gc, block = (w.row + b) * a.gen_blocks + j;
+      info = (j == ng - 1 ? a.slot % kTileKeys + 1 | kAppend : kTileKeys) | kGenerated | b << kBeamShift;
+    } else if (pe >= np) {
+      tile = a.oc, block = tile8_first_block(w.st, w.seq) + (pe - np);
+      info = min(kTileKeys, w.len - (pe - np) * kTileKeys);
+    }
+    ring.issue(tile + (block * a.Hkv + w.h) * tile4_bytes(HD), w, info);
     pe += S::NW;
   };
 #pragma unroll 1
@@ -748,7 +773,7 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
   Columns4::of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
   {
     uint4 raw[At::NQ];
-    At::fetch(raw, query_of<HD, PAIRS>(a, w.seq, inner, my_beam, my_head));
+    At::fetch(raw, query_of(a, HD, w.row, w.h, w.beams, my_beam, my_head));
     at.begin(raw, a.scale_log2);
   }
   const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
@@ -757,11 +782,11 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
     const int info = ring.head().info, b = info >> kBeamShift & 15;
     if (info & kAppend) {
       Token4<HD> token;
-      token.load(key_of<HD>(a, w.seq, inner, b), kd);
-      append<HD>(a, token, ring.slot(), w.seq, inner, b);
+      token.place(a.slot % kTileKeys);
+      token.load(key_of(a, HD, w.row + b, w.h), kd);
+      append<HD>(a, token, ring.slot(), w.row + b, w.h);
     }
-    const bool all = !(info & kGenerated);
-    at.tile(ring.slot(), info & kKeys, all || beam[0] == b, all || beam[1] == b);
+    at.tile(ring.slot(), info & kKeys, (info & kGenerated) && w.beams > 1, beam[0] == b, beam[1] == b);
     ring.used();
     if (info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
     __syncwarp();
@@ -789,10 +814,9 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
       for (int i = 0; i < At::FR; ++i) dst[i] = make_float2(at.o[c][i][j], at.o[c][i][2 + j]);
     }
   __syncthreads();
-  const int columns = beams_of(a, inner) * a.G;
+  const int columns = w.beams * a.G;
   const auto row_of = [&](int column) {
-    const int64_t row = static_cast<int64_t>(w.seq) * a.beams + beam_of(a, inner) + column / a.G;
-    return a.out + (row * a.Hq + head_of(a, inner) * a.G + column % a.G) * HD;
+    return a.out + (static_cast<int64_t>(w.row + column / a.G) * a.Hq + w.h * a.G + column % a.G) * HD;
   };
   // [inner][unit]: maxima, sums, outputs of up to eight columns
   const int most = a.wide * a.G, size = most * (HD + 2);
