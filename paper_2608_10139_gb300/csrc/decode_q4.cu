@@ -57,6 +57,17 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 
+// A word's eight codes as the four registers of an A fragment's row or rows: codes 0 and 4,
+// 16 times 1 and 5, 2 and 6, 16 times 3 and 7.  Extraction is what the ALU pipe has most to do
+// with, and that pipe has most to do: the last is a difference, which the FMA pipe takes.
+__device__ __forceinline__ void unpack4(uint32_t w, uint32_t (&a)[4]) {
+  a[0] = w & 0x000f000fu;
+  a[1] = w & 0x00f000f0u;
+  const uint32_t x = __byte_perm(w, 0u, 0x4341);
+  a[2] = x & 0x000f000fu;
+  a[3] = as_u32(__hsub2(as_h2(x), as_h2(a[2])));
+}
+
 // 2^x to 2^-22 of it; 0 for -infinity.
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -127,7 +138,8 @@ struct Attn4 {
   static constexpr int FR = KS / C;      // 16-element fragments of a group
   static constexpr int NQ = HD / 32;     // 16-byte loads of a lane's query elements
   static constexpr float kAbove = 11.f, kLag = 4.f, kLow = -1e30f;
-  uint32_t q[KS][2];
+  // PAIRS: [0] in columns 0 .. 3, [1] in 4 .. 7, else zeros
+  uint32_t q[PAIRS ? 2 : 1][KS][2];
   float scale[2], sum[C][2];  // of columns 2 t, 2 t + 1
   // [c][i][2 r + column]: element 64 c + 8 g + 2 i + r (HD 32: 4 g + 2 i + r) of columns 2 t, 2 t + 1
   float o[C][FR][4];
@@ -184,7 +196,13 @@ struct Attn4 {
       for (int j = 0; j < 4; ++j) {
         const float2 v = __half22float2(as_h2(b[j]));
         const float by = j & 1 ? f16 : f;
-        q[2 * i + j / 2][j & 1] = as_u32(__floats2half2_rn(v.x * by, v.y * by));
+        const uint32_t x = as_u32(__floats2half2_rn(v.x * by, v.y * by));
+        if constexpr (PAIRS) {
+          q[0][2 * i + j / 2][j & 1] = lane & 16 ? 0u : x;
+          q[1][2 * i + j / 2][j & 1] = lane & 16 ? x : 0u;
+        } else {
+          q[0][2 * i + j / 2][j & 1] = x;
+        }
       }
     }
     const float unit = power2(e - 1), rest = power2(1 - e);  // 2^24 / f, and sum(q) in its units
@@ -213,14 +231,13 @@ struct Attn4 {
     const uint4* kin = reinterpret_cast<const uint4*>(tile);
     const uint4* vin = reinterpret_cast<const uint4*>(tile + kTileKeys * HD / 2);
     const uint4* pairs = reinterpret_cast<const uint4*>(tile + tile4_pairs(HD));
-    constexpr uint32_t kLo = 0x000f000fu, kHi = 0x00f000f0u;
-    // Scores of keys 16 k + 8 h + g ([k][2 h + column]).  With PAIRS a column's numbers are in two lanes:
-    // one takes keys 0 .. 15 of the tile on, the other 16 .. 31.
+    // Scores of keys 16 k + 8 h + g ([k][2 h + column]).  With PAIRS a column's queries meet keys 0 .. 15 in
+    // columns 0 .. 3, keys 16 .. 31 in 4 .. 7: two lanes share its numbers.
     constexpr int K = PAIRS ? 1 : 2;
     float sc[K][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float acc[2][4];
+      float acc[K][4];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint4 v = kin[HD == 32 ? lane : (k * C + c) * 32 + lane];
@@ -230,15 +247,19 @@ struct Attn4 {
         } else {
           a[0] = v.x, a[1] = v.y, b[0] = v.z, b[1] = v.w;
         }
+        float(&d)[4] = acc[k % K];
+        const auto& qk = q[PAIRS ? k : 0];
 #pragma unroll
         for (int w = 0; w < FR / 2; ++w) {
-          const uint32_t(&q0)[2] = q[c * FR + 2 * w];
-          if (w == 0)
-            mma16816<true>(acc[k], a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
+          uint32_t x[4], y[4];
+          unpack4(a[w], x);
+          unpack4(b[w], y);
+          const uint32_t(&q0)[2] = qk[c * FR + 2 * w];
+          if (w == 0 && k < K)
+            mma16816<true>(d, x[0], y[0], x[1], y[1], q0);
           else
-            mma16816<false>(acc[k], a[w] & kLo, b[w] & kLo, a[w] & kHi, b[w] & kHi, q0);
-          const uint32_t a8 = a[w] >> 8, b8 = b[w] >> 8;
-          mma16816<false>(acc[k], a8 & kLo, b8 & kLo, a8 & kHi, b8 & kHi, q[c * FR + 2 * w + 1]);
+            mma16816<false>(d, x[0], y[0], x[1], y[1], q0);
+          mma16816<false>(d, x[2], y[2], x[3], y[3], qk[c * FR + 2 * w + 1]);
         }
       }
       const uint4 kp = pairs[16 * c + g];
@@ -250,28 +271,18 @@ struct Attn4 {
           const float2 sm = __half22float2(as_h2(p[2 * k + h]));
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float x = second ? acc[1][2 * h + e] : acc[k][2 * h + e];
             const float base = c ? fmaf(sm.y, sum[c][e], sc[k][2 * h + e]) : sm.y * sum[c][e];
-            sc[k][2 * h + e] = fmaf(sm.x, x, base);
+            sc[k][2 * h + e] = fmaf(sm.x, acc[k][2 * h + e], base);
           }
         }
     }
     const int from = second ? 16 + g : g;  // the lane's first key
-    if (n < kTileKeys) {
+    if (n < kTileKeys || some) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (16 * k + 8 * (e / 2) + from >= n) sc[k][e] = -INFINITY;
-    }
-    if (some) {
-#pragma unroll
-      for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!mine0) sc[k][2 * h] = -INFINITY;
-          if (!mine1) sc[k][2 * h + 1] = -INFINITY;
-        }
+          if (16 * k + 8 * (e / 2) + from >= n || (some && !(e & 1 ? mine1 : mine0))) sc[k][e] = -INFINITY;
     }
 
     // Probabilities relative to m, which lies kAbove to kAbove + kLag below the largest score so
@@ -280,18 +291,19 @@ struct Attn4 {
     float mb[2], by[2] = {scale[0], scale[1]};
 #pragma unroll
     for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[K - 1][e], sc[K - 1][2 + e])) * by[e];
-    if (fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f) {
-      // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
-      // score that is not rounded (in the fma below) could lie so far above a rounded m that
-      // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
-      // most, and the largest probability stays between 1 and 2^15 whatever the last place.
+    const bool big = fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f;
+    if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag) || big)) {
+      if (__any_sync(0xffffffffu, big)) {
+        // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
+        // score that is not rounded (in the fma below) could lie so far above a rounded m that
+        // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
+        // most, and the largest probability stays between 1 and 2^15 whatever the last place.
 #pragma unroll
-      for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[k][e] *= by[e & 1];
-      by[0] = by[1] = 1.f;
-    }
-    if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag))) {
+          for (int e = 0; e < 4; ++e) sc[k][e] *= by[e & 1];
+        by[0] = by[1] = 1.f;
+      }
 #pragma unroll
       for (int d = PAIRS ? 2 : 4; d < 32; d <<= 1) {
         mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
@@ -299,7 +311,9 @@ struct Attn4 {
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float mn = fmaxf(m[e], __fsub_ru(mb[e], kAbove)), f = exp2_approx(m[e] - mn);
+        // (a maximum that need not grow stays: its columns' numbers hang on their own keys alone)
+        const float mn = mb[e] > __fadd_rd(m[e], kAbove + kLag) ? fmaxf(m[e], __fsub_ru(mb[e], kAbove)) : m[e];
+        const float f = exp2_approx(m[e] - mn);
         m[e] = mn;
         l[e] *= f;
 #pragma unroll
@@ -376,12 +390,13 @@ struct Attn4 {
             w = k ? (i ? v[0].w : v[0].z) : (i ? v[0].y : v[0].x);
           else
             w = i == 0 ? v[k].x : i == 1 ? v[k].y : i == 2 ? v[k].z : v[k].w;
-          const uint32_t a0 = w & kLo, a1 = w & kHi, w8 = w >> 8, a2 = w8 & kLo, a3 = w8 & kHi;
+          uint32_t x[4];
+          unpack4(w, x);
           if (k == 0)
-            mma16816<true>(acc, a0, a1, a2, a3, hi[k]);
+            mma16816<true>(acc, x[0], x[1], x[2], x[3], hi[k]);
           else
-            mma16816<false>(acc, a0, a1, a2, a3, hi[k]);
-          if constexpr (!PAIRS) mma16816<false>(acc, a0, a1, a2, a3, lo[k]);
+            mma16816<false>(acc, x[0], x[1], x[2], x[3], hi[k]);
+          if constexpr (!PAIRS) mma16816<false>(acc, x[0], x[1], x[2], x[3], lo[k]);
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -392,7 +407,8 @@ struct Attn4 {
     }
   }
 
-  // The sums over all keys; the output with its share of the smallest values.
+  // The sums over all keys; the output with its share of the smallest values (PAIRS: column
+  // (2 t & 3) + t / 2 in place 0).
   __device__ __forceinline__ void finish() {
 #pragma unroll
     for (int d = PAIRS ? 2 : 4; d < 32; d <<= 1)
@@ -407,9 +423,16 @@ struct Attn4 {
 #pragma unroll
       for (int i = 0; i < FR; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (PAIRS) o[c][i][e] += __shfl_xor_sync(0xffffffffu, o[c][i][e], 2);
-          o[c][i][e] += low[c][e & 1];
+        for (int r = 0; r < 2; ++r) {
+          float(&x)[4] = o[c][i];
+          if constexpr (PAIRS) {  // the two lanes of the columns 2 t and 2 t + 1 end up with one each, in place 0
+            const bool odd = threadIdx.x & 2;
+            x[2 * r] = (odd ? x[2 * r + 1] : x[2 * r]) + __shfl_xor_sync(0xffffffffu, odd ? x[2 * r] : x[2 * r + 1], 2);
+            x[2 * r] += odd ? low[c][1] : low[c][0];
+          } else {
+            x[2 * r] += low[c][0];
+            x[2 * r + 1] += low[c][1];
+          }
         }
   }
 };
@@ -447,37 +470,36 @@ __device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int at, int inner) 
   return t;
 }
 
-// What a tile is to its task: its number of keys, whether they are generated ones, and of
-// which beam; whether the step's token goes into it; the task's first and last.
-constexpr int kKeys = 63, kGenerated = 64, kAppend = 128, kBeamShift = 8, kFirst = 1 << 12, kLast = 1 << 13;
+// What an entry of the ring is: one tile or two (kTwo, the first full) of a task, the number of
+// keys of the last, whether they are generated ones, and of which beam; whether the step's token
+// goes into it; the task's first and last entry.
+constexpr int kKeys = 63, kGenerated = 64, kAppend = 128, kBeamShift = 8, kFirst = 1 << 12, kLast = 1 << 13, kTwo = 1 << 14;
 
-// A warp's ring of tiles in shared memory, filled by bulk copies.
+// A warp's ring of entries in shared memory, filled by bulk copies.
 struct __align__(16) Head4 {
   int row, h, beams, info;
 };
 template <int HD, int STAGES>
 struct Ring4 {
-  static constexpr int TB = tile4_bytes(HD);
+  static constexpr int TB = tile4_bytes(HD), EB = 2 * TB;  // a tile, an entry
+  static_assert((STAGES & (STAGES - 1)) == 0, "slots and phases by bits");
   uint8_t* slots;
   Head4* heads;
   uint64_t* full;
   volatile int* abort_flag;
   int* err;
-  int put, get;
-  uint32_t phases;  // bit s: the phase of slot s's barrier that is waited for next
-  uint32_t busy;    // bit s: a tile is on its way to slot s or there
+  uint32_t put, got;  // entries, so far
 
-  // The whole block calls.  smem: SMEM bytes, 128-byte aligned.
-  static constexpr int smem(int warps) { return warps * STAGES * (TB + static_cast<int>(sizeof(Head4)) + 8); }
+  static constexpr int smem(int warps) { return warps * STAGES * (EB + static_cast<int>(sizeof(Head4)) + 8); }
+  // The whole block calls.  smem: that many bytes, 128-byte aligned.
   __device__ __forceinline__ void begin(uint8_t* smem, int warps, int* abort_word, int* err_) {
     const int warp = threadIdx.x >> 5;
-    slots = smem + warp * STAGES * TB;
-    heads = reinterpret_cast<Head4*>(smem + warps * STAGES * TB) + warp * STAGES;
-    full = reinterpret_cast<uint64_t*>(smem + warps * STAGES * (TB + sizeof(Head4))) + warp * STAGES;
+    slots = smem + warp * STAGES * EB;
+    heads = reinterpret_cast<Head4*>(smem + warps * STAGES * EB) + warp * STAGES;
+    full = reinterpret_cast<uint64_t*>(smem + warps * STAGES * (EB + sizeof(Head4))) + warp * STAGES;
     abort_flag = abort_word;
     err = err_;
-    put = get = 0;
-    phases = busy = 0;
+    put = got = 0;
     if ((threadIdx.x & 31) == 0)
       for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1);
     if (threadIdx.x == 0) *abort_word = 0;
@@ -485,39 +507,37 @@ struct Ring4 {
     __syncthreads();
   }
   // All lanes call; the slot must have been used up by every lane before.
-  __device__ __forceinline__ void issue(const uint8_t* tile, const Task4& w, int info) {
-    if ((threadIdx.x & 31) == 0) {
-      heads[put] = Head4{w.row, w.h, w.beams, info};
-      mbar_arrive_expect_tx(&full[put], TB);
-      bulk_copy_g2s(slots + put * TB, tile, TB, &full[put]);
-    }
-    busy |= 1u << put;
-    put = put + 1 == STAGES ? 0 : put + 1;
+  __device__ __forceinline__ void issue(const uint8_t* tile, int64_t stride, const Task4& w, int info) {
+    const uint32_t at = put++ % STAGES, dst = smem_u32(slots + at * EB);
+    asm volatile(  // one lane, by a predicate
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.eq.u32 p, %0, 0;\n\t"
+        "setp.eq.and.u32 q, %10, %11, p;\n\t"
+        "@p st.shared.v4.b32 [%1], {%2, %3, %4, %5};\n\t"
+        "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%6], %10;\n\t"
+        "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%8], [%9], %7, [%6];\n\t"
+        "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%12], [%13], %7, [%6];\n\t}" ::"r"(threadIdx.x & 31),
+        "r"(smem_u32(&heads[at])), "r"(w.row), "r"(w.h), "r"(w.beams), "r"(info), "r"(smem_u32(&full[at])), "r"(TB), "r"(dst),
+        "l"(tile), "r"(info & kTwo ? EB : TB), "r"(EB), "r"(dst + TB), "l"(tile + stride)
+        : "memory");
   }
-  // The next tile has arrived.  False: a wait ran out somewhere; the warp's copies are then awaited.
+  // The next entry has arrived.  False: a wait ran out somewhere; the warp's copies are then awaited.
   __device__ __forceinline__ bool wait() {
-    const uint32_t phase = phases >> get & 1;
-    bool ok = mbar_try_wait(&full[get], phase);
-    if (!ok) ok = longer(&full[get], phase, abort_flag, err);
-    if (__all_sync(0xffffffffu, ok)) {
-      phases ^= 1u << get;
-      return true;
-    }
+    bool ok = mbar_try_wait(&full[got % STAGES], got / STAGES & 1);
+    if (__all_sync(0xffffffffu, ok)) return true;
+    if (!ok) ok = longer(&full[got % STAGES], got / STAGES & 1, abort_flag, err);
+    if (__all_sync(0xffffffffu, ok)) return true;
     volatile int never = 0;
-    for (int i = 0; i < STAGES; ++i)  // a barrier without copies in flight stands at the phase before
-      if (busy >> i & 1) mbar_wait_bounded(&full[i], phases >> i & 1, &never, nullptr, 200000000ull);
+    for (uint32_t i = got; i != put; ++i)
+      mbar_wait_bounded(&full[i % STAGES], i / STAGES & 1, &never, nullptr, 200000000ull);
     return false;
   }
   static __device__ __noinline__ bool longer(uint64_t* bar, uint32_t phase, volatile int* abort_flag, int* err) {
     return mbar_wait_bounded(bar, phase, abort_flag, err);
   }
-  // Every lane is done with the slot.
-  __device__ __forceinline__ void used() {
-    busy &= ~(1u << get);
-    get = get + 1 == STAGES ? 0 : get + 1;
-  }
-  __device__ __forceinline__ uint8_t* slot() const { return slots + get * TB; }
-  __device__ __forceinline__ const Head4& head() const { return heads[get]; }
+  __device__ __forceinline__ bool more() const { return got != put; }
+  __device__ __forceinline__ uint8_t* slot() const { return slots + got % STAGES * EB; }
+  __device__ __forceinline__ const Head4& head(uint32_t ahead = 0) const { return heads[(got + ahead) % STAGES]; }
 };
 
 // The query of a task's beam and head (null: it has none), the step's key of a beam.
@@ -552,7 +572,7 @@ struct Columns4 {
 template <int HD>
 struct Stream4 {
   static constexpr int NW = 4;                     // warps per CTA
-  static constexpr int STAGES = HD == 128 ? 3 : 4;
+  static constexpr int STAGES = 2;
   static constexpr int CTAS = HD == 128 ? 3 : 4;   // per SM
   static constexpr int SMEM = Ring4<HD, STAGES>::smem(NW);
   static_assert(CTAS * (SMEM + 1024 + 64) <= 233472, "shared memory per SM");
@@ -581,36 +601,46 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
   // the copies run ahead of the products by the ring's length, over the tasks' borders
   int64_t pi = first;
   Task4 pt{};
-  if (pi < n_tasks) pt = task_of(a, first / a.inner, first % a.inner);
   const int64_t stride = static_cast<int64_t>(a.Hkv) * tile4_bytes(HD);
   const uint8_t* tile = nullptr;
-  int run = -1, left = 0;  // prefix, prompt, the beams' tokens; keys left of the run that `tile` is in
-  int flag = kFirst;
-  const auto produce = [&] {
-    if (pi >= n_tasks) return;
-    while (left <= 0) {
-      ++run;
+  int run = -1, left = 0, info = 0;  // prefix, prompt, the beams' tokens; keys left of the run that `tile` is in, what they are
+  const auto next_run = [&] {  // one that has keys; left is 0 behind the last task's
+    while (left == 0) {
+      if (++run == pt.beams + 2) {
+        pi += odd ? down : up;
+        if (pi >= n_tasks) return;
+        const int inner = pt.inner + (odd ? down_inner : up_inner);
+        const bool carry = inner >= a.inner;
+        pt = task_of(a, pt.at + (odd ? down_rows : up_rows) + carry, inner - (carry ? a.inner : 0));
+        odd = !odd;
+        run = 0;
+      }
+      if (run == 0) info = kFirst;
       const uint8_t* from = run == 0 ? a.pc : run == 1 ? a.oc : a.gc;
       const int64_t block = run == 0 ? 0 : run == 1 ? tile8_first_block(pt.st, pt.seq) : (pt.row + run - 2) * a.gen_blocks;
       left = run == 0 ? a.P : run == 1 ? pt.len : a.slot + 1;
+      info = info & kFirst | (run >= 2 ? kGenerated | (run - 2) << kBeamShift : 0);
       tile = from + (block * a.Hkv + pt.h) * tile4_bytes(HD);
     }
-    const bool ends = left <= kTileKeys && run >= 2, last = ends && run == pt.beams + 1;
-    ring.issue(tile, pt, min(left, kTileKeys) | (run >= 2 ? kGenerated | (run - 2) << kBeamShift : 0) | (ends ? kAppend : 0) | flag |
-                             (last ? kLast : 0));
-    flag = 0;
-    tile += stride;
-    left -= kTileKeys;
-    if (!last) return;
-    run = -1, left = 0, flag = kFirst;
-    pi += odd ? down : up;
-    if (pi < n_tasks) {
-      const int inner = pt.inner + (odd ? down_inner : up_inner);
-      const bool carry = inner >= a.inner;
-      pt = task_of(a, pt.at + (odd ? down_rows : up_rows) + carry, inner - (carry ? a.inner : 0));
-    }
-    odd = !odd;
   };
+  const auto produce = [&] {
+    if (left > 2 * kTileKeys) {
+      ring.issue(tile, stride, pt, info | kTileKeys | kTwo);
+      info &= ~kFirst;
+      tile += 2 * stride;
+      left -= 2 * kTileKeys;
+    } else if (left > 0) {  // a run's last
+      const bool two = left > kTileKeys;
+      ring.issue(tile, stride, pt, info | (two ? left - kTileKeys | kTwo : left) | (run >= 2 ? kAppend : 0) | (run == pt.beams + 1 ? kLast : 0));
+      info &= ~kFirst;
+      left = 0;
+      next_run();
+    }
+  };
+  if (pi < n_tasks) {
+    pt = task_of(a, first / a.inner, first % a.inner);
+    next_run();
+  }
 #pragma unroll 1
   for (int i = 0; i < S::STAGES; ++i) produce();
 
@@ -629,53 +659,64 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
     token.load(key_of(a, HD, x.row, x.h), kd);
   };
   __syncwarp();  // the heads that lane 0 wrote
-  if (ring.busy) fetch(ring.head());
-  while (ring.busy) {
+  if (ring.more()) fetch(ring.head());
+  while (ring.more()) {
     if (!ring.wait()) return;
     const Head4 x = ring.head();
-    const int info = x.info, n = info & kKeys, b = info >> kBeamShift & 15;
-    if (info & kFirst) at.begin(raw, a.scale_log2);
-    if (info & kAppend) {
-      append<HD>(a, token, ring.slot(), x.row + b, x.h);
-      if (!(info & kLast)) token.load(key_of(a, HD, x.row + b + 1, x.h), kd);
+    const int b = x.info >> kBeamShift & 15;
+    if (x.info & (kFirst | kAppend | kLast)) {
+      if (x.info & kFirst) at.begin(raw, a.scale_log2);
+      if (x.info & kAppend) {
+        append<HD>(a, token, ring.slot() + (x.info & kTwo ? ring.TB : 0), x.row + b, x.h);
+        if (!(x.info & kLast)) token.load(key_of(a, HD, x.row + b + 1, x.h), kd);
+      }
+      // the next task's queries are on their way while this one ends
+      if ((x.info & kLast) && ring.got + 1 != ring.put) fetch(ring.head(1));
     }
-    if (info & kLast) {  // the next task's queries are on their way while this one ends
-      const int after = ring.get + 1 == S::STAGES ? 0 : ring.get + 1;
-      if (ring.busy >> after & 1) fetch(ring.heads[after]);
+    const bool some = (x.info & kGenerated) && x.beams > 1;
+    const uint8_t* tile = ring.slot();
+    int two = x.info & kTwo;
+#pragma unroll 1
+    while (true) {
+      at.tile(tile, two ? kTileKeys : x.info & kKeys, some, beam[0] == b, beam[1] == b);
+      if (!two) break;
+      two = 0;
+      tile += ring.TB;
     }
-    at.tile(ring.slot(), n, (info & kGenerated) && x.beams > 1, beam[0] == b, beam[1] == b);
-    ring.used();
-    if (info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
+    ++ring.got;
+    if (x.info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
     __syncwarp();  // every lane is done with the slot before it is refilled
     produce();
-    if (!(info & kLast)) continue;
+    if (!(x.info & kLast)) continue;
     at.finish();
     bool fine = true;
-    const auto store = [&](int beam, int head, bool odd, float l) {
+    const auto store = [&](int beam, int head, int e, float l) {
       if (head < 0 || beam >= x.beams) return;
-      const float inv = 1.f / l;
+      const float inv = __fdividef(1.f, l);
       __half* to = a.out + (static_cast<int64_t>(x.row + beam) * a.Hq + x.h * a.G + head) * HD + 2 * At::FR * g;
+      __half2 big = as_h2(0u);
 #pragma unroll
       for (int c = 0; c < At::C; ++c) {
         uint32_t v[At::FR];
 #pragma unroll
         for (int i = 0; i < At::FR; ++i) {
-          const float x0 = (odd ? at.o[c][i][1] : at.o[c][i][0]) * inv, x1 = (odd ? at.o[c][i][3] : at.o[c][i][2]) * inv;
-          fine = fine && fabsf(x0) <= 65504.f && fabsf(x1) <= 65504.f;
-          v[i] = as_u32(__floats2half2_rn(x0, x1));
+          const __half2 y = __floats2half2_rn(at.o[c][i][e] * inv, at.o[c][i][2 + e] * inv);
+          big = __hmax2_nan(big, __habs2(y));
+          v[i] = as_u32(y);
         }
         if constexpr (HD == 32)
           *reinterpret_cast<uint2*>(to) = make_uint2(v[0], v[1]);
         else
           *reinterpret_cast<uint4*>(to + 64 * c) = make_uint4(v[0], v[1], v[2], v[3]);
       }
+      fine = fine && __hmax_nan(__low2half(big), __high2half(big)) <= __ushort_as_half(0x7bff);
     };
-    if constexpr (PAIRS) {  // two lanes have the same two columns
+    if constexpr (PAIRS) {
       const bool odd = t >> 1;
-      store(odd ? beam[1] : beam[0], odd ? head[1] : head[0], odd, odd ? at.l[1] : at.l[0]);
+      store(odd ? beam[1] : beam[0], odd ? head[1] : head[0], 0, odd ? at.l[1] : at.l[0]);
     } else {
-      store(beam[0], head[0], false, at.l[0]);
-      store(beam[1], head[1], true, at.l[1]);
+      store(beam[0], head[0], 0, at.l[0]);
+      store(beam[1], head[1], 1, at.l[1]);
     }
     if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
   }
@@ -760,7 +801,7 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
       tile = a.oc, block = tile8_first_block(w.st, w.seq) + (pe - np);
       info = min(kTileKeys, w.len - (pe - np) * kTileKeys);
     }
-    ring.issue(tile + (block * a.Hkv + w.h) * tile4_bytes(HD), w, info);
+    ring.issue(tile + (block * a.Hkv + w.h) * tile4_bytes(HD), 0, w, info);
     pe += S::NW;
   };
 #pragma unroll 1
@@ -787,7 +828,7 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
       append<HD>(a, token, ring.slot(), w.row + b, w.h);
     }
     at.tile(ring.slot(), info & kKeys, (info & kGenerated) && w.beams > 1, beam[0] == b, beam[1] == b);
-    ring.used();
+    ++ring.got;
     if (info & kAppend) fence_proxy_async_smem();  // stores went to the slot that a bulk copy refills
     __syncwarp();
     produce();
@@ -806,10 +847,11 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
     }
   }
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < (PAIRS ? 1 : 2); ++j)
 #pragma unroll
     for (int c = 0; c < At::C; ++c) {
-      float2* dst = reinterpret_cast<float2*>(so + (warp * 8 + 2 * t + j) * HD + 64 * c + 2 * At::FR * g);
+      const int column = PAIRS ? (2 * t & 3) + (t >> 1) : 2 * t + j;
+      float2* dst = reinterpret_cast<float2*>(so + (warp * 8 + column) * HD + 64 * c + 2 * At::FR * g);
 #pragma unroll
       for (int i = 0; i < At::FR; ++i) dst[i] = make_float2(at.o[c][i][j], at.o[c][i][2 + j]);
     }
