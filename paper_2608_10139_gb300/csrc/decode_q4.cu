@@ -941,7 +941,8 @@ template <int HD>
 int units_of(const Plan& p, int num_sms) {
   using S = Stream4<HD>;
   const int64_t ctas = static_cast<int64_t>(num_sms) * S::CTAS, tasks = p.seqs * p.inner;
-  if ((p.tiles + 0.5 * p.seqs) * ctas <= 2.25 * p.seqs * tasks) return 0;
+  const double per_task = p.tiles / p.seqs, rounds = static_cast<double>(tasks) / ctas;
+  if (per_task <= std::min(4.5 * rounds, 2.2 * rounds + 4)) return 0;
   if (tasks > kSplitTasksMax) return static_cast<int>(p.seqs);
   const int64_t most = static_cast<int64_t>(p.tiles / (4 * Split4<HD>::NW));
   return static_cast<int>(std::max<int64_t>(p.seqs, std::min<int64_t>({ctas / p.inner, most, p.seqs + kMaxRanges - 1})));
