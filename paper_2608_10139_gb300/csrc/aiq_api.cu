@@ -2465,9 +2465,9 @@ aiq_status aiq_op_beam_select(aiq_ctx* c, const void* logits, int32_t type, int6
   if (n == 0) return AIQ_OK;
   CUDA_TRY(cudaSetDevice(c->device));
   uint8_t* scratch = nullptr;
-  AIQ_TRY(with_room(c, [&] { return ws(c, "op.beam", beam_select_bytes(n, beams, keep), &scratch); }));
   const BeamSelect b{logits, type, ldl, n, beams, V, scores, done, eos_id, pad_id, keep, parents, tokens, scores_out, done_out};
-  const int e = launch_beam_select(b, scratch, c->d_err, c->stream);
+  AIQ_TRY(with_room(c, [&] { return ws(c, "op.beam", beam_select_bytes(b, c->num_sms), &scratch); }));
+  const int e = launch_beam_select(b, scratch, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("beam selection launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);

@@ -6,13 +6,25 @@
 #include <algorithm>
 #include <cmath>
 
+#include "candidates.cuh"
 #include "common.cuh"
 #include "kernels.h"
 
 namespace aiq {
 namespace {
 
-using Key = unsigned long long;  // a logit's order bits, then ~index
+constexpr int kRowThreads = 128;
+constexpr int kRowCtas = 8;      // per SM
+constexpr int kPerThread = 16;   // elements of a chunk
+constexpr int kChunk = kRowThreads * kPerThread;
+constexpr int kKeepMax = 2 * kBeamsMax;
+static_assert(kKeepMax <= 32, "a lane per offer of a row");
+// What a row's list is cut back to at most, what it may hold before it is, and its size: a chunk
+// more, and the unaligned elements before the first and after the last.
+constexpr int list_most(int k) { return k + 8; }
+constexpr int kListHold = 2 * kRowThreads;
+constexpr int kListSize = kListHold + kChunk + 32;
+constexpr int kMergeList = 1280;  // of a row: its slices' lists
 
 struct SelectArgs {
   const void* logits;
@@ -21,119 +33,443 @@ struct SelectArgs {
   const float* scores;  // [groups][beams]
   const int32_t* done;  // [groups][beams] or null
   int eos, pad;
-  Key* keys;            // [rows][keep] descending; 0: none
-  double* lse;          // [rows]; NaN: a logit is NaN or +inf
+  int slices, slice_len;
+  Key* keys;            // [rows][slices][list_most(keep)]
+  float2* rests;        // [rows][slices]: the other elements' sum of e^(z - y), and y
+  int* counts;          // [rows][slices] keys; -1: a NaN or +inf
   int32_t *parents, *tokens, *done_out;
   float* scores_out;
   int* err;
 };
 
-__device__ __forceinline__ float logit(float v) { return v; }
-__device__ __forceinline__ float logit(__half v) { return __half2float(v); }
-__device__ __forceinline__ float logit(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ uint32_t order_bits(float v) {
-  const uint32_t b = __float_as_uint(v + 0.f);
-  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float order_value(uint32_t o) {
-  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+// Whether a hypothesis' logits are read.
+__device__ __forceinline__ bool is_read(const SelectArgs& a, int64_t row) {
+  return a.scores[row] != -INFINITY && !(a.done && a.done[row]);
 }
 
-constexpr int kThreads = 256;
+constexpr float kLog2e = 0x1.715476p+0f, kLog2eLow = 0x1.4ae0c0p-26f, kLn2 = 0x1.62e430p-1f, kLn2Low = -0x1.05c610p-29f;
+// 2^(j / 32) in two parts.
+__device__ const float2 kExp2[32] = {
+    {0x1.000000p+0f, 0x0.0p+0f}, {0x1.059b0ep+0f, -0x1.9d4f52p-25f},
+    {0x1.0b5586p+0f, 0x1.9f3122p-25f}, {0x1.11301ep+0f, -0x1.fdb496p-25f},
+    {0x1.172b84p+0f, -0x1.c15742p-27f}, {0x1.1d4874p+0f, -0x1.d2e8cap-25f},
+    {0x1.2387a6p+0f, 0x1.ceac48p-25f}, {0x1.29e9e0p+0f, -0x1.5c0424p-25f},
+    {0x1.306fe0p+0f, 0x1.4636e2p-25f}, {0x1.371a74p+0f, -0x1.18aac6p-25f},
+    {0x1.3dea64p+0f, 0x1.824684p-25f}, {0x1.44e086p+0f, 0x1.8624b4p-30f},
+    {0x1.4bfdaep+0f, -0x1.593abcp-25f}, {0x1.5342b6p+0f, -0x1.2c5610p-25f},
+    {0x1.5ab07ep+0f, -0x1.5bd5ecp-27f}, {0x1.6247ecp+0f, -0x1.f8b550p-25f},
+    {0x1.6a09e6p+0f, 0x1.9fcef4p-26f}, {0x1.71f75ep+0f, 0x1.1d8beep-25f},
+    {0x1.7a1148p+0f, -0x1.829fd0p-25f}, {0x1.82589ap+0f, -0x1.accc7cp-26f},
+    {0x1.8ace54p+0f, 0x1.15506ep-27f}, {0x1.93737cp+0f, -0x1.e64744p-25f},
+    {0x1.9c4918p+0f, 0x1.51f848p-27f}, {0x1.a5503cp+0f, -0x1.b83b54p-25f},
+    {0x1.ae89fap+0f, -0x1.a94b14p-26f}, {0x1.b7f770p+0f, -0x1.a09438p-25f},
+    {0x1.c199bep+0f, -0x1.3d56b2p-27f}, {0x1.cb720ep+0f, -0x1.8837ccp-27f},
+    {0x1.d5818ep+0f, -0x1.822dbcp-27f}, {0x1.dfc974p+0f, -0x1.908c94p-25f},
+    {0x1.ea4afap+0f, 0x1.52486cp-27f}, {0x1.f50766p+0f, -0x1.246eb0p-26f},
+};
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
-// A CTA per row: its largest logits, one after the other, and the sum.
+// e^(z - y) for z <= y as a sum of three numbers, to 2^-35 of it, and 0 below e^-80: with
+// pairs of 32-bit numbers, since an SM has 64 times as many units for those as for 64 bits.
+// z - y in two parts (Knuth's sum), their product with log2(e) in two; 2^t is 2^(n / 32) 2^r,
+// n = 32 t rounded, with the first from the table and r log(2) in two parts again, and its
+// square and on, which are below 2^-13, to the fifth power.
+struct Exp3 {
+  float h, m, l;
+  __device__ __forceinline__ Exp3(float z, float y) : h(0.f), m(0.f), l(0.f) {
+    const float d = z - y;
+    if (!(d >= -80.f)) return;
+    const float b = d - z, dl = (z - (d - b)) - (y + b);
+    const float t = d * kLog2e, tl = fmaf(d, kLog2e, -t) + fmaf(d, kLog2eLow, dl * kLog2e);
+    const float magic = 12582912.f, w = fmaf(t, 32.f, magic);  // its last place is 1
+    const int n = __float_as_int(w) - __float_as_int(magic);
+    const float r = fmaf(w - magic, -1.f / 32, t);
+    const float p = r * kLn2, pl = fmaf(r, kLn2, -p) + fmaf(r, kLn2Low, tl * kLn2);
+    const float q = p * p * fmaf(p, fmaf(p, fmaf(p, 1.f / 120, 1.f / 24), 1.f / 6), 0.5f);
+    const float2 c = kExp2[n & 31];
+    const float up = __int_as_float((127 + (n >> 5)) << 23);
+    const float x = c.x * p, xl = fmaf(c.x, p, -x);
+    h = c.x * up;
+    m = x * up;
+    l = (xl + fmaf(c.x, fmaf(pl, p + q, pl) + q, fmaf(c.y, p, c.y))) * up;
+  }
+  __device__ __forceinline__ float sum() const { return h + (m + l); }
+  __device__ __forceinline__ double wide() const { return static_cast<double>(h) + (static_cast<double>(m) + l); }
+};
+
+// A sum in two parts.
+struct Sum2 {
+  float h = 0.f, l = 0.f;
+  __device__ __forceinline__ void add(float x) {
+    const float s = h + x, b = s - h;
+    l += (h - (s - b)) + (x - b);
+    h = s;
+  }
+  __device__ __forceinline__ void over_warp() {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+      const float x = __shfl_xor_sync(0xffffffffu, h, d), xl = __shfl_xor_sync(0xffffffffu, l, d);
+      add(x);
+      l += xl;
+    }
+  }
+};
+
+struct Row {
+  int n;             // entries of the list
+  int part[2][32];   // as candidates.cuh wants them
+  unsigned int highest, lowest;
+  uint32_t kth;
+  Sum2 sums[kRowThreads / 32];
+  alignas(16) uint32_t tops[kRowThreads];
+  __device__ __forceinline__ Key* list() { return reinterpret_cast<Key*>(this + 1); }
+};
+static_assert(sizeof(Row) % sizeof(Key) == 0, "the list is aligned");
+constexpr int kRowShared = static_cast<int>(sizeof(Row)) + kListSize * static_cast<int>(sizeof(Key));
+
+// A CTA per slice of a row: its largest `keep` logits, a few more, and the other ones' sum of
+// exponentials.  What the threads' largest elements of the first two chunks give as a bound,
+// `keep` elements reach, so that what lies below it (most of the row) goes into the sum alone;
+// the others are listed, and cut back to the largest where they grow many.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_beam_rows(SelectArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs a) {
   grid_launch_next();
   grid_wait();
-  __shared__ Key best[kThreads];
-  __shared__ double sums[kThreads];
-  const int64_t r = blockIdx.x;
+  constexpr int NT = kRowThreads, VEC = 16 / sizeof(T), GROUPS = kPerThread / VEC;
+  extern __shared__ __align__(16) uint8_t smem[];
+  Row& s = *reinterpret_cast<Row*>(smem);
   const int tid = threadIdx.x;
-  if (a.scores[r] == -INFINITY || (a.done && a.done[r])) return;
+  const int64_t r = blockIdx.x / a.slices;
+  if (!is_read(a, r)) return;
   const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-  Key last = ~0ull;
-  bool bad = false;
-  double z0 = 0;
-  for (int k = 0; k < a.keep; ++k) {
-    Key mine = 0;
-    for (int i = tid; i < a.V; i += kThreads) {
-      const float z = logit(row[i]);
-      bad = bad || !(z < INFINITY);
-      const Key key = z == -INFINITY ? 0 : static_cast<Key>(order_bits(z)) << 32 | ~static_cast<uint32_t>(i);
-      if (key < last) mine = max(mine, key);
+  const int s0 = static_cast<int>(blockIdx.x % a.slices) * a.slice_len, s1 = min(a.V, s0 + a.slice_len);
+  // 16-byte loads between the first and the last 16-byte boundary
+  const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row + s0) / sizeof(T) % VEC);
+  const int v0 = min(s1, s0 + (skew ? VEC - skew : 0)), v1 = v0 + (s1 - v0) / VEC * VEC;
+  const auto index = [&](int base, int j) { return base + (j / VEC * NT + tid) * VEC + j % VEC; };
+  const auto load = [&](int base, float (&v)[kPerThread]) {
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      const bool in = index(base, i * VEC) < v1;
+      if (in) w = *reinterpret_cast<const uint4*>(row + index(base, i * VEC));
+      const T* x = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[i * VEC + e] = in ? logit(x[e]) : -INFINITY;
     }
-    best[tid] = mine;
-    __syncthreads();
-    for (int s = kThreads / 2; s; s >>= 1) {
-      if (tid < s) best[tid] = max(best[tid], best[tid + s]);
+  };
+  float v[kPerThread], next[kPerThread];
+  load(v0, v);
+  load(v0 + kChunk, next);
+  float mx = fmaxf(v[0], next[0]);
+#pragma unroll
+  for (int j = 1; j < kPerThread; ++j) mx = fmaxf(mx, fmaxf(v[j], next[j]));
+  const uint32_t mine = order_bits(mx);
+  if (tid == 0) s.n = 0;
+  s.tops[tid] = mine;
+  __syncthreads();
+  int before = 0;
+  for (int i = 0; i < NT; i += 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(s.tops + i);
+    before += (x.x > mine || (x.x == mine && i < tid)) + (x.y > mine || (x.y == mine && i + 1 < tid)) +
+              (x.z > mine || (x.z == mine && i + 2 < tid)) + (x.w > mine || (x.w == mine && i + 3 < tid));
+  }
+  if (before == a.keep - 1) s.kth = mine;
+  __syncthreads();
+  const uint32_t kth = s.kth;
+  constexpr uint32_t kNone = 0x007fffffu, kZero = 0x80000000u;  // -infinity, 0
+  // Listed is what is larger than `bound`, the number before the kth's (of 0 that is -2^-149, not
+  // -0); exponentials are relative to `base`, which no element of the sum exceeds.
+  float bound = -INFINITY, base = -3.402823466e38f, seen = -INFINITY;
+  if (kth > kNone) {
+    bound = order_value(kth - (kth == kZero ? 2 : 1));
+    base = order_value(kth);
+  }
+  Sum2 rest;
+  const auto term = [&](float z) { return exp2_approx((z - base) * kLog2e); };
+  const auto single = [&](int at, int end) {
+    if (at >= end) return;
+    const float z = logit(row[at]);
+    seen = max_nan(seen, z);
+    if (z > bound)
+      s.list()[place(s)] = key_of(z, at);
+    else
+      rest.add(term(z));
+  };
+  int round = 0;
+  const auto cut_list = [&] {
+    Sum2 dropped;
+    const Key from = cut<NT>(s, round, a.keep, list_most(a.keep), [&](Key x, Key mid) {
+      dropped.add(exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - order_value(static_cast<uint32_t>(mid >> 32))) * kLog2e));
+    });
+    if (from == 0) return;
+    // of what follows, only larger values can be among the largest: equal ones come later
+    const float to = order_value(static_cast<uint32_t>(from >> 32)), f = Exp3(base, to).sum();
+    rest.h *= f, rest.l *= f;
+    rest.add(dropped.h);
+    rest.l += dropped.l;
+    bound = fmaxf(bound, to);
+    base = to;
+  };
+  single(s0 + tid, v0);
+  for (int at = v0; at < v1; at += kChunk) {
+    float part[GROUPS];
+#pragma unroll
+    for (int w = 0; w < GROUPS; ++w) {
+      float(&x)[kPerThread] = v;
+      float top = x[w * VEC];
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) top = max_nan(top, x[w * VEC + e]);
+      seen = max_nan(seen, top);
+      if (top > bound) {  // few lanes list anything, and most of those one element
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (x[w * VEC + e] > bound) {
+            s.list()[place(s)] = key_of(x[w * VEC + e], index(at, w * VEC + e));
+            x[w * VEC + e] = -INFINITY;
+          }
+      }
+      float y[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) y[e] = term(x[w * VEC + e]);
+#pragma unroll
+      for (int d = VEC / 2; d; d >>= 1)
+#pragma unroll
+        for (int e = 0; e < d; ++e) y[e] += y[e + d];
+      part[w] = y[0];
+    }
+#pragma unroll
+    for (int d = GROUPS / 2; d; d >>= 1)
+#pragma unroll
+      for (int w = 0; w < d; ++w) part[w] += part[w + d];
+    rest.add(part[0]);
+    load(at + kChunk, v);
+    // (whoever lists last sees its own entries counted)
+    if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > kListHold)) {
+      cut_list();
       __syncthreads();
     }
-    last = best[0];
-    __syncthreads();
-    if (k == 0) z0 = last ? order_value(static_cast<uint32_t>(last >> 32)) : 0.f;
-    if (tid == 0) a.keys[r * a.keep + k] = last;
-    if (last == 0) {
-      for (int j = k + tid; j < a.keep; j += kThreads) a.keys[r * a.keep + j] = 0;
-      break;
-    }
   }
-  double sum = 0;
-  for (int i = tid; i < a.V; i += kThreads) sum += exp(logit(row[i]) - z0);
-  sums[tid] = sum;
-  bad = __syncthreads_or(bad);
+  single(v1 + tid, s1);
+  __syncthreads();
+  cut_list();
+  const bool bad = __syncthreads_or(!(seen < INFINITY));
+  rest.over_warp();
+  if (tid % 32 == 0) s.sums[tid / 32] = rest;
+  __syncthreads();
+  const int n = s.n;
+  Key* out = a.keys + blockIdx.x * static_cast<int64_t>(list_most(a.keep));
+  for (int i = tid; i < n; i += NT) out[i] = s.list()[i];
   if (tid == 0) {
-    for (int i = 1; i < kThreads; ++i) sum += sums[i];
-    a.lse[r] = bad ? NAN : z0 + log(sum);
+    Sum2 all = s.sums[0];
+    for (int w = 1; w < NT / 32; ++w) {
+      all.add(s.sums[w].h);
+      all.l += s.sums[w].l;
+    }
+    a.rests[blockIdx.x] = make_float2(all.h + all.l, base);
+    a.counts[blockIdx.x] = bad ? -1 : n;
   }
 }
 
-// A thread per group: its beams' lists merged.
-__global__ void k_beam_merge(SelectArgs a, int n) {
+// A score's bits in the order of the values, and back.
+__device__ __forceinline__ Key order_score(double s) {
+  const long long b = __double_as_longlong(s + 0.0);
+  return static_cast<Key>(b ^ (b >> 63 | static_cast<long long>(1ull << 63)));
+}
+__device__ __forceinline__ double score_of(Key k) {
+  return __longlong_as_double(static_cast<long long>(k & 1ull << 63 ? k & ~(1ull << 63) : ~k));
+}
+// How many of 32 descending keys are larger than x (or equal, where `equal`).
+__device__ __forceinline__ int larger(const Key* keys, Key x, bool equal) {
+  int n = 0;
+#pragma unroll
+  for (int step = 16; step; step >>= 1) {
+    const Key k = keys[n + step - 1];
+    if (k > x || (equal && k == x)) n += step;
+  }
+  return n + (keys[n] > x || (equal && keys[n] == x));
+}
+
+// A CTA per group, a warp per row: the slices' lists in one, the row's sum, its offers' scores,
+// and their places among the group's.
+//
+// Which offers come first is a matter of 64 bits: where two of different hypotheses are closer
+// to one another than the 32-bit sums' error allows to tell, the group's rows are summed once
+// more, to 2^-35.  The error of a row's log is at most `rest / total`, the share of the tokens
+// that are not among its largest, times 2^-22 of the exponential, 2^-19 of sums and rounded
+// arguments, and 2.4 * 2^-24 for each unit of |log2 e^(z - y)|, of which the average, weighted
+// by the terms, is at most log2(V) less log2 of their sum (the entropy of V numbers).
+template <typename T>
+__global__ void k_beam_merge(SelectArgs a) {
   grid_launch_next();
   grid_wait();
-  const int64_t g = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (g >= n) return;
-  int next[kBeamsMax];
-  bool bad = false;
-  for (int b = 0; b < a.beams; ++b) {
-    const int64_t r = g * a.beams + b;
-    const float c = a.scores[r];
-    next[b] = 0;
-    bad = bad || !(c < INFINITY);
-    if (c > -INFINITY && !(a.done && a.done[r])) bad = bad || isnan(a.lse[r]);
-  }
-  if (bad) set_dev_error(a.err, DEVERR_LOGIT);
-  for (int k = 0; k < a.keep; ++k) {
-    int from = -1, token = a.pad;
-    double top = -INFINITY;
-    for (int b = 0; b < a.beams && !bad; ++b) {
-      const int64_t r = g * a.beams + b;
-      const double c = a.scores[r];
-      if (c == -INFINITY || next[b] == a.keep) continue;
-      const bool ended = a.done && a.done[r];
-      double s = c;
-      int t = a.pad;
-      if (ended) {
-        if (next[b]) continue;
-      } else {
-        const Key key = a.keys[r * a.keep + next[b]];
-        if (key == 0) continue;
-        s = c + (order_value(static_cast<uint32_t>(key >> 32)) - a.lse[r]);
-        t = static_cast<int>(~static_cast<uint32_t>(key));
-      }
-      if (s > top) top = s, from = b, token = t;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ Key offers[kBeamsMax][32], first[kKeepMax + 1];
+  __shared__ int tokens[kBeamsMax][32], from[kKeepMax + 1];
+  __shared__ double totals[kBeamsMax], logs[kBeamsMax], sums[32];
+  __shared__ float errors[kBeamsMax], tops[kBeamsMax];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int64_t g = blockIdx.x, r = g * a.beams + warp;
+  const bool mine = warp < a.beams;
+  float c = -INFINITY;
+  if (mine) c = a.scores[r];
+  const bool ended = mine && c > -INFINITY && a.done && a.done[r], live = mine && c != -INFINITY && !ended;
+  bool bad = !(c < INFINITY);
+  Key key = 0;  // lane i: the row's i-th largest
+  if (live && !bad) {
+    const int most = list_most(a.keep), all = a.slices * most;
+    Key* list = reinterpret_cast<Key*>(smem) + static_cast<int64_t>(warp) * all;
+    Key best = 0;
+    int at = 0;
+    for (int i = lane; i < all; i += 32) {
+      const int slice = i / most, n = a.counts[r * a.slices + slice];
+      bad = bad || n < 0;
+      const Key x = i % most < n ? a.keys[r * all + i] : 0;
+      list[i] = x;
+      if (x > best) best = x, at = i;
     }
-    const int64_t at = g * a.keep + k;
-    a.parents[at] = max(from, 0);
-    a.tokens[at] = token;
-    a.scores_out[at] = static_cast<float>(top);
-    if (a.done_out) a.done_out[at] = from < 0 || (a.done && a.done[g * a.beams + from]) || token == a.eos;
-    if (from >= 0) ++next[from];
+    bad = __any_sync(0xffffffffu, bad);
+    for (int k = 0; k < a.keep; ++k) {
+      const uint32_t high = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(best >> 32));
+      const uint32_t low = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0u);
+      const Key top = static_cast<Key>(high) << 32 | low;
+      if (top == 0) break;
+      if (lane == k) key = top;
+      if (best == top) {  // (keys are all different)
+        list[at] = 0;
+        best = 0;
+        for (int i = lane; i < all; i += 32)
+          if (list[i] > best) best = list[i], at = i;
+      }
+    }
+    // the sum, relative to the largest
+    const uint32_t top = __shfl_sync(0xffffffffu, static_cast<uint32_t>(key >> 32), 0);
+    const float y = order_value(top);
+    float rest = 0.f;
+    double sum = 0;
+    if (top) {
+      for (int i = lane; i < all; i += 32)
+        if (list[i]) rest += exp2_approx((order_value(static_cast<uint32_t>(list[i] >> 32)) - y) * kLog2e);
+      for (int i = lane; i < a.slices; i += 32) {
+        const float2 x = a.rests[r * a.slices + i];
+        if (x.x > 0.f) rest += x.x * Exp3(x.y, y).sum();
+      }
+      if (key) sum = Exp3(order_value(static_cast<uint32_t>(key >> 32)), y).wide();
+    }
+    rest = warp_sum(rest);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane == 0) {
+      const float total = static_cast<float>(sum) + rest;
+      const float spread = fmaxf(0.f, __log2f(static_cast<float>(a.V)) - __log2f(rest)) + 1.f;
+      tops[warp] = y;
+      totals[warp] = top ? sum + rest : 1.0;
+      errors[warp] = rest > 0.f ? rest / total * (0x1p-22f + 0x1p-19f + spread * 2.4f * 0x1p-24f) : 0.f;
+    }
   }
+  bad = __syncthreads_or(bad);
+  bool again = false;
+  while (true) {
+    if (warp == 0 && lane < a.beams) logs[lane] = log(totals[lane]);  // (of rows without a sum nobody asks)
+    if (threadIdx.x <= a.keep) first[threadIdx.x] = 0;
+    __syncthreads();
+    Key offer = 0;
+    int token = a.pad;
+    if (!bad && ended && lane == 0) offer = order_score(c);
+    if (!bad && live && key) {
+      token = static_cast<int>(~static_cast<uint32_t>(key));
+      offer = order_score(c + ((static_cast<double>(order_value(static_cast<uint32_t>(key >> 32))) - tops[warp]) - logs[warp]));
+    }
+    if (mine) {
+      offers[warp][lane] = offer;
+      tokens[warp][lane] = token;
+    }
+    __syncthreads();
+    if (offer) {
+      int place = lane;
+      for (int b = 0; b < a.beams; ++b)
+        if (b != warp) place += larger(offers[b], offer, b < warp);
+      if (place <= a.keep) {
+        first[place] = offer;
+        from[place] = warp << 8 | lane;
+      }
+    }
+    __syncthreads();
+    if (again) break;
+    bool close = false;
+    if (threadIdx.x < a.keep && first[threadIdx.x + 1]) {
+      const int b0 = from[threadIdx.x] >> 8, b1 = from[threadIdx.x + 1] >> 8;
+      const auto error = [&](int b) { return a.done && a.done[g * a.beams + b] ? 0.f : errors[b]; };
+      const double e = static_cast<double>(error(b0)) + error(b1);
+      close = b0 != b1 && e > 0 && score_of(first[threadIdx.x]) - score_of(first[threadIdx.x + 1]) <= e;
+    }
+    if (!__syncthreads_or(close)) break;
+    again = true;
+    for (int b = 0; b < a.beams; ++b) {
+      const int64_t row = g * a.beams + b;
+      if (!is_read(a, row) || offers[b][0] == 0) continue;
+      const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+      const float y = tops[b];
+      Sum2 sum;
+      for (int i = threadIdx.x; i < a.V; i += blockDim.x) {
+        const Exp3 e(logit(z[i]), y);
+        sum.add(e.h);
+        sum.add(e.m);
+        sum.l += e.l;
+      }
+      double total = static_cast<double>(sum.h) + sum.l;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+      if (lane == 0) sums[warp] = total;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        for (int w = 1; w < warps; ++w) total += sums[w];
+        totals[b] = total;
+      }
+      __syncthreads();
+    }
+  }
+  if (bad && threadIdx.x == 0) set_dev_error(a.err, DEVERR_LOGIT);
+  if (threadIdx.x < a.keep) {
+    const int64_t at = g * a.keep + threadIdx.x;
+    const Key k = first[threadIdx.x];
+    const int b = k ? from[threadIdx.x] >> 8 : 0, token = k ? tokens[b][from[threadIdx.x] & 255] : a.pad;
+    a.parents[at] = b;
+    a.tokens[at] = token;
+    a.scores_out[at] = k ? static_cast<float>(score_of(k)) : -INFINITY;
+    if (a.done_out) a.done_out[at] = !k || (a.done && a.done[g * a.beams + b]) || token == a.eos;
+  }
+}
+
+struct Plan {
+  int slices, slice_len;
+};
+Plan plan_of(int64_t rows, int V, int keep, int num_sms) {
+  // few rows: as many slices as fill the GPU, of two chunks at least
+  const int64_t pairs = (static_cast<int64_t>(V) + 2 * kChunk - 1) / (2 * kChunk);
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({pairs, static_cast<int64_t>(num_sms) * kRowCtas / rows,
+                                                               kMergeList / list_most(keep)}));
+  const int64_t len = (pairs + want - 1) / want * 2 * kChunk;
+  return len >= V ? Plan{1, V} : Plan{static_cast<int>((V + len - 1) / len), static_cast<int>(len)};
+}
+
+template <typename T>
+int launch_select(const SelectArgs& a, int groups, cudaStream_t s) {
+  static_assert(kRowShared <= 48 * 1024, "no larger shared memory to ask for");
+  cudaError_t e = launch_chained(k_beam_rows<T>, dim3(static_cast<unsigned>(groups) * a.beams * a.slices), kRowThreads, kRowShared, s, 1, a);
+  if (e != cudaSuccess) return e;
+  const int smem = a.beams * a.slices * list_most(a.keep) * static_cast<int>(sizeof(Key));
+  e = cudaFuncSetAttribute(k_beam_merge<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBeamsMax * kMergeList * static_cast<int>(sizeof(Key)));
+  if (e != cudaSuccess) return e;
+  return launch_chained(k_beam_merge<T>, dim3(static_cast<unsigned>(groups)), 32 * std::max(4, a.beams), smem, s, 1, a);
 }
 
 // ------------------------------------------------------------- reordering ---
+constexpr int kThreads = 256;
 struct ReorderArgs {
   const uint8_t* src;
   uint8_t* dst;
@@ -189,22 +525,27 @@ int launch_reorder(ReorderArgs a, int64_t bytes, cudaStream_t s) {
 
 }  // namespace
 
-size_t beam_select_bytes(int groups, int beams, int keep) {
-  return static_cast<size_t>(groups) * beams * (keep * sizeof(Key) + sizeof(double));
-}
-
-int launch_beam_select(const BeamSelect& b, void* scratch, int* err, cudaStream_t s) {
+size_t beam_select_bytes(const BeamSelect& b, int num_sms) {
   if (b.groups <= 0) return 0;
   const int64_t rows = static_cast<int64_t>(b.groups) * b.beams;
+  return rows * plan_of(rows, b.V, b.keep, num_sms).slices * (list_most(b.keep) * sizeof(Key) + sizeof(float2) + sizeof(int));
+}
+
+int launch_beam_select(const BeamSelect& b, void* scratch, int* err, int num_sms, cudaStream_t s) {
+  if (b.groups <= 0) return 0;
+  const int64_t rows = static_cast<int64_t>(b.groups) * b.beams;
+  const Plan p = plan_of(rows, b.V, b.keep, num_sms);
+  const int64_t lists = rows * p.slices;
   Key* keys = static_cast<Key*>(scratch);
-  const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, keys,
-                     reinterpret_cast<double*>(keys + rows * b.keep), b.parents, b.tokens, b.done_out, b.scores_out, err};
-  void (*kernel)(SelectArgs) = b.type == LOGITS_F32   ? k_beam_rows<float>
-                               : b.type == LOGITS_F16 ? k_beam_rows<__half>
-                                                      : k_beam_rows<__nv_bfloat16>;
-  const int e = launch_chained(kernel, dim3(static_cast<unsigned>(rows)), kThreads, 0, s, 1, a);
-  if (e) return e;
-  return launch_chained(k_beam_merge, dim3((b.groups + 63) / 64), 64, 0, s, 1, a, b.groups);
+  float2* rests = reinterpret_cast<float2*>(keys + lists * list_most(b.keep));
+  const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, p.slices, p.slice_len, keys, rests,
+                     reinterpret_cast<int*>(rests + lists), b.parents, b.tokens, b.done_out, b.scores_out, err};
+  switch (b.type) {
+    case LOGITS_F32: return launch_select<float>(a, b.groups, s);
+    case LOGITS_F16: return launch_select<__half>(a, b.groups, s);
+    case LOGITS_BF16: return launch_select<__nv_bfloat16>(a, b.groups, s);
+    default: return cudaErrorInvalidValue;
+  }
 }
 
 int launch_beam_reorder(const void* src, void* dst, int64_t bytes, int64_t pitch, int groups, int beams,

@@ -174,8 +174,8 @@ def select(z, scores, done, keep, eos, pad):
             continue
         top = row[order[0]]
         e = np.sort(np.exp(row - top))
-        lse = top + np.log(e.sum())
-        offers += [(-(c + (row[t] - lse)), b, i, int(t)) for i, t in enumerate(order)]
+        log = np.log(e.sum())  # (not added to the largest logit, in which it may be lost)
+        offers += [(-(c + ((row[t] - top) - log)), b, i, int(t)) for i, t in enumerate(order)]
     offers.sort(key=lambda o: o[:3])
     out = [(b, t, -s, int(bool(done[b]) or t == eos)) for s, b, _, t in offers[:keep]]
     out += [(0, pad, -np.inf, 1)] * (keep - len(out))
