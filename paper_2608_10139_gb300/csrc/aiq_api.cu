@@ -2467,7 +2467,7 @@ aiq_status aiq_op_beam_select(aiq_ctx* c, const void* logits, int32_t type, int6
   uint8_t* scratch = nullptr;
   const BeamSelect b{logits, type, ldl, n, beams, V, scores, done, eos_id, pad_id, keep, parents, tokens, scores_out, done_out};
   AIQ_TRY(with_room(c, [&] { return ws(c, "op.beam", beam_select_bytes(b, c->num_sms), &scratch); }));
-  const int e = launch_beam_select(b, scratch, c->d_err, c->num_sms, c->stream);
+  const int e = launch_beam_select(b, scratch, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("beam selection launch: ") +
                                             cudaGetErrorString(static_cast<cudaError_t>(e)));
   return sync_and_check(c);

@@ -19,12 +19,15 @@ constexpr int kPerThread = 16;   // elements of a chunk
 constexpr int kChunk = kRowThreads * kPerThread;
 constexpr int kKeepMax = 2 * kBeamsMax;
 static_assert(kKeepMax <= 32, "a lane per offer of a row");
-// What a row's list is cut back to at most, what it may hold before it is, and its size: a chunk
-// more, and the unaligned elements before the first and after the last.
-constexpr int list_most(int k) { return k + 8; }
+// What a slice's list is cut back to at most (which most lists never reach), what it may hold
+// before it is, and its size: a chunk more, and the unaligned elements before the first and after
+// the last.
+constexpr int kListMost = 64;
+constexpr int list_most(int keep, int slices) { return slices == 1 ? kListMost : keep + 8; }
 constexpr int kListHold = 2 * kRowThreads;
 constexpr int kListSize = kListHold + kChunk + 32;
-constexpr int kMergeList = 1280;  // of a row: its slices' lists
+static_assert(kKeepMax + 8 <= kListMost, "there is a bound that cuts between");
+constexpr int kMergeList = 20 * 1024;  // of a group: its rows' and slices' lists
 
 struct SelectArgs {
   const void* logits;
@@ -34,9 +37,11 @@ struct SelectArgs {
   const int32_t* done;  // [groups][beams] or null
   int eos, pad;
   int slices, slice_len;
-  Key* keys;            // [rows][slices][list_most(keep)]
+  int most;             // of a slice's list
+  Key* keys;            // [rows][slices][most], zeros behind a list's end
   float2* rests;        // [rows][slices]: the other elements' sum of e^(z - y), and y
-  int* counts;          // [rows][slices] keys; -1: a NaN or +inf
+  int* bad;             // [rows][slices]: whether a NaN or +inf came by
+  unsigned int* arrived;  // [groups] rows that are done, 0 between launches; null: the merge is a launch of its own
   int32_t *parents, *tokens, *done_out;
   float* scores_out;
   int* err;
@@ -136,15 +141,9 @@ constexpr int kRowShared = static_cast<int>(sizeof(Row)) + kListSize * static_ca
 // `keep` elements reach, so that what lies below it (most of the row) goes into the sum alone;
 // the others are listed, and cut back to the largest where they grow many.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs a) {
-  grid_launch_next();
-  grid_wait();
+__device__ __forceinline__ void scan_row(const SelectArgs& a, Row& s, int64_t r) {
   constexpr int NT = kRowThreads, VEC = 16 / sizeof(T), GROUPS = kPerThread / VEC;
-  extern __shared__ __align__(16) uint8_t smem[];
-  Row& s = *reinterpret_cast<Row*>(smem);
   const int tid = threadIdx.x;
-  const int64_t r = blockIdx.x / a.slices;
-  if (!is_read(a, r)) return;
   const T* row = static_cast<const T*>(a.logits) + r * a.ld;
   const int s0 = static_cast<int>(blockIdx.x % a.slices) * a.slice_len, s1 = min(a.V, s0 + a.slice_len);
   // 16-byte loads between the first and the last 16-byte boundary
@@ -168,15 +167,22 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs 
   float mx = fmaxf(v[0], next[0]);
 #pragma unroll
   for (int j = 1; j < kPerThread; ++j) mx = fmaxf(mx, fmaxf(v[j], next[j]));
-  const uint32_t mine = order_bits(mx);
+  // (of few, four threads' largest at a time: a quarter of the comparisons for a bound that lists little more)
+  uint32_t mine = order_bits(mx);
+  const int by = a.keep <= 8 ? 4 : 1, of = tid / by;
+  if (by == 4) {
+    mine = max(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
+    mine = max(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
+  }
   if (tid == 0) s.n = 0;
-  s.tops[tid] = mine;
+  if (tid % by == 0) s.tops[of] = mine;
   __syncthreads();
   int before = 0;
-  for (int i = 0; i < NT; i += 4) {
+#pragma unroll 8
+  for (int i = 0; i < NT / by; i += 4) {
     const uint4 x = *reinterpret_cast<const uint4*>(s.tops + i);
-    before += (x.x > mine || (x.x == mine && i < tid)) + (x.y > mine || (x.y == mine && i + 1 < tid)) +
-              (x.z > mine || (x.z == mine && i + 2 < tid)) + (x.w > mine || (x.w == mine && i + 3 < tid));
+    before += (x.x > mine || (x.x == mine && i < of)) + (x.y > mine || (x.y == mine && i + 1 < of)) +
+              (x.z > mine || (x.z == mine && i + 2 < of)) + (x.w > mine || (x.w == mine && i + 3 < of));
   }
   if (before == a.keep - 1) s.kth = mine;
   __syncthreads();
@@ -203,7 +209,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs 
   int round = 0;
   const auto cut_list = [&] {
     Sum2 dropped;
-    const Key from = cut<NT>(s, round, a.keep, list_most(a.keep), [&](Key x, Key mid) {
+    const Key from = cut<NT>(s, round, a.keep, a.most, [&](Key x, Key mid) {
       dropped.add(exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - order_value(static_cast<uint32_t>(mid >> 32))) * kLog2e));
     });
     if (from == 0) return;
@@ -216,11 +222,11 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs 
     base = to;
   };
   single(s0 + tid, v0);
-  for (int at = v0; at < v1; at += kChunk) {
+  // Two chunks are on their way or at work at any time.
+  const auto take = [&](float (&x)[kPerThread], int at) {
     float part[GROUPS];
 #pragma unroll
     for (int w = 0; w < GROUPS; ++w) {
-      float(&x)[kPerThread] = v;
       float top = x[w * VEC];
 #pragma unroll
       for (int e = 1; e < VEC; ++e) top = max_nan(top, x[w * VEC + e]);
@@ -247,12 +253,16 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs 
 #pragma unroll
       for (int w = 0; w < d; ++w) part[w] += part[w + d];
     rest.add(part[0]);
-    load(at + kChunk, v);
+    load(at + 2 * kChunk, x);
     // (whoever lists last sees its own entries counted)
     if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > kListHold)) {
       cut_list();
       __syncthreads();
     }
+  };
+  for (int at = v0; at < v1; at += 2 * kChunk) {
+    take(v, at);
+    if (at + kChunk < v1) take(next, at + kChunk);
   }
   single(v1 + tid, s1);
   __syncthreads();
@@ -262,8 +272,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs 
   if (tid % 32 == 0) s.sums[tid / 32] = rest;
   __syncthreads();
   const int n = s.n;
-  Key* out = a.keys + blockIdx.x * static_cast<int64_t>(list_most(a.keep));
-  for (int i = tid; i < n; i += NT) out[i] = s.list()[i];
+  Key* out = a.keys + blockIdx.x * static_cast<int64_t>(a.most);
+  for (int i = tid; i < a.most; i += NT) out[i] = i < n ? s.list()[i] : 0;
   if (tid == 0) {
     Sum2 all = s.sums[0];
     for (int w = 1; w < NT / 32; ++w) {
@@ -271,7 +281,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs 
       all.l += s.sums[w].l;
     }
     a.rests[blockIdx.x] = make_float2(all.h + all.l, base);
-    a.counts[blockIdx.x] = bad ? -1 : n;
+    a.bad[blockIdx.x] = bad;
   }
 }
 
@@ -282,6 +292,23 @@ __device__ __forceinline__ Key order_score(double s) {
 }
 __device__ __forceinline__ double score_of(Key k) {
   return __longlong_as_double(static_cast<long long>(k & 1ull << 63 ? k & ~(1ull << 63) : ~k));
+}
+// How many of the lanes' keys are larger than a lane's, equal ones by lane.
+__device__ __forceinline__ int place_of(Key x, int lane) {
+  int n = 0;
+#pragma unroll
+  for (int d = 1; d < 32; ++d) {
+    const Key k = __shfl_xor_sync(0xffffffffu, x, d);
+    n += k > x || (k == x && (lane ^ d) < lane);
+  }
+  return n;
+}
+// log(x) for 1 <= x < 2^30 by Newton's step on its 32-bit value, to 2^-34: a step's
+// remainder, x e^-y - 1, is below 2^-20.
+__device__ __forceinline__ double log_of(double x) {
+  const float y = logf(static_cast<float>(x));
+  const double d = fma(x, Exp3(-y, 0.f).wide(), -1.0);
+  return y + fma(d * d, -0.5, d);
 }
 // How many of 32 descending keys are larger than x (or equal, where `equal`).
 __device__ __forceinline__ int larger(const Key* keys, Key x, bool equal) {
@@ -294,8 +321,88 @@ __device__ __forceinline__ int larger(const Key* keys, Key x, bool equal) {
   return n + (keys[n] > x || (equal && keys[n] == x));
 }
 
-// A CTA per group, a warp per row: the slices' lists in one, the row's sum, its offers' scores,
-// and their places among the group's.
+// What a group's merge shares, and behind it [beams][slices * most] keys.
+struct Merge {
+  Key sorted[kBeamsMax][32], offers[kBeamsMax][32], first[kKeepMax + 1];
+  int tokens[kBeamsMax][32], from[kKeepMax + 1];
+  double totals[kBeamsMax], logs[kBeamsMax], sums[32];
+  float errors[kBeamsMax], tops[kBeamsMax];
+  __device__ __forceinline__ Key* lists() { return reinterpret_cast<Key*>(this + 1); }
+};
+static_assert(sizeof(Merge) % sizeof(Key) == 0, "the lists are aligned");
+
+// A row's largest `keep` logits in order, by one warp, and its sum relative to the largest.
+// False: a logit is NaN or +infinity.
+__device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t r, int b) {
+  const int lane = threadIdx.x & 31, all = a.slices * a.most;
+  Key* list = s.lists() + b * all;
+  Key* sorted = s.sorted[b];
+  Key best = 0;
+  bool bad = false;
+  for (int i = lane; i < a.slices; i += 32) bad = bad || __ldcg(a.bad + r * a.slices + i);
+#pragma unroll 8
+  for (int i = lane; i < all; i += 32) {
+    const Key x = __ldcg(a.keys + r * all + i);
+    list[i] = x;
+    best = max(best, x);
+  }
+  // The lanes' largest, in order: what the keep-th of them reaches has the largest `keep` of all
+  // among it, and little more.
+  const Key least = place_of(best, lane) == a.keep - 1 ? best : 0;
+  const int owner = __ffs(__ballot_sync(0xffffffffu, least != 0)) - 1;
+  const Key from = owner < 0 ? 1 : __shfl_sync(0xffffffffu, least, owner);
+  const uint32_t top = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(best >> 32));
+  const float y = order_value(top);
+  const auto light = [&](Key x) { return exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - y) * kLog2e); };
+  int n = 0;
+  float rest = 0.f;
+  __syncwarp();
+#pragma unroll 4
+  for (int i = lane; i - lane < all; i += 32) {  // (an entry moves to a place that was read before)
+    const Key x = i < all ? list[i] : 0;
+    const uint32_t kept = __ballot_sync(0xffffffffu, x >= from);
+    if (x >= from)
+      list[n + __popc(kept & ((1u << lane) - 1))] = x;
+    else if (x)
+      rest += light(x);
+    n += __popc(kept);
+  }
+  sorted[lane] = 0;
+  __syncwarp();
+  for (int i = lane; i < n; i += 32) {
+    const Key x = list[i];
+    int before = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) before += list[j] > x;  // (keys are all different)
+    if (before < a.keep)
+      sorted[before] = x;
+    else
+      rest += light(x);
+  }
+  __syncwarp();
+  const Key key = sorted[lane];
+  double sum = 0;
+  if (top) {
+    for (int i = lane; i < a.slices; i += 32) {
+      const float2 x = __ldcg(a.rests + r * a.slices + i);
+      if (x.x > 0.f) rest += x.x * Exp3(x.y, y).sum();
+    }
+    if (key) sum = Exp3(order_value(static_cast<uint32_t>(key >> 32)), y).wide();
+  }
+  rest = warp_sum(rest);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0) {
+    const float total = static_cast<float>(sum) + rest;
+    const float spread = fmaxf(0.f, __log2f(static_cast<float>(a.V)) - __log2f(rest)) + 1.f;
+    s.tops[b] = y;
+    s.totals[b] = top ? sum + rest : 1.0;
+    s.errors[b] = rest > 0.f ? rest / total * (0x1p-22f + 0x1p-19f + spread * 2.4f * 0x1p-24f) : 0.f;
+  }
+  return !__any_sync(0xffffffffu, bad);
+}
+
+// A group's rows' offers, and their places among the group's, by a block of whole warps, four at least.
 //
 // Which offers come first is a matter of 64 bits: where two of different hypotheses are closer
 // to one another than the 32-bit sums' error allows to tell, the group's rows are summed once
@@ -304,116 +411,66 @@ __device__ __forceinline__ int larger(const Key* keys, Key x, bool equal) {
 // arguments, and 2.4 * 2^-24 for each unit of |log2 e^(z - y)|, of which the average, weighted
 // by the terms, is at most log2(V) less log2 of their sum (the entropy of V numbers).
 template <typename T>
-__global__ void k_beam_merge(SelectArgs a) {
-  grid_launch_next();
-  grid_wait();
-  extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ Key offers[kBeamsMax][32], first[kKeepMax + 1];
-  __shared__ int tokens[kBeamsMax][32], from[kKeepMax + 1];
-  __shared__ double totals[kBeamsMax], logs[kBeamsMax], sums[32];
-  __shared__ float errors[kBeamsMax], tops[kBeamsMax];
+__device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64_t g) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int64_t g = blockIdx.x, r = g * a.beams + warp;
-  const bool mine = warp < a.beams;
-  float c = -INFINITY;
-  if (mine) c = a.scores[r];
-  const bool ended = mine && c > -INFINITY && a.done && a.done[r], live = mine && c != -INFINITY && !ended;
-  bool bad = !(c < INFINITY);
-  Key key = 0;  // lane i: the row's i-th largest
-  if (live && !bad) {
-    const int most = list_most(a.keep), all = a.slices * most;
-    Key* list = reinterpret_cast<Key*>(smem) + static_cast<int64_t>(warp) * all;
-    Key best = 0;
-    int at = 0;
-    for (int i = lane; i < all; i += 32) {
-      const int slice = i / most, n = a.counts[r * a.slices + slice];
-      bad = bad || n < 0;
-      const Key x = i % most < n ? a.keys[r * all + i] : 0;
-      list[i] = x;
-      if (x > best) best = x, at = i;
-    }
-    bad = __any_sync(0xffffffffu, bad);
-    for (int k = 0; k < a.keep; ++k) {
-      const uint32_t high = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(best >> 32));
-      const uint32_t low = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0u);
-      const Key top = static_cast<Key>(high) << 32 | low;
-      if (top == 0) break;
-      if (lane == k) key = top;
-      if (best == top) {  // (keys are all different)
-        list[at] = 0;
-        best = 0;
-        for (int i = lane; i < all; i += 32)
-          if (list[i] > best) best = list[i], at = i;
-      }
-    }
-    // the sum, relative to the largest
-    const uint32_t top = __shfl_sync(0xffffffffu, static_cast<uint32_t>(key >> 32), 0);
-    const float y = order_value(top);
-    float rest = 0.f;
-    double sum = 0;
-    if (top) {
-      for (int i = lane; i < all; i += 32)
-        if (list[i]) rest += exp2_approx((order_value(static_cast<uint32_t>(list[i] >> 32)) - y) * kLog2e);
-      for (int i = lane; i < a.slices; i += 32) {
-        const float2 x = a.rests[r * a.slices + i];
-        if (x.x > 0.f) rest += x.x * Exp3(x.y, y).sum();
-      }
-      if (key) sum = Exp3(order_value(static_cast<uint32_t>(key >> 32)), y).wide();
-    }
-    rest = warp_sum(rest);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) {
-      const float total = static_cast<float>(sum) + rest;
-      const float spread = fmaxf(0.f, __log2f(static_cast<float>(a.V)) - __log2f(rest)) + 1.f;
-      tops[warp] = y;
-      totals[warp] = top ? sum + rest : 1.0;
-      errors[warp] = rest > 0.f ? rest / total * (0x1p-22f + 0x1p-19f + spread * 2.4f * 0x1p-24f) : 0.f;
-    }
+  const auto ended = [&](int b) { return a.done && a.done[g * a.beams + b]; };
+  bool bad = false;
+  for (int b = warp; b < a.beams; b += warps) {
+    const int64_t r = g * a.beams + b;
+    bad = bad || !(a.scores[r] < INFINITY);
+    if (!bad && is_read(a, r))
+      bad = !merge_row(a, s, r, b);
+    else if (lane == 0)
+      s.totals[b] = 1.0, s.errors[b] = 0.f;
   }
   bad = __syncthreads_or(bad);
   bool again = false;
   while (true) {
-    if (warp == 0 && lane < a.beams) logs[lane] = log(totals[lane]);  // (of rows without a sum nobody asks)
-    if (threadIdx.x <= a.keep) first[threadIdx.x] = 0;
+    if (warp == 0 && lane < a.beams) s.logs[lane] = log_of(s.totals[lane]);
+    if (threadIdx.x <= a.keep) s.first[threadIdx.x] = 0;
     __syncthreads();
-    Key offer = 0;
-    int token = a.pad;
-    if (!bad && ended && lane == 0) offer = order_score(c);
-    if (!bad && live && key) {
-      token = static_cast<int>(~static_cast<uint32_t>(key));
-      offer = order_score(c + ((static_cast<double>(order_value(static_cast<uint32_t>(key >> 32))) - tops[warp]) - logs[warp]));
-    }
-    if (mine) {
-      offers[warp][lane] = offer;
-      tokens[warp][lane] = token;
+    for (int b = warp; b < a.beams; b += warps) {
+      const float c = a.scores[g * a.beams + b];
+      Key offer = 0;
+      int token = a.pad;
+      if (!bad && c > -INFINITY) {
+        if (ended(b)) {
+          if (lane == 0) offer = order_score(c);
+        } else if (const Key key = s.sorted[b][lane]) {
+          token = static_cast<int>(~static_cast<uint32_t>(key));
+          offer = order_score(c + ((static_cast<double>(order_value(static_cast<uint32_t>(key >> 32))) - s.tops[b]) - s.logs[b]));
+        }
+      }
+      s.offers[b][lane] = offer;
+      s.tokens[b][lane] = token;
     }
     __syncthreads();
-    if (offer) {
+    for (int b = warp; b < a.beams; b += warps) {
+      const Key offer = s.offers[b][lane];
+      if (!offer) continue;
       int place = lane;
-      for (int b = 0; b < a.beams; ++b)
-        if (b != warp) place += larger(offers[b], offer, b < warp);
+#pragma unroll 4
+      for (int o = 0; o < a.beams; ++o) place += o == b ? 0 : larger(s.offers[o], offer, o < b);
       if (place <= a.keep) {
-        first[place] = offer;
-        from[place] = warp << 8 | lane;
+        s.first[place] = offer;
+        s.from[place] = b << 8 | lane;
       }
     }
     __syncthreads();
     if (again) break;
     bool close = false;
-    if (threadIdx.x < a.keep && first[threadIdx.x + 1]) {
-      const int b0 = from[threadIdx.x] >> 8, b1 = from[threadIdx.x + 1] >> 8;
-      const auto error = [&](int b) { return a.done && a.done[g * a.beams + b] ? 0.f : errors[b]; };
-      const double e = static_cast<double>(error(b0)) + error(b1);
-      close = b0 != b1 && e > 0 && score_of(first[threadIdx.x]) - score_of(first[threadIdx.x + 1]) <= e;
+    if (threadIdx.x < a.keep && s.first[threadIdx.x + 1]) {
+      const int b0 = s.from[threadIdx.x] >> 8, b1 = s.from[threadIdx.x + 1] >> 8;
+      const double e = static_cast<double>(s.errors[b0]) + s.errors[b1];
+      close = b0 != b1 && e > 0 && score_of(s.first[threadIdx.x]) - score_of(s.first[threadIdx.x + 1]) <= e;
     }
     if (!__syncthreads_or(close)) break;
     again = true;
     for (int b = 0; b < a.beams; ++b) {
       const int64_t row = g * a.beams + b;
-      if (!is_read(a, row) || offers[b][0] == 0) continue;
+      if (!is_read(a, row) || s.offers[b][0] == 0) continue;
       const T* z = static_cast<const T*>(a.logits) + row * a.ld;
-      const float y = tops[b];
+      const float y = s.tops[b];
       Sum2 sum;
       for (int i = threadIdx.x; i < a.V; i += blockDim.x) {
         const Exp3 e(logit(z[i]), y);
@@ -424,11 +481,11 @@ __global__ void k_beam_merge(SelectArgs a) {
       double total = static_cast<double>(sum.h) + sum.l;
 #pragma unroll
       for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-      if (lane == 0) sums[warp] = total;
+      if (lane == 0) s.sums[warp] = total;
       __syncthreads();
       if (threadIdx.x == 0) {
-        for (int w = 1; w < warps; ++w) total += sums[w];
-        totals[b] = total;
+        for (int w = 1; w < warps; ++w) total += s.sums[w];
+        s.totals[b] = total;
       }
       __syncthreads();
     }
@@ -436,36 +493,70 @@ __global__ void k_beam_merge(SelectArgs a) {
   if (bad && threadIdx.x == 0) set_dev_error(a.err, DEVERR_LOGIT);
   if (threadIdx.x < a.keep) {
     const int64_t at = g * a.keep + threadIdx.x;
-    const Key k = first[threadIdx.x];
-    const int b = k ? from[threadIdx.x] >> 8 : 0, token = k ? tokens[b][from[threadIdx.x] & 255] : a.pad;
+    const Key k = s.first[threadIdx.x];
+    const int b = k ? s.from[threadIdx.x] >> 8 : 0, token = k ? s.tokens[b][s.from[threadIdx.x] & 255] : a.pad;
     a.parents[at] = b;
     a.tokens[at] = token;
     a.scores_out[at] = k ? static_cast<float>(score_of(k)) : -INFINITY;
-    if (a.done_out) a.done_out[at] = !k || (a.done && a.done[g * a.beams + b]) || token == a.eos;
+    if (a.done_out) a.done_out[at] = !k || ended(b) || token == a.eos;
   }
+}
+
+// Many rows: a CTA each, of which a group's last merges it, while others still read.  Few rows:
+// several CTAs each, and a merge of its own.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs a) {
+  grid_launch_next();
+  grid_wait();
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ bool last;
+  const int64_t r = blockIdx.x / a.slices, g = r / a.beams;
+  if (is_read(a, r)) scan_row<T>(a, *reinterpret_cast<Row*>(smem), r);
+  if (!a.arrived) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(&a.arrived[g], 1u) == static_cast<unsigned>(a.beams) - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  if (threadIdx.x == 0) a.arrived[g] = 0;  // for the next launch
+  merge_group<T>(a, *reinterpret_cast<Merge*>(smem), g);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(32 * kBeamsMax) k_beam_merge(SelectArgs a) {
+  grid_launch_next();
+  grid_wait();
+  extern __shared__ __align__(16) uint8_t smem[];
+  merge_group<T>(a, *reinterpret_cast<Merge*>(smem), blockIdx.x);
 }
 
 struct Plan {
   int slices, slice_len;
 };
-Plan plan_of(int64_t rows, int V, int keep, int num_sms) {
+Plan plan_of(int64_t rows, int V, int beams, int num_sms) {
   // few rows: as many slices as fill the GPU, of two chunks at least
-  const int64_t pairs = (static_cast<int64_t>(V) + 2 * kChunk - 1) / (2 * kChunk);
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({pairs, static_cast<int64_t>(num_sms) * kRowCtas / rows,
-                                                               kMergeList / list_most(keep)}));
+  const int64_t pairs = (static_cast<int64_t>(V) + 2 * kChunk - 1) / (2 * kChunk), room = static_cast<int64_t>(num_sms) * kRowCtas;
+  const int64_t limit = std::min<int64_t>(pairs, kMergeList / (beams * kListMost));
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(limit, room / rows));
   const int64_t len = (pairs + want - 1) / want * 2 * kChunk;
   return len >= V ? Plan{1, V} : Plan{static_cast<int>((V + len - 1) / len), static_cast<int>(len)};
 }
+
+constexpr int merge_bytes(int beams, int slices, int most) {
+  return static_cast<int>(sizeof(Merge)) + beams * slices * most * static_cast<int>(sizeof(Key));
+}
+static_assert(merge_bytes(kBeamsMax, 1, kListMost) <= kRowShared, "a group's last CTA merges it in its list's room");
 
 template <typename T>
 int launch_select(const SelectArgs& a, int groups, cudaStream_t s) {
   static_assert(kRowShared <= 48 * 1024, "no larger shared memory to ask for");
   cudaError_t e = launch_chained(k_beam_rows<T>, dim3(static_cast<unsigned>(groups) * a.beams * a.slices), kRowThreads, kRowShared, s, 1, a);
+  if (e != cudaSuccess || a.arrived) return e;
+  e = cudaFuncSetAttribute(k_beam_merge<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, merge_bytes(1, 1, kMergeList));
   if (e != cudaSuccess) return e;
-  const int smem = a.beams * a.slices * list_most(a.keep) * static_cast<int>(sizeof(Key));
-  e = cudaFuncSetAttribute(k_beam_merge<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBeamsMax * kMergeList * static_cast<int>(sizeof(Key)));
-  if (e != cudaSuccess) return e;
-  return launch_chained(k_beam_merge<T>, dim3(static_cast<unsigned>(groups)), 32 * std::max(4, a.beams), smem, s, 1, a);
+  return launch_chained(k_beam_merge<T>, dim3(static_cast<unsigned>(groups)), 32 * std::max(4, a.beams),
+                        merge_bytes(a.beams, a.slices, a.most), s, 1, a);
 }
 
 // ------------------------------------------------------------- reordering ---
@@ -528,18 +619,21 @@ int launch_reorder(ReorderArgs a, int64_t bytes, cudaStream_t s) {
 size_t beam_select_bytes(const BeamSelect& b, int num_sms) {
   if (b.groups <= 0) return 0;
   const int64_t rows = static_cast<int64_t>(b.groups) * b.beams;
-  return rows * plan_of(rows, b.V, b.keep, num_sms).slices * (list_most(b.keep) * sizeof(Key) + sizeof(float2) + sizeof(int));
+  const int slices = plan_of(rows, b.V, b.beams, num_sms).slices;
+  return rows * slices * (list_most(b.keep, slices) * sizeof(Key) + sizeof(float2) + sizeof(int));
 }
 
-int launch_beam_select(const BeamSelect& b, void* scratch, int* err, int num_sms, cudaStream_t s) {
+int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived, int* err, int num_sms, cudaStream_t s) {
   if (b.groups <= 0) return 0;
   const int64_t rows = static_cast<int64_t>(b.groups) * b.beams;
-  const Plan p = plan_of(rows, b.V, b.keep, num_sms);
+  const Plan p = plan_of(rows, b.V, b.beams, num_sms);
   const int64_t lists = rows * p.slices;
+  const int most = list_most(b.keep, p.slices);
   Key* keys = static_cast<Key*>(scratch);
-  float2* rests = reinterpret_cast<float2*>(keys + lists * list_most(b.keep));
-  const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, p.slices, p.slice_len, keys, rests,
-                     reinterpret_cast<int*>(rests + lists), b.parents, b.tokens, b.done_out, b.scores_out, err};
+  float2* rests = reinterpret_cast<float2*>(keys + lists * most);
+  const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, p.slices, p.slice_len, most, keys, rests,
+                     reinterpret_cast<int*>(rests + lists), p.slices == 1 && b.groups <= kSplitTasksMax ? arrived : nullptr,
+                     b.parents, b.tokens, b.done_out, b.scores_out, err};
   switch (b.type) {
     case LOGITS_F32: return launch_select<float>(a, b.groups, s);
     case LOGITS_F16: return launch_select<__half>(a, b.groups, s);

@@ -362,7 +362,8 @@ struct BeamSelect {
   int32_t* done_out;    // or null
 };
 size_t beam_select_bytes(const BeamSelect& b, int num_sms);  // scratch that the call takes (16-byte aligned)
-int launch_beam_select(const BeamSelect& b, void* scratch, int* err, int num_sms, cudaStream_t s);
+// arrived: kSplitTasksMax counters, zero between launches.
+int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived, int* err, int num_sms, cudaStream_t s);
 int launch_beam_reorder(const void* src, void* dst, int64_t bytes, int64_t pitch, int groups, int beams,
                         const int32_t* parents, int layers, int64_t layer_pitch, int* err, cudaStream_t s);
 
