@@ -7,6 +7,17 @@
 namespace aiq {
 namespace {
 
+// The block and KV head of a unit: a division of 64 bits costs as much as a quarter of a tile.
+__device__ __forceinline__ void unit_of(const CacheArgs& a, int64_t u, int64_t& block, int& head) {
+  if (a.units <= UINT32_MAX) {
+    block = static_cast<uint32_t>(u) / static_cast<uint32_t>(a.Hkv);
+    head = static_cast<int>(static_cast<uint32_t>(u) - static_cast<uint32_t>(block) * static_cast<uint32_t>(a.Hkv));
+  } else {
+    block = u / a.Hkv;
+    head = static_cast<int>(u % a.Hkv);
+  }
+}
+
 // A tile's keys: row(key) points at a token's HD elements (16-byte aligned; only keys
 // < n are read, the others are zeros).  Lane 4 g + t has 16 (HD 32: 8) elements of the
 // keys 8 j + g; their extents are halved over t, so that each lane makes one key's pair.
@@ -43,7 +54,7 @@ __device__ __forceinline__ bool quantize_keys(Row row, int n, uint8_t* tile) {
     uint32_t code[4][W / 4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const Group4 p = group4_of_pair(__shfl_sync(0xffffffffu, pair, lane & 28 | j));
+      const Group4 p = group4_of(mine, pair, lane & 28 | j);
 #pragma unroll
       for (int w = 0; w < W / 4; ++w) code[j][w] = codes4<8>(x[c][j] + 4 * w, p);
     }
@@ -98,7 +109,7 @@ __device__ __forceinline__ bool quantize_values(Row row, int n, uint8_t* tile) {
     *reinterpret_cast<uint32_t*>(tile + tile4_pair_at<HD>(key_of(g), true, c)) = pair;
     uint32_t code[8];  // byte i: elements 2 i and 2 i + 1
 #pragma unroll
-    for (int r = 0; r < 8; ++r) code[r] = codes4<2 * W>(x[c][r], group4_of_pair(__shfl_sync(0xffffffffu, pair, 4 * r + t)));
+    for (int r = 0; r < 8; ++r) code[r] = codes4<2 * W>(x[c][r], group4_of(mine, pair, 4 * r + t));
     uint32_t w[2][4];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {  // byte 2 e + h of word i: byte i of the key's
@@ -120,13 +131,14 @@ __device__ __forceinline__ bool quantize_values(Row row, int n, uint8_t* tile) {
 }
 
 template <int HD>
-__global__ void __launch_bounds__(kCacheWarps * 32) k_kv_quantize4(CacheArgs a, const __half* kv, int64_t ld, uint8_t* cache) {
+__global__ void __launch_bounds__(kCacheWarps * 32, HD == 128 ? 2 : HD == 64 ? 4 : 5) k_kv_quantize4(CacheArgs a, const __half* kv, int64_t ld, uint8_t* cache) {
   grid_launch_next();
   grid_wait();
   const int64_t u = static_cast<int64_t>(blockIdx.x) * kCacheWarps + (threadIdx.x >> 5);
   if (u >= a.units) return;
-  const int64_t b = u / a.Hkv;
-  const int h = static_cast<int>(u % a.Hkv);
+  int64_t b;
+  int h;
+  unit_of(a, u, b, h);
   const CacheBlock at = block_of(a, b);
   if (at.n == 0) return;
   const __half* k = kv + at.token * ld + h * HD;
@@ -143,8 +155,9 @@ __global__ void __launch_bounds__(kCacheWarps * 32) k_kv_dequantize4(CacheArgs a
   grid_wait();
   const int64_t u = static_cast<int64_t>(blockIdx.x) * kCacheWarps + (threadIdx.x >> 5);
   if (u >= a.units) return;
-  const int64_t b = u / a.Hkv;
-  const int h = static_cast<int>(u % a.Hkv);
+  int64_t b;
+  int h;
+  unit_of(a, u, b, h);
   const CacheBlock at = block_of(a, b);
   if (at.n == 0) return;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;

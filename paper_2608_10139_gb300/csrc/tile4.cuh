@@ -55,7 +55,7 @@ __host__ __device__ __forceinline__ int tile4_pair_at(int key, bool value, int c
 #ifdef __CUDACC__
 // A group's pair, and what its codes take.
 struct Group4 {
-  float m, s, inv, half;  // half: s / 2, or 1 where s is 0
+  float m, s, inv;  // inv: 1 / s and a little more, 0 where s is 0
   __device__ __forceinline__ uint32_t pair() const { return as_u32(__floats2half2_rn(s, m)); }  // (fp16 numbers both)
   __device__ __forceinline__ bool finite() const { return fabsf(m) <= 65504.f && s <= 65504.f; }
 };
@@ -70,17 +70,13 @@ __device__ __forceinline__ Group4 group4(float mn, float mx) {
   if (15.f * __half2float(h) < range) h = __ushort_as_half(__half_as_ushort(h) + 1);
   r.m = mn;
   r.s = __half2float(h);
-  r.inv = r.s > 0.f ? __fdividef(1.f, r.s) : 0.f;
-  r.half = r.s > 0.f ? 0.5f * r.s : 1.f;
+  r.inv = r.s > 0.f ? __fdividef(1.f, r.s) * (1.f + 0x1p-21f) : 0.f;
   return r;
 }
-__device__ __forceinline__ Group4 group4_of_pair(uint32_t pair) {
-  Group4 r;
-  r.m = __high2float(as_h2(pair));
-  r.s = __low2float(as_h2(pair));
-  r.inv = r.s > 0.f ? __fdividef(1.f, r.s) : 0.f;
-  r.half = r.s > 0.f ? 0.5f * r.s : 1.f;
-  return r;
+// A group that another lane made.
+__device__ __forceinline__ Group4 group4_of(const Group4& mine, uint32_t pair, int lane) {
+  const uint32_t x = __shfl_sync(0xffffffffu, pair, lane);
+  return Group4{__high2float(as_h2(x)), __low2float(as_h2(x)), __shfl_sync(0xffffffffu, mine.inv, lane)};
 }
 
 // The smallest and the largest element (negated) of N words of pairs; NaN where one is.
@@ -105,40 +101,71 @@ __device__ __forceinline__ void halve4(__half2* e, int lane_bit) {
   const bool upper = threadIdx.x & lane_bit;
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) {
-    const __half2 keep = upper ? e[i + N / 2] : e[i], give = upper ? e[i] : e[i + N / 2];
-    e[i] = __hmin2_nan(keep, as_h2(__shfl_xor_sync(0xffffffffu, as_u32(give), lane_bit)));
+    const uint32_t a = as_u32(e[i]), b = as_u32(e[i + N / 2]);  // (chosen as values: a choice of places would live in memory)
+    e[i] = __hmin2_nan(as_h2(upper ? b : a), as_h2(__shfl_xor_sync(0xffffffffu, upper ? a : b, lane_bit)));
   }
 }
 
-// The codes of N (4 or 8) elements, in order from the lowest bits.  d is rounded down: a
-// border between two codes, (n + 1/2) s, has 16 bits, so that d reaches it where the exact
-// difference does and not otherwise.  The nearest whole number of d / s, taken by a product
-// that is off by 2^-22, is right unless d lies next to a border; what is left over, exact
-// since |d - n s| < s and both have 24 bits from 2^-10 of s on, says so.
+// Pairs of 32-bit numbers, an instruction for both.
+struct Two {
+  uint64_t v;
+  Two() = default;
+  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Two(float2 x) : Two(x.x, x.y) {}
+  __device__ __forceinline__ float2 parts() const {
+    float2 x;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x.x), "=f"(x.y) : "l"(v));
+    return x;
+  }
+};
+__device__ __forceinline__ Two add_rd(Two a, Two b) {
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+  return a;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return a;
+}
+
+// The codes of N (2, 4 or 8) elements, in order from the lowest bits.  d = x - m is rounded down:
+// a border between two codes, (n + 1/2) s, has 16 bits, so that d reaches it where the exact
+// difference does and not otherwise.  The nearest whole number of d / s is taken by a product
+// that is 2^-22 to 2^-20 too large, so that halves go up; it is right unless d lies less than that
+// below a border.  What is left over, exact since |d - n s| < s and both have 24 bits from 2^-10
+// of s on, says so: it is then below -s / 2.
 template <int N>
 __device__ __forceinline__ uint32_t codes4(const uint32_t* x, const Group4& p) {
   constexpr float magic = 12582912.f;  // 3 * 2^22: the sum's last place is 1
-  uint32_t w = 0;
+  const Two low(-p.m, -p.m), inv(p.inv, p.inv), step(p.s, p.s), big(magic, magic), minus(-1.f, -1.f);
   float worst = 0.f;
+  Two n[N / 2] = {};  // the codes, negative
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float v = i & 1 ? __high2float(as_h2(x[i / 2])) : __low2float(as_h2(x[i / 2]));
-    const float d = __fsub_rd(v, p.m), y = fmaf(d, p.inv, magic);
-    worst = fmaxf(worst, fabsf(fmaf(magic - y, p.s, d)));
-    w += __float_as_uint(y) << (4 * i);
+  for (int i = 0; i < N / 2; ++i) {
+    const Two d = add_rd(Two(__half22float2(as_h2(x[i]))), low);
+    n[i] = fma2(fma2(d, inv, big), minus, big);
+    const float2 r = fma2(n[i], step, d).parts();
+    worst = fmaxf(fmaxf(worst, fabsf(r.x)), fabsf(r.y));
   }
-  w -= 0x4b400000u + (0x4b400000u << 4) + (0x4b400000u << 8);  // the magic's own bits, as far as they are within the word
-  if (worst >= p.half) {
-    w = 0;
+  const float half = 0.5f * p.s;
+  if (worst > half) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float v = i & 1 ? __high2float(as_h2(x[i / 2])) : __low2float(as_h2(x[i / 2]));
-      const float d = __fsub_rd(v, p.m), y = fmaf(d, p.inv, magic) - magic, r = fmaf(-y, p.s, d);
-      const float n = y + (r >= p.half ? 1.f : 0.f) - (r < -p.half ? 1.f : 0.f);
-      w |= (static_cast<uint32_t>(n) & 15u) << (4 * i);
+    for (int i = 0; i < N / 2; ++i) {
+      const float2 v = __half22float2(as_h2(x[i]));
+      float2 q = n[i].parts();
+      const auto right = [&](float v, float n) {
+        return fmaf(n, p.s, __fsub_rd(v, p.m)) < -half ? n + 1.f : n;
+      };
+      n[i] = Two(right(v.x, q.x), right(v.y, q.y));
     }
   }
-  return w;
+  // four codes are a number of 16 bits, the lowest ones of that and 2^23
+  const auto four = [&](Two a, Two b) {
+    const float2 v = fma2(b, Two(256.f, 256.f), a).parts();
+    return __float_as_uint(fmaf(v.y, -16.f, 8388608.f - v.x));
+  };
+  if constexpr (N == 8) return __byte_perm(four(n[0], n[1]), four(n[2], n[3]), 0x5410);
+  else if constexpr (N == 4) return four(n[0], n[1]) & 0xffffu;
+  else return four(n[0], Two(0.f, 0.f)) & 0xffu;
 }
 
 // Codes as fp16 numbers (n holds them) to m + n s, rounded once, at most 65504.
