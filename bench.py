@@ -73,7 +73,7 @@ def parse():
                    help="AI_TRANSFORM: greedy tokens per candidate row (0: the AI_IF query)")
     p.add_argument("--like", default="", help="AI_TRANSFORM ... LIKE pattern, comma-separated token ids")
     p.add_argument("--decode-rows", type=int, default=0, help="AI_TRANSFORM rows per decode batch (0: library default)")
-    p.add_argument("--kv-bits", type=int, default=16, choices=[8, 16], help="AI_TRANSFORM: bits of cached keys and values")
+    p.add_argument("--kv-bits", type=int, default=16, choices=[4, 8, 16], help="AI_TRANSFORM: bits of cached keys and values")
     p.add_argument("--top-k", type=int, default=0, help="AI_TRANSFORM: draw tokens from that many (0: greedy)")
     p.add_argument("--pairs", action="store_true", help="Table 2 Q4: AI_IF over the reviews self-joined on movie id")
     return p.parse_args()
@@ -697,7 +697,8 @@ def transform_bench(args):
     like = [int(x) for x in args.like.split(",")] if args.like else None
     if args.decode_rows:
         ctx.set_option("decode_rows", args.decode_rows)
-    ctx.set_option("kv_bits", args.kv_bits)
+    ctx.set_option("kv_bits", max(args.kv_bits, 8))
+    ctx.set_option("kv4", args.kv_bits == 4)
     draws = {}
     if args.top_k:
         u = np.random.default_rng(w.data_seed).random((w.n_rows, args.transform), dtype=np.float32)

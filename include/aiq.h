@@ -321,7 +321,12 @@ const char* aiq_last_error(void);
  * aiq_ops.h states; about half the reads of a decode step, and of the memory half for
  * whole blocks, while a row's open block takes 32 fp16 tokens a layer however few are
  * generated (texts of 137 tokens and 32 new ones: a third less, 2 new ones: a sixth);
- * logits differ by the rounding; up to 8 query heads per KV head), "device_bytes_max"
+ * logits differ by the rounding; up to 8 query heads per KV head), "kv4"
+ * (aiq_run_transform: 0, the default, or 1: cached keys and values in 4 bits, whatever
+ * kv_bits says, a scale and a smallest value for each token, KV head, keys / values and at
+ * most 64 elements, as aiq_ops.h states; 0.28 of the fp16 cache's memory and reads (head_dim 32:
+ * 0.31), with no open blocks; a generated token attends what the cache holds, itself
+ * among it; up to 8 query heads per KV head), "device_bytes_max"
  * (the context's device byte cap, as AIQ_DEVICE_BYTES_MAX at aiq_init; <= 0
  * lifts it; tables and models already held stay; a load or a query that finds no
  * room takes back the context's workspace, and a query runs again in the least

@@ -21,6 +21,7 @@
 #include "aiq_ops.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "tile4.cuh"
 #include "tile8.cuh"
 
 using namespace aiq;
@@ -198,7 +199,8 @@ struct aiq_ctx {
   // fp16 path's label-logit error reaches the 2e-2 parity tolerance
   int mlp_split = -1;
   int64_t decode_rows = 4096;  // generation: target rows per prefill chunk (= decode batch)
-  int kv_bits = 16;            // generation: bits of the cached keys and values
+  int kv_bits = 16;            // generation: bits of the cached keys and values (8, 16)
+  bool kv4 = false;            // generation: 4 bits instead
   std::vector<ProfRec> prof;
   std::vector<cudaEvent_t> ev_pool;
   std::map<std::string, StatAcc> stats;
@@ -611,18 +613,32 @@ aiq_status kv8_bufs(aiq_ctx* c, const aiq_model_config& g, const char* cache, co
   return AIQ_OK;
 }
 
+// A 4-bit cache of every layer: [L][blocks][Hkv] tiles.
+struct Kv4 {
+  uint8_t* cache = nullptr;
+  int64_t blocks = 0;
+  uint8_t* tiles(int l, const aiq_model_config& g) const {
+    return cache + l * blocks * g.n_kv_heads * tile4_bytes(g.head_dim);
+  }
+};
+aiq_status kv4_bufs(aiq_ctx* c, const aiq_model_config& g, const char* cache, int64_t blocks, Kv4* k) {
+  AIQ_TRY(ws(c, cache, std::max<int64_t>(blocks, 1) * g.n_layers * g.n_kv_heads * tile4_bytes(g.head_dim), &k->cache));
+  k->blocks = blocks;
+  return AIQ_OK;
+}
+
 // Decoder forward over one packed chunk of n_seqs sequences / T tokens.
 // The shared prefix that every sequence attends: its per-layer keys/values
 // pkv_in [L][P_in][2 Hkv hd], or, with prefix_first, the chunk's own first
 // sequence of P_in tokens.  kv_out (optional): where this pass stores the
-// keys/values of its first kv_rows tokens per layer; kv8_out (optional): the
-// 8-bit cache that takes those of all its tokens.
+// keys/values of its first kv_rows tokens per layer; kv8_out, kv4_out
+// (optional): the 8-bit or 4-bit cache that takes those of all its tokens.
 // rows_only_last: the final layer's O-projection and MLP run only on each
 // sequence's last token (the only position whose output reaches the label
 // head); the result lands in b.resid_last, rows in sequence order.
 aiq_status run_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, int64_t T, int64_t n_seqs, const __half* pkv_in,
                       int P_in, bool prefix_first, __half* kv_out, int64_t kv_rows, bool rows_only_last,
-                      const Kv8* kv8_out = nullptr) {
+                      const Kv8* kv8_out = nullptr, const Kv4* kv4_out = nullptr) {
   const aiq_model_config& g = m.cfg;
   const int d = g.d_model, hd = g.head_dim, Hq = g.n_heads, Hkv = g.n_kv_heads, f = g.d_ffn;
   const int nqkv = (Hq + 2 * Hkv) * hd;
@@ -662,10 +678,13 @@ aiq_status run_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, int64_t T, in
     e1.d_norm = static_cast<float>(d);
     e1.eps = g.rms_eps;
     AIQ_TRY(gemm(c, "gemm_qkv_rope", b.xn, d, L.wqkv, d, M, nqkv, d, m.bn_qkv, e1));
-    if (kv8_out) {
-      ProfScope p(c, "kv_quantize", 0, 3.0 * double(T) * ldkv);
-      const int e = launch_kv_quantize(b.qkv + Hq * hd, nqkv, T, b.seq_start, static_cast<int>(n_seqs), Hkv, hd,
-                                       kv8_out->tiles(l, g), kv8_out->pairs(l, g), c->d_err, c->stream);
+    if (kv8_out || kv4_out) {
+      ProfScope p(c, "kv_quantize", 0, (kv8_out ? 3.0 : 2.0 + tile4_bytes(hd) / (64.0 * hd)) * double(T) * ldkv);
+      const int n = static_cast<int>(n_seqs);
+      const int e = kv8_out ? launch_kv_quantize(b.qkv + Hq * hd, nqkv, T, b.seq_start, n, Hkv, hd, kv8_out->tiles(l, g),
+                                                 kv8_out->pairs(l, g), c->d_err, c->stream)
+                            : launch_kv_quantize4(b.qkv + Hq * hd, nqkv, T, b.seq_start, n, Hkv, hd, kv4_out->tiles(l, g),
+                                                  c->d_err, c->stream);
       counted(c, T > 0);
       if (e != 0)
         return fail(AIQ_ERR_CUDA, std::string("cache quantisation launch: ") +
@@ -808,6 +827,9 @@ struct DecodeBufs {
   bool bits8;
   Kv8 prefix8, own8, gen8;
   __half* tail;
+  // or the 4-bit cache, which has no open blocks
+  bool bits4;
+  Kv4 prefix4, own4, gen4;
   const int4* order;  // of the chunk's rows, for the attention; may be null
 };
 
@@ -903,7 +925,7 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
     {
       // keys read per row: P + len + slot + 1; summed over the rows: R (P + slot + 1) + Tc
       const double keys = double(R) * (P + slot + 1) + double(Tc);
-      const double per_key = d.bits8 ? ldkv * 1.0 : ldkv * 2.0;
+      const double per_key = ldkv * (d.bits4 ? tile4_bytes(hd) / (64.0 * hd) : d.bits8 ? 1.0 : 2.0);
       ProfScope p(c, "decode_attention", 4.0 * Hq * hd * keys,
                   keys * per_key + double(R) * (nqkv + Hq * hd + ldkv) * 2.0);
       int e;
@@ -915,6 +937,12 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
         float* partial = nullptr;
         if (const size_t floats = decode_q8_floats(q, c->num_sms)) AIQ_TRY(ws(c, "op.q8_partial", floats, &partial));
         e = launch_decode_attention_q8(q, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
+      } else if (d.bits4) {
+        const DecodeQ4 q{b.qkv, nqkv, R, 1, Hq, Hkv, hd, P ? d.prefix4.tiles(l, g) : nullptr, P, d.own4.tiles(l, g), Tc,
+                         b.seq_start, d.gen4.tiles(l, g), d.gcap, slot, b.att, nullptr, d.order};
+        float* partial = nullptr;
+        if (const size_t floats = decode_q4_floats(q, c->num_sms)) AIQ_TRY(ws(c, "op.q4_partial", floats, &partial));
+        e = launch_decode_attention_q4(q, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
       } else {
         e = launch_decode_attention(b.qkv, nqkv, R, Hq, Hkv, hd, pkv ? pkv + l * P * ldkv : nullptr, P,
                                     d.kvc + l * Tc * ldkv, b.seq_start,
@@ -956,19 +984,25 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
   return AIQ_OK;
 }
 
-// The order of a batch's rows for the attention over an 8-bit cache, or null.
-aiq_status q8_order(aiq_ctx* c, const DecodeQ8& d, bool once, const int4** order) {
+// The order of a batch's rows for the attention over an 8-bit or 4-bit cache: an int4 for
+// each of `rows` sequences, or null (0).
+aiq_status seq_order(aiq_ctx* c, const int32_t* seq_start, int rows, int64_t T, const int4** order) {
   *order = nullptr;
-  const int rows = decode_q8_order_rows(d, once, c->num_sms);
   if (!rows) return AIQ_OK;
   int4* o;
   AIQ_TRY(ws(c, "op.q8_order", rows, &o));
-  const int e = launch_decode_q8_order(d.seq_start, rows, d.T, o, c->d_err, c->stream);
+  const int e = launch_decode_q8_order(seq_start, rows, T, o, c->d_err, c->stream);
   counted(c, 1);
   if (e != 0)
     return fail(AIQ_ERR_CUDA, std::string("row order launch: ") + cudaGetErrorString(static_cast<cudaError_t>(e)));
   *order = o;
   return AIQ_OK;
+}
+aiq_status q8_order(aiq_ctx* c, const DecodeQ8& d, bool once, const int4** order) {
+  return seq_order(c, d.seq_start, decode_q8_order_rows(d, once, c->num_sms), d.T, order);
+}
+aiq_status q4_order(aiq_ctx* c, const DecodeQ4& d, bool once, const int4** order) {
+  return seq_order(c, d.seq_start, decode_q4_order_seqs(d, once, c->num_sms), d.T, order);
 }
 
 // max_new steps for the R rows of one chunk whose prefill just ran
@@ -980,6 +1014,11 @@ aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, DecodeBufs 
     DecodeQ8 q{};
     q.R = R, q.Hq = g.n_heads, q.Hkv = g.n_kv_heads, q.hd = g.head_dim, q.P = P, q.T = Tc, q.seq_start = b.seq_start;
     AIQ_TRY(q8_order(c, q, false, &d.order));
+  }
+  if (d.bits4 && gp->max_new > 1) {
+    DecodeQ4 q{};
+    q.R = R, q.beams = 1, q.Hq = g.n_heads, q.Hkv = g.n_kv_heads, q.hd = g.head_dim, q.P = P, q.T = Tc, q.seq_start = b.seq_start;
+    AIQ_TRY(q4_order(c, q, false, &d.order));
   }
   launch_patch_empty_rows(b.resid_last, b.last_compact, prefix_last, R, g.d_model, c->stream);
   {
@@ -1071,7 +1110,11 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
     const int64_t per_row = T / S + 1;
     const int64_t kv_row = 2 * int64_t(m.cfg.n_layers) * 2 * m.cfg.n_kv_heads * m.cfg.head_dim;  // bytes/token
     int64_t prompt_row = kv_row * per_row, gen_row = kv_row * std::max(gp->max_new - 1, 1);
-    if (c->kv_bits == 8) {
+    if (c->kv4) {
+      const int64_t block = int64_t(m.cfg.n_layers) * m.cfg.n_kv_heads * tile4_bytes(m.cfg.head_dim);
+      prompt_row = block * (per_row / AIQ_KV_BLOCK + 1);  // (a block more per row than its tokens need)
+      gen_row = block * ((gp->max_new + AIQ_KV_BLOCK - 1) / AIQ_KV_BLOCK);
+    } else if (c->kv_bits == 8) {
       // a block more per row than its tokens need, and the open block in fp16
       const int64_t block = int64_t(m.cfg.n_layers) * m.cfg.n_kv_heads * (tile8_bytes(m.cfg.head_dim) + 8);
       prompt_row = block * (per_row / AIQ_KV_BLOCK + 1);
@@ -1123,8 +1166,13 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
   if (gp) {
     AIQ_TRY(ensure_lm_f16(c, m));
     db.gcap = std::max(gp->max_new - 1, 1);
-    db.bits8 = c->kv_bits == 8;
-    if (db.bits8) {
+    db.bits4 = c->kv4;
+    db.bits8 = !c->kv4 && c->kv_bits == 8;
+    if (db.bits4) {
+      AIQ_TRY(kv4_bufs(c, g, "g.own4", tile8_blocks(Bmax, Rmax), &db.own4));
+      AIQ_TRY(kv4_bufs(c, g, "g.gen4", Rmax * ((db.gcap + AIQ_KV_BLOCK - 1) / AIQ_KV_BLOCK), &db.gen4));
+      AIQ_TRY(kv4_bufs(c, g, "g.prefix4", tile8_blocks(P, 1), &db.prefix4));
+    } else if (db.bits8) {
       AIQ_TRY(kv8_bufs(c, g, "g.own8", "g.own8s", tile8_blocks(Bmax, Rmax), &db.own8));
       AIQ_TRY(kv8_bufs(c, g, "g.gen8", "g.gen8s", Rmax * (db.gcap / AIQ_KV_BLOCK), &db.gen8));
       AIQ_TRY(kv8_bufs(c, g, "g.prefix8", "g.prefix8s", tile8_blocks(P, 1), &db.prefix8));
@@ -1149,7 +1197,8 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
     NvtxPhase pr("prefix");
     launch_pack_prefix(prefix_d, P, pb.tok, pb.pos, pb.seq_start, pb.last_idx, c->stream);
     counted(c, 1);
-    AIQ_TRY(run_layers(c, m, pb, P, 1, nullptr, 0, false, pkv, P, false, db.bits8 ? &db.prefix8 : nullptr));
+    AIQ_TRY(run_layers(c, m, pb, P, 1, nullptr, 0, false, pkv, P, false, db.bits8 ? &db.prefix8 : nullptr,
+                       db.bits4 ? &db.prefix4 : nullptr));
     CUDA_TRY(cudaMemcpyAsync(prefix_last, pb.resid + static_cast<int64_t>(P - 1) * g.d_model, g.d_model * sizeof(float),
                              cudaMemcpyDeviceToDevice, c->stream));
   }
@@ -1170,7 +1219,8 @@ aiq_status prefill_phase(aiq_ctx* c, const TableD& t, ModelD& m, const aiq_selec
     // generation keeps every layer's prompt keys/values of the chunk for the decode
     // steps; a first chunk keeps the prefix's for the chunks after it
     AIQ_TRY(run_layers(c, m, pb, tok0 + Tc, seq0 + r1 - r0, first ? nullptr : pkv, static_cast<int>(P), first,
-                       gp ? db.kvc : (first ? pkv : nullptr), gp ? Tc : P, true, db.bits8 ? &db.own8 : nullptr));
+                       gp ? db.kvc : (first ? pkv : nullptr), gp ? Tc : P, true, db.bits8 ? &db.own8 : nullptr,
+                       db.bits4 ? &db.own4 : nullptr));
     if (first)  // the final hidden state of the prefix's last token, for rows without text
       CUDA_TRY(cudaMemcpyAsync(prefix_last, pb.resid_last, g.d_model * sizeof(float), cudaMemcpyDeviceToDevice, c->stream));
     if (gp) {
@@ -1550,7 +1600,7 @@ aiq_status run_transform(aiq_ctx* c, const TableD& t, ModelD* m, const aiq_selec
     if (!gen->sampling || !gen->uniforms) return fail(AIQ_ERR_INVALID_ARG, "AIQ_GEN_SAMPLE needs sampling and uniforms");
     AIQ_TRY(check_sampling(*gen->sampling, V));
   }
-  if (c->kv_bits == 8 && m->cfg.n_heads / m->cfg.n_kv_heads > 8)
+  if ((c->kv_bits == 8 || c->kv4) && m->cfg.n_heads / m->cfg.n_kv_heads > 8)
     return fail(AIQ_ERR_UNSUPPORTED, "the 8-bit cache takes up to 8 query heads per KV head");
   PredSet ps{};
   AIQ_TRY(make_pred_set(t, q->preds, q->n_preds, &ps));
@@ -2207,6 +2257,11 @@ aiq_status aiq_set_option(aiq_ctx* c, const char* name, int64_t value) {
     c->decode_rows = value;
     return AIQ_OK;
   }
+  if (!std::strcmp(name, "kv4")) {
+    if (value != 0 && value != 1) return fail(AIQ_ERR_INVALID_ARG, "kv4 must be 0 or 1");
+    c->kv4 = value != 0;
+    return AIQ_OK;
+  }
   if (!std::strcmp(name, "kv_bits")) {
     if (value != 8 && value != 16) return fail(AIQ_ERR_INVALID_ARG, "kv_bits must be 8 or 16");
     c->kv_bits = static_cast<int>(value);
@@ -2435,10 +2490,11 @@ aiq_status aiq_op_decode_attention_q4(aiq_ctx* c, const void* qkv, int32_t R, in
   if (int64_t(R) * Hq > INT32_MAX) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^31 - 1 (row, head) pairs");
   if (R == 0) return AIQ_OK;
   CUDA_TRY(cudaSetDevice(c->device));
-  const DecodeQ4 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, beams, Hq, Hkv,
+  DecodeQ4 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, beams, Hq, Hkv,
                    hd, static_cast<const uint8_t*>(prefix_cache), P, static_cast<const uint8_t*>(own_cache), T, seq_start,
                    static_cast<uint8_t*>(gen_cache), gen_cap, slot, static_cast<__half*>(out), static_cast<__half*>(held),
                    nullptr};
+  AIQ_TRY(with_room(c, [&] { return q4_order(c, d, true, &d.order); }));
   float* partial = nullptr;
   if (const size_t floats = decode_q4_floats(d, c->num_sms))
     AIQ_TRY(with_room(c, [&] { return ws(c, "op.q4_partial", floats, &partial); }));

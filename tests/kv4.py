@@ -181,3 +181,32 @@ def select(z, scores, done, keep, eos, pad):
     out += [(0, pad, -np.inf, 1)] * (keep - len(out))
     p, t, s, d = zip(*out)
     return np.array(p), np.array(t), np.array(s), np.array(d)
+
+
+def logits_on_4_bits(m, prefix, text, generated):
+    """Vocabulary logits [len(generated) + 1, V] of an oracle model for the steps that
+    follow prefix ++ text, teacher-forced on `generated`, where a generated token attends
+    the 4-bit cache, itself among it.  (Keys and values are rounded to fp16 first, as they
+    are before they are quantised.)"""
+    from oracle import transformer as tf
+    s, n0 = m.s, len(prefix) + len(text)
+    ids = np.concatenate([prefix, text, generated]).astype(np.int64)
+    n, pos = len(ids), np.arange(len(ids))
+    x = m.embed_rows(ids)
+    for l in range(s.n_layers):
+        w = {name: m.get(f"l{l}.{name}") for name in tf.LAYER_TENSORS}
+        h = tf.rmsnorm(x, w["attn_norm"], s.rms_eps)
+        q = tf.rope((h @ w["wq"].T).reshape(n, s.n_heads, s.head_dim), pos, s.rope_theta)
+        k = tf.rope((h @ w["wk"].T).reshape(n, s.n_kv_heads, s.head_dim), pos, s.rope_theta)
+        v = (h @ w["wv"].T).reshape(n, s.n_kv_heads, s.head_dim)
+        a = np.zeros((n, s.n_heads, s.head_dim))
+        a[:n0] = tf.causal_attention(q[:n0], k[:n0], v[:n0])
+        held = values(*quantize(np.stack([k, v], 1).astype(np.float16)))
+        one = np.ones(held.shape[:1] + held.shape[2:3])
+        for i in range(n0, n):
+            a[i], _ = attend(q[i], held[:i + 1, 0], held[:i + 1, 1], one[:i + 1], one[:i + 1])
+        x = x + a.reshape(n, -1) @ w["wo"].T
+        h = tf.rmsnorm(x, w["mlp_norm"], s.rms_eps)
+        x = x + (tf.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
+    h = tf.rmsnorm(x[n0 - 1:], m.get("final_norm"), s.rms_eps)
+    return h @ tf.bf16_to_f64(m.w["lm_head"]).T + tf.bf16_to_f64(m.w["lm_bias"])
