@@ -181,7 +181,7 @@ struct aiq_ctx {
   int64_t* h_pin = nullptr;  // pinned staging for control scalars
   int64_t* d_pin = nullptr;  // its device address
   bool tight = false;        // a call's second try: the routes that need the least device memory
-  // arrival counters, zero between launches: the tile-count scans', then those of kSplitTasksMax attention tasks
+  // arrival counters, zero between launches: the tile-count scans', then kArrivedMax of attention tasks and groups of beams
   unsigned int* d_arrived = nullptr;
   size_t bytes_max = SIZE_MAX;
   size_t bytes_used = 0;
@@ -309,7 +309,7 @@ aiq_status sync_and_check(aiq_ctx* c) {
   if (err) {
     *c->h_err = 0;  // no kernel is in flight
     // a kernel that gave up, or was given sequences that do not ascend, may have left counts behind
-    CUDA_TRY(cudaMemsetAsync(c->d_arrived, 0, (1 + kSplitTasksMax) * sizeof(unsigned int), c->stream));
+    CUDA_TRY(cudaMemsetAsync(c->d_arrived, 0, (1 + kArrivedMax) * sizeof(unsigned int), c->stream));
     if (err & (DEVERR_DUP_BUILD_KEY | DEVERR_SENTINEL_KEY))
       return fail(AIQ_ERR_INVALID_ARG, "join build keys must be unique and differ from INT64_MIN");
     if (err & DEVERR_HASH_FULL) return fail(AIQ_ERR_CAPACITY, "hash table probe sequence exhausted");
@@ -939,7 +939,7 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
         e = launch_decode_attention_q8(q, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
       } else if (d.bits4) {
         const DecodeQ4 q{b.qkv, nqkv, R, 1, Hq, Hkv, hd, P ? d.prefix4.tiles(l, g) : nullptr, P, d.own4.tiles(l, g), Tc,
-                         b.seq_start, d.gen4.tiles(l, g), d.gcap, slot, b.att, nullptr, d.order};
+                         b.seq_start, d.gen4.tiles(l, g), d.gcap, slot, b.att, nullptr};
         float* partial = nullptr;
         if (const size_t floats = decode_q4_floats(q, c->num_sms)) AIQ_TRY(ws(c, "op.q4_partial", floats, &partial));
         e = launch_decode_attention_q4(q, partial, c->d_arrived + 1, c->d_err, c->num_sms, c->stream);
@@ -984,25 +984,19 @@ aiq_status decode_layers(aiq_ctx* c, ModelD& m, const PrefillBufs& b, const Deco
   return AIQ_OK;
 }
 
-// The order of a batch's rows for the attention over an 8-bit or 4-bit cache: an int4 for
-// each of `rows` sequences, or null (0).
-aiq_status seq_order(aiq_ctx* c, const int32_t* seq_start, int rows, int64_t T, const int4** order) {
+// The order of a batch's rows for the attention over an 8-bit cache, or null.
+aiq_status q8_order(aiq_ctx* c, const DecodeQ8& d, bool once, const int4** order) {
   *order = nullptr;
+  const int rows = decode_q8_order_rows(d, once, c->num_sms);
   if (!rows) return AIQ_OK;
   int4* o;
   AIQ_TRY(ws(c, "op.q8_order", rows, &o));
-  const int e = launch_decode_q8_order(seq_start, rows, T, o, c->d_err, c->stream);
+  const int e = launch_decode_q8_order(d.seq_start, rows, d.T, o, c->d_err, c->stream);
   counted(c, 1);
   if (e != 0)
     return fail(AIQ_ERR_CUDA, std::string("row order launch: ") + cudaGetErrorString(static_cast<cudaError_t>(e)));
   *order = o;
   return AIQ_OK;
-}
-aiq_status q8_order(aiq_ctx* c, const DecodeQ8& d, bool once, const int4** order) {
-  return seq_order(c, d.seq_start, decode_q8_order_rows(d, once, c->num_sms), d.T, order);
-}
-aiq_status q4_order(aiq_ctx* c, const DecodeQ4& d, bool once, const int4** order) {
-  return seq_order(c, d.seq_start, decode_q4_order_seqs(d, once, c->num_sms), d.T, order);
 }
 
 // max_new steps for the R rows of one chunk whose prefill just ran
@@ -1014,11 +1008,6 @@ aiq_status decode_chunk(aiq_ctx* c, ModelD& m, const PrefillBufs& b, DecodeBufs 
     DecodeQ8 q{};
     q.R = R, q.Hq = g.n_heads, q.Hkv = g.n_kv_heads, q.hd = g.head_dim, q.P = P, q.T = Tc, q.seq_start = b.seq_start;
     AIQ_TRY(q8_order(c, q, false, &d.order));
-  }
-  if (d.bits4 && gp->max_new > 1) {
-    DecodeQ4 q{};
-    q.R = R, q.beams = 1, q.Hq = g.n_heads, q.Hkv = g.n_kv_heads, q.hd = g.head_dim, q.P = P, q.T = Tc, q.seq_start = b.seq_start;
-    AIQ_TRY(q4_order(c, q, false, &d.order));
   }
   launch_patch_empty_rows(b.resid_last, b.last_compact, prefix_last, R, g.d_model, c->stream);
   {
@@ -1895,8 +1884,8 @@ aiq_status aiq_init(int device, aiq_ctx** out) {
   }
   if (e == cudaSuccess) e = cudaHostAlloc(&c->h_pin, 64 * sizeof(int64_t), cudaHostAllocMapped);
   if (e == cudaSuccess) e = cudaHostGetDevicePointer(&c->d_pin, c->h_pin, 0);
-  if (e == cudaSuccess) e = cudaMalloc(&c->d_arrived, (1 + kSplitTasksMax) * sizeof(unsigned int));
-  if (e == cudaSuccess) e = cudaMemsetAsync(c->d_arrived, 0, (1 + kSplitTasksMax) * sizeof(unsigned int), c->stream);
+  if (e == cudaSuccess) e = cudaMalloc(&c->d_arrived, (1 + kArrivedMax) * sizeof(unsigned int));
+  if (e == cudaSuccess) e = cudaMemsetAsync(c->d_arrived, 0, (1 + kArrivedMax) * sizeof(unsigned int), c->stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -2490,11 +2479,9 @@ aiq_status aiq_op_decode_attention_q4(aiq_ctx* c, const void* qkv, int32_t R, in
   if (int64_t(R) * Hq > INT32_MAX) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^31 - 1 (row, head) pairs");
   if (R == 0) return AIQ_OK;
   CUDA_TRY(cudaSetDevice(c->device));
-  DecodeQ4 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, beams, Hq, Hkv,
+  const DecodeQ4 d{static_cast<const __half*>(qkv), static_cast<int64_t>(Hq + 2 * int64_t(Hkv)) * hd, R, beams, Hq, Hkv,
                    hd, static_cast<const uint8_t*>(prefix_cache), P, static_cast<const uint8_t*>(own_cache), T, seq_start,
-                   static_cast<uint8_t*>(gen_cache), gen_cap, slot, static_cast<__half*>(out), static_cast<__half*>(held),
-                   nullptr};
-  AIQ_TRY(with_room(c, [&] { return q4_order(c, d, true, &d.order); }));
+                   static_cast<uint8_t*>(gen_cache), gen_cap, slot, static_cast<__half*>(out), static_cast<__half*>(held)};
   float* partial = nullptr;
   if (const size_t floats = decode_q4_floats(d, c->num_sms))
     AIQ_TRY(with_room(c, [&] { return ws(c, "op.q4_partial", floats, &partial); }));

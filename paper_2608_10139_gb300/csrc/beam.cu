@@ -632,7 +632,7 @@ int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived
   Key* keys = static_cast<Key*>(scratch);
   float2* rests = reinterpret_cast<float2*>(keys + lists * most);
   const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, p.slices, p.slice_len, most, keys, rests,
-                     reinterpret_cast<int*>(rests + lists), p.slices == 1 && b.groups <= kSplitTasksMax ? arrived : nullptr,
+                     reinterpret_cast<int*>(rests + lists), p.slices == 1 && b.groups <= kArrivedMax ? arrived : nullptr,
                      b.parents, b.tokens, b.done_out, b.scores_out, err};
   switch (b.type) {
     case LOGITS_F32: return launch_select<float>(a, b.groups, s);

@@ -36,7 +36,6 @@ struct DecQ4Args {
   __half* out;        // [R][Hq HD]
   __half* held;       // [R][2 Hkv HD] or null
   int* err;
-  const int4* order;  // sequences, first tokens and lengths, long ones first; null: as they come
 };
 
 // d (+)= A B.
@@ -440,27 +439,20 @@ struct Attn4 {
 // A sequence's KV head and up to `wide` of its beams: its tiles are the prefix's, the
 // prompt's and, beam by beam, the generated tokens'.
 struct Task4 {
-  int at;        // the sequence's place
-  int inner;     // KV head + Hkv * (the first beam / wide)
   int seq, len;
   int64_t st;    // first prompt token
   int h, beams;  // KV head, number of beams
   int row;       // the first beam's
 };
 __device__ __forceinline__ int tiles_of(int keys) { return keys / kTileKeys + (keys % kTileKeys != 0); }
-__device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int at, int inner) {
-  Task4 t{at, inner, at, 0, 0, inner, a.beams, 0};
-  if (a.order) {
-    const int4 x = a.order[at];
-    t.seq = x.x, t.st = x.y, t.len = x.z;
-  } else {
-    const int64_t st = a.seq_start[at], end = a.seq_start[at + 1];
-    if (st < 0 || end < st || end > a.T)
-      set_dev_error(a.err, DEVERR_BOUNDS);
-    else
-      t.st = st, t.len = static_cast<int>(end - st);
-  }
-  t.row = t.seq * a.beams;
+// inner: KV head + Hkv * (the first beam / wide)
+__device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int seq, int inner) {
+  Task4 t{seq, 0, 0, inner, a.beams, seq * a.beams};
+  const int64_t st = a.seq_start[seq], end = a.seq_start[seq + 1];
+  if (st < 0 || end < st || end > a.T)
+    set_dev_error(a.err, DEVERR_BOUNDS);
+  else
+    t.st = st, t.len = static_cast<int>(end - st);
   if (a.wide < a.beams) {
     const int before = inner / a.Hkv * a.wide;
     t.h = inner % a.Hkv;
@@ -473,11 +465,12 @@ __device__ __forceinline__ Task4 task_of(const DecQ4Args& a, int at, int inner) 
 // What an entry of the ring is: one tile or two (kTwo, the first full) of a task, the number of
 // keys of the last, whether they are generated ones, and of which beam; whether the step's token
 // goes into it; the task's first and last entry.
-constexpr int kKeys = 63, kGenerated = 64, kAppend = 128, kBeamShift = 8, kFirst = 1 << 12, kLast = 1 << 13, kTwo = 1 << 14;
+constexpr int kKeys = 63, kGenerated = 64, kAppend = 128, kBeamShift = 8, kFirst = 1 << 12, kLast = 1 << 13, kTwo = 1 << 14,
+              kWhole = 1 << 15, kBeams = 1 << 16;  // (and the task's number of beams from there on)
 
 // A warp's ring of entries in shared memory, filled by bulk copies.
 struct __align__(16) Head4 {
-  int row, h, beams, info;
+  int row, h, range, info;
 };
 template <int HD, int STAGES>
 struct Ring4 {
@@ -507,7 +500,7 @@ struct Ring4 {
     __syncthreads();
   }
   // All lanes call; the slot must have been used up by every lane before.
-  __device__ __forceinline__ void issue(const uint8_t* tile, int64_t stride, const Task4& w, int info) {
+  __device__ __forceinline__ void issue(const uint8_t* tile, int64_t stride, const Task4& w, int range, int info) {
     const uint32_t at = put++ % STAGES, dst = smem_u32(slots + at * EB);
     asm volatile(  // one lane, by a predicate
         "{\n\t.reg .pred p, q;\n\t"
@@ -517,7 +510,7 @@ struct Ring4 {
         "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%6], %10;\n\t"
         "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%8], [%9], %7, [%6];\n\t"
         "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%12], [%13], %7, [%6];\n\t}" ::"r"(threadIdx.x & 31),
-        "r"(smem_u32(&heads[at])), "r"(w.row), "r"(w.h), "r"(w.beams), "r"(info), "r"(smem_u32(&full[at])), "r"(TB), "r"(dst),
+        "r"(smem_u32(&heads[at])), "r"(w.row), "r"(w.h), "r"(range), "r"(info + w.beams * kBeams), "r"(smem_u32(&full[at])), "r"(TB), "r"(dst),
         "l"(tile), "r"(info & kTwo ? EB : TB), "r"(EB), "r"(dst + TB), "l"(tile + stride)
         : "memory");
   }
@@ -578,10 +571,139 @@ struct Stream4 {
   static_assert(CTAS * (SMEM + 1024 + 64) <= 233472, "shared memory per SM");
 };
 
-// Many tasks: a persistent warp per task, the tiles of all its tasks as one stream
-// through its ring.
+constexpr int kTaskCost = 3;  // tiles that a task's own steps take as long as
+constexpr int kNear = 8;      // a border between ranges so many tiles from a task's end is taken to lie there
+// Where the tiles of an inner task's sequences lie on a line: sequence i's end at place(i + 1),
+// which its start in the packed cache gives without the lengths before it; the places before its
+// first tile stand for what a task costs beside its tiles.
+struct Line4 {
+  int none, more;  // the first sequence's block; places of a sequence beside its prompt's
+  __device__ __forceinline__ Line4(const DecQ4Args& a)
+      : none(a.seq_start[0] / kTileKeys), more(tiles_of(a.P) + a.wide * (a.slot / kTileKeys + 1) + kTaskCost) {}
+  __device__ __forceinline__ int place(const DecQ4Args& a, int i) const { return a.seq_start[i] / kTileKeys - none + i * (more + 1); }
+};
+// The last range that begins at a place or before it, and where a range begins.
+__device__ __forceinline__ int range_of(int place, int ranges, int all) {
+  return static_cast<int>(((place + int64_t(1)) * ranges - 1) / all);
+}
+// The border that a place so many tiles from a task's first makes in the task.
+__device__ __forceinline__ int cut_at(int tile, int tiles) {
+  return tile >= tiles ? tiles : tile <= kNear ? 0 : tile >= tiles - kNear ? tiles : tile;
+}
+__device__ __forceinline__ int range_at(int range, int ranges, int all) { return static_cast<int>(static_cast<int64_t>(all) * range / ranges); }
+
+// A task that several ranges have a part of: this warp's part, and, where it comes last, the merge.
 template <int HD, bool PAIRS>
-__global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_decode_q4_stream(DecQ4Args a, int64_t n_tasks) {
+__device__ __forceinline__ void pieces(const DecQ4Args& a, const Attn4<HD, PAIRS>& at, const Head4& x, int n_seqs, int ranges,
+                                       float* partial, unsigned int* arrived) {
+  using At = Attn4<HD, PAIRS>;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int seq = x.row / a.beams, beams = x.info / kBeams, columns = beams * a.G, most = a.wide * a.G, size = most * (HD + 2);
+  const int range = x.range, inner = x.h + (x.row - seq * a.beams) / a.wide * a.Hkv;
+  // the ranges of the task's first and last tile (where the starts do not ascend, anything within bounds will do)
+  const Line4 line(a);
+  const int all = line.place(a, n_seqs), end = line.place(a, seq + 1);
+  const int tiles = tiles_of(a.P) + tiles_of(a.seq_start[seq + 1] - a.seq_start[seq]) + beams * (a.slot / kTileKeys + 1);
+  const int first = min(max(range_of(end - tiles + kNear, ranges, all), 0), ranges - 1);
+  const int count = max(min(range_of(end - kNear - 1, ranges, all), ranges - 1) - first, 0) + 1;
+  // [inner][range][continued, continues]: maxima, sums, outputs of up to eight columns
+  const auto place = [&](int range) { return partial + ((static_cast<int64_t>(inner) * ranges + range) * 2 + (range == first)) * size; };
+  {
+    float* p = place(range);
+#pragma unroll
+    for (int j = 0; j < (PAIRS ? 1 : 2); ++j) {
+      const int e = PAIRS ? t >> 1 : j, column = PAIRS ? (2 * t & 3) + e : 2 * t + j;
+      if (column >= columns) continue;
+      if (g == 0) {
+        p[column] = e ? at.m[1] : at.m[0];
+        p[most + column] = e ? at.l[1] : at.l[0];
+      }
+#pragma unroll
+      for (int c = 0; c < At::C; ++c) {
+        float2* dst = reinterpret_cast<float2*>(p + 2 * most + column * HD + 64 * c + 2 * At::FR * g);
+#pragma unroll
+        for (int i = 0; i < At::FR; ++i) dst[i] = make_float2(at.o[c][i][j], at.o[c][i][2 + j]);
+      }
+    }
+  }
+  __threadfence();
+  __syncwarp();
+  unsigned int before = 0;
+  unsigned int* counter = arrived + inner * ranges + first;
+  if (lane == 0) before = atomicAdd(counter, 1u);
+  if (__shfl_sync(0xffffffffu, before, 0) != static_cast<unsigned>(count) - 1) return;
+  __threadfence();
+  if (lane == 0) *counter = 0;  // for the next launch
+  bool fine = true;
+  const auto row_of = [&](int column) {
+    return a.out + (static_cast<int64_t>(x.row + column / a.G) * a.Hq + x.h * a.G + column % a.G) * HD + lane;
+  };
+  if (columns * count <= 32) {  // a lane for each column's part: what is to be read is asked for in two rounds
+    const int column = lane % columns, j = lane / columns;
+    float m = At::kLow, l = 0.f;
+    if (j < count) {
+      m = __ldcg(place(first + j) + column);
+      l = __ldcg(place(first + j) + most + column);
+    }
+    float M = m;
+    for (int k = 0; k < count; ++k) M = fmaxf(M, __shfl_sync(0xffffffffu, m, k * columns + column));
+    const float w = exp2_approx(m - M);
+    float L = 0.f;
+    for (int k = 0; k < count; ++k) L += __shfl_sync(0xffffffffu, w * l, k * columns + column);
+    const float share = __fdividef(w, L);
+    const int n = columns * (HD / 32);
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) {
+      const int c = k / (HD / 32);
+      float v = 0.f;
+      for (int j = 0; j < count; ++j)
+        v = fmaf(__ldcg(place(first + j) + 2 * most + 32 * k + lane), __shfl_sync(0xffffffffu, share, j * columns + c), v);
+      fine = fine && fabsf(v) <= 65504.f;
+      row_of(c)[k % (HD / 32) * 32] = __float2half_rn(v);
+    }
+  } else {
+    for (int column = 0; column < columns; ++column) {
+      float M = At::kLow, L = 0.f, O[HD / 32];
+      for (int j = lane; j < count; j += 32) M = fmaxf(M, __ldcg(place(first + j) + column));
+#pragma unroll
+      for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) O[k] = 0.f;
+      for (int j0 = 0; j0 < count; j0 += 32) {
+        float w = 0.f;
+        if (j0 + lane < count) {
+          const float* p = place(first + j0 + lane);
+          w = exp2_approx(__ldcg(p + column) - M);
+          L += __ldcg(p + most + column) * w;
+        }
+#pragma unroll 8
+        for (int j = 0; j < min(32, count - j0); ++j) {
+          const float* p = place(first + j0 + j) + 2 * most + column * HD + lane;
+          const float f = __shfl_sync(0xffffffffu, w, j);
+#pragma unroll
+          for (int k = 0; k < HD / 32; ++k) O[k] = fmaf(__ldcg(p + 32 * k), f, O[k]);
+        }
+      }
+      L = warp_sum(L);
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) {
+        const float v = O[k] / L;
+        fine = fine && fabsf(v) <= 65504.f;
+        row_of(column)[32 * k] = __float2half_rn(v);
+      }
+    }
+  }
+  if (!fine) set_dev_error(a.err, DEVERR_FP16_RANGE);
+}
+
+// Many tasks: a warp takes the tiles of all its tasks as one stream through its ring.  Where there
+// are many tasks a warp, they are dealt out.  Of fewer (RANGES) the longest would be waited for:
+// the line of an inner task's tiles is cut into `ranges` of equal length, a warp each.  A task that
+// lies within a range is the warp's alone; of one that does not, each warp leaves its (maximum, sum,
+// output), and the last to arrive merges them in their order.
+template <int HD, bool PAIRS, bool RANGES>
+__global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
+    k_decode_q4_stream(DecQ4Args a, int n_seqs, int ranges, float* partial, unsigned int* arrived) {
   using S = Stream4<HD>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int abort_word;
@@ -591,58 +713,108 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
   grid_launch_next();
   grid_wait();
 
-  const int first = blockIdx.x * S::NW + warp;
-  // from a warp's task to its next: every other round of tasks is dealt out backwards, so that
-  // whoever had the longest gets the shortest
-  const int up = 2 * (static_cast<int>(gridDim.x) * S::NW - first) - 1, down = 2 * first + 1;
-  const int up_rows = up / a.inner, up_inner = up % a.inner, down_rows = down / a.inner, down_inner = down % a.inner;
-  bool odd = false;
+  // where the starts do not ascend, a sequence may be no warp's, which would have reported it
+  for (int64_t k = blockIdx.x * static_cast<int64_t>(S::NW * 32) + threadIdx.x; k < n_seqs; k += gridDim.x * static_cast<int64_t>(S::NW * 32))
+    if (a.seq_start[k] < 0 || a.seq_start[k + 1] < a.seq_start[k] || a.seq_start[k + 1] > a.T) set_dev_error(a.err, DEVERR_BOUNDS);
 
-  // the copies run ahead of the products by the ring's length, over the tasks' borders
-  int64_t pi = first;
+  const int first = blockIdx.x * S::NW + warp;
+  int inner = first % a.inner, i = first / a.inner;
+  const int range = i;
+  // By whole tasks: from a warp's to its next every other round is dealt out backwards, so that
+  // whoever had the longest gets the shortest.
+  int up_seqs, up_inner, down_seqs, down_inner;
+  bool odd = false, begun = false;
+  // By ranges: the warp's, and the sequence before the last whose places begin at its start or
+  // before, found 32 probes at a time.
+  int x0, x1;
+  if constexpr (!RANGES) {
+    const int up = 2 * (static_cast<int>(gridDim.x) * S::NW - first) - 1, down = 2 * first + 1;
+    up_seqs = up / a.inner, up_inner = up % a.inner, down_seqs = down / a.inner, down_inner = down % a.inner;
+  } else {
+    const Line4 line(a);
+    const int all = line.place(a, n_seqs);
+    x0 = range_at(range, ranges, all);
+    x1 = range_at(range + 1, ranges, all);
+    i = range < ranges ? 0 : n_seqs;
+    for (int hi = n_seqs; hi - i > 1;) {
+      const int step = (hi - i + 31) / 32, k = i + lane * step;
+      const uint32_t found = __ballot_sync(0xffffffffu, k < hi && line.place(a, k) <= x0);
+      if (found) i += (31 - __clz(found)) * step;
+      hi = i + step < hi ? i + step : hi;
+    }
+    --i;
+  }
+  // the copies run ahead of the products by the ring's length
   Task4 pt{};
   const int64_t stride = static_cast<int64_t>(a.Hkv) * tile4_bytes(HD);
+  const int np = tiles_of(a.P), ng = a.slot / kTileKeys + 1;
   const uint8_t* tile = nullptr;
-  int run = -1, left = 0, info = 0;  // prefix, prompt, the beams' tokens; keys left of the run that `tile` is in, what they are
-  const auto next_run = [&] {  // one that has keys; left is 0 behind the last task's
-    while (left == 0) {
-      if (++run == pt.beams + 2) {
-        pi += odd ? down : up;
-        if (pi >= n_tasks) return;
-        const int inner = pt.inner + (odd ? down_inner : up_inner);
-        const bool carry = inner >= a.inner;
-        pt = task_of(a, pt.at + (odd ? down_rows : up_rows) + carry, inner - (carry ? a.inner : 0));
-        odd = !odd;
-        run = 0;
+  int t0 = 0, t1 = 0;                 // the warp's tiles of the task that are still to be asked for
+  int left = 0, info = 0, runs = 0;   // keys left of the run that `tile` is in, what they are, and where it ends
+  const auto next_run = [&] {         // left is 0 behind the last task's
+    while (t0 >= t1) {
+      if constexpr (!RANGES) {
+        if (begun) {
+          inner += odd ? down_inner : up_inner;
+          const bool carry = inner >= a.inner;
+          inner -= carry ? a.inner : 0;
+          i += (odd ? down_seqs : up_seqs) + carry;
+          odd = !odd;
+        }
+        begun = true;
+        if (i >= n_seqs) return;
+      } else if (++i >= n_seqs || Line4(a).place(a, i) >= x1) {
+        i = n_seqs;
+        return;
       }
-      if (run == 0) info = kFirst;
-      const uint8_t* from = run == 0 ? a.pc : run == 1 ? a.oc : a.gc;
-      const int64_t block = run == 0 ? 0 : run == 1 ? tile8_first_block(pt.st, pt.seq) : (pt.row + run - 2) * a.gen_blocks;
-      left = run == 0 ? a.P : run == 1 ? pt.len : a.slot + 1;
-      info = info & kFirst | (run >= 2 ? kGenerated | (run - 2) << kBeamShift : 0);
-      tile = from + (block * a.Hkv + pt.h) * tile4_bytes(HD);
+      pt = task_of(a, i, inner);
+      const int tiles = np + tiles_of(pt.len) + pt.beams * ng;
+      t0 = 0, t1 = tiles;
+      if constexpr (RANGES) {
+        const int at = Line4(a).place(a, i + 1) - tiles;  // the first tile's
+        t0 = cut_at(x0 - at, tiles);
+        t1 = cut_at(x1 - at, tiles);
+      }
+      info = kFirst | (t0 == 0 && t1 == tiles ? kWhole : 0);
     }
+    // the run that t0 is in: prefix, prompt, a beam's tokens
+    const int no = tiles_of(pt.len);
+    const uint8_t* from;
+    int64_t block;
+    int begin, keys;
+    info &= kFirst | kWhole;
+    if (t0 < np) {
+      from = a.pc, block = 0, begin = 0, keys = a.P, runs = np;
+    } else if (t0 < np + no) {
+      from = a.oc, block = tile8_first_block(pt.st, pt.seq), begin = np, keys = pt.len, runs = np + no;
+    } else {
+      const int b = ng == 1 ? t0 - np - no : (t0 - np - no) / ng;
+      from = a.gc, block = (pt.row + b) * a.gen_blocks, begin = np + no + b * ng, keys = a.slot + 1, runs = begin + ng;
+      info |= kGenerated | b << kBeamShift;
+    }
+    left = min(keys, (t1 - begin) * kTileKeys) - (t0 - begin) * kTileKeys;
+    tile = from + ((block + t0 - begin) * a.Hkv + pt.h) * tile4_bytes(HD);
   };
   const auto produce = [&] {
     if (left > 2 * kTileKeys) {
-      ring.issue(tile, stride, pt, info | kTileKeys | kTwo);
+      ring.issue(tile, stride, pt, range, info | kTileKeys | kTwo);
       info &= ~kFirst;
       tile += 2 * stride;
+      t0 += 2;
       left -= 2 * kTileKeys;
-    } else if (left > 0) {  // a run's last
+    } else if (left > 0) {  // a run's last here
       const bool two = left > kTileKeys;
-      ring.issue(tile, stride, pt, info | (two ? left - kTileKeys | kTwo : left) | (run >= 2 ? kAppend : 0) | (run == pt.beams + 1 ? kLast : 0));
+      t0 += two ? 2 : 1;
+      ring.issue(tile, stride, pt, range, info | (two ? left - kTileKeys | kTwo : left) | ((info & kGenerated) && t0 == runs ? kAppend : 0) |
+                                       (t0 == t1 ? kLast : 0));
       info &= ~kFirst;
       left = 0;
       next_run();
     }
   };
-  if (pi < n_tasks) {
-    pt = task_of(a, first / a.inner, first % a.inner);
-    next_run();
-  }
+  next_run();
 #pragma unroll 1
-  for (int i = 0; i < S::STAGES; ++i) produce();
+  for (int k = 0; k < S::STAGES; ++k) produce();
 
   using At = Attn4<HD, PAIRS>;
   At at;
@@ -655,8 +827,8 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
   Token4<HD> token;
   token.place(a.slot % kTileKeys);
   const auto fetch = [&](const Head4& x) {
-    At::fetch(raw, query_of(a, HD, x.row, x.h, x.beams, my_beam, my_head));
-    token.load(key_of(a, HD, x.row, x.h), kd);
+    At::fetch(raw, query_of(a, HD, x.row, x.h, x.info / kBeams, my_beam, my_head));
+    token.load(key_of(a, HD, x.row + (x.info >> kBeamShift & 15), x.h), kd);
   };
   __syncwarp();  // the heads that lane 0 wrote
   if (ring.more()) fetch(ring.head());
@@ -668,12 +840,12 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
       if (x.info & kFirst) at.begin(raw, a.scale_log2);
       if (x.info & kAppend) {
         append<HD>(a, token, ring.slot() + (x.info & kTwo ? ring.TB : 0), x.row + b, x.h);
-        if (!(x.info & kLast)) token.load(key_of(a, HD, x.row + b + 1, x.h), kd);
+        if (b + 1 < x.info / kBeams) token.load(key_of(a, HD, x.row + b + 1, x.h), kd);
       }
       // the next task's queries are on their way while this one ends
       if ((x.info & kLast) && ring.got + 1 != ring.put) fetch(ring.head(1));
     }
-    const bool some = (x.info & kGenerated) && x.beams > 1;
+    const bool some = (x.info & kGenerated) && x.info / kBeams > 1;
     const uint8_t* tile = ring.slot();
     int two = x.info & kTwo;
 #pragma unroll 1
@@ -689,9 +861,15 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS) k_dec
     produce();
     if (!(x.info & kLast)) continue;
     at.finish();
+    if constexpr (RANGES) {
+      if (!(x.info & kWhole)) {
+        pieces<HD, PAIRS>(a, at, x, n_seqs, ranges, partial, arrived);
+        continue;
+      }
+    }
     bool fine = true;
     const auto store = [&](int beam, int head, int e, float l) {
-      if (head < 0 || beam >= x.beams) return;
+      if (head < 0 || beam >= x.info / kBeams) return;
       const float inv = __fdividef(1.f, l);
       __half* to = a.out + (static_cast<int64_t>(x.row + beam) * a.Hq + x.h * a.G + head) * HD + 2 * At::FR * g;
       __half2 big = as_h2(0u);
@@ -801,7 +979,7 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
       tile = a.oc, block = tile8_first_block(w.st, w.seq) + (pe - np);
       info = min(kTileKeys, w.len - (pe - np) * kTileKeys);
     }
-    ring.issue(tile + (block * a.Hkv + w.h) * tile4_bytes(HD), 0, w, info);
+    ring.issue(tile + (block * a.Hkv + w.h) * tile4_bytes(HD), 0, w, 0, info);
     pe += S::NW;
   };
 #pragma unroll 1
@@ -931,21 +1109,36 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
 }
 
 // How a call runs: beams of a task, tasks of a sequence, and CTAs per inner task (at
-// least one a sequence; 0: a warp per task).
+// least one a sequence; 0: a warp's tasks are a range of the line, of which there are `ranges`, or,
+// where that is 0 too, dealt out).
 struct Plan {
-  int wide, inner, units;
+  int wide, inner, units, ranges;
   int64_t seqs;
   double tiles;  // of an inner task, over all sequences
 };
 template <int HD>
-int units_of(const Plan& p, int num_sms) {
+void cut(Plan& p, int64_t least, int64_t most_places, int num_sms) {
   using S = Stream4<HD>;
   const int64_t ctas = static_cast<int64_t>(num_sms) * S::CTAS, tasks = p.seqs * p.inner;
+  p.units = p.ranges = 0;
+  // Calls from a cold cache, dealt out, by ranges and by CTAs, in us (8 KV heads of 4, head_dim 64, a
+  // prefix of 64): 64 texts of about 60 tokens 29, 30, 27, of 700 68, 51, 39; 130 of 60 31, 32, 32, of
+  // 350 52, 45, 44; 260 of 60 35, 35, 44, of 700 86, 68, 68; 500 of 60 41, 43, 61, of 350 75, 68, 82;
+  // 1,000 of 60 58, 61, 98, of 350 114, 102, 138; 3,263 of 120 147, 151, 287.  head_dim 128: 130 of
+  // 350 72, 60, 58; 260 of 200 69, 60, 67, of 700 149, 104, 97; 500 of 350 129, 104, 120; 2,000 of 200
+  // 218, 206, 330.  head_dim 64, four beams a text: 50 of 200 41, 51, 39; 100 of 1,000 113, 82, 88.
+  // A CTA per task costs its start and its merge, a warp per task the time of the longest ones.
   const double per_task = p.tiles / p.seqs, rounds = static_cast<double>(tasks) / ctas;
-  if (per_task <= std::min(4.5 * rounds, 2.2 * rounds + 4)) return 0;
-  if (tasks > kSplitTasksMax) return static_cast<int>(p.seqs);
+  if (rounds >= 5 || per_task <= 5 * rounds) {
+    // a range is a tile at least, so that each has a part of a task that others have parts of
+    if (per_task >= std::max(10.0, 1.2 * rounds / S::NW) && most_places <= INT32_MAX)
+      p.ranges = static_cast<int>(std::min<int64_t>({ctas * S::NW / p.inner, least, kArrivedMax / p.inner}));
+    return;
+  }
+  p.units = static_cast<int>(p.seqs);
+  if (tasks > kSplitTasksMax) return;
   const int64_t most = static_cast<int64_t>(p.tiles / (4 * Split4<HD>::NW));
-  return static_cast<int>(std::max<int64_t>(p.seqs, std::min<int64_t>({ctas / p.inner, most, p.seqs + kMaxRanges - 1})));
+  p.units = static_cast<int>(std::max<int64_t>(p.seqs, std::min<int64_t>({ctas / p.inner, most, p.seqs + kMaxRanges - 1})));
 }
 Plan plan_of(const DecodeQ4& d, int num_sms) {
   Plan p;
@@ -953,25 +1146,31 @@ Plan plan_of(const DecodeQ4& d, int num_sms) {
   p.wide = std::min(d.beams, 8 / G);
   p.inner = d.Hkv * ((d.beams + p.wide - 1) / p.wide);
   p.seqs = d.R / d.beams;
-  p.tiles = d.T / 32.0 + 0.5 * p.seqs + static_cast<double>(p.seqs) * (d.P / 32 + p.wide * (d.slot / 32 + 1));
-  p.units = d.hd == 32 ? units_of<32>(p, num_sms) : d.hd == 64 ? units_of<64>(p, num_sms) : units_of<128>(p, num_sms);
+  const int64_t more = (d.P + 31) / 32 + static_cast<int64_t>(p.wide) * (d.slot / 32 + 1);
+  p.tiles = d.T / 32.0 + 0.5 * p.seqs + static_cast<double>(p.seqs) * more;
+  const int64_t least = p.seqs * (more + kTaskCost);
+  const int64_t most_places = d.T / 32 + (p.seqs + 1) * (more + kTaskCost + 1);
+  d.hd == 32   ? cut<32>(p, least, most_places, num_sms)
+  : d.hd == 64 ? cut<64>(p, least, most_places, num_sms)
+               : cut<128>(p, least, most_places, num_sms);
   return p;
 }
 
 template <int HD, bool PAIRS>
 int launch_pairs(const DecQ4Args& a, const Plan& p, float* partial, unsigned int* arrived, int num_sms, cudaStream_t s) {
+  const int seqs = static_cast<int>(p.seqs);
   if (p.units == 0) {
     using S = Stream4<HD>;
-    const cudaError_t e = cudaFuncSetAttribute(k_decode_q4_stream<HD, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    void (*kernel)(DecQ4Args, int, int, float*, unsigned int*) = p.ranges ? k_decode_q4_stream<HD, PAIRS, true> : k_decode_q4_stream<HD, PAIRS, false>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess) return e;
-    return launch_chained(k_decode_q4_stream<HD, PAIRS>, dim3(static_cast<unsigned>(num_sms * S::CTAS)), S::NW * 32, S::SMEM, s, 1,
-                          a, p.seqs * p.inner);
+    return launch_chained(kernel, dim3(static_cast<unsigned>(num_sms * S::CTAS)), S::NW * 32, S::SMEM, s, 1, a, seqs, p.ranges, partial, arrived);
   }
   using S = Split4<HD>;
   const cudaError_t e = cudaFuncSetAttribute(k_decode_q4_split<HD, PAIRS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
   if (e != cudaSuccess) return e;
   return launch_chained(k_decode_q4_split<HD, PAIRS>, dim3(static_cast<unsigned>(p.units) * a.inner), S::NW * 32, S::SMEM, s, 1, a,
-                        static_cast<int>(p.seqs), p.units, partial, arrived);
+                        seqs, p.units, partial, arrived);
 }
 
 }  // namespace
@@ -979,13 +1178,8 @@ int launch_pairs(const DecQ4Args& a, const Plan& p, float* partial, unsigned int
 size_t decode_q4_floats(const DecodeQ4& d, int num_sms) {
   if (d.R <= 0) return 0;
   const Plan p = plan_of(d, num_sms);
-  return p.units <= p.seqs ? 0 : static_cast<size_t>(p.units) * p.inner * p.wide * (d.Hq / d.Hkv) * (d.hd + 2);
-}
-
-int decode_q4_order_seqs(const DecodeQ4& d, bool once, int num_sms) {
-  (void)once;
-  if (d.R <= 0 || plan_of(d, num_sms).units != 0) return 0;
-  return 0;
+  const size_t parts = p.units == 0 ? (p.ranges > 1 ? 2 * static_cast<size_t>(p.ranges) : 0) : p.units <= p.seqs ? 0 : p.units;
+  return parts * p.inner * p.wide * (d.Hq / d.Hkv) * (d.hd + 2);
 }
 
 int launch_decode_attention_q4(const DecodeQ4& d, float* partial, unsigned int* arrived, int* err, int num_sms,
@@ -994,7 +1188,7 @@ int launch_decode_attention_q4(const DecodeQ4& d, float* partial, unsigned int* 
   const Plan p = plan_of(d, num_sms);
   const DecQ4Args a{d.qkv, d.ldq, d.Hq, d.Hkv, d.Hq / d.Hkv, d.beams, p.wide, p.inner, d.prefix, d.P, d.own, d.T, d.seq_start,
                     d.gen, (d.gen_cap + kTileKeys - 1) / kTileKeys, d.slot,
-                    1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, d.held, err, p.units ? nullptr : d.order};
+                    1.4426950408889634f / sqrtf(static_cast<float>(d.hd)), d.out, d.held, err};
   const bool pairs = p.wide * a.G <= 4;
   switch (d.hd) {
     case 32: return (pairs ? launch_pairs<32, true> : launch_pairs<32, false>)(a, p, partial, arrived, num_sms, s);

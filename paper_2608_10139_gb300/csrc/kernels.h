@@ -309,6 +309,7 @@ struct DecodeQ8 {
 // Workspace that the call takes, in floats (few rows: partial states of ranges of keys).
 size_t decode_q8_floats(const DecodeQ8& d, int num_sms);
 constexpr int kSplitTasksMax = 1024;
+constexpr int kArrivedMax = 4096;  // arrival counters of a context, zero between launches
 // The order in which many rows of different lengths keep the GPU evenly busy: an int4
 // per row, as many as decode_q8_order_rows says (0: the call does without).  once: it is
 // made for one call, not for all layers and steps of a batch.
@@ -339,11 +340,9 @@ struct DecodeQ4 {
   int gen_cap, slot;
   __half* out;
   __half* held;  // [R][2 Hkv hd] the step's key and value as the cache holds them, or null
-  const int4* order;  // of the sequences, as launch_decode_q8_order writes it, or null
 };
-// As decode_q8_floats, decode_q8_order_rows (sequences here) and launch_decode_attention_q8.
+// As decode_q8_floats and launch_decode_attention_q8; kArrivedMax counters.
 size_t decode_q4_floats(const DecodeQ4& d, int num_sms);
-int decode_q4_order_seqs(const DecodeQ4& d, bool once, int num_sms);
 int launch_decode_attention_q4(const DecodeQ4& d, float* partial, unsigned int* arrived, int* err, int num_sms,
                                cudaStream_t s);
 
@@ -362,7 +361,7 @@ struct BeamSelect {
   int32_t* done_out;    // or null
 };
 size_t beam_select_bytes(const BeamSelect& b, int num_sms);  // scratch that the call takes (16-byte aligned)
-// arrived: kSplitTasksMax counters, zero between launches.
+// arrived: kArrivedMax counters, zero between launches.
 int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived, int* err, int num_sms, cudaStream_t s);
 int launch_beam_reorder(const void* src, void* dst, int64_t bytes, int64_t pitch, int groups, int beams,
                         const int32_t* parents, int layers, int64_t layer_pitch, int* err, cudaStream_t s);
