@@ -9,6 +9,7 @@
 #include "candidates.cuh"
 #include "common.cuh"
 #include "kernels.h"
+#include "pairs32.cuh"
 
 namespace aiq {
 namespace {
@@ -104,6 +105,41 @@ struct Exp3 {
   }
   __device__ __forceinline__ float sum() const { return h + (m + l); }
   __device__ __forceinline__ double wide() const { return static_cast<double>(h) + (static_cast<double>(m) + l); }
+};
+
+// Two sums of such exponentials, each in two parts (Knuth's sum).
+struct Sums2 {
+  Two h{0.f, 0.f}, l{0.f, 0.f};
+  __device__ __forceinline__ void add(Two x) {
+    const Two s = add2(h, x), b = sub2(s, h);
+    l = add2(l, add2(sub2(h, sub2(s, b)), sub2(x, b)));
+    h = s;
+  }
+  // e^(z - y) for two z, as Exp3 has it.
+  __device__ __forceinline__ void add_exp(float z0, float z1, float y) {
+    const bool in0 = z0 - y >= -80.f, in1 = z1 - y >= -80.f;
+    const Two z(in0 ? z0 : y, in1 ? z1 : y), yy(y, y), lg(kLog2e, kLog2e), ln(kLn2, kLn2), magic(12582912.f, 12582912.f);
+    const Two d = sub2(z, yy), b = sub2(d, z), dl = sub2(sub2(z, sub2(d, b)), add2(yy, b));
+    const Two t = mul2(d, lg), tl = add2(fma2(d, lg, mul2(t, Two(-1.f, -1.f))), fma2(d, Two(kLog2eLow, kLog2eLow), mul2(dl, lg)));
+    const Two w = fma2(t, Two(32.f, 32.f), magic), r = fma2(sub2(w, magic), Two(-1.f / 32, -1.f / 32), t);
+    const Two p = mul2(r, ln), pl = add2(fma2(r, ln, mul2(p, Two(-1.f, -1.f))), fma2(r, Two(kLn2Low, kLn2Low), mul2(tl, ln)));
+    Two q = fma2(p, Two(1.f / 120, 1.f / 120), Two(1.f / 24, 1.f / 24));
+    q = fma2(p, fma2(p, q, Two(1.f / 6, 1.f / 6)), Two(0.5f, 0.5f));
+    q = mul2(mul2(p, p), q);
+    const float2 ws = w.parts();
+    const int n0 = __float_as_int(ws.x) - __float_as_int(12582912.f), n1 = __float_as_int(ws.y) - __float_as_int(12582912.f);
+    const float2 c0 = kExp2[n0 & 31], c1 = kExp2[n1 & 31];
+    const Two c(c0.x, c1.x), cl(c0.y, c1.y);
+    const Two up(in0 ? __int_as_float((127 + (n0 >> 5)) << 23) : 0.f, in1 ? __int_as_float((127 + (n1 >> 5)) << 23) : 0.f);
+    const Two x = mul2(c, p), xl = fma2(c, p, mul2(x, Two(-1.f, -1.f)));
+    add(mul2(c, up));
+    add(mul2(x, up));
+    l = fma2(add2(xl, fma2(c, add2(fma2(pl, add2(p, q), pl), q), fma2(cl, p, cl))), up, l);
+  }
+  __device__ __forceinline__ double total() const {
+    const float2 a = h.parts(), b = l.parts();
+    return (static_cast<double>(a.x) + b.x) + (static_cast<double>(a.y) + b.y);
+  }
 };
 
 // A sum in two parts.
@@ -327,6 +363,7 @@ struct Merge {
   int tokens[kBeamsMax][32], from[kKeepMax + 1];
   double totals[kBeamsMax], logs[kBeamsMax], sums[32];
   float errors[kBeamsMax], tops[kBeamsMax];
+  unsigned int close, unused;  // hypotheses that are close to others
   __device__ __forceinline__ Key* lists() { return reinterpret_cast<Key*>(this + 1); }
 };
 static_assert(sizeof(Merge) % sizeof(Key) == 0, "the lists are aligned");
@@ -405,8 +442,8 @@ __device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t
 // A group's rows' offers, and their places among the group's, by a block of whole warps, four at least.
 //
 // Which offers come first is a matter of 64 bits: where two of different hypotheses are closer
-// to one another than the 32-bit sums' error allows to tell, the group's rows are summed once
-// more, to 2^-35.  The error of a row's log is at most `rest / total`, the share of the tokens
+// to one another than the 32-bit sums' error allows to tell, their rows are summed once more,
+// to 2^-35.  The error of a row's log is at most `rest / total`, the share of the tokens
 // that are not among its largest, times 2^-22 of the exponential, 2^-19 of sums and rounded
 // arguments, and 2.4 * 2^-24 for each unit of |log2 e^(z - y)|, of which the average, weighted
 // by the terms, is at most log2(V) less log2 of their sum (the entropy of V numbers).
@@ -424,10 +461,10 @@ __device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64
       s.totals[b] = 1.0, s.errors[b] = 0.f;
   }
   bad = __syncthreads_or(bad);
-  bool again = false;
   while (true) {
     if (warp == 0 && lane < a.beams) s.logs[lane] = log_of(s.totals[lane]);
     if (threadIdx.x <= a.keep) s.first[threadIdx.x] = 0;
+    if (threadIdx.x == 0) s.close = 0;
     __syncthreads();
     for (int b = warp; b < a.beams; b += warps) {
       const float c = a.scores[g * a.beams + b];
@@ -457,28 +494,29 @@ __device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64
       }
     }
     __syncthreads();
-    if (again) break;
-    bool close = false;
     if (threadIdx.x < a.keep && s.first[threadIdx.x + 1]) {
       const int b0 = s.from[threadIdx.x] >> 8, b1 = s.from[threadIdx.x + 1] >> 8;
       const double e = static_cast<double>(s.errors[b0]) + s.errors[b1];
-      close = b0 != b1 && e > 0 && score_of(s.first[threadIdx.x]) - score_of(s.first[threadIdx.x + 1]) <= e;
+      if (b0 != b1 && e > 0 && score_of(s.first[threadIdx.x]) - score_of(s.first[threadIdx.x + 1]) <= e) atomicOr(&s.close, 1u << b0 | 1u << b1);
     }
-    if (!__syncthreads_or(close)) break;
-    again = true;
+    __syncthreads();
+    const unsigned int close = s.close;
+    if (!close) break;  // (each round leaves fewer rows whose error is not 0)
+    __syncthreads();
     for (int b = 0; b < a.beams; ++b) {
-      const int64_t row = g * a.beams + b;
-      if (!is_read(a, row) || s.offers[b][0] == 0) continue;
-      const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+      if (!(close >> b & 1) || s.errors[b] == 0.f) continue;
+      const T* z = static_cast<const T*>(a.logits) + (g * a.beams + b) * a.ld;
       const float y = s.tops[b];
-      Sum2 sum;
-      for (int i = threadIdx.x; i < a.V; i += blockDim.x) {
-        const Exp3 e(logit(z[i]), y);
-        sum.add(e.h);
-        sum.add(e.m);
-        sum.l += e.l;
+      Sums2 sum;
+      constexpr int AHEAD = 8;
+      for (int i = threadIdx.x; i < a.V; i += AHEAD * blockDim.x) {
+        float x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) x[k] = i + k * static_cast<int>(blockDim.x) < a.V ? logit(z[i + k * blockDim.x]) : -INFINITY;
+#pragma unroll
+        for (int k = 0; k < AHEAD; k += 2) sum.add_exp(x[k], x[k + 1], y);
       }
-      double total = static_cast<double>(sum.h) + sum.l;
+      double total = sum.total();
 #pragma unroll
       for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
       if (lane == 0) s.sums[warp] = total;
@@ -486,6 +524,7 @@ __device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64
       if (threadIdx.x == 0) {
         for (int w = 1; w < warps; ++w) total += s.sums[w];
         s.totals[b] = total;
+        s.errors[b] = 0.f;
       }
       __syncthreads();
     }

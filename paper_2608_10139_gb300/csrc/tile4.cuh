@@ -26,6 +26,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "pairs32.cuh"
 #include "tile8.cuh"
 
 namespace aiq {
@@ -104,27 +105,6 @@ __device__ __forceinline__ void halve4(__half2* e, int lane_bit) {
     const uint32_t a = as_u32(e[i]), b = as_u32(e[i + N / 2]);  // (chosen as values: a choice of places would live in memory)
     e[i] = __hmin2_nan(as_h2(upper ? b : a), as_h2(__shfl_xor_sync(0xffffffffu, upper ? a : b, lane_bit)));
   }
-}
-
-// Pairs of 32-bit numbers, an instruction for both.
-struct Two {
-  uint64_t v;
-  Two() = default;
-  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ explicit Two(float2 x) : Two(x.x, x.y) {}
-  __device__ __forceinline__ float2 parts() const {
-    float2 x;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(x.x), "=f"(x.y) : "l"(v));
-    return x;
-  }
-};
-__device__ __forceinline__ Two add_rd(Two a, Two b) {
-  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
-  return a;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return a;
 }
 
 // The codes of N (2, 4 or 8) elements, in order from the lowest bits.  d = x - m is rounded down:
