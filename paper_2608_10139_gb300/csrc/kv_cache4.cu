@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32, HD == 128 ? 2 : HD == 64 ? 4
 }
 
 template <int HD>
-__global__ void __launch_bounds__(kCacheWarps * 32) k_kv_dequantize4(CacheArgs a, const uint8_t* cache, __half* kv, int64_t ld) {
+__global__ void __launch_bounds__(kCacheWarps * 32, HD == 128 ? 3 : 4) k_kv_dequantize4(CacheArgs a, const uint8_t* cache, __half* kv, int64_t ld) {
   grid_launch_next();
   grid_wait();
   const int64_t u = static_cast<int64_t>(blockIdx.x) * kCacheWarps + (threadIdx.x >> 5);
@@ -164,42 +164,43 @@ __global__ void __launch_bounds__(kCacheWarps * 32) k_kv_dequantize4(CacheArgs a
   __half* k = kv + at.token * ld + h * HD;
   __half* v = k + a.Hkv * HD;
   const uint8_t* tile = cache + u * tile4_bytes(HD);
-  const uint4* kin = reinterpret_cast<const uint4*>(tile);
   const uint4* vin = reinterpret_cast<const uint4*>(tile + kTileKeys * HD / 2);
   constexpr int C = HD == 32 ? 1 : HD / 64, K = HD == 32 ? 1 : 2;
-  uint4 kw[K][C], vw[K][C], kp[C], vp[C][2];
+  // Keys: a lane has a word of codes, eight elements, of every key that is `first` more than a multiple
+  // of `by`, so that the lanes of a key store its elements side by side.  (As the tile lies, 16
+  // elements a lane, they would store halves of sectors.)
+  constexpr int LANES = HD == 32 ? 4 : 8, by = 32 / LANES, N = kTileKeys / by;
+  const int first = lane / LANES, word = lane % LANES;
+  uint32_t kw[C][N], kp[C][N];
+  uint4 vw[K][C], vp[C][2];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int key = by * j + first;
+      kw[c][j] = *reinterpret_cast<const uint32_t*>(tile + tile4_key_at<HD>(key, 64 * c + 8 * word));
+      kp[c][j] = *reinterpret_cast<const uint32_t*>(tile + tile4_pair_at<HD>(key, false, c));
+    }
 #pragma unroll
   for (int i = 0; i < K; ++i)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      kw[i][c] = vw[i][c] = make_uint4(0u, 0u, 0u, 0u);
-      if (16 * i < at.n) {
-        kw[i][c] = kin[(i * C + c) * 32 + lane];
-        vw[i][c] = vin[(i * C + c) * 32 + lane];
-      }
+      vw[i][c] = make_uint4(0u, 0u, 0u, 0u);
+      if (16 * i < at.n) vw[i][c] = vin[(i * C + c) * 32 + lane];
     }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const uint4* pairs = reinterpret_cast<const uint4*>(tile + tile4_pairs(HD) + 256 * c);
-    kp[c] = pairs[g];
     vp[c][0] = pairs[8 + 2 * t];
     vp[c][1] = pairs[8 + 2 * t + 1];
   }
   const auto part = [](const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int key = 8 * j + g;
+  for (int j = 0; j < N; ++j) {
+    const int key = by * j + first;
     if (key >= at.n) continue;
-    if constexpr (HD == 32) {
-      *reinterpret_cast<uint4*>(k + key * ld + 8 * t) = values4(part(kw[0][0], j), part(kp[0], j));
-    } else {
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-          *reinterpret_cast<uint4*>(k + key * ld + 64 * c + 16 * t + 8 * w) =
-              values4(part(kw[j / 2][c], 2 * (j & 1) + w), part(kp[c], j));
-    }
+    for (int c = 0; c < C; ++c) *reinterpret_cast<uint4*>(k + key * ld + 64 * c + 8 * word) = values4(kw[c][j], kp[c][j]);
   }
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
