@@ -160,12 +160,24 @@ struct Sum2 {
   }
 };
 
+// Terms of lists, whose order is that of arrival, are added up as whole numbers of 2^-46 (they are
+// at most 1, and fewer than 2^15): a sum that hung on their order would make a score's last bit do so.
+constexpr float kFixed = 0x1p46f;
+__device__ __forceinline__ long long fixed(float x) { return __float2ll_rn(x * kFixed); }
+__device__ __forceinline__ double unfixed(long long x) { return static_cast<double>(x) * (1.0 / kFixed); }
+__device__ __forceinline__ long long warp_total(long long x) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  return x;
+}
+
 struct Row {
   int n;             // entries of the list
   int part[2][32];   // as candidates.cuh wants them
   unsigned int highest, lowest;
   uint32_t kth;
   Sum2 sums[kRowThreads / 32];
+  unsigned long long dropped;  // by a cut
   alignas(16) uint32_t tops[kRowThreads];
   __device__ __forceinline__ Key* list() { return reinterpret_cast<Key*>(this + 1); }
 };
@@ -244,16 +256,19 @@ __device__ __forceinline__ void scan_row(const SelectArgs& a, Row& s, int64_t r)
   };
   int round = 0;
   const auto cut_list = [&] {
-    Sum2 dropped;
+    long long dropped = 0;
+    if (tid == 0) s.dropped = 0;
     const Key from = cut<NT>(s, round, a.keep, a.most, [&](Key x, Key mid) {
-      dropped.add(exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - order_value(static_cast<uint32_t>(mid >> 32))) * kLog2e));
+      dropped += fixed(exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - order_value(static_cast<uint32_t>(mid >> 32))) * kLog2e));
     });
     if (from == 0) return;
+    dropped = warp_total(dropped);
+    if (tid % 32 == 0) atomicAdd(&s.dropped, static_cast<unsigned long long>(dropped));
     // of what follows, only larger values can be among the largest: equal ones come later
     const float to = order_value(static_cast<uint32_t>(from >> 32)), f = Exp3(base, to).sum();
     rest.h *= f, rest.l *= f;
-    rest.add(dropped.h);
-    rest.l += dropped.l;
+    __syncthreads();
+    if (tid == 0) rest.add(static_cast<float>(unfixed(s.dropped)));
     bound = fmaxf(bound, to);
     base = to;
   };
@@ -390,9 +405,9 @@ __device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t
   const Key from = owner < 0 ? 1 : __shfl_sync(0xffffffffu, least, owner);
   const uint32_t top = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(best >> 32));
   const float y = order_value(top);
-  const auto light = [&](Key x) { return exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - y) * kLog2e); };
+  const auto light = [&](Key x) { return fixed(exp2_approx((order_value(static_cast<uint32_t>(x >> 32)) - y) * kLog2e)); };
   int n = 0;
-  float rest = 0.f;
+  long long listed = 0;  // of the elements of the lists that are not among the largest
   __syncwarp();
 #pragma unroll 4
   for (int i = lane; i - lane < all; i += 32) {  // (an entry moves to a place that was read before)
@@ -401,7 +416,7 @@ __device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t
     if (x >= from)
       list[n + __popc(kept & ((1u << lane) - 1))] = x;
     else if (x)
-      rest += light(x);
+      listed += light(x);
     n += __popc(kept);
   }
   sorted[lane] = 0;
@@ -414,11 +429,12 @@ __device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t
     if (before < a.keep)
       sorted[before] = x;
     else
-      rest += light(x);
+      listed += light(x);
   }
   __syncwarp();
   const Key key = sorted[lane];
   double sum = 0;
+  float rest = 0.f;
   if (top) {
     for (int i = lane; i < a.slices; i += 32) {
       const float2 x = __ldcg(a.rests + r * a.slices + i);
@@ -427,14 +443,15 @@ __device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t
     if (key) sum = Exp3(order_value(static_cast<uint32_t>(key >> 32)), y).wide();
   }
   rest = warp_sum(rest);
+  const double others = rest + unfixed(warp_total(listed));
 #pragma unroll
   for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   if (lane == 0) {
-    const float total = static_cast<float>(sum) + rest;
-    const float spread = fmaxf(0.f, __log2f(static_cast<float>(a.V)) - __log2f(rest)) + 1.f;
+    const float part = static_cast<float>(others), total = static_cast<float>(sum + others);
+    const float spread = fmaxf(0.f, __log2f(static_cast<float>(a.V)) - __log2f(part)) + 1.f;
     s.tops[b] = y;
-    s.totals[b] = top ? sum + rest : 1.0;
-    s.errors[b] = rest > 0.f ? rest / total * (0x1p-22f + 0x1p-19f + spread * 2.4f * 0x1p-24f) : 0.f;
+    s.totals[b] = top ? sum + others : 1.0;
+    s.errors[b] = part > 0.f ? part / total * (0x1p-22f + 0x1p-19f + spread * 2.4f * 0x1p-24f) : 0.f;
   }
   return !__any_sync(0xffffffffu, bad);
 }

@@ -1,0 +1,127 @@
+"""Calls on the 4-bit cache and of beam search that meet each other or that no single batch reaches:
+two contexts at once, many groups, few rows of close hypotheses, many rows with starts that do not
+ascend."""
+import threading
+
+import numpy as np
+import pytest
+
+from helpers import gpu_ctx
+from paper_2608_10139_gb300 import aiq
+from test_gpu_beam import _check, _select
+from test_gpu_kv_cache4 import Batch, _d, _rows
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = gpu_ctx()
+    yield c
+    c.close()
+
+
+def test_more_groups_than_counters(ctx):
+    rng = np.random.default_rng(1)
+    z = rng.standard_normal((5000, 2, 60)).astype(np.float32)
+    scores = -rng.uniform(0, 4, (5000, 2))
+    held, out = _select(ctx, z, scores, None, 4, "f16", eos=7)
+    _check(held, out, scores, None, 4, eos=7, groups=range(0, 5000, 97))
+
+
+@pytest.mark.parametrize("n,beams,V", [(1, 4, 128256), (2, 16, 40000), (5000, 2, 300)])
+def test_close_hypotheses_of_few_and_of_many_rows(ctx, n, beams, V):
+    """Alike but for some light tokens, which decide: rows in several parts, and more groups than are merged by the
+    row kernel."""
+    rng = np.random.default_rng(n + beams)
+    z = np.repeat(rng.standard_normal((n, 1, V)).astype(np.float32), beams, 1)
+    for b in range(1, beams):
+        at = rng.integers(0, V, (n, 5))
+        for g in range(n):
+            z[g, b, at[g]] = np.float32(-6) + np.float32(1e-3) * rng.standard_normal(5).astype(np.float32)
+    scores = np.full((n, beams), -2.25)
+    held, out = _select(ctx, z, scores, None, 2 * beams)
+    _check(held, out, scores, None, 2 * beams, groups=range(0, n, max(1, n // 30)))
+
+
+@pytest.mark.parametrize("rows,beams", [(1200, 1), (60, 4), (3, 1)])
+def test_starts_that_do_not_ascend_and_the_call_behind_them(ctx, rows, beams):
+    """Reported, with nothing written outside; the next call is not disturbed.  The 1,200 rows are cut into ranges."""
+    rng = np.random.default_rng(rows)
+    lens = [int(x) for x in rng.integers(100, 400, rows)]
+    b = Batch(ctx, rng, 64, 8, 2, beams, lens, 40, 33)
+    good = b.st.clone()
+    qkv = _rows(rng, b.R, 12 * 64)
+    for at, value in ((rows // 2, 3), (rows, 2 ** 31 - 1), (0, -5), (rows // 3, 2 ** 31 - 1)):
+        b.st.copy_(good)
+        b.st[at] = value
+        torch.cuda.synchronize()
+        with pytest.raises(aiq.AiqError) as e:
+            b.step(qkv, 0)
+        assert e.value.status == aiq.ERR_DEVICE_CHECK
+        assert (b.out[b.R] == 9).all() and (b.guard[-1] == 77).all()
+    b.st.copy_(good)
+    torch.cuda.synchronize()
+    b.check(rng, [0], rows=rng.choice(b.R, min(b.R, 20), replace=False).tolist())
+
+
+def test_two_contexts_at_once():
+    """Each has its own stream, workspace and counters."""
+    rng = np.random.default_rng(9)
+    work = []
+    for k in range(2):
+        c = gpu_ctx()
+        b = Batch(c, rng, 64, 8, 2, 1, [int(x) for x in rng.integers(100, 700, 900 if k else 12)], 40, 33)
+        z = torch.as_tensor(rng.standard_normal((40, 4, 5000)).astype(np.float32)).cuda()
+        s = torch.as_tensor(-rng.uniform(0, 4, (40, 4)).astype(np.float32)).cuda()
+        p, t = (torch.zeros(40 * 4, dtype=torch.int32, device="cuda") for _ in range(2))
+        work.append((c, b, _rows(rng, b.R, 12 * 64), z, s, p, t, torch.zeros(160, device="cuda")))
+    torch.cuda.synchronize()
+
+    def run(w, outs, times):
+        c, b, qkv, z, s, p, t, so = w
+        for _ in range(times):
+            out, _ = b.step(qkv, 0)
+            c.op_beam_select(z.data_ptr(), aiq.LOGITS_F32, 5000, 40, 4, 5000, s.data_ptr(), 4, p.data_ptr(), t.data_ptr(), so.data_ptr())
+            outs.append((out.copy(), p.cpu().numpy(), t.cpu().numpy(), so.cpu().numpy()))
+
+    alone = [[], []]
+    for w, o in zip(work, alone):
+        run(w, o, 1)
+    both = [[], []]
+    threads = [threading.Thread(target=run, args=(w, o, 15)) for w, o in zip(work, both)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    for o, ref in zip(both, alone):
+        assert len(o) == 15
+        for got in o:
+            assert [np.array_equal(x, y) for x, y in zip(got, ref[0])] == [True] * 4
+    for w in work:
+        w[0].close()
+
+
+@pytest.mark.parametrize("hd,beams,rows", [(64, 3, 300), (64, 1, 250), (128, 1, 200), (32, 1, 250)])
+def test_texts_cut_anywhere(ctx, hd, beams, rows):
+    """A text's tiles over the ranges of one to many warps: lengths 0 to 500, two much longer."""
+    rng = np.random.default_rng(hd + beams)
+    lens = [int(x) for x in rng.integers(0, 500, rows) * (rng.random(rows) < 0.9)]
+    lens[rows // 3] = 9000
+    lens[-1] = 5000
+    b = Batch(ctx, rng, hd, 16, 8, beams, lens, 70, 40)
+    b.check(rng, [0], rows=rng.choice(b.R, 40, replace=False).tolist() + [rows // 3 * beams, b.R - 1, 0])
+
+
+@pytest.mark.parametrize("n,beams,V,keep,type", [(900, 4, 3000, 4, "f16"), (2, 8, 70000, 16, "f32"), (200, 1, 30000, 32, "bf16")])
+def test_equal_selections_give_equal_bits(ctx, n, beams, V, keep, type):
+    """Rows in ascending order too, whose lists are cut many times: the order in which entries arrive must not show."""
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((n, beams, V)).astype(np.float32)
+    z[::3] = np.sort(z[::3], -1)
+    scores = -rng.uniform(0, 4, (n, beams))
+    _, first = _select(ctx, z, scores, None, keep, type)
+    for _ in range(12):
+        _, out = _select(ctx, z, scores, None, keep, type)
+        assert [np.array_equal(x, y) for x, y in zip(first, out)] == [True] * 4
