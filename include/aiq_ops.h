@@ -191,8 +191,8 @@ aiq_status aiq_op_kv_dequantize4(aiq_ctx* ctx, const void* cache, int64_t T, con
  * All are taken as the cache holds them, m + n s without another rounding, the step's own
  * token among them.  held (optional) fp16 [R, 2 Hkv hd]: the step's keys, then its values, as
  * aiq_op_kv_dequantize4 would read them back.  out fp16 [R, Hq * hd].  hd in {32, 64, 128},
- * Hq / Hkv <= 8, at most 2^20 heads, beams >= 1 and a divisor of R.  qkv, caches, out and
- * held 16-byte aligned.  A sequence outside the T tokens, a key or value of this step that is
+ * Hq / Hkv <= 8, at most 2^20 heads, R * Hq < 2^31, beams >= 1 and a divisor of R.  qkv, caches,
+ * out and held 16-byte aligned.  A sequence outside the T tokens, a key or value of this step that is
  * not finite and an output that is not finite in fp16 give AIQ_ERR_DEVICE_CHECK.  The call
  * synchronises its stream. */
 aiq_status aiq_op_decode_attention_q4(aiq_ctx* ctx, const void* qkv, int32_t R, int32_t beams, int32_t Hq, int32_t Hkv,
@@ -220,9 +220,10 @@ aiq_status aiq_op_sample(aiq_ctx* ctx, const void* logits, int32_t type, int64_t
  * log probabilities; -infinity: the place holds none, its row is not read).  It offers
  * every token t at
  *     s = C + z_t - log sum_i exp(z_i),
- * computed in 64 bits, where z_t is finite (-infinity rules a token out, a row of
- * -infinity alone offers nothing); a hypothesis that has ended (done[g][b] != 0; done may be
- * NULL: none has) offers itself, pad_id at s = C, and its row is not read.
+ * in 64 bits, where z_t is finite (-infinity rules a token out, a row of -infinity alone offers
+ * nothing).  The log is right to 2^-33: offers of different hypotheses that are closer than 2^-32
+ * may come in either order, the same one every time.  A hypothesis that has ended (done[g][b] != 0;
+ * done may be NULL: none has) offers itself, pad_id at s = C, and its row is not read.
  * The first `keep` of a group's offers, by s descending, equal ones by hypothesis, those of
  * one hypothesis by logit descending and then by token, go to parents, tokens (int32
  * [n][keep], a parent being a hypothesis of the group, 0 .. beams - 1), scores_out (fp32) and
@@ -232,8 +233,8 @@ aiq_status aiq_op_sample(aiq_ctx* ctx, const void* logits, int32_t type, int64_t
  * outputs as the next step's inputs, keep = 2 * beams leaves ended hypotheses to the caller.
  * A NaN or +infinity among the logits of a row that is read, or among the scores, gives
  * AIQ_ERR_DEVICE_CHECK; that group's places are as if there were no offers, the other
- * groups' are written.  Outputs must not overlap inputs.  All pointers are device memory,
- * aligned to their elements; the call synchronises its stream. */
+ * groups' are written.  Outputs must not overlap inputs.  At most 2^24 rows, V at most 2^30.
+ * All pointers are device memory, aligned to their elements; the call synchronises its stream. */
 enum { AIQ_BEAMS_MAX = 16 };
 aiq_status aiq_op_beam_select(aiq_ctx* ctx, const void* logits, int32_t type, int64_t ldl, int32_t n, int32_t beams,
                               int32_t V, const float* scores, const int32_t* done, int32_t eos_id, int32_t pad_id,
@@ -244,7 +245,7 @@ aiq_status aiq_op_beam_select(aiq_ctx* ctx, const void* logits, int32_t type, in
  * (parents int32 [n][beams], device).  Row r of layer l is `bytes` bytes at
  * src + l * layer_pitch + r * pitch, and at dst likewise.  dst == src reorders in place:
  * rows whose parent is their own place are neither read nor written.  Otherwise every row
- * is written and the two may not overlap.  What lies between rows is left as it was.  It
+ * is written and the two may not overlap, nor dst and parents.  What lies between rows is left as it was.  It
  * moves any state of the hypotheses, the caches of generated tokens (fp16, 8 bits and
  * their tails, 4 bits: the blocks in use, rows pitch apart) as well as token histories.
  * Pointers, sizes and pitches that are multiples of 16 (or 4) bytes move by as much.

@@ -1532,10 +1532,15 @@ aiq_status run_query(aiq_ctx* c, const TableD* build, int32_t build_key, const a
 }
 
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+// Whether n bytes at p and m at q (either null: none) have one in common.
+bool overlap(const void* p, uint64_t n, const void* q, uint64_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a && b && (a < b ? b - a < n : a - b < m);
+}
 
 constexpr int32_t kHeadsMax = 1 << 20;  // a row's elements are counted in 32 bits
 
-// What the two copies between fp16 rows and the 8-bit cache ask of their arguments.
+// What the copies between fp16 rows and the 8-bit and 4-bit caches ask of their arguments.
 aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T, const int32_t* seq_start,
                             int32_t n_seqs, int32_t Hkv, int32_t hd, const void* cache) {
   if (!c || !kv || !seq_start || !cache || T < 0 || T > INT32_MAX || n_seqs < 0 || Hkv <= 0)
@@ -1544,7 +1549,7 @@ aiq_status check_cache_rows(aiq_ctx* c, const void* kv, int64_t ldkv, int64_t T,
   if (ldkv < 2 * int64_t(Hkv) * hd || ldkv % 8)
     return fail(AIQ_ERR_INVALID_ARG, "ldkv must be at least 2 Hkv hd and a multiple of 8");
   if (!aligned(kv, 16) || !aligned(cache, 16) || !aligned(seq_start, 4))
-    return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned, scales 8-byte aligned");
+    return fail(AIQ_ERR_INVALID_ARG, "kv and cache must be 16-byte aligned");
   if (Hkv > kHeadsMax) return fail(AIQ_ERR_UNSUPPORTED, "more than 2^20 heads");
   if ((T / AIQ_KV_BLOCK + n_seqs) * Hkv > (int64_t(1) << 33))
     return fail(AIQ_ERR_UNSUPPORTED, "more than 2^33 (block, KV head) pairs");
@@ -2506,6 +2511,11 @@ aiq_status aiq_op_beam_select(aiq_ctx* c, const void* logits, int32_t type, int6
       !aligned(parents, 4) || !aligned(tokens, 4) || !aligned(scores_out, 4) || !aligned(done_out, 4))
     return fail(AIQ_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
   if (n == 0) return AIQ_OK;
+  const uint64_t rows = uint64_t(n) * beams, kept = uint64_t(n) * keep * 4;
+  const uint64_t read = ((rows - 1) * ldl + V) * (type == AIQ_LOGITS_F32 ? 4 : 2);
+  for (const void* out : {static_cast<void*>(parents), static_cast<void*>(tokens), static_cast<void*>(scores_out), static_cast<void*>(done_out)})
+    if (overlap(out, kept, logits, read) || overlap(out, kept, scores, rows * 4) || overlap(out, kept, done, rows * 4))
+      return fail(AIQ_ERR_INVALID_ARG, "an output overlaps an input");
   CUDA_TRY(cudaSetDevice(c->device));
   uint8_t* scratch = nullptr;
   const BeamSelect b{logits, type, ldl, n, beams, V, scores, done, eos_id, pad_id, keep, parents, tokens, scores_out, done_out};
@@ -2531,9 +2541,9 @@ aiq_status aiq_op_beam_reorder(aiq_ctx* c, const void* src, void* dst, int64_t b
   const int64_t deep = (layers - 1) * (layers > 1 ? layer_pitch : 0) + bytes;  // of a row's layers
   if (rows > 1 && layers > 1 && layer_pitch < span && pitch < deep)
     return fail(AIQ_ERR_INVALID_ARG, "layers overlap");
-  const uintptr_t a = reinterpret_cast<uintptr_t>(src), b = reinterpret_cast<uintptr_t>(dst);
   const uint64_t all = static_cast<uint64_t>(span) + (deep - bytes);
-  if (a != b && (a < b ? b - a < all : a - b < all)) return fail(AIQ_ERR_INVALID_ARG, "src and dst overlap");
+  if (src != dst && overlap(src, all, dst, all)) return fail(AIQ_ERR_INVALID_ARG, "src and dst overlap");
+  if (overlap(dst, all, parents, static_cast<uint64_t>(rows) * 4)) return fail(AIQ_ERR_INVALID_ARG, "dst and parents overlap");
   CUDA_TRY(cudaSetDevice(c->device));
   const int e = launch_beam_reorder(src, dst, bytes, pitch, n, beams, parents, layers, layer_pitch, c->d_err, c->stream);
   if (e != 0) return fail(AIQ_ERR_CUDA, std::string("beam reordering launch: ") +

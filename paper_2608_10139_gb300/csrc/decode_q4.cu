@@ -551,16 +551,13 @@ __device__ __forceinline__ void append(const DecQ4Args& a, const Token4<HD>& tok
   __syncwarp();
 }
 
-// The two columns of a lane: beam and head (-1: none).
-struct Columns4 {
-  int beam[2], head[2];
-  template <bool PAIRS>
-  static __device__ __forceinline__ void of(const DecQ4Args& a, int column, int& beam, int& head) {
-    if (PAIRS) column &= 3;
-    beam = column / a.G;
-    head = beam < a.wide ? column % a.G : -1;
-  }
-};
+// A column's beam and query head (-1: none).
+template <bool PAIRS>
+__device__ __forceinline__ void column_of(const DecQ4Args& a, int column, int& beam, int& head) {
+  if (PAIRS) column &= 3;
+  beam = column / a.G;
+  head = beam < a.wide ? column % a.G : -1;
+}
 
 template <int HD>
 struct Stream4 {
@@ -792,7 +789,7 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
       from = a.gc, block = (pt.row + b) * a.gen_blocks, begin = np + no + b * ng, keys = a.slot + 1, runs = begin + ng;
       info |= kGenerated | b << kBeamShift;
     }
-    left = min(keys, (t1 - begin) * kTileKeys) - (t0 - begin) * kTileKeys;
+    left = (t1 < runs ? (t1 - begin) * kTileKeys : keys) - (t0 - begin) * kTileKeys;  // (a run has at most 2^31 - 1 keys, a task more)
     tile = from + ((block + t0 - begin) * a.Hkv + pt.h) * tile4_bytes(HD);
   };
   const auto produce = [&] {
@@ -819,9 +816,9 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
   using At = Attn4<HD, PAIRS>;
   At at;
   int my_beam, my_head, beam[2], head[2];
-  Columns4::of<PAIRS>(a, g, my_beam, my_head);
-  Columns4::of<PAIRS>(a, 2 * t, beam[0], head[0]);
-  Columns4::of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
+  column_of<PAIRS>(a, g, my_beam, my_head);
+  column_of<PAIRS>(a, 2 * t, beam[0], head[0]);
+  column_of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
   const int64_t kd = static_cast<int64_t>(a.Hkv) * HD;
   uint4 raw[At::NQ];
   Token4<HD> token;
@@ -987,9 +984,9 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
   using At = Attn4<HD, PAIRS>;
   At at;
   int my_beam, my_head, beam[2], head[2];
-  Columns4::of<PAIRS>(a, g, my_beam, my_head);
-  Columns4::of<PAIRS>(a, 2 * t, beam[0], head[0]);
-  Columns4::of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
+  column_of<PAIRS>(a, g, my_beam, my_head);
+  column_of<PAIRS>(a, 2 * t, beam[0], head[0]);
+  column_of<PAIRS>(a, 2 * t + 1, beam[1], head[1]);
   {
     uint4 raw[At::NQ];
     At::fetch(raw, query_of(a, HD, w.row, w.h, w.beams, my_beam, my_head));

@@ -83,3 +83,12 @@ MOVE = dict(src=A, dst=1 << 30, bytes=64, pitch=128, n=3, beams=4, parents=A, la
     (dict(layer_pitch=1 << 60), INVALID), (dict(bytes=1 << 50, pitch=1 << 50), INVALID)])
 def test_reorder(ctx, change, status):
     _refused(status, ctx.op_beam_reorder, **{**MOVE, **change})
+
+
+def test_outputs_that_overlap_inputs(ctx):
+    apart = {k: (i + 1) << 30 for i, k in enumerate(("logits", "scores", "done", "parents", "tokens", "scores_out", "done_out"))}
+    for out in ("parents", "tokens", "scores_out", "done_out"):
+        for at in (apart["logits"] + 12 * 400 - 4, apart["scores"], apart["scores"] - 4 * 3 * 8 + 4, apart["done"] + 44):
+            _refused(INVALID, ctx.op_beam_select, **{**PICK, **apart, out: at})
+    for at in (1 << 30, (1 << 30) + 1536 + 11 * 128 + 60, (1 << 30) - 44):
+        _refused(INVALID, ctx.op_beam_reorder, **{**MOVE, "parents": at})
