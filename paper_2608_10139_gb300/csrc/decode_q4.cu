@@ -698,6 +698,15 @@ __device__ __forceinline__ void pieces(const DecQ4Args& a, const Attn4<HD, PAIRS
 // the line of an inner task's tiles is cut into `ranges` of equal length, a warp each.  A task that
 // lies within a range is the warp's alone; of one that does not, each warp leaves its (maximum, sum,
 // output), and the last to arrive merges them in their order.
+//
+// Bound by instruction issue and its latency, not by HBM: 3,263 rows of 218 keys, 32 query heads of 64
+// on 8 (329 MB, 48 us at the copy's rate), take 128 us (132 with caches cold) for 88 million warp
+// instructions, 65 % of the issue slots while warps are at work; 250 to 290 a tile and some 1,400 a
+// task of seven tiles.  Of a tile's, 80 make operands out of codes and 24 are products.  Long rows come
+// to 0.8 of the copy.  head_dim 128 has three CTAs an SM for its registers: 700 rows, four beams a
+// text of 200 tokens, take 79 us, where two groups of eight columns read a prompt's tiles in turn
+// (all sixteen at once would leave eight warps an SM).  Measured slower: five CTAs, 18 warps, four
+// entries a ring, one tile an entry, scores of two tiles first, ranges for batches of thousands.
 template <int HD, bool PAIRS, bool RANGES>
 __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
     k_decode_q4_stream(DecQ4Args a, int n_seqs, int ranges, float* partial, unsigned int* arrived) {
@@ -905,6 +914,10 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
 // An inner task (KV head, beams) has `units` CTAs, at least one a sequence, the others
 // shared out by the sequences' lengths, which only the device knows: sequence i's are
 // share(i) .. share(i + 1) - 1.
+//
+// Four documents of 17,979 to 57,262 tokens, 8 KV heads of 128 (188 MB), take 47 us, 0.59 of the copy:
+// bound by instruction issue (54 % of the slots by 11.4 warps an SM) and the start and end of a call that
+// each warp has some 23 tiles for.  Entries of two tiles took 2 us more.
 constexpr int kMaxRanges = 512;  // of a task
 template <int HD>
 struct Split4 {
