@@ -694,13 +694,14 @@ __device__ __forceinline__ void pieces(const DecQ4Args& a, const Attn4<HD, PAIRS
 }
 
 // Many tasks: a warp takes the tiles of all its tasks as one stream through its ring.  Where there
-// are many tasks a warp, they are dealt out.  Of fewer (RANGES) the longest would be waited for:
+// are many tasks a warp, they are drawn one by one (dealt out by number they took 10 % more: 3,000
+// texts of 200, head_dim 128, 315 us, drawn 273).  Of fewer (RANGES) the longest would be waited for:
 // the line of an inner task's tiles is cut into `ranges` of equal length, a warp each.  A task that
 // lies within a range is the warp's alone; of one that does not, each warp leaves its (maximum, sum,
 // output), and the last to arrive merges them in their order.
 //
 // Bound by instruction issue and its latency, not by HBM: 3,263 rows of 218 keys, 32 query heads of 64
-// on 8 (329 MB, 48 us at the copy's rate), take 128 us (132 with caches cold) for 88 million warp
+// on 8 (329 MB, 48 us at the copy's rate), take 126 us (132 with caches cold) for 88 million warp
 // instructions, 65 % of the issue slots while warps are at work; 250 to 290 a tile and some 1,400 a
 // task of seven tiles.  Of a tile's, 80 make operands out of codes and 24 are products.  Long rows come
 // to 0.8 of the copy.  head_dim 128 has three CTAs an SM for its registers: 700 rows, four beams a
@@ -726,17 +727,13 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
   const int first = blockIdx.x * S::NW + warp;
   int inner = first % a.inner, i = first / a.inner;
   const int range = i;
-  // By whole tasks: from a warp's to its next every other round is dealt out backwards, so that
-  // whoever had the longest gets the shortest.
-  int up_seqs, up_inner, down_seqs, down_inner;
-  bool odd = false, begun = false;
+  // By whole tasks: a warp's first two by its number, the second dealt out backwards, so that whoever
+  // has the longest gets the shortest; the others drawn, each while the one before is at work.
+  unsigned int task = first, drawn = 0;  // (lane 0's)
   // By ranges: the warp's, and the sequence before the last whose places begin at its start or
   // before, found 32 probes at a time.
   int x0, x1;
-  if constexpr (!RANGES) {
-    const int up = 2 * (static_cast<int>(gridDim.x) * S::NW - first) - 1, down = 2 * first + 1;
-    up_seqs = up / a.inner, up_inner = up % a.inner, down_seqs = down / a.inner, down_inner = down % a.inner;
-  } else {
+  if constexpr (RANGES) {
     const Line4 line(a);
     const int all = line.place(a, n_seqs);
     x0 = range_at(range, ranges, all);
@@ -760,15 +757,23 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
   const auto next_run = [&] {         // left is 0 behind the last task's
     while (t0 >= t1) {
       if constexpr (!RANGES) {
-        if (begun) {
-          inner += odd ? down_inner : up_inner;
-          const bool carry = inner >= a.inner;
-          inner -= carry ? a.inner : 0;
-          i += (odd ? down_seqs : up_seqs) + carry;
-          odd = !odd;
+        constexpr unsigned kDraw = UINT32_MAX;
+        const unsigned tasks = n_seqs * a.inner, warps = gridDim.x * S::NW;
+        if (task == kDraw) task = 2 * warps + __shfl_sync(0xffffffffu, drawn, 0);
+        if (task >= tasks) {
+          if (tasks > 2 * warps && lane == 0 && atomicAdd(&arrived[1], 1u) == warps - 1) arrived[0] = arrived[1] = 0;  // for the next launch
+          return;
         }
-        begun = true;
-        if (i >= n_seqs) return;
+        i = task / a.inner;
+        inner = task - i * a.inner;
+        if (task < warps) {
+          task = 2 * warps - 1 - task;
+        } else if (tasks > 2 * warps) {
+          task = kDraw;
+          if (lane == 0) drawn = atomicAdd(&arrived[0], 1u);
+        } else {
+          task = tasks;
+        }
       } else if (++i >= n_seqs || Line4(a).place(a, i) >= x1) {
         i = n_seqs;
         return;
@@ -1120,7 +1125,7 @@ __global__ void __launch_bounds__(Split4<HD>::NW * 32, Split4<HD>::CTAS)
 
 // How a call runs: beams of a task, tasks of a sequence, and CTAs per inner task (at
 // least one a sequence; 0: a warp's tasks are a range of the line, of which there are `ranges`, or,
-// where that is 0 too, dealt out).
+// where that is 0 too, drawn).
 struct Plan {
   int wide, inner, units, ranges;
   int64_t seqs;
@@ -1131,17 +1136,18 @@ void cut(Plan& p, int64_t least, int64_t most_places, int num_sms) {
   using S = Stream4<HD>;
   const int64_t ctas = static_cast<int64_t>(num_sms) * S::CTAS, tasks = p.seqs * p.inner;
   p.units = p.ranges = 0;
-  // Calls from a cold cache, dealt out, by ranges and by CTAs, in us (8 KV heads of 4, head_dim 64, a
+  // Calls from a cold cache, by whole tasks, by ranges and by CTAs, in us (8 KV heads of 4, head_dim 64, a
   // prefix of 64): 64 texts of about 60 tokens 29, 30, 27, of 700 68, 51, 39; 130 of 60 31, 32, 32, of
-  // 350 52, 45, 44; 260 of 60 35, 35, 44, of 700 86, 68, 68; 500 of 60 41, 43, 61, of 350 75, 68, 82;
-  // 1,000 of 60 58, 61, 98, of 350 114, 102, 138; 3,263 of 120 147, 151, 287.  head_dim 128: 130 of
-  // 350 72, 60, 58; 260 of 200 69, 60, 67, of 700 149, 104, 97; 500 of 350 129, 104, 120; 2,000 of 200
-  // 218, 206, 330.  head_dim 64, four beams a text: 50 of 200 41, 51, 39; 100 of 1,000 113, 82, 88.
+  // 350 52, 45, 44; 260 of 60 35, 35, 44, of 700 70, 68, 68; 500 of 60 41, 43, 61, of 350 68, 67, 82;
+  // 1,000 of 60 57, 60, 98, of 350 104, 103, 138, of 2,000 340, 293; 2,400 of 350 185, 195; 3,263 of 135
+  // 147, 153, 287; 3,000 of 1,000 429, 441.  head_dim 128: 130 of 350 72, 60, 58; 260 of 200 69, 60, 67;
+  // 300 of 250 72, 71; 400 of 200 69, 75; 1,000 of 200 126, 137, of 700 260, 242; 2,000 of 200 194, 206,
+  // 330, of 350 268, 278.  head_dim 64, four beams a text: 50 of 200 41, 51, 39; 100 of 1,000 113, 79, 88.
   // A CTA per task costs its start and its merge, a warp per task the time of the longest ones.
   const double per_task = p.tiles / p.seqs, rounds = static_cast<double>(tasks) / ctas;
   if (rounds >= 5 || per_task <= 5 * rounds) {
     // a range is a tile at least, so that each has a part of a task that others have parts of
-    if (per_task >= std::max(10.0, 1.2 * rounds / S::NW) && most_places <= INT32_MAX)
+    if (per_task >= std::max(12.0, rounds) && most_places <= INT32_MAX)
       p.ranges = static_cast<int>(std::min<int64_t>({ctas * S::NW / p.inner, least, kArrivedMax / p.inner}));
     return;
   }
