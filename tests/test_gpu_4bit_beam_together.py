@@ -6,6 +6,7 @@ import threading
 import numpy as np
 import pytest
 
+import kv4
 from helpers import gpu_ctx
 from paper_2608_10139_gb300 import aiq
 from test_gpu_beam import _check, _select
@@ -45,11 +46,12 @@ def test_close_hypotheses_of_few_and_of_many_rows(ctx, n, beams, V):
     _check(held, out, scores, None, 2 * beams, groups=range(0, n, max(1, n // 30)))
 
 
-@pytest.mark.parametrize("rows,beams", [(1200, 1), (60, 4), (3, 1)])
-def test_starts_that_do_not_ascend_and_the_call_behind_them(ctx, rows, beams):
-    """Reported, with nothing written outside; the next call is not disturbed.  The 1,200 rows are cut into ranges."""
+@pytest.mark.parametrize("rows,beams,low,high", [(1200, 1, 250, 550), (3000, 1, 0, 60), (60, 4, 100, 400), (3, 1, 100, 400)])
+def test_starts_that_do_not_ascend_and_the_call_behind_them(ctx, rows, beams, low, high):
+    """Reported, with nothing written outside; the next call is not disturbed.  1,200 long rows are cut into
+    ranges, 3,000 short ones drawn, the others split."""
     rng = np.random.default_rng(rows)
-    lens = [int(x) for x in rng.integers(100, 400, rows)]
+    lens = [int(x) for x in rng.integers(low, high, rows)]
     b = Batch(ctx, rng, 64, 8, 2, beams, lens, 40, 33)
     good = b.st.clone()
     qkv = _rows(rng, b.R, 12 * 64)
@@ -125,3 +127,71 @@ def test_equal_selections_give_equal_bits(ctx, n, beams, V, keep, type):
     for _ in range(12):
         _, out = _select(ctx, z, scores, None, keep, type)
         assert [np.array_equal(x, y) for x, y in zip(first, out)] == [True] * 4
+
+
+def test_a_cache_beyond_32_bits(ctx):
+    """Tokens, tiles and generated blocks whose offsets pass 2^32 bytes: as the same ones near the start."""
+    rng = np.random.default_rng(12)
+    Hq, Hkv, hd, n = 8, 8, 128, 100
+    w, tb, T = 2 * Hkv * hd, kv4.tile_bytes(hd), 3_800_001
+    rows = _d(_rows(rng, n, w))
+    kv = torch.empty((T, w), dtype=torch.float16, device="cuda")
+    kv[T - n:] = rows
+    far, near = (torch.full((nb, Hkv, tb), 7, dtype=torch.uint8, device="cuda") for nb in (T // 32 + 1, n // 32 + 1))
+    assert far.numel() > 2 ** 32
+    st_far, st_near = _d(np.array([T - n, T], np.int32)), _d(np.array([0, n], np.int32))
+    ctx.op_kv_quantize4(kv.data_ptr(), w, T, st_far.data_ptr(), 1, Hkv, hd, far.data_ptr())
+    ctx.op_kv_quantize4(rows.data_ptr(), w, n, st_near.data_ptr(), 1, Hkv, hd, near.data_ptr())
+    assert torch.equal(far[(T - n) // 32:][:4], near) and (far[:(T - n) // 32] == 7).all()
+    kv[T - n:] = 0
+    ctx.op_kv_dequantize4(far.data_ptr(), T, st_far.data_ptr(), 1, Hkv, hd, kv.data_ptr(), w)
+    back = torch.zeros_like(rows)
+    torch.cuda.synchronize()
+    ctx.op_kv_dequantize4(near.data_ptr(), n, st_near.data_ptr(), 1, Hkv, hd, back.data_ptr(), w)
+    assert torch.equal(kv[T - n:], back)
+    del kv
+    # two rows of the sequence, as beams, whose generated tokens have room for a million more
+    qkv = _d(_rows(rng, 2, (Hq + 2 * Hkv) * hd))
+    outs = []
+    for own, st, t, cap in ((far, st_far, T, 4_000_000), (near, st_near, n, 40)):
+        gen = torch.full((2, -(-cap // 32), Hkv, tb), 9, dtype=torch.uint8, device="cuda")
+        out = torch.zeros((2, Hq * hd), dtype=torch.float16, device="cuda")
+        torch.cuda.synchronize()
+        ctx.op_decode_attention_q4(qkv.data_ptr(), 2, Hq, Hkv, hd, own.data_ptr(), t, st.data_ptr(), gen.data_ptr(), cap, 0,
+                                   out.data_ptr(), beams=2)
+        outs.append((out.cpu().numpy(), gen[:, 0].clone(), bool((gen[:, 1] == 9).all())))
+        del gen
+    assert torch.equal(outs[0][1], outs[1][1]) and outs[0][2] and outs[1][2]
+    q = qkv.cpu().numpy()
+    held = kv4.quantize(rows.cpu().numpy().reshape(n, 2, Hkv, hd))
+    for r in range(2):
+        new = kv4.quantize(q[r, Hq * hd:].reshape(1, 2, Hkv, hd))
+        c, sc, m = (np.concatenate(x) for x in zip(held, new))
+        x, big = kv4.values(c, sc, m), (np.abs(m.astype(np.float64)) + 15 * sc.astype(np.float64)).max(-1)
+        ref, tol = kv4.attend(q[r, :Hq * hd].astype(np.float64).reshape(Hq, hd), x[:, 0], x[:, 1], big[:, 0], big[:, 1])
+        for out, _, _ in outs:
+            assert (np.abs(out[r].astype(np.float64).reshape(Hq, hd) - ref) <= tol).all()
+
+
+def test_rows_beyond_32_bits_of_selection_and_reordering(ctx):
+    rng = np.random.default_rng(13)
+    ld = 2 ** 30 + 24
+    big = torch.zeros(2 * ld + 5000, dtype=torch.float16, device="cuda")
+    z = rng.standard_normal((1, 3, 5000)).astype(np.float16)
+    for b in range(3):
+        big[b * ld:b * ld + 5000] = torch.as_tensor(z[0, b]).cuda()
+    s = torch.as_tensor(np.array([[-1.0, -2.0, -0.5]], np.float32)).cuda()
+    p, t = (torch.zeros(6, dtype=torch.int32, device="cuda") for _ in range(2))
+    so = torch.zeros(6, device="cuda")
+    torch.cuda.synchronize()
+    ctx.op_beam_select(big.data_ptr(), aiq.LOGITS_F16, ld, 1, 3, 5000, s.data_ptr(), 6, p.data_ptr(), t.data_ptr(), so.data_ptr())
+    rp, rt, rs, _ = kv4.select(z[0].astype(np.float32), s.cpu().numpy()[0], np.zeros(3), 6, -1, 0)
+    assert np.array_equal(p.cpu().numpy(), rp) and np.array_equal(t.cpu().numpy(), rt)
+    assert np.abs(so.cpu().numpy() - rs).max() <= 2.0 ** -18 + np.abs(rs).max() * 2.0 ** -24
+    # and the rows themselves, 2 GB apart, moved in place
+    parents = torch.as_tensor(np.array([[2, 0, 0]], np.int32)).cuda()
+    torch.cuda.synchronize()
+    ctx.op_beam_reorder(big.data_ptr(), big.data_ptr(), 9998, 2 * ld, 1, 3, parents.data_ptr())
+    for b, a in enumerate((2, 0, 0)):
+        got = big[b * ld:b * ld + 5000].cpu().numpy()
+        assert np.array_equal(got[:4999], z[0, a, :4999]) and got[4999] == z[0, b, 4999]
