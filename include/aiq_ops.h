@@ -248,7 +248,8 @@ aiq_status aiq_op_beam_select(aiq_ctx* ctx, const void* logits, int32_t type, in
  * is written and the two may not overlap, nor dst and parents.  What lies between rows is left as it was.  It
  * moves any state of the hypotheses, the caches of generated tokens (fp16, 8 bits and
  * their tails, 4 bits: the blocks in use, rows pitch apart) as well as token histories.
- * Pointers, sizes and pitches that are multiples of 16 (or 4) bytes move by as much.
+ * Rows may begin and end anywhere; pointers, sizes and pitches that are multiples of 16 bytes are
+ * moved fastest.
  * beams 1 .. AIQ_BEAMS_MAX.  pitch >= bytes where there is more than one row; layers must not
  * overlap.  A parent outside the group gives AIQ_ERR_DEVICE_CHECK and leaves the group's rows as
  * they were.  The call synchronises its stream. */

@@ -624,28 +624,28 @@ int launch_select(const SelectArgs& a, int groups, cudaStream_t s) {
 
 // ------------------------------------------------------------- reordering ---
 constexpr int kThreads = 256;
+constexpr int kWordsMost = 1 << 20;  // bytes that 4-byte words move as fast as pieces do, or faster
 struct ReorderArgs {
   const uint8_t* src;
   uint8_t* dst;
-  int64_t pitch, layer_pitch;
-  int64_t units;  // words of a row
+  int64_t bytes, pitch, layer_pitch;
   int groups, beams, layers;
   const int32_t* parents;
   int* err;
 };
 
-// A thread takes one word of every beam of a group and layer: it has read all of
-// them before it writes one, so that rows may trade places in place without a second buffer.
-// Bound by HBM: of 16 layers of 1,200 rows of 36 KB what has to (530 MB read and written) moves in
-// 81 us, 0.97 of the copy.
+// Rows of whole, aligned words.  A thread takes one word of every beam of a group and layer: it
+// has read all of them before it writes one, so that rows may trade places in place without a second
+// buffer.  Bound by HBM: of 16 layers of 1,200 rows of 36 KB what has to (530 MB read and written) moves
+// in 81 us, 0.97 of the copy.
 template <typename W, int B>
 __global__ void __launch_bounds__(kThreads) k_beam_reorder(ReorderArgs a, int64_t chunks) {
   grid_launch_next();
   grid_wait();
   const int64_t block = blockIdx.x, chunk = block % chunks, rest = block / chunks;
   const int64_t g = rest % a.groups, l = rest / a.groups;
-  const int64_t u = chunk * kThreads + threadIdx.x;
-  const int64_t base = l * a.layer_pitch + g * a.beams * a.pitch;
+  const int64_t at = (chunk * kThreads + threadIdx.x) * static_cast<int>(sizeof(W));
+  const int64_t base = l * a.layer_pitch + g * a.beams * a.pitch + at;
   int p[B];
   bool fine = true;
 #pragma unroll
@@ -657,26 +657,97 @@ __global__ void __launch_bounds__(kThreads) k_beam_reorder(ReorderArgs a, int64_
     if (threadIdx.x == 0) set_dev_error(a.err, DEVERR_BOUNDS);
     return;
   }
-  if (u >= a.units) return;
+  if (at >= a.bytes) return;
   W w[B];
   const bool in_place = a.src == a.dst;
 #pragma unroll
   for (int i = 0; i < B; ++i)
-    if (i < a.beams && !(in_place && p[i] == i))
-      w[i] = *reinterpret_cast<const W*>(a.src + base + p[i] * a.pitch + u * static_cast<int64_t>(sizeof(W)));
+    if (i < a.beams && !(in_place && p[i] == i)) w[i] = *reinterpret_cast<const W*>(a.src + base + p[i] * a.pitch);
 #pragma unroll
   for (int i = 0; i < B; ++i)
-    if (i < a.beams && !(in_place && p[i] == i))
-      *reinterpret_cast<W*>(a.dst + base + i * a.pitch + u * static_cast<int64_t>(sizeof(W))) = w[i];
+    if (i < a.beams && !(in_place && p[i] == i)) *reinterpret_cast<W*>(a.dst + base + i * a.pitch) = w[i];
+}
+template <typename W>
+int launch_words(const ReorderArgs& a, cudaStream_t s) {
+  const int64_t chunks = (a.bytes / static_cast<int>(sizeof(W)) + kThreads - 1) / kThreads, sets = static_cast<int64_t>(a.groups) * a.layers;
+  if (chunks > INT32_MAX / sets) return cudaErrorInvalidValue;
+  void (*kernel)(ReorderArgs, int64_t) = a.beams <= 4 ? k_beam_reorder<W, 4> : a.beams <= 8 ? k_beam_reorder<W, 8> : k_beam_reorder<W, kBeamsMax>;
+  return launch_chained(kernel, dim3(static_cast<unsigned>(chunks * sets)), kThreads, 0, s, 1, a, chunks);
 }
 
-template <typename W>
-int launch_reorder(ReorderArgs a, int64_t bytes, cudaStream_t s) {
-  a.units = bytes / static_cast<int64_t>(sizeof(W));
-  const int64_t chunks = (a.units + kThreads - 1) / kThreads, blocks = chunks * a.groups * a.layers;
-  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-  void (*kernel)(ReorderArgs, int64_t) = a.beams <= 4 ? k_beam_reorder<W, 4> : a.beams <= 8 ? k_beam_reorder<W, 8> : k_beam_reorder<W, kBeamsMax>;
-  return launch_chained(kernel, dim3(static_cast<unsigned>(blocks)), kThreads, 0, s, 1, a, chunks);
+// Bytes `shift` (0 .. 15) to shift + 15 of two words.
+__device__ __forceinline__ uint4 shifted(uint4 x, uint4 y, int shift) {
+  const uint32_t v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  const int q = shift >> 2;
+  uint32_t w[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = q == 0 ? v[i] : q == 1 ? v[i + 1] : q == 2 ? v[i + 2] : v[min(i + 3, 7)];
+  const int bits = (shift & 3) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                    __funnelshift_r(w[3], w[4], bits));
+}
+
+// The first n of 16 bytes (the others become zeros).
+__device__ __forceinline__ void cp_async_16(void* to, const void* from, int n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Other rows, that begin and end anywhere.  A warp takes a piece of every beam of a group and layer
+// through shared memory: it reads the 16-byte words that the pieces lie in, so that each has the
+// alignment of its source there, then writes the words that they fill, shifted, and their ends byte by
+// byte.  No read reaches behind its row, nor before the first.  (What another warp's piece has of a
+// word is read as it may be, and not used.)  16 layers of 4,000 rows of 3,999 bytes in place take 63 us,
+// a call from a cold cache (28 at the copy's rate; rows of 4,000 aligned 52, byte by byte 383).
+constexpr int kMoveWarps = 4, kMoveBytes = 8192;
+constexpr int move_piece(int beams) { return kMoveBytes / (beams <= 1 ? 1 : beams <= 2 ? 2 : beams <= 4 ? 4 : beams <= 8 ? 8 : 16); }
+constexpr int kMoveRoom = kMoveBytes + 32 * kBeamsMax;
+__global__ void __launch_bounds__(kMoveWarps * 32) k_beam_move(ReorderArgs a, int64_t pieces, int piece) {
+  grid_launch_next();
+  grid_wait();
+  __shared__ __align__(16) uint8_t room[kMoveWarps][kMoveRoom];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kMoveWarps + warp, part = unit % pieces, rest = unit / pieces;
+  const int64_t g = rest % a.groups, l = rest / a.groups;
+  if (l >= a.layers) return;
+  const int parent = lane < a.beams ? a.parents[g * a.beams + lane] : 0;
+  if (__any_sync(0xffffffffu, parent < 0 || parent >= a.beams)) {
+    if (lane == 0) set_dev_error(a.err, DEVERR_BOUNDS);
+    return;
+  }
+  const int64_t c0 = part * piece, base = l * a.layer_pitch + g * a.beams * a.pitch + c0;
+  const int len = static_cast<int>(min(static_cast<int64_t>(piece), a.bytes - c0)), stride = piece + 32;
+  const bool in_place = a.src == a.dst;
+  for (int i = 0; i < a.beams; ++i) {
+    const int p = __shfl_sync(0xffffffffu, parent, i);
+    if (in_place && p == i) continue;
+    const uint8_t* from = a.src + base + p * a.pitch;
+    uint8_t* to = room[warp] + i * stride;
+    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(from) % 16), words = (skew + len + 15) / 16;
+    const bool before = reinterpret_cast<uintptr_t>(from) - skew < reinterpret_cast<uintptr_t>(a.src);
+    for (int k = before + lane; k < words; k += 32)
+      cp_async_16(to + 16 * k, from - skew + 16 * k, static_cast<int>(min(int64_t(16), a.bytes - c0 + skew - 16 * k)));
+    if (before && lane >= skew && lane < min(16, skew + len)) to[lane] = from[lane - skew];
+  }
+  cp_async_wait_all();
+  __syncwarp();
+  for (int i = 0; i < a.beams; ++i) {
+    const int p = __shfl_sync(0xffffffffu, parent, i);
+    if (in_place && p == i) continue;
+    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(a.src + base + p * a.pitch) % 16);
+    uint8_t* to = a.dst + base + i * a.pitch;
+    const uint8_t* from = room[warp] + i * stride + skew;
+    const int head = min(static_cast<int>(-reinterpret_cast<uintptr_t>(to) % 16), len), words = (len - head) / 16, done = head + 16 * words;
+    if (lane < 16 && lane < head) to[lane] = from[lane];
+    if (lane >= 16 && done + lane - 16 < len) to[done + lane - 16] = from[done + lane - 16];
+    const int shift = (skew + head) % 16;
+    const uint4* w = reinterpret_cast<const uint4*>(from + head - shift);
+    for (int k = lane; k < words; k += 32) {
+      uint4 x = w[k];
+      if (shift) x = shifted(x, w[k + 1], shift);
+      *reinterpret_cast<uint4*>(to + head + 16 * k) = x;
+    }
+  }
 }
 
 }  // namespace
@@ -710,14 +781,20 @@ int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived
 int launch_beam_reorder(const void* src, void* dst, int64_t bytes, int64_t pitch, int groups, int beams,
                         const int32_t* parents, int layers, int64_t layer_pitch, int* err, cudaStream_t s) {
   if (bytes <= 0 || groups <= 0 || layers <= 0) return 0;
-  const ReorderArgs a{static_cast<const uint8_t*>(src), static_cast<uint8_t*>(dst), pitch, layer_pitch, 0, groups, beams,
+  const ReorderArgs a{static_cast<const uint8_t*>(src), static_cast<uint8_t*>(dst), bytes, pitch, layer_pitch, groups, beams,
                       layers, parents, err};
-  // the widest word that every row is made of
   const uint64_t all = reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) | static_cast<uint64_t>(bytes) |
                        static_cast<uint64_t>(groups > 1 || beams > 1 ? pitch : 0) | static_cast<uint64_t>(layers > 1 ? layer_pitch : 0);
-  if (all % 16 == 0) return launch_reorder<uint4>(a, bytes, s);
-  if (all % 4 == 0) return launch_reorder<uint32_t>(a, bytes, s);
-  return launch_reorder<uint8_t>(a, bytes, s);
+  if (all % 16 == 0) return launch_words<uint4>(a, s);
+  const int64_t sets = static_cast<int64_t>(groups) * layers;
+  // (a group of eight rows of 148 bytes: 13 us by 4-byte words, 15 through shared memory; 4,000 rows of 4,004
+  // in 16 layers 112 and 62)
+  if (all % 4 == 0 && bytes <= kWordsMost / beams / sets) return launch_words<uint32_t>(a, s);
+  const int piece = move_piece(beams);
+  const int64_t pieces = (bytes + piece - 1) / piece;
+  if (pieces > INT32_MAX / sets) return cudaErrorInvalidValue;
+  return launch_chained(k_beam_move, dim3(static_cast<unsigned>((pieces * sets + kMoveWarps - 1) / kMoveWarps)), kMoveWarps * 32, 0, s, 1,
+                        a, pieces, piece);
 }
 
 }  // namespace aiq

@@ -195,3 +195,29 @@ def test_rows_beyond_32_bits_of_selection_and_reordering(ctx):
     for b, a in enumerate((2, 0, 0)):
         got = big[b * ld:b * ld + 5000].cpu().numpy()
         assert np.array_equal(got[:4999], z[0, a, :4999]) and got[4999] == z[0, b, 4999]
+
+
+@pytest.mark.parametrize("beams,bytes,pitch,offset", [(3, 9000, 9013, 5), (4, 1024, 1027, 0), (4, 1025, 1027, 3), (16, 257, 260, 1),
+                                                      (16, 4099, 4100, 15), (2, 2047, 2048, 8), (1, 8193, 8200, 2), (7, 15, 17, 9),
+                                                      (8, 513, 520, 4), (5, 4004, 4012, 12)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_reorder_of_rows_that_begin_anywhere(ctx, beams, bytes, pitch, offset, in_place):
+    """Pieces of rows that source and destination cut at different bytes, their ends, and what lies beside them."""
+    rng = np.random.default_rng(bytes + beams)
+    n, layers, other = 9, 2, offset if in_place else (offset * 7 + 3) % 16
+    lp = n * beams * pitch + 1
+    src = rng.integers(0, 256, layers * lp + 64, dtype=np.uint8)
+    dst = src if in_place else rng.integers(0, 256, len(src), dtype=np.uint8)
+    p = rng.integers(0, beams, (n, beams)).astype(np.int32)
+    ref = dst.copy()
+    for l in range(layers):
+        for g in range(n):
+            for i in range(beams):
+                a, b = (l * lp + (g * beams + k) * pitch for k in (i, p[g, i]))
+                ref[other + a:other + a + bytes] = src[offset + b:offset + b + bytes]
+    ds = torch.as_tensor(src).cuda()
+    dd = ds if in_place else torch.as_tensor(dst).cuda()
+    dp = torch.as_tensor(p).cuda()
+    torch.cuda.synchronize()
+    ctx.op_beam_reorder(ds.data_ptr() + offset, dd.data_ptr() + other, bytes, pitch, n, beams, dp.data_ptr(), layers=layers, layer_pitch=lp)
+    assert np.array_equal(dd.cpu().numpy(), ref)
