@@ -1138,16 +1138,16 @@ void cut(Plan& p, int64_t least, int64_t most_places, int num_sms) {
   p.units = p.ranges = 0;
   // Calls from a cold cache, by whole tasks, by ranges and by CTAs, in us (8 KV heads of 4, head_dim 64, a
   // prefix of 64): 64 texts of about 60 tokens 29, 30, 27, of 700 68, 51, 39; 130 of 60 31, 32, 32, of
-  // 350 52, 45, 44; 260 of 60 35, 35, 44, of 700 70, 68, 68; 500 of 60 41, 43, 61, of 350 68, 67, 82;
+  // 350 52, 45, 44; 260 of 60 35, 35, 44, of 700 70, 68, 68; 300 of 350 48, 55, 57, of 1,000 82, 82, 87; 500 of 60 41, 43, 61, of 350 68, 67, 82;
   // 1,000 of 60 57, 60, 98, of 350 104, 103, 138, of 2,000 340, 293; 2,400 of 350 185, 195; 3,263 of 135
   // 147, 153, 287; 3,000 of 1,000 429, 441.  head_dim 128: 130 of 350 72, 60, 58; 260 of 200 69, 60, 67;
-  // 300 of 250 72, 71; 400 of 200 69, 75; 1,000 of 200 126, 137, of 700 260, 242; 2,000 of 200 194, 206,
+  // 200 of 350 55, 66, 64; 300 of 250 72, 71; 400 of 200 69, 75; 1,000 of 200 126, 137, of 700 260, 242; 2,000 of 200 194, 206,
   // 330, of 350 268, 278.  head_dim 64, four beams a text: 50 of 200 41, 51, 39; 100 of 1,000 113, 79, 88.
   // A CTA per task costs its start and its merge, a warp per task the time of the longest ones.
   const double per_task = p.tiles / p.seqs, rounds = static_cast<double>(tasks) / ctas;
-  if (rounds >= 5 || per_task <= 5 * rounds) {
+  if (rounds >= 5 || per_task <= 6 * rounds) {
     // a range is a tile at least, so that each has a part of a task that others have parts of
-    if (per_task >= std::max(12.0, rounds) && most_places <= INT32_MAX)
+    if (rounds >= 5 && per_task >= std::max(12.0, rounds) && most_places <= INT32_MAX)
       p.ranges = static_cast<int>(std::min<int64_t>({ctas * S::NW / p.inner, least, kArrivedMax / p.inner}));
     return;
   }
