@@ -5,6 +5,7 @@
 // then by logit and token.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "candidates.cuh"
 #include "common.cuh"
@@ -198,23 +199,21 @@ __device__ __forceinline__ void scan_row(const SelectArgs& a, Row& s, int64_t r)
   const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row + s0) / sizeof(T) % VEC);
   const int v0 = min(s1, s0 + (skew ? VEC - skew : 0)), v1 = v0 + (s1 - v0) / VEC * VEC;
   const auto index = [&](int base, int j) { return base + (j / VEC * NT + tid) * VEC + j % VEC; };
-  const auto load = [&](int base, float (&v)[kPerThread]) {
+  constexpr uint32_t kOut = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;  // -infinity
+  const auto load = [&](int base, uint4 (&v)[GROUPS]) {
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      const bool in = index(base, i * VEC) < v1;
-      if (in) w = *reinterpret_cast<const uint4*>(row + index(base, i * VEC));
-      const T* x = reinterpret_cast<const T*>(&w);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[i * VEC + e] = in ? logit(x[e]) : -INFINITY;
+      v[i] = make_uint4(kOut, kOut, kOut, kOut);
+      if (index(base, i * VEC) < v1) v[i] = *reinterpret_cast<const uint4*>(row + index(base, i * VEC));
     }
   };
-  float v[kPerThread], next[kPerThread];
+  const auto element = [](const uint4 (&v)[GROUPS], int j) { return logit(reinterpret_cast<const T*>(v)[j]); };
+  uint4 v[GROUPS], next[GROUPS];
   load(v0, v);
   load(v0 + kChunk, next);
-  float mx = fmaxf(v[0], next[0]);
+  float mx = fmaxf(element(v, 0), element(next, 0));
 #pragma unroll
-  for (int j = 1; j < kPerThread; ++j) mx = fmaxf(mx, fmaxf(v[j], next[j]));
+  for (int j = 1; j < kPerThread; ++j) mx = fmaxf(mx, fmaxf(element(v, j), element(next, j)));
   // (of few, four threads' largest at a time: a quarter of the comparisons for a bound that lists little more)
   uint32_t mine = order_bits(mx);
   const int by = a.keep <= 8 ? 4 : 1, of = tid / by;
@@ -245,15 +244,6 @@ __device__ __forceinline__ void scan_row(const SelectArgs& a, Row& s, int64_t r)
   }
   Sum2 rest;
   const auto term = [&](float z) { return exp2_approx((z - base) * kLog2e); };
-  const auto single = [&](int at, int end) {
-    if (at >= end) return;
-    const float z = logit(row[at]);
-    seen = max_nan(seen, z);
-    if (z > bound)
-      s.list()[place(s)] = key_of(z, at);
-    else
-      rest.add(term(z));
-  };
   int round = 0;
   const auto cut_list = [&] {
     long long dropped = 0;
@@ -272,51 +262,84 @@ __device__ __forceinline__ void scan_row(const SelectArgs& a, Row& s, int64_t r)
     bound = fmaxf(bound, to);
     base = to;
   };
-  single(s0 + tid, v0);
-  // Two chunks are on their way or at work at any time.
-  const auto take = [&](float (&x)[kPerThread], int at) {
-    float part[GROUPS];
+  // Few elements come on the list, as a rule.  Where it does not hold all of them, the row is read
+  // again, with a look at the list's length after each chunk and cuts: without, the warps need not wait for
+  // one another.
+  const auto scan = [&](auto checked) {
+    constexpr bool CHECKED = decltype(checked)::value;
+    const auto put = [&](float z, int at) {
+      const int to = place(s);
+      if (CHECKED || to < kListSize) s.list()[to] = key_of(z, at);
+    };
+    const auto single = [&](int at, int end) {
+      if (at >= end) return;
+      const float z = logit(row[at]);
+      seen = max_nan(seen, z);
+      if (z > bound)
+        put(z, at);
+      else
+        rest.add(term(z));
+    };
+    single(s0 + tid, v0);
+    // Two chunks are on their way or at work at any time.
+    const auto take = [&](uint4 (&raw)[GROUPS], int at) {
+      float part[GROUPS];
 #pragma unroll
-    for (int w = 0; w < GROUPS; ++w) {
-      float top = x[w * VEC];
+      for (int w = 0; w < GROUPS; ++w) {
+        float x[VEC];
 #pragma unroll
-      for (int e = 1; e < VEC; ++e) top = max_nan(top, x[w * VEC + e]);
-      seen = max_nan(seen, top);
-      if (top > bound) {  // few lanes list anything, and most of those one element
+        for (int e = 0; e < VEC; ++e) x[e] = element(raw, w * VEC + e);
+        float top = x[0];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (x[w * VEC + e] > bound) {
-            s.list()[place(s)] = key_of(x[w * VEC + e], index(at, w * VEC + e));
-            x[w * VEC + e] = -INFINITY;
-          }
+        for (int e = 1; e < VEC; ++e) top = max_nan(top, x[e]);
+        seen = max_nan(seen, top);
+        if (top > bound) {  // few lanes list anything, and most of those one element
+#pragma unroll
+          for (int e = 0; e < VEC; ++e)
+            if (x[e] > bound) {
+              put(x[e], index(at, w * VEC + e));
+              x[e] = -INFINITY;
+            }
+        }
+        float y[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) y[e] = term(x[e]);
+#pragma unroll
+        for (int d = VEC / 2; d; d >>= 1)
+#pragma unroll
+          for (int e = 0; e < d; ++e) y[e] += y[e + d];
+        part[w] = y[0];
       }
-      float y[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) y[e] = term(x[w * VEC + e]);
+      for (int d = GROUPS / 2; d; d >>= 1)
 #pragma unroll
-      for (int d = VEC / 2; d; d >>= 1)
-#pragma unroll
-        for (int e = 0; e < d; ++e) y[e] += y[e + d];
-      part[w] = y[0];
+        for (int w = 0; w < d; ++w) part[w] += part[w + d];
+      rest.add(part[0]);
+      load(at + 2 * kChunk, raw);
+      if constexpr (CHECKED) {  // (whoever lists last sees its own entries counted)
+        if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > kListHold)) {
+          cut_list();
+          __syncthreads();
+        }
+      }
+    };
+    for (int at = v0; at < v1; at += 2 * kChunk) {
+      take(v, at);
+      if (at + kChunk < v1) take(next, at + kChunk);
     }
-#pragma unroll
-    for (int d = GROUPS / 2; d; d >>= 1)
-#pragma unroll
-      for (int w = 0; w < d; ++w) part[w] += part[w + d];
-    rest.add(part[0]);
-    load(at + 2 * kChunk, x);
-    // (whoever lists last sees its own entries counted)
-    if (__syncthreads_or(*static_cast<volatile int*>(&s.n) > kListHold)) {
-      cut_list();
-      __syncthreads();
-    }
+    single(v1 + tid, s1);
+    __syncthreads();
   };
-  for (int at = v0; at < v1; at += 2 * kChunk) {
-    take(v, at);
-    if (at + kChunk < v1) take(next, at + kChunk);
+  scan(std::false_type());
+  if (s.n > kListSize) {
+    __syncthreads();
+    if (tid == 0) s.n = 0;
+    rest = Sum2();
+    load(v0, v);
+    load(v0 + kChunk, next);
+    __syncthreads();
+    scan(std::true_type());
   }
-  single(v1 + tid, s1);
-  __syncthreads();
   cut_list();
   const bool bad = __syncthreads_or(!(seen < INFINITY));
   rest.over_warp();
@@ -558,14 +581,18 @@ __device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64
   }
 }
 
-// Many rows: a CTA each, of which a group's last merges it, while others still read.  Few rows:
-// several CTAs each, and a merge of its own.
+// Many rows: a CTA each.  Where they are a group's four, one for each warp of a CTA, the last of them
+// merges the group while others still read; so it does where all rows are at work at once.  Other
+// groups, and rows cut in slices (few ones), are merged by a launch of its own.  (Calls from a cold
+// cache, merged by the last CTA and by a launch, 32,000 logits: 800 groups of four fp32 rows 103 and
+// 109 us, 1,200 of one 58 and 60; 2,000 of two fp16 rows 117 and 102, 100 of sixteen 108 and 83.)
 //
-// A row's logits are read once: 3,045 rows of 32,000 fp32 (390 MB, 57 us at the copy's rate) take 79 us,
-// 0.73 of it; 52 % of the issue slots are used, and a row's steps (first load, bound, chunks between
-// barriers, cut, merge) follow one another, eight rows an SM.  Six rows an SM took 4 us more, two to four
-// slices a row for a fuller last wave no less.  Exponentials are half the work: those of the row in
-// 64 bits took 3.4 ms.
+// A row's logits are read once: 3,045 rows of 32,000 fp32 (390 MB, 57 us at the copy's rate) take 76 us,
+// 0.76 of it; a row's steps (first load, bound, chunks, cut, merge) follow one another, eight rows
+// an SM.  Rows of 16 bits take as long for half the bytes: some eight instructions an element and
+// their latency, half the issue slots.  Measured no faster: six rows an SM, two to four slices a row for
+// a fuller last wave, two elements an instruction; a barrier after each chunk took 3 to 15 % more.
+// Exponentials are half the work: those of the row in 64 bits took 3.4 ms.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, kRowCtas) k_beam_rows(SelectArgs a) {
   grid_launch_next();
@@ -767,8 +794,10 @@ int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived
   const int most = list_most(b.keep, p.slices);
   Key* keys = static_cast<Key*>(scratch);
   float2* rests = reinterpret_cast<float2*>(keys + lists * most);
+  const bool within = p.slices == 1 && b.groups <= kArrivedMax &&
+                      (b.beams == 4 || (b.beams < 4 && rows <= static_cast<int64_t>(num_sms) * kRowCtas));
   const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, p.slices, p.slice_len, most, keys, rests,
-                     reinterpret_cast<int*>(rests + lists), p.slices == 1 && b.groups <= kArrivedMax ? arrived : nullptr,
+                     reinterpret_cast<int*>(rests + lists), within ? arrived : nullptr,
                      b.parents, b.tokens, b.done_out, b.scores_out, err};
   switch (b.type) {
     case LOGITS_F32: return launch_select<float>(a, b.groups, s);

@@ -221,3 +221,17 @@ def test_reorder_of_rows_that_begin_anywhere(ctx, beams, bytes, pitch, offset, i
     torch.cuda.synchronize()
     ctx.op_beam_reorder(ds.data_ptr() + offset, dd.data_ptr() + other, bytes, pitch, n, beams, dp.data_ptr(), layers=layers, layer_pitch=lp)
     assert np.array_equal(dd.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("type", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,beams,V,keep", [(400, 4, 9000, 8), (3, 3, 9001, 6), (700, 2, 12289, 4)])
+def test_rows_whose_largest_logits_come_late(ctx, type, n, beams, V, keep):
+    """More than a list holds lie above the bound of the first chunks: ascending rows, and a few among others."""
+    rng = np.random.default_rng(V)
+    z = (rng.standard_normal((n, beams, V)) * 2).astype(np.float32)
+    late = rng.random((n, beams)) < 0.3
+    z[late] = np.sort(z[late], -1)
+    z[0, 0, 4096:] += 30  # nearly all of the row
+    scores = -rng.uniform(0, 3, (n, beams))
+    held, out = _select(ctx, z, scores, None, keep, type, ld=V + 3, offset=1)
+    _check(held, out, scores, None, keep, groups=range(0, n, max(1, n // 40)))
