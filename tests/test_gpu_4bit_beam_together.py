@@ -235,3 +235,19 @@ def test_rows_whose_largest_logits_come_late(ctx, type, n, beams, V, keep):
     scores = -rng.uniform(0, 3, (n, beams))
     held, out = _select(ctx, z, scores, None, keep, type, ld=V + 3, offset=1)
     _check(held, out, scores, None, keep, groups=range(0, n, max(1, n // 40)))
+
+
+@pytest.mark.parametrize("bytes,pitch", [(33, 35), (5001, 5003), (600000, 600004)])
+def test_a_parent_outside_leaves_its_group(ctx, bytes, pitch):
+    """Rows that begin anywhere, and 4-byte words: the group stays as it was, the others are moved."""
+    rng = np.random.default_rng(bytes)
+    x = rng.integers(0, 256, 9 * pitch, dtype=np.uint8)
+    d = torch.as_tensor(x).cuda()
+    p = torch.as_tensor(np.array([[1, 0, 2], [0, 3, 1], [2, 2, 0]], np.int32)).cuda()
+    torch.cuda.synchronize()
+    with pytest.raises(aiq.AiqError) as e:
+        ctx.op_beam_reorder(d.data_ptr(), d.data_ptr(), bytes, pitch, 3, 3, p.data_ptr())
+    assert e.value.status == aiq.ERR_DEVICE_CHECK
+    ref = x.reshape(9, pitch).copy()
+    ref[:, :bytes] = ref[[1, 0, 2, 3, 4, 5, 8, 8, 6], :bytes]
+    assert np.array_equal(d.cpu().numpy().reshape(9, pitch), ref)
