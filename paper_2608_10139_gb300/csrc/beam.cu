@@ -397,8 +397,8 @@ __device__ __forceinline__ int larger(const Key* keys, Key x, bool equal) {
 
 // What a group's merge shares, and behind it [beams][slices * most] keys.
 struct Merge {
-  Key sorted[kBeamsMax][32], offers[kBeamsMax][32], first[kKeepMax + 1];
-  int tokens[kBeamsMax][32], from[kKeepMax + 1];
+  Key sorted[kBeamsMax][32], offers[kBeamsMax][32], first[kKeepMax], next[kBeamsMax];
+  int tokens[kBeamsMax][32], from[kKeepMax];
   double totals[kBeamsMax], logs[kBeamsMax], sums[32];
   float errors[kBeamsMax], tops[kBeamsMax];
   unsigned int close, unused;  // hypotheses that are close to others
@@ -483,8 +483,11 @@ __device__ __forceinline__ bool merge_row(const SelectArgs& a, Merge& s, int64_t
 //
 // Which offers come first is a matter of 64 bits: where two of different hypotheses are closer
 // to one another than the 32-bit sums' error allows to tell, their rows are summed once more,
-// to 2^-35.  The error of a row's log is at most `rest / total`, the share of the tokens
-// that are not among its largest, times 2^-22 of the exponential, 2^-19 of sums and rounded
+// to 2^-35.  Looked at are neighbours among what is kept (a hypothesis' own offers are in the order of
+// its logits, whatever its sum), and the last of what is kept beside the first of every other
+// hypothesis that is not: that need not be the next offer, which may be of the same row, or of
+// one whose sum is more exact.  The error of a row's log is at most `rest / total`, the share of the
+// tokens that are not among its largest, times 2^-22 of the exponential, 2^-19 of sums and rounded
 // arguments, and 2.4 * 2^-24 for each unit of |log2 e^(z - y)|, of which the average, weighted
 // by the terms, is at most log2(V) less log2 of their sum (the entropy of V numbers).
 template <typename T>
@@ -503,7 +506,7 @@ __device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64
   bad = __syncthreads_or(bad);
   while (true) {
     if (warp == 0 && lane < a.beams) s.logs[lane] = log_of(s.totals[lane]);
-    if (threadIdx.x <= a.keep) s.first[threadIdx.x] = 0;
+    if (threadIdx.x < a.keep) s.first[threadIdx.x] = 0;
     if (threadIdx.x == 0) s.close = 0;
     __syncthreads();
     for (int b = warp; b < a.beams; b += warps) {
@@ -524,21 +527,27 @@ __device__ __forceinline__ void merge_group(const SelectArgs& a, Merge& s, int64
     __syncthreads();
     for (int b = warp; b < a.beams; b += warps) {
       const Key offer = s.offers[b][lane];
-      if (!offer) continue;
-      int place = lane;
+      int place = kKeepMax;
+      if (offer) {
+        place = lane;
 #pragma unroll 4
-      for (int o = 0; o < a.beams; ++o) place += o == b ? 0 : larger(s.offers[o], offer, o < b);
-      if (place <= a.keep) {
+        for (int o = 0; o < a.beams; ++o) place += o == b ? 0 : larger(s.offers[o], offer, o < b);
+      }
+      if (place < a.keep) {
         s.first[place] = offer;
         s.from[place] = b << 8 | lane;
       }
+      const int kept = __popc(__ballot_sync(0xffffffffu, place < a.keep));
+      if (lane == kept % 32) s.next[b] = kept < 32 ? offer : 0;
     }
     __syncthreads();
-    if (threadIdx.x < a.keep && s.first[threadIdx.x + 1]) {
-      const int b0 = s.from[threadIdx.x] >> 8, b1 = s.from[threadIdx.x + 1] >> 8;
+    const auto compare = [&](Key x, int b0, Key y, int b1) {
       const double e = static_cast<double>(s.errors[b0]) + s.errors[b1];
-      if (b0 != b1 && e > 0 && score_of(s.first[threadIdx.x]) - score_of(s.first[threadIdx.x + 1]) <= e) atomicOr(&s.close, 1u << b0 | 1u << b1);
-    }
+      if (y && b0 != b1 && e > 0 && score_of(x) - score_of(y) <= e) atomicOr(&s.close, 1u << b0 | 1u << b1);
+    };
+    const int i = threadIdx.x;
+    if (i + 1 < a.keep && s.first[i + 1]) compare(s.first[i], s.from[i] >> 8, s.first[i + 1], s.from[i + 1] >> 8);
+    if (i < a.beams && s.first[a.keep - 1]) compare(s.first[a.keep - 1], s.from[a.keep - 1] >> 8, s.next[i], i);
     __syncthreads();
     const unsigned int close = s.close;
     if (!close) break;  // (each round leaves fewer rows whose error is not 0)
@@ -636,7 +645,8 @@ Plan plan_of(int64_t rows, int V, int beams, int num_sms) {
 constexpr int merge_bytes(int beams, int slices, int most) {
   return static_cast<int>(sizeof(Merge)) + beams * slices * most * static_cast<int>(sizeof(Key));
 }
-static_assert(merge_bytes(kBeamsMax, 1, kListMost) <= kRowShared, "a group's last CTA merges it in its list's room");
+constexpr int kWithinBeams = kRowThreads / 32;  // of the groups that a CTA of the rows' merges, a row a warp, at most
+static_assert(merge_bytes(kWithinBeams, 1, kListMost) <= kRowShared, "a group's last CTA merges it in its list's room");
 
 template <typename T>
 int launch_select(const SelectArgs& a, int groups, cudaStream_t s) {
@@ -795,7 +805,7 @@ int launch_beam_select(const BeamSelect& b, void* scratch, unsigned int* arrived
   Key* keys = static_cast<Key*>(scratch);
   float2* rests = reinterpret_cast<float2*>(keys + lists * most);
   const bool within = p.slices == 1 && b.groups <= kArrivedMax &&
-                      (b.beams == 4 || (b.beams < 4 && rows <= static_cast<int64_t>(num_sms) * kRowCtas));
+                      (b.beams == kWithinBeams || (b.beams < kWithinBeams && rows <= static_cast<int64_t>(num_sms) * kRowCtas));
   const SelectArgs a{b.logits, b.ld, b.V, b.beams, b.keep, b.scores, b.done, b.eos, b.pad, p.slices, p.slice_len, most, keys, rests,
                      reinterpret_cast<int*>(rests + lists), within ? arrived : nullptr,
                      b.parents, b.tokens, b.done_out, b.scores_out, err};
