@@ -854,7 +854,10 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
         if (b + 1 < x.info / kBeams) token.load(key_of(a, HD, x.row + b + 1, x.h), kd);
       }
       // the next task's queries are on their way while this one ends
-      if ((x.info & kLast) && ring.got + 1 != ring.put) fetch(ring.head(1));
+      if ((x.info & kLast) && ring.got + 1 != ring.put) {
+        __syncwarp();  // its head, which lane 0 wrote: this lane has not waited for that entry
+        fetch(ring.head(1));
+      }
     }
     const bool some = (x.info & kGenerated) && x.info / kBeams > 1;
     const uint8_t* tile = ring.slot();

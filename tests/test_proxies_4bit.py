@@ -32,3 +32,18 @@ def test_a_slot_is_refilled_only_once_it_is_used_up():
             continue
         loop = body[body.index("ring.wait()"):]
         assert loop.index("at.tile(") < loop.index("++ring.got;") < loop.index("produce()")
+
+
+def test_heads_that_no_wait_orders_are_read_behind_a_barrier():
+    """Lane 0 stores an entry's head; the others read it behind their wait for that entry's copies, or, where
+    they have not waited for it (the first, the one ahead), behind a barrier of the warp."""
+    body = _kernels()["k_decode_q4_stream"]
+    reads = [m.start() for m in re.finditer(r"ring\.head\(", body)]
+    assert len(reads) == 3
+    first, waited, ahead = (body[:at] for at in reads)
+    assert re.search(r"__syncwarp\(\);\s*if \(ring\.more\(\)\) fetch\($", first)
+    assert re.search(r"if \(!ring\.wait\(\)\) return;\s*const Head4 x = $", waited)
+    assert re.search(r"\{\s*__syncwarp\(\);\s*fetch\($", ahead) and body[reads[2]:].startswith("ring.head(1)")
+    split = _kernels()["k_decode_q4_split"]
+    assert len(re.findall(r"ring\.head\(", split)) == 1
+    assert re.search(r"if \(!ring\.wait\(\)\) break;\s*const int info = ring\.head\(\)", split)
