@@ -290,19 +290,21 @@ struct Attn4 {
     float mb[2], by[2] = {scale[0], scale[1]};
 #pragma unroll
     for (int e = 0; e < 2; ++e) mb[e] = fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[K - 1][e], sc[K - 1][2 + e])) * by[e];
-    const bool big = fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f;
-    if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag) || big)) {
-      if (__any_sync(0xffffffffu, big)) {
-        // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
-        // score that is not rounded (in the fma below) could lie so far above a rounded m that
-        // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
-        // most, and the largest probability stays between 1 and 2^15 whatever the last place.
+    if (fmaxf(fabsf(mb[0]), fabsf(mb[1])) > 0x1p22f) {
+      // Scores of 2^22 and more have a last place of half a bit of the exponent and more: a
+      // score that is not rounded (in the fma below) could lie so far above a rounded m that
+      // its probability leaves fp16.  They are rounded first, and m up: a score is then mb at
+      // most, and the largest probability stays between 1 and 2^15 whatever the last place.  (A lane
+      // whose keys are all masked comes here too, which changes none of its numbers.)
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+      for (int e = 0; e < 2; ++e)
+        if (fabsf(mb[e]) > 0x1p22f) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[k][e] *= by[e & 1];
-        by[0] = by[1] = 1.f;
-      }
+          for (int k = 0; k < K; ++k) sc[k][e] *= by[e], sc[k][2 + e] *= by[e];
+          by[e] = 1.f;
+        }
+    }
+    if (__any_sync(0xffffffffu, mb[0] > __fadd_rd(m[0], kAbove + kLag) || mb[1] > __fadd_rd(m[1], kAbove + kLag))) {
 #pragma unroll
       for (int d = PAIRS ? 2 : 4; d < 32; d <<= 1) {
         mb[0] = fmaxf(mb[0], __shfl_xor_sync(0xffffffffu, mb[0], d));
