@@ -1595,7 +1595,7 @@ aiq_status run_transform(aiq_ctx* c, const TableD& t, ModelD* m, const aiq_selec
     AIQ_TRY(check_sampling(*gen->sampling, V));
   }
   if ((c->kv_bits == 8 || c->kv4) && m->cfg.n_heads / m->cfg.n_kv_heads > 8)
-    return fail(AIQ_ERR_UNSUPPORTED, "the 8-bit cache takes up to 8 query heads per KV head");
+    return fail(AIQ_ERR_UNSUPPORTED, std::string(c->kv4 ? "the 4-bit" : "the 8-bit") + " cache takes up to 8 query heads per KV head");
   PredSet ps{};
   AIQ_TRY(make_pred_set(t, q->preds, q->n_preds, &ps));
 

@@ -139,3 +139,18 @@ def test_refusals(ctx):
     with pytest.raises(aiq.AiqError) as e:
         _run(ctx, shape, W, table, prefix, [], 2)
     assert e.value.status == aiq.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("option,value,cache", [("kv4", 1, "4-bit"), ("kv_bits", 8, "8-bit")])
+def test_a_refusal_names_the_cache_in_use(ctx, option, value, cache):
+    shape = replace(SHAPES["gqa4_hd64"], n_heads=18, n_kv_heads=1, head_dim=64)
+    W = synth.make_weights(shape, 1)
+    table, prefix = _inputs(shape, 4, 1)
+    before = {"kv4": 0, "kv_bits": 16}[option]
+    ctx.set_option(option, value)
+    try:
+        with pytest.raises(aiq.AiqError, match=f"the {cache} cache takes up to 8 query heads per KV head") as e:
+            _run(ctx, shape, W, table, prefix, [], 2, on=int(option == "kv4"))
+    finally:
+        ctx.set_option(option, before)
+    assert e.value.status == aiq.ERR_UNSUPPORTED
