@@ -151,6 +151,12 @@ struct Sum2 {
     l += (h - (s - b)) + (x - b);
     h = s;
   }
+  // (To 2^-40: a row that ascends is cut hundreds of times, whose roundings must not add up.)
+  __device__ __forceinline__ void times(const Exp3& f) {
+    const float fh = f.sum(), fl = ((f.h - fh) + f.m) + f.l, x = h * fh;
+    l = fmaf(h, fh, -x) + fmaf(h, fl, l * fh);
+    h = x;
+  }
   __device__ __forceinline__ void over_warp() {
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
@@ -255,8 +261,8 @@ __device__ __forceinline__ void scan_row(const SelectArgs& a, Row& s, int64_t r)
     dropped = warp_total(dropped);
     if (tid % 32 == 0) atomicAdd(&s.dropped, static_cast<unsigned long long>(dropped));
     // of what follows, only larger values can be among the largest: equal ones come later
-    const float to = order_value(static_cast<uint32_t>(from >> 32)), f = Exp3(base, to).sum();
-    rest.h *= f, rest.l *= f;
+    const float to = order_value(static_cast<uint32_t>(from >> 32));
+    rest.times(Exp3(base, to));
     __syncthreads();
     if (tid == 0) rest.add(static_cast<float>(unfixed(s.dropped)));
     bound = fmaxf(bound, to);

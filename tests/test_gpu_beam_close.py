@@ -6,6 +6,7 @@ import pytest
 import beam_close
 import kv4
 from helpers import gpu_ctx
+from paper_2608_10139_gb300 import aiq
 from test_gpu_beam import TYPES, _select
 
 torch = pytest.importorskip("torch")
@@ -73,3 +74,24 @@ def test_more_ties_than_are_kept(ctx, type, keep):
         free = np.flatnonzero(z[g, 0] == z[g, 1])
         z[g][:, rng.permutation(free)[:keep + 1]] = 4.5
     _compare(ctx, (z, scores, done, keep), type)
+
+
+def test_rows_that_ascend_little_by_little(ctx):
+    """Each chunk of a row is above what was read before, so that its list is cut back, and the sum of the others
+    brought to another number, hundreds of times.  Beside it the same row backwards, whose score alone tells them apart."""
+    V, n = 3_000_000, 310
+    up = (np.arange(V) / V * 0.01).astype(np.float32)
+    z = torch.as_tensor(np.stack([up, up[::-1]])).cuda().expand(n, 2, V).contiguous()
+    scores = np.full((n, 2), -1, np.float32)
+    scores[:, 1] += np.float32(2.0) ** -np.arange(18, 23)[np.arange(n) % 5] * np.where(np.arange(n) % 2, 1, -1)
+    sc = torch.as_tensor(scores).cuda()
+    p, t = (torch.zeros((n, 2), dtype=torch.int32, device="cuda") for _ in range(2))
+    so = torch.zeros((n, 2), device="cuda")
+    torch.cuda.synchronize()
+    ctx.op_beam_select(z.data_ptr(), aiq.LOGITS_F32, V, n, 2, V, sc.data_ptr(), 2, p.data_ptr(), t.data_ptr(), so.data_ptr())
+    p, t, so = (x.cpu().numpy() for x in (p, t, so))
+    first = (scores[:, 1] > scores[:, 0]).astype(np.int32)  # (by 2^-22 at least, the row's two largest by 2^-27)
+    want = scores.max(1)[:, None] + (up[::-1][:2].astype(np.float64) - beam_close.log_sum(up))
+    assert (np.abs(so - want) <= np.abs(want) * 2.0 ** -24 + 2.0 ** -17).all(), np.abs(so - want).max()
+    assert np.array_equal(p, np.repeat(first[:, None], 2, 1)), (p != first[:, None]).any(1).sum()
+    assert np.array_equal(t, np.where(first[:, None], [0, 1], [V - 1, V - 2]))
