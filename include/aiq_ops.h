@@ -220,10 +220,14 @@ aiq_status aiq_op_sample(aiq_ctx* ctx, const void* logits, int32_t type, int64_t
  * log probabilities; -infinity: the place holds none, its row is not read).  It offers
  * every token t at
  *     s = C + z_t - log sum_i exp(z_i),
- * in 64 bits, where z_t is finite (-infinity rules a token out, a row of -infinity alone offers
- * nothing).  The log is right to 2^-33: offers of different hypotheses that are closer than 2^-32
- * may come in either order, the same one every time.  A hypothesis that has ended (done[g][b] != 0;
- * done may be NULL: none has) offers itself, pad_id at s = C, and its row is not read.
+ * where z_t is finite (-infinity rules a token out, a row of -infinity alone offers nothing).
+ * Which offers come first, and in which order, is decided in 64 bits with logs that are right to
+ * 2^-33: offers of different hypotheses that are closer than 2^-32 may come in either order, the
+ * same one every time.  Where the order does not ask for that, the log in scores_out is right to
+ * 2^-17 (of up to 2^16 logits, 2^-18), and the closer the less the tokens that are not among the
+ * row's `keep` largest weigh; a score is then rounded to fp32 once.  A hypothesis that has ended
+ * (done[g][b] != 0; done may be NULL: none has) offers itself, pad_id at s = C, and its row is
+ * not read.
  * The first `keep` of a group's offers, by s descending, equal ones by hypothesis, those of
  * one hypothesis by logit descending and then by token, go to parents, tokens (int32
  * [n][keep], a parent being a hypothesis of the group, 0 .. beams - 1), scores_out (fp32) and
