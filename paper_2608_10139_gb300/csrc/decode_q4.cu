@@ -697,18 +697,18 @@ __device__ __forceinline__ void pieces(const DecQ4Args& a, const Attn4<HD, PAIRS
 
 // Many tasks: a warp takes the tiles of all its tasks as one stream through its ring.  Where there
 // are many tasks a warp, they are drawn one by one (dealt out by number they took 10 % more: 3,000
-// texts of 200, head_dim 128, 315 us, drawn 273).  Of fewer (RANGES) the longest would be waited for:
+// texts of 200, head_dim 128, 315 us, drawn 273).  Of few for their length (RANGES) the longest would be waited for:
 // the line of an inner task's tiles is cut into `ranges` of equal length, a warp each.  A task that
 // lies within a range is the warp's alone; of one that does not, each warp leaves its (maximum, sum,
 // output), and the last to arrive merges them in their order.
 //
 // Bound by instruction issue and its latency, not by HBM: 3,263 rows of 218 keys, 32 query heads of 64
-// on 8 (329 MB, 48 us at the copy's rate), take 126 us (132 with caches cold) for 88 million warp
-// instructions, 65 % of the issue slots while warps are at work; 250 to 290 a tile and some 1,400 a
+// on 8 (329 MB, 48 us at the copy's rate), take 126 us (130 with caches cold) for 87 million warp
+// instructions, 63 % of the issue slots while warps are at work; 250 to 290 a tile and some 1,400 a
 // task of seven tiles.  Of a tile's, 80 make operands out of codes and 24 are products.  Long rows come
 // to 0.8 of the copy.  head_dim 128 has three CTAs an SM for its registers: 700 rows, four beams a
-// text of 200 tokens, take 79 us, where two groups of eight columns read a prompt's tiles in turn
-// (all sixteen at once would leave eight warps an SM).  Measured slower: five CTAs, 18 warps, four
+// text of 200 tokens, take 79 us with half the issue slots busy, latency of ten warps an SM, where
+// two groups of eight columns read a prompt's tiles in turn (all sixteen at once would leave eight warps an SM).  Measured slower: five CTAs, 18 warps, four
 // entries a ring, one tile an entry, scores of two tiles first, ranges for batches of thousands.
 template <int HD, bool PAIRS, bool RANGES>
 __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
@@ -926,7 +926,7 @@ __global__ void __launch_bounds__(Stream4<HD>::NW * 32, Stream4<HD>::CTAS)
 // share(i) .. share(i + 1) - 1.
 //
 // Four documents of 17,979 to 57,262 tokens, 8 KV heads of 128 (188 MB), take 47 us, 0.59 of the copy:
-// bound by instruction issue (54 % of the slots by 11.4 warps an SM) and the start and end of a call that
+// bound by latency (11.4 warps an SM fill 53 % of the issue slots) and the start and end of a call that
 // each warp has some 23 tiles for.  Entries of two tiles took 2 us more.
 constexpr int kMaxRanges = 512;  // of a task
 template <int HD>
@@ -1148,7 +1148,9 @@ void cut(Plan& p, int64_t least, int64_t most_places, int num_sms) {
   // 147, 153, 287; 3,000 of 1,000 429, 441.  head_dim 128: 130 of 350 72, 60, 58; 260 of 200 69, 60, 67;
   // 200 of 350 55, 66, 64; 300 of 250 72, 71; 400 of 200 69, 75; 1,000 of 200 126, 137, of 700 260, 242; 2,000 of 200 194, 206,
   // 330, of 350 268, 278.  head_dim 64, four beams a text: 50 of 200 41, 51, 39; 100 of 1,000 113, 79, 88.
-  // A CTA per task costs its start and its merge, a warp per task the time of the longest ones.
+  // A CTA per task costs its start and its merge, a warp per task the time of the longest ones.  Just below
+  // five rounds the rule is not the best of the three: 260 of 200 at head_dim 128 take 15 % more than ranges,
+  // 100 of 1,000 of four beams 11 %, 300 of 1,000 6 %.
   const double per_task = p.tiles / p.seqs, rounds = static_cast<double>(tasks) / ctas;
   if (rounds >= 5 || per_task <= 6 * rounds) {
     // a range is a tile at least, so that each has a part of a task that others have parts of
